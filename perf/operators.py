@@ -31,6 +31,7 @@ own = False
 
 DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 SIZE = {"f32": 4, "bf16": 2, "f16": 2}
+GATE = {"raw": 0, "sigmoid": 1}  # POLYGLOT_GATE_*
 
 
 def _drop(name, kind, dtype, rows, d, p, table=0, residual=False, whole=False):
@@ -380,14 +381,15 @@ def _own_run(s):
                           prompt=s["prompt"], repetition=s["repetition"], presence=s["presence"],
                           frequency=s["frequency"], bias=s["bias"], mask=s["mask"],
                           mask_rows=s["mask_rows"])
+    form = GATE[s["form"]]
     if kind == "step":
-        return _context().recurrence_step(s["gate"], s["x"], s["h0"], form=s["form"])
+        return _context().recurrence_step(s["gate"], s["x"], s["h0"], form=form)
     ctx = _context(s["tokens"], s["D"])
     if kind == "forward":
-        return ctx.recurrence(s["gate"], s["x"], s["offsets"], h0=s["h0"], form=s["form"],
+        return ctx.recurrence(s["gate"], s["x"], s["offsets"], h0=s["h0"], form=form,
                               reverse=s["reverse"])
     return ctx.recurrence_backward(s["gate"], s["x"], s["h"], s["dh"], s["offsets"], h0=s["h0"],
-                                   dlast=s["dlast"], form=s["form"], reverse=s["reverse"])
+                                   dlast=s["dlast"], form=form, reverse=s["reverse"])
 
 
 def run(s):
