@@ -59,6 +59,8 @@ extern "C" {
 #define POLYGLOT_EHIP -4   /* HIP runtime error; text in polyglot_last_error() */
 #define POLYGLOT_EID -5    /* an id was outside [0, V) (reported by polyglot_status) */
 #define POLYGLOT_ESTATE -6 /* call not valid in the context's current state */
+#define POLYGLOT_EOFFSETS -7 /* sequence offsets did not ascend from 0 to the token count
+                                (reported by polyglot_status) */
 
 /* How the embedding-gradient rows are added into the table (§4.3). */
 #define POLYGLOT_SCATTER_SORTED 0 /* stable radix sort by row id, segmented sum: deterministic */
@@ -254,8 +256,202 @@ int polyglot_touched_rows(polyglot_ctx* ctx, int32_t* ids_host, int32_t cap, int
 int polyglot_set_timing(polyglot_ctx* ctx, int enable);
 int polyglot_kernel_times(polyglot_ctx* ctx, double* ms, int32_t* launches);
 
+/* ------------------------------------------------------------------ sequences
+ * Operators of a language model that reads all of its context and not a
+ * window of it, over the same word table: rows gathered with dropout, a gated
+ * linear recurrence over packed sequences, and the choice of a word among a
+ * vocabulary's scores.  They need a context for its stream, its error words
+ * and its workspace; the context's model shape does not matter to them.
+ *
+ * Common to all: tensors are device pointers owned by the caller, in the
+ * storage format `dtype` (POLYGLOT_F32, POLYGLOT_BF16, POLYGLOT_F16) unless a
+ * type is stated, aligned to their element size, with rows of consecutive
+ * elements; ld_* is the distance between rows in elements, at least a row's
+ * length.  Element offsets may pass 2^32.  Arithmetic, sums and states are in
+ * 32 bits; each output is rounded to its format once (to nearest even).  Calls
+ * are asynchronous on the context's stream and may be captured into a HIP
+ * graph.  The argument blocks are read before the call returns; fields that
+ * are not set must be zero.  Vector loads and stores are used where rows and
+ * pointers are aligned to 16 bytes (8 for rows of 16-bit elements); results
+ * do not depend on it.  Host-detectable errors: POLYGLOT_ENULL, POLYGLOT_EINVAL,
+ * POLYGLOT_EBATCH (above the reserved workspace), nothing enqueued. */
+
+/* Dropout with a mask that is computed and never stored.
+ *
+ *   y[r][c] = keep(r, c) ? x[r][c] / (1 - p') : 0,   plus add[r][c] if add
+ *
+ * keep(r, c) compares 16 random bits with t = round(65536 p); p' = t / 65536.
+ * The bits are piece c % 8 (low half of a word first) of the four words that
+ * Philox 4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy
+ * as 1, 2, 3", SC 2011) gives for the counter
+ *   {c / 8, low and high word of first_row + r, site + *site_dev}
+ * and the key `seed` (low word first).  They depend on nothing else: not on the
+ * format, the strides, or how rows are divided among calls.  The gradient of y
+ * with respect to x is the same operator on dy with the same seed, site and
+ * first_row (and no add); that of add is dy itself.
+ *   whole_rows != 0: a row is kept or dropped as a whole, by piece 0 at c / 8 = 2^32 - 1.
+ *   ids != NULL: row r of x is row ids[r] of a table x[table_rows][d].  An id
+ *     outside the table makes its row NaN (as in polyglot_gather) and raises the
+ *     sticky flag (POLYGLOT_EID).
+ * A dropped element is exactly 0 (plus add) also where x is not finite; p = 0
+ * copies, p = 1 drops everything.  y may be x (without ids) or add, with the same
+ * ld.  rows = 0 does nothing. */
+typedef struct {
+  const void* x;
+  const void* add; /* [rows][d] or NULL */
+  void* y;         /* [rows][d] */
+  const void* ids; /* [rows] int32 or int64, or NULL */
+  const uint32_t* site_dev; /* device word added to site (a step counter of a captured
+                               graph), or NULL */
+  int64_t rows, ld_x, ld_add, ld_y;
+  uint64_t seed, first_row;
+  uint32_t site;      /* which dropout of which step */
+  float p;            /* in [0, 1] */
+  int32_t d;          /* >= 1 */
+  int32_t dtype;
+  int32_t id_bytes;   /* 4 or 8 with ids */
+  int32_t table_rows; /* >= 1 with ids */
+  int32_t whole_rows;
+} polyglot_dropout_args;
+int polyglot_dropout(polyglot_ctx* ctx, const polyglot_dropout_args* args);
+
+/* Gated linear recurrence over packed sequences.
+ *
+ *   POLYGLOT_GATE_RAW:      h_t = a_t h_{t-1} + x_t             a = gate
+ *   POLYGLOT_GATE_SIGMOID:  h_t = a_t h_{t-1} + (1 - a_t) x_t   a = 1 / (1 + e^-gate)
+ *
+ * for each of D channels on its own; `group` consecutive channels share a gate
+ * (a head), so gate has D / group columns.  Sequence s is the tokens
+ * [offsets[s], offsets[s+1]); without offsets all nseq sequences have
+ * tokens / nseq tokens.  Sequences may be empty.  h_{-1} is h0[s] (zeros if
+ * NULL); last[s], if not NULL, receives the state after the sequence's last
+ * token (h0[s] or zeros for an empty one); last may be h0.  reverse != 0 reads
+ * every sequence from its last token to its first.  The state is carried in
+ * 32 bits from the sequence's start to its end; h holds its roundings to dtype.
+ *
+ * With one token per sequence (tokens == nseq, no offsets) this is a model's
+ * step for single tokens: one pass over the rows, no workspace.  Other calls
+ * use the workspace of polyglot_reserve_recurrence.
+ * Offsets that do not ascend from 0 to `tokens` raise POLYGLOT_EOFFSETS
+ * (polyglot_status); the outputs are then unspecified, and no access leaves
+ * the tensors. */
+#define POLYGLOT_GATE_RAW 0
+#define POLYGLOT_GATE_SIGMOID 1
+typedef struct {
+  const void* gate;    /* [tokens][D / group] */
+  const void* x;       /* [tokens][D] */
+  const float* h0;     /* [nseq][D] or NULL */
+  const void* offsets; /* [nseq + 1] int32 or int64, or NULL */
+  void* h;             /* [tokens][D] */
+  float* last;         /* [nseq][D] or NULL */
+  int64_t tokens;      /* 0 .. 2^31 - 1 */
+  int64_t ld_gate, ld_x, ld_h;
+  int32_t nseq;         /* >= 1 */
+  int32_t D;            /* >= 1 */
+  int32_t group;        /* 1, or 2..256 dividing D */
+  int32_t dtype;
+  int32_t offset_bytes; /* 4 or 8 with offsets */
+  int32_t form;         /* POLYGLOT_GATE_* */
+  int32_t reverse;
+} polyglot_recurrence_args;
+int polyglot_recurrence(polyglot_ctx* ctx, const polyglot_recurrence_args* args);
+
+/* The gradient of polyglot_recurrence.  With dh the gradient of h and dlast that
+ * of last, going from a sequence's last token to its first:
+ *
+ *   lambda_t = dh_t + mu_{t+1},  mu_t = a_t lambda_t  (mu after the last token: dlast[s])
+ *   RAW:      dx_t = lambda_t             dgate_t = sum over the group of lambda_t h_{t-1}
+ *   SIGMOID:  dx_t = (1 - a_t) lambda_t   dgate_t = a_t (1 - a_t) sum lambda_t (h_{t-1} - x_t)
+ *   dh0[s] = mu of the sequence's first token (dlast[s] or zeros for an empty one)
+ *
+ * h is the forward call's output: h_{t-1} enters with its rounding to dtype.
+ * x may be NULL for POLYGLOT_GATE_RAW.  dgate must not overlap an input; dx may
+ * be dh or x, with the same ld.  dh0 may be dlast. */
+typedef struct {
+  const void* gate;    /* [tokens][D / group] */
+  const void* x;       /* [tokens][D] */
+  const void* h;       /* [tokens][D] */
+  const void* dh;      /* [tokens][D] */
+  const float* h0;     /* [nseq][D] or NULL */
+  const float* dlast;  /* [nseq][D] or NULL */
+  const void* offsets; /* [nseq + 1] or NULL */
+  void* dgate;         /* [tokens][D / group] */
+  void* dx;            /* [tokens][D] */
+  float* dh0;          /* [nseq][D] or NULL */
+  int64_t tokens;
+  int64_t ld_gate, ld_x, ld_h, ld_dh, ld_dgate, ld_dx;
+  int32_t nseq, D, group, dtype, offset_bytes, form, reverse;
+} polyglot_recurrence_grad_args;
+int polyglot_recurrence_grad(polyglot_ctx* ctx, const polyglot_recurrence_grad_args* args);
+
+/* Sizes the recurrence's workspace for calls of up to max_tokens tokens and
+ * max_D channels.  Waits for the context's stream, frees what an earlier call
+ * reserved and allocates: to be called outside of graph capture, and graphs that
+ * were captured with the earlier workspace must not be replayed afterwards. */
+int polyglot_reserve_recurrence(polyglot_ctx* ctx, int64_t max_tokens, int32_t max_D);
+
+/* The scores of a vocabulary made ready for a choice, one row for each live
+ * sequence, and the choice.  For every row r and word v, in this order and in
+ * 32 bits:
+ *
+ *   l = logits[r][v]
+ *   v in history[r]:            l = l > 0 ? l / repetition[r] : l * repetition[r]
+ *   n times in its made part:   l = l - (frequency[r] n + presence[r])     (n > 0)
+ *   l = l + bias[v]
+ *   v not allowed by the mask:  l = -infinity, whatever it was
+ *
+ * history[r] holds the first lengths[r] ids of its row (all `history_cap` if
+ * lengths is NULL); those before prompt[r] are the prompt, the others were made
+ * by the model (all of them if prompt is NULL).  Negative ids are padding; ids
+ * >= V raise the sticky flag (POLYGLOT_EID) and count for nothing.  Lengths and
+ * prompts outside [0, history_cap] are taken as the nearer end.
+ * repetition, frequency and presence are per row; NULL stands for 1, 0 and 0.
+ * bias[V] is float32, shared (ld_bias 0) or one row per row.
+ * A mask row is ceil(V / 32) words of 32 bits, bit v % 32 of word v / 32 set where
+ * v is allowed; row r takes row mask_rows[r] (negative: no mask), or without
+ * mask_rows its own (masks == rows) or the only one (masks == 1).  A mask_rows
+ * entry >= masks raises the sticky flag and masks nothing.
+ *
+ * out receives l in dtype and may be logits (with the same ld) or NULL.
+ * token[r], if not NULL, receives the word of the largest l (before its rounding
+ * to dtype), the lowest one of equals; NaN is never chosen; -1 if no l is above
+ * -infinity.  lse[r], if not NULL, receives log(sum_v e^l) (-infinity for a row
+ * that the mask leaves empty; NaN if an l is NaN).
+ * rows = 0 does nothing.  token and lse use the workspace of polyglot_reserve_logits. */
+typedef struct {
+  const void* logits;
+  void* out;
+  const int32_t* history; /* [rows][history_cap], or NULL */
+  const int32_t* lengths; /* [rows] or NULL */
+  const int32_t* prompt;  /* [rows] or NULL */
+  const float* repetition;
+  const float* presence;
+  const float* frequency;
+  const float* bias;
+  const uint32_t* mask;
+  const int32_t* mask_rows;
+  int32_t* token;
+  float* lse;
+  int64_t ld_logits, ld_out, ld_history, ld_bias, ld_mask;
+  int32_t rows, V, dtype, history_cap, masks;
+} polyglot_logits_args;
+int polyglot_logits(polyglot_ctx* ctx, const polyglot_logits_args* args);
+
+/* Sizes the workspace that joins the parts of a row, for calls of up to max_rows
+ * rows of max_V scores; otherwise as polyglot_reserve_recurrence. */
+int polyglot_reserve_logits(polyglot_ctx* ctx, int32_t max_rows, int32_t max_V);
+
+/* The operators' kernels under polyglot_set_timing, as polyglot_kernel_times
+ * reports the others. */
+#define POLYGLOT_OPK_DROPOUT 0
+#define POLYGLOT_OPK_RECURRENCE 1
+#define POLYGLOT_OPK_RECURRENCE_GRAD 2
+#define POLYGLOT_OPK_LOGITS 3
+#define POLYGLOT_NOPKERNELS 4
+int polyglot_operator_times(polyglot_ctx* ctx, double* ms, int32_t* launches);
+
 /* Synchronises the stream and returns the sticky device error
- * (POLYGLOT_OK or POLYGLOT_EID), then clears it. */
+ * (POLYGLOT_OK, POLYGLOT_EID or POLYGLOT_EOFFSETS), then clears it. */
 int polyglot_status(polyglot_ctx* ctx);
 
 /* Text of the last error recorded on this context ("" if none). */

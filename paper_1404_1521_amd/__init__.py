@@ -20,21 +20,27 @@ import torch  # loaded first: the library then binds to torch's HIP runtime
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpolyglot.so")
 
-OK, EINVAL, ENULL, EBATCH, EHIP, EID, ESTATE = 0, -1, -2, -3, -4, -5, -6
+OK, EINVAL, ENULL, EBATCH, EHIP, EID, ESTATE, EOFFSETS = 0, -1, -2, -3, -4, -5, -6, -7
 SCATTER_SORTED, SCATTER_ATOMIC = 0, 1
 F32, BF16, F16 = 0, 1, 2      # storage formats of scatter_update
 OP_INC, OP_SET = 0, 1         # its operations
+GATE_RAW, GATE_SIGMOID = 0, 1  # what a recurrence's gate tensor holds
 _CODE_NAMES = {EINVAL: "EINVAL", ENULL: "ENULL", EBATCH: "EBATCH", EHIP: "EHIP", EID: "EID",
-               ESTATE: "ESTATE"}
+               ESTATE: "ESTATE", EOFFSETS: "EOFFSETS"}
+_FORMATS = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 # Every entry point declared in include/polyglot.h.
 EXPORTS = ("polyglot_init", "polyglot_destroy", "polyglot_set_stream", "polyglot_train_step",
            "polyglot_train_step_sync", "polyglot_train_steps", "polyglot_score", "polyglot_gather", "polyglot_scatter_add",
            "polyglot_scatter_update", "polyglot_scatter_add_noalloc",
            "polyglot_touched_rows", "polyglot_status", "polyglot_last_error",
-           "polyglot_set_timing", "polyglot_kernel_times")
+           "polyglot_set_timing", "polyglot_kernel_times",
+           "polyglot_dropout", "polyglot_recurrence", "polyglot_recurrence_grad",
+           "polyglot_reserve_recurrence", "polyglot_logits", "polyglot_reserve_logits",
+           "polyglot_operator_times")
 KERNEL_NAMES = ("fwdbwd", "sort", "update", "gather", "scatter", "score", "segfix", "wide_dw1",
                 "wide_g")
+OPERATOR_NAMES = ("dropout", "recurrence", "recurrence_grad", "logits")
 
 
 class PolyglotError(RuntimeError):
@@ -49,6 +55,30 @@ class Config(ctypes.Structure):
                 ("scatter_mode", ctypes.c_int32), ("max_scatter", ctypes.c_int32),
                 ("max_rows", ctypes.c_int32)]
 
+
+def _args(name, *fields):
+    """The ctypes mirror of an argument block of include/polyglot.h."""
+    kinds = {"p": ctypes.c_void_p, "i": ctypes.c_int32, "q": ctypes.c_int64,
+             "u": ctypes.c_uint32, "Q": ctypes.c_uint64, "f": ctypes.c_float}
+    return type(name, (ctypes.Structure,), {
+        "_fields_": [(n, kinds[k]) for k, names in fields for n in names.split()]})
+
+
+DropoutArgs = _args("DropoutArgs", ("p", "x add y ids site_dev"), ("q", "rows ld_x ld_add ld_y"),
+                    ("Q", "seed first_row"), ("u", "site"), ("f", "p"),
+                    ("i", "d dtype id_bytes table_rows whole_rows"))
+RecurrenceArgs = _args("RecurrenceArgs", ("p", "gate x h0 offsets h last"),
+                       ("q", "tokens ld_gate ld_x ld_h"),
+                       ("i", "nseq D group dtype offset_bytes form reverse"))
+RecurrenceGradArgs = _args("RecurrenceGradArgs",
+                           ("p", "gate x h dh h0 dlast offsets dgate dx dh0"),
+                           ("q", "tokens ld_gate ld_x ld_h ld_dh ld_dgate ld_dx"),
+                           ("i", "nseq D group dtype offset_bytes form reverse"))
+LogitsArgs = _args("LogitsArgs",
+                   ("p", "logits out history lengths prompt repetition presence frequency bias "
+                         "mask mask_rows token lse"),
+                   ("q", "ld_logits ld_out ld_history ld_bias ld_mask"),
+                   ("i", "rows V dtype history_cap masks"))
 
 _lib = None
 
@@ -79,6 +109,13 @@ def load_library():
         "polyglot_last_error": [p],
         "polyglot_set_timing": [p, ctypes.c_int],
         "polyglot_kernel_times": [p, p, p],
+        "polyglot_dropout": [p, ctypes.POINTER(DropoutArgs)],
+        "polyglot_recurrence": [p, ctypes.POINTER(RecurrenceArgs)],
+        "polyglot_recurrence_grad": [p, ctypes.POINTER(RecurrenceGradArgs)],
+        "polyglot_reserve_recurrence": [p, ctypes.c_int64, i32],
+        "polyglot_logits": [p, ctypes.POINTER(LogitsArgs)],
+        "polyglot_reserve_logits": [p, i32, i32],
+        "polyglot_operator_times": [p, p, p],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -100,6 +137,63 @@ def _dev_tensor(t, dtype, name, shape=None):
     if shape is not None and tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     return ctypes.c_void_p(t.data_ptr())
+
+
+def _row_tensor(t, dtype, name, rows, width):
+    """Pointer and row distance of a device tensor [rows][width] whose rows are
+    consecutive elements, any distance apart."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device (cuda) tensor")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != (rows, width):
+        raise ValueError(f"{name} must have shape {(rows, width)}, got {tuple(t.shape)}")
+    if t.is_contiguous():
+        return t.data_ptr(), width
+    ld, one = t.stride()
+    if one != 1 and width > 1 and rows > 0:
+        raise ValueError(f"{name} must have consecutive elements in its rows")
+    return t.data_ptr(), ld if rows > 1 else width
+
+
+def _vector(t, dtype, name, n):
+    """Pointer of a contiguous device vector of n values (None: NULL)."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous device (cuda) tensor")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != (n,):
+        raise ValueError(f"{name} must have shape {(n,)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _state(t, name, nseq, D):
+    """Pointer of a contiguous float32 device tensor [nseq][D] (None: NULL)."""
+    if t is None:
+        return None
+    p, ld = _row_tensor(t, torch.float32, name, nseq, D)
+    if ld != D:
+        raise ValueError(f"{name} must be contiguous")
+    return p
+
+
+def _format(t, name):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype not in _FORMATS:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return _FORMATS[t.dtype]
+
+
+def _flat(t, name):
+    """A [nseq][T][width] tensor as rows of tokens."""
+    return None if t is None else t if t.dim() == 2 else t.view(-1, t.shape[-1])
 
 
 NOALLOC_MAX_N = 8192  # POLYGLOT_NOALLOC_MAX_N
@@ -259,8 +353,183 @@ class Context:
         self._check(self._lib.polyglot_kernel_times(self._h, ms, n), "kernel_times")
         return {name: (ms[i], n[i]) for i, name in enumerate(KERNEL_NAMES)}
 
+    # ------------------------------------------------------------ sequences
+    def reserve_recurrence(self, max_tokens: int, max_width: int) -> None:
+        """Workspace for recurrences of up to max_tokens tokens and max_width channels."""
+        self._check(self._lib.polyglot_reserve_recurrence(self._h, max_tokens, max_width),
+                    "reserve_recurrence")
+
+    def reserve_logits(self, max_rows: int, max_vocab: int) -> None:
+        """Workspace for the choices of up to max_rows rows of max_vocab scores."""
+        self._check(self._lib.polyglot_reserve_logits(self._h, max_rows, max_vocab),
+                    "reserve_logits")
+
+    def dropout(self, x, p: float, seed: int, *, site: int = 0, site_dev=None, first_row: int = 0,
+                ids=None, add=None, whole_rows: bool = False, out=None):
+        """out[r] = dropout(x[r]) (+ add[r]), or of the rows ids[r] of a table x.  The mask
+        is a function of (seed, site + site_dev, first_row + r, column) alone and is never
+        stored; dropout_backward computes it again.  float32, bfloat16 or float16."""
+        a = DropoutArgs()
+        a.dtype = _format(x, "x")
+        if x.dim() != 2:
+            raise ValueError("x must have two dimensions")
+        rows, d = x.shape
+        a.x, a.ld_x = _row_tensor(x, x.dtype, "x", rows, d)
+        if ids is not None:
+            if ids.dtype not in (torch.int32, torch.int64):
+                raise TypeError(f"ids must be int32 or int64, got {ids.dtype}")
+            a.table_rows, rows = rows, ids.shape[0]
+            a.ids, a.id_bytes = _vector(ids, ids.dtype, "ids", rows), ids.element_size()
+        if add is not None:
+            a.add, a.ld_add = _row_tensor(add, x.dtype, "add", rows, d)
+        if out is None:
+            out = torch.empty((rows, d), dtype=x.dtype, device=x.device)
+        a.y, a.ld_y = _row_tensor(out, x.dtype, "out", rows, d)
+        a.site_dev = _vector(site_dev, torch.int32, "site_dev", 1)
+        a.rows, a.d, a.p, a.whole_rows = rows, d, p, whole_rows
+        a.seed, a.site, a.first_row = seed, site, first_row
+        self._check(self._lib.polyglot_dropout(self._h, ctypes.byref(a)), "dropout")
+        return out
+
+    def dropout_backward(self, dy, p: float, seed: int, *, site: int = 0, site_dev=None,
+                         first_row: int = 0, whole_rows: bool = False, out=None):
+        """The gradient of dropout's x (per row read, when x was a table), for the same
+        seed, site and first_row.  That of its add is dy itself."""
+        return self.dropout(dy, p, seed, site=site, site_dev=site_dev, first_row=first_row,
+                            whole_rows=whole_rows, out=out)
+
+    @staticmethod
+    def _sequences(a, x, gate, offsets, form, reverse):
+        """Fills what a recurrence and its gradient share; returns (tokens, D, gates)."""
+        a.dtype = _format(x, "x")
+        tokens, D = x.shape
+        gates = gate.shape[-1]
+        if gates < 1 or D % gates:
+            raise ValueError(f"gate has {gates} columns, which do not divide {D} channels")
+        a.gate, a.ld_gate = _row_tensor(gate, x.dtype, "gate", tokens, gates)
+        a.x, a.ld_x = _row_tensor(x, x.dtype, "x", tokens, D)
+        if offsets is not None:
+            if offsets.dtype not in (torch.int32, torch.int64):
+                raise TypeError(f"offsets must be int32 or int64, got {offsets.dtype}")
+            a.offsets = _vector(offsets, offsets.dtype, "offsets", offsets.shape[0])
+            a.offset_bytes = offsets.element_size()
+            a.nseq = offsets.shape[0] - 1
+        a.tokens, a.D, a.group, a.form, a.reverse = tokens, D, D // gates, form, reverse
+        return tokens, D, gates
+
+    def recurrence(self, gate, x, offsets=None, *, h0=None, form: int = GATE_SIGMOID,
+                   reverse: bool = False, out=None, last=None):
+        """h_t = a_t h_{t-1} + x_t (GATE_RAW) or a_t h_{t-1} + (1 - a_t) x_t (GATE_SIGMOID,
+        a the gate's sigmoid) over the sequences of x: [tokens][D] with offsets[nseq + 1],
+        [nseq][T][D] without, or one sequence [T][D].  gate has D columns, or fewer that
+        divide D, each for D / columns consecutive channels.  h0 and last are float32
+        [nseq][D].  Returns (h, last)."""
+        a = RecurrenceArgs()
+        shape = x.shape
+        a.nseq = shape[0] if x.dim() == 3 else 1
+        x, gate = _flat(x, "x"), _flat(gate, "gate")
+        tokens, D, _ = self._sequences(a, x, gate, offsets, form, reverse)
+        if out is None:
+            out = torch.empty(shape, dtype=x.dtype, device=x.device)
+        if last is None:
+            last = torch.empty((a.nseq, D), dtype=torch.float32, device=x.device)
+        a.h, a.ld_h = _row_tensor(_flat(out, "out"), x.dtype, "out", tokens, D)
+        a.h0, a.last = _state(h0, "h0", a.nseq, D), _state(last, "last", a.nseq, D)
+        self._check(self._lib.polyglot_recurrence(self._h, ctypes.byref(a)), "recurrence")
+        return out, last
+
+    def recurrence_step(self, gate, x, state=None, *, form: int = GATE_SIGMOID, out=None,
+                        last=None):
+        """One token x[nseq][D] for each of nseq sequences whose float32 states are
+        state[nseq][D].  Returns (h, the new states); last=state updates them in place."""
+        a = RecurrenceArgs()
+        a.nseq = x.shape[0]
+        tokens, D, _ = self._sequences(a, x, gate, None, form, False)
+        if out is None:
+            out = torch.empty((tokens, D), dtype=x.dtype, device=x.device)
+        if last is None:
+            last = torch.empty((tokens, D), dtype=torch.float32, device=x.device)
+        a.h, a.ld_h = _row_tensor(out, x.dtype, "out", tokens, D)
+        a.h0, a.last = _state(state, "state", tokens, D), _state(last, "last", tokens, D)
+        self._check(self._lib.polyglot_recurrence(self._h, ctypes.byref(a)), "recurrence_step")
+        return out, last
+
+    def recurrence_backward(self, gate, x, h, dh, offsets=None, *, h0=None, dlast=None,
+                            form: int = GATE_SIGMOID, reverse: bool = False, dgate=None, dx=None,
+                            dh0=None):
+        """The gradient of recurrence, for its inputs, its output h and the gradients dh of h
+        and dlast of last.  Returns (dgate, dx, dh0); dh0 is None unless h0 or dh0 is given."""
+        a = RecurrenceGradArgs()
+        shape, gate_shape = x.shape, gate.shape
+        a.nseq = shape[0] if x.dim() == 3 else 1
+        x, gate, h, dh = (_flat(t, n) for t, n in ((x, "x"), (gate, "gate"), (h, "h"), (dh, "dh")))
+        tokens, D, gates = self._sequences(a, x, gate, offsets, form, reverse)
+        if dgate is None:
+            dgate = torch.empty(gate_shape, dtype=x.dtype, device=x.device)
+        if dx is None:
+            dx = torch.empty(shape, dtype=x.dtype, device=x.device)
+        if dh0 is None and h0 is not None:
+            dh0 = torch.empty((a.nseq, D), dtype=torch.float32, device=x.device)
+        a.h, a.ld_h = _row_tensor(h, x.dtype, "h", tokens, D)
+        a.dh, a.ld_dh = _row_tensor(dh, x.dtype, "dh", tokens, D)
+        a.dgate, a.ld_dgate = _row_tensor(_flat(dgate, "dgate"), x.dtype, "dgate", tokens, gates)
+        a.dx, a.ld_dx = _row_tensor(_flat(dx, "dx"), x.dtype, "dx", tokens, D)
+        a.h0, a.dlast = _state(h0, "h0", a.nseq, D), _state(dlast, "dlast", a.nseq, D)
+        a.dh0 = _state(dh0, "dh0", a.nseq, D)
+        self._check(self._lib.polyglot_recurrence_grad(self._h, ctypes.byref(a)),
+                    "recurrence_backward")
+        return dgate, dx, dh0
+
+    def logits(self, logits, *, history=None, lengths=None, prompt=None, repetition=None,
+               presence=None, frequency=None, bias=None, mask=None, mask_rows=None, out=None,
+               write: bool = True):
+        """The scores logits[rows][V] with penalties for the words of history[rows][cap], a
+        bias[V] or [rows][V], and the mask's bits (int32 words; see polyglot_logits).
+        Returns (out, token, lse): the scores in their own dtype (out may be logits itself;
+        None with write=False), the int32 choice of each row and its float32 log-sum-exp."""
+        a = LogitsArgs()
+        a.dtype = _format(logits, "logits")
+        if logits.dim() != 2:
+            raise ValueError("logits must have two dimensions")
+        rows, V = logits.shape
+        a.rows, a.V = rows, V
+        a.logits, a.ld_logits = _row_tensor(logits, logits.dtype, "logits", rows, V)
+        if out is None and write:
+            out = torch.empty((rows, V), dtype=logits.dtype, device=logits.device)
+        if out is not None:
+            a.out, a.ld_out = _row_tensor(out, logits.dtype, "out", rows, V)
+        if history is not None:
+            a.history_cap = history.shape[1]
+            a.history, a.ld_history = _row_tensor(history, torch.int32, "history", rows,
+                                                  a.history_cap)
+            a.lengths = _vector(lengths, torch.int32, "lengths", rows)
+            a.prompt = _vector(prompt, torch.int32, "prompt", rows)
+        a.repetition = _vector(repetition, torch.float32, "repetition", rows)
+        a.presence = _vector(presence, torch.float32, "presence", rows)
+        a.frequency = _vector(frequency, torch.float32, "frequency", rows)
+        if bias is not None and bias.dim() == 1:
+            a.bias = _vector(bias, torch.float32, "bias", V)
+        elif bias is not None:
+            a.bias, a.ld_bias = _row_tensor(bias, torch.float32, "bias", rows, V)
+        if mask is not None:
+            a.masks = mask.shape[0]
+            a.mask, a.ld_mask = _row_tensor(mask, torch.int32, "mask", a.masks, (V + 31) // 32)
+            a.mask_rows = _vector(mask_rows, torch.int32, "mask_rows", rows)
+        token = torch.empty(rows, dtype=torch.int32, device=logits.device)
+        lse = torch.empty(rows, dtype=torch.float32, device=logits.device)
+        a.token, a.lse = token.data_ptr(), lse.data_ptr()
+        self._check(self._lib.polyglot_logits(self._h, ctypes.byref(a)), "logits")
+        return out, token, lse
+
+    def operator_times(self) -> dict:
+        """kernel_times for the sequence operators: {operator: (total ms, launches)}."""
+        ms = (ctypes.c_double * len(OPERATOR_NAMES))()
+        n = (ctypes.c_int32 * len(OPERATOR_NAMES))()
+        self._check(self._lib.polyglot_operator_times(self._h, ms, n), "operator_times")
+        return {name: (ms[i], n[i]) for i, name in enumerate(OPERATOR_NAMES)}
+
     def status(self) -> int:
-        """Synchronises; returns OK or EID (the sticky device flag), clearing it."""
+        """Synchronises; returns OK, EID or EOFFSETS (the sticky device flag), clearing it."""
         return self._lib.polyglot_status(self._h)
 
     def close(self):

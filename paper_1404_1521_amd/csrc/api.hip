@@ -3,81 +3,17 @@
 // event timing.
 #include "polyglot.h"
 
-#include <hip/hip_ext.h>
-#include <hip/hip_runtime.h>
-
-#include <algorithm>
 #include <cmath>
-#include <cstring>
 #include <mutex>
-#include <string>
-#include <utility>
 #include <vector>
 
+#include "context.h"
 #include "launch.h"
 #include "seg_dev.h"
 
 using namespace pg;
 
 namespace {
-
-struct GraphKey {
-  const void* p[7];
-  const void* losses;
-  int S, B;
-  float lr;
-  hipStream_t stream;
-  bool operator==(const GraphKey& o) const {
-    return std::memcmp(p, o.p, sizeof(p)) == 0 && losses == o.losses && S == o.S && B == o.B &&
-           std::memcmp(&lr, &o.lr, sizeof(float)) == 0 && stream == o.stream;
-  }
-};
-
-}  // namespace
-
-struct polyglot_ctx {
-  polyglot_config cfg{};
-  hipStream_t stream = nullptr;
-  // a step's sort depends only on its ids: it runs on a second stream,
-  // forked from `stream` and joined back before the table update.  In a
-  // multi-step call the sort of step s+1 (sort set (s+1)&1) runs while step s
-  // computes.
-  hipStream_t side = nullptr;
-  hipEvent_t ev_fork = nullptr, ev_sorted[2] = {nullptr, nullptr},
-             ev_done[2] = {nullptr, nullptr};
-  int device = 0;
-  int Hp = 0, NT = 0, K = 0, c = 0, cpw = 0;
-  bool large = false;  // hidden layer above 64 units: the three-contraction path
-  int max_entries = 0, max_tiles = 0, max_parts = 0, max_chunks = 0;
-  int seg_stride = 0, part_stride = 0;
-  Workspace ws{};
-  std::vector<void*> allocs;
-  std::string err;
-  bool have_sorted = false;
-  int last_N = 0, last_passes = 0, last_set = 0;
-  bool set_dirty = false;  // an assignment marked its rows and failed to take the marks back
-  hipGraphExec_t gexec = nullptr;
-  GraphKey gkey{};
-  bool gvalid = false;
-  // per-kernel timing
-  bool timing = false;
-  bool capturing = false;
-  std::vector<hipEvent_t> ev_pool;
-  std::vector<std::pair<int, std::pair<hipEvent_t, hipEvent_t>>> ev_marks;
-};
-
-namespace {
-
-int fail(polyglot_ctx* ctx, int code, const std::string& msg) {
-  if (ctx) ctx->err = msg;
-  return code;
-}
-
-int hip_fail(polyglot_ctx* ctx, hipError_t e, const char* what) {
-  return fail(ctx, POLYGLOT_EHIP, std::string(what) + ": " + hipGetErrorString(e));
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int bits_for(uint32_t n) {  // smallest b >= 1 with n <= 2^b
   int b = 1;
@@ -151,17 +87,6 @@ ZeroRanges sort_zero_ranges(polyglot_ctx* ctx, const SortPlan& plan, int set) {
   return z;
 }
 
-template <class T>
-hipError_t alloc(polyglot_ctx* ctx, T** p, size_t count) {
-  void* q = nullptr;
-  hipError_t e = hipMalloc(&q, std::max<size_t>(count, 1) * sizeof(T));
-  if (e == hipSuccess) {
-    ctx->allocs.push_back(q);
-    *p = static_cast<T*>(q);
-  }
-  return e;
-}
-
 void free_all(polyglot_ctx* ctx) {
   for (auto& m : ctx->ev_marks) {
     ctx->ev_pool.push_back(m.second.first);
@@ -182,49 +107,6 @@ void free_all(polyglot_ctx* ctx) {
   for (void* q : ctx->allocs) hipFree(q);
   ctx->allocs.clear();
 }
-
-hipEvent_t take_event(polyglot_ctx* ctx) {
-  if (!ctx->ev_pool.empty()) {
-    hipEvent_t ev = ctx->ev_pool.back();
-    ctx->ev_pool.pop_back();
-    return ev;
-  }
-  hipEvent_t ev = nullptr;
-  if (hipEventCreate(&ev) != hipSuccess) return nullptr;
-  return ev;
-}
-
-// Launch parameters for kernel id `kid` on stream `st`.  When timing is on
-// (and no graph is being captured) every launch made with it gets its own
-// start/stop event pair, bound to the kernel's dispatch.
-struct Timed {
-  polyglot_ctx* ctx;
-  int kid;
-  Launch L;
-  Timed(polyglot_ctx* c, int k, hipStream_t st) : ctx(c), kid(k) {
-    L.s = st;
-    if (ctx->timing && !ctx->capturing) {
-      L.owner = this;
-      L.take = &Timed::take;
-    }
-  }
-  Timed(polyglot_ctx* c, int k) : Timed(c, k, c->stream) {}
-  Timed(const Timed&) = delete;
-  Timed& operator=(const Timed&) = delete;
-  static bool take(void* owner, hipEvent_t* start, hipEvent_t* stop) {
-    Timed* t = static_cast<Timed*>(owner);
-    hipEvent_t a = take_event(t->ctx), b = take_event(t->ctx);
-    if (!a || !b) {
-      if (a) t->ctx->ev_pool.push_back(a);
-      if (b) t->ctx->ev_pool.push_back(b);
-      return false;
-    }
-    t->ctx->ev_marks.push_back({t->kid, {a, b}});
-    *start = a;
-    *stop = b;
-    return true;
-  }
-};
 
 SegArgs seg_args(polyglot_ctx* ctx, float* table, const float* Y, const SortPlan& plan, int set,
                  int N, int d, float alpha, bool step) {
@@ -1072,6 +954,8 @@ int polyglot_status(polyglot_ctx* ctx) {
     e = hipMemset(ctx->ws.flag, 0, sizeof(w));
     if (e != hipSuccess) return hip_fail(ctx, e, "status: clear flag");
     if (f & kFlagBadId) return fail(ctx, POLYGLOT_EID, "an id was outside its table");
+    if (f & kFlagBadOffset)
+      return fail(ctx, POLYGLOT_EOFFSETS, "sequence offsets did not ascend from 0 to the tokens");
     return fail(ctx, POLYGLOT_EHIP, "internal: sort position outside the entry range");
   }
   return POLYGLOT_OK;
@@ -1085,24 +969,7 @@ int polyglot_set_timing(polyglot_ctx* ctx, int enable) {
 
 int polyglot_kernel_times(polyglot_ctx* ctx, double* ms, int32_t* launches) {
   if (!ctx || !ms || !launches) return POLYGLOT_ENULL;
-  hipError_t e = hipStreamSynchronize(ctx->stream);
-  if (e == hipSuccess) e = hipStreamSynchronize(ctx->side);
-  if (e != hipSuccess) return hip_fail(ctx, e, "kernel_times: sync");
-  for (int k = 0; k < POLYGLOT_NKERNELS; ++k) {
-    ms[k] = 0.0;
-    launches[k] = 0;
-  }
-  for (auto& m : ctx->ev_marks) {
-    float t = 0.f;
-    if (hipEventElapsedTime(&t, m.second.first, m.second.second) == hipSuccess) {
-      ms[m.first] += t;
-      launches[m.first] += 1;
-    }
-    ctx->ev_pool.push_back(m.second.first);
-    ctx->ev_pool.push_back(m.second.second);
-  }
-  ctx->ev_marks.clear();
-  return POLYGLOT_OK;
+  return collect_times(ctx, 0, POLYGLOT_NKERNELS, ms, launches, "kernel_times: sync");
 }
 
 const char* polyglot_last_error(const polyglot_ctx* ctx) { return ctx ? ctx->err.c_str() : ""; }

@@ -36,6 +36,7 @@ constexpr int kSmallBins = 1 << kSmallDigitBits;
 // Sticky device error bits.
 constexpr uint32_t kFlagBadId = 1u;
 constexpr uint32_t kFlagInternal = 2u;  // a sort position fell outside [0, N): a library bug
+constexpr uint32_t kFlagBadOffset = 4u; // sequence offsets not ascending from 0 to the token count
 // Status words written on the device (the values of POLYGLOT_OK and POLYGLOT_EID).
 constexpr int32_t kStatusOk = 0;
 constexpr int32_t kStatusBadId = -5;
