@@ -12,7 +12,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libpolyglot.so")
-SOURCES = ["kernels.hip", "api.hip", "operators.hip", "operators_api.hip"]
+SOURCES = ["kernels.hip", "api.hip", "operators.hip",
+           "recurrence.hip", "operators_api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",

@@ -104,6 +104,8 @@ void free_all(polyglot_ctx* ctx) {
   }
   if (ctx->side) hipStreamDestroy(ctx->side);
   ctx->side = nullptr;
+  if (ctx->op.rec_head) hipFree(ctx->op.rec_head);
+  ctx->op = OpWorkspace{};
   for (void* q : ctx->allocs) hipFree(q);
   ctx->allocs.clear();
 }

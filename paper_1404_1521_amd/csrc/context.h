@@ -32,6 +32,7 @@ struct GraphKey {
 struct OpWorkspace {
   int64_t rec_tokens = 0;
   int rec_D = 0;
+  uint64_t *rec_head = nullptr, *rec_words = nullptr;  // one block
   int log_rows = 0, log_V = 0;
 };
 

@@ -4,6 +4,7 @@
 #include "polyglot.h"
 
 #include "common.h"
+#include "formats.h"
 #include "launch.h"
 
 namespace pg {
@@ -35,13 +36,35 @@ struct RecCall {
   int down;            // 1: the scan goes from a sequence's last token to its first
 };
 
+// How a scan is cut (ScanLds has the rest).
+struct ScanPlan {
+  int lanes_log2;        // lanes of a row of threads: four channels each
+  int tiles, chunks;     // of the channels and of the tokens; a workgroup for each pair
+  int lanes_per_group, groups_per_tile;  // shared gates
+  uint64_t* head;        // {tag << 32 | next chunk, workgroups done}; null: no chunk waits
+  uint64_t* words;       // [chunks * tiles][2][4][lanes]
+};
+
 struct LogitsCall {
   polyglot_logits_args a;
   uint32_t* flag;
 };
 
+// Calls f with a value of the storage type `dtype` (POLYGLOT_F32, _BF16, _F16).
+template <class F>
+hipError_t by_format(int dtype, F f) {
+  if (dtype == POLYGLOT_F32) return f(float{});
+  if (dtype == POLYGLOT_BF16) return f(BF16{});
+  return f(F16{});
+}
+
 hipError_t launch_dropout(const DropoutCall& c, const Launch& L);
-hipError_t launch_recurrence(const RecCall& c, int dtype, int form, bool grad, const Launch& L);
+// head: {.., ..} zeroed once with head[0] = 1 << 32, words: zeroed once; both only for
+// calls of other than one token per sequence, sized by scan_words.
+hipError_t launch_recurrence(const RecCall& c, int dtype, int form, bool grad, uint64_t* head,
+                             uint64_t* words, const Launch& L);
+// Words of the scans of up to `tokens` tokens and D channels.
+size_t scan_words(int64_t tokens, int D);
 hipError_t launch_logits(const LogitsCall& c, const Launch& L);
 
 }  // namespace pg

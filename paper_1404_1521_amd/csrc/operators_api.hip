@@ -15,6 +15,8 @@ namespace {
 // Kernel ids of these operators among a context's timing marks.
 constexpr int kOpKernels = POLYGLOT_NKERNELS;
 
+constexpr size_t kHeadWords = 64;  // the launch's own words, before those that join its parts
+
 // Runs an entry point's body; nothing that it throws (a message that finds no
 // memory) passes the C boundary.
 template <class F>
@@ -92,7 +94,7 @@ int check_recurrence(polyglot_ctx* ctx, const A& a, const std::string& what) {
     return fail(ctx, POLYGLOT_EINVAL, what + ": misaligned offsets");
   // one token per sequence needs no scan; other calls use the reserved workspace
   if ((a.offsets || a.tokens != a.nseq) &&
-      (a.tokens > ctx->op.rec_tokens || a.D > ctx->op.rec_D))
+      (!ctx->op.rec_head || a.tokens > ctx->op.rec_tokens || a.D > ctx->op.rec_D))
     return fail(ctx, POLYGLOT_EBATCH, what + ": above the reserved tokens or channels");
   return POLYGLOT_OK;
 }
@@ -159,7 +161,7 @@ int polyglot_recurrence(polyglot_ctx* ctx, const polyglot_recurrence_args* args)
     c.fin = a.last;
     c.down = a.reverse != 0;
     Timed tm(ctx, kOpKernels + POLYGLOT_OPK_RECURRENCE);
-    const hipError_t e = launch_recurrence(c, a.dtype, a.form, false, tm.L);
+    const hipError_t e = launch_recurrence(c, a.dtype, a.form, false, ctx->op.rec_head, ctx->op.rec_words, tm.L);
     return e == hipSuccess ? POLYGLOT_OK : hip_fail(ctx, e, "recurrence launch");
   });
 }
@@ -198,7 +200,7 @@ int polyglot_recurrence_grad(polyglot_ctx* ctx, const polyglot_recurrence_grad_a
     c.fin = a.dh0;
     c.down = a.reverse == 0;
     Timed tm(ctx, kOpKernels + POLYGLOT_OPK_RECURRENCE_GRAD);
-    const hipError_t e = launch_recurrence(c, a.dtype, a.form, true, tm.L);
+    const hipError_t e = launch_recurrence(c, a.dtype, a.form, true, ctx->op.rec_head, ctx->op.rec_words, tm.L);
     return e == hipSuccess ? POLYGLOT_OK : hip_fail(ctx, e, "recurrence_grad launch");
   });
 }
@@ -208,8 +210,25 @@ int polyglot_reserve_recurrence(polyglot_ctx* ctx, int64_t max_tokens, int32_t m
   return entry([&] {
     if (max_tokens < 0 || max_tokens > INT32_MAX || max_D < 0)
       return fail(ctx, POLYGLOT_EINVAL, "reserve_recurrence: bad token count or width");
-    ctx->op.rec_tokens = max_tokens;
-    ctx->op.rec_D = max_D;
+    OpWorkspace& op = ctx->op;
+    hipError_t e = hipStreamSynchronize(ctx->stream);
+    if (e != hipSuccess) return hip_fail(ctx, e, "reserve_recurrence: sync");
+    if (op.rec_head) e = hipFree(op.rec_head);
+    op.rec_head = op.rec_words = nullptr;
+    op.rec_tokens = op.rec_D = 0;
+    // {tag, next chunk} and {workgroups done}, 64 words apart from the chunks' words;
+    // the tag of words that nothing has written is 0, the first launch's is 1
+    const size_t n = kHeadWords + scan_words(max_tokens, max_D);
+    const uint64_t first = (uint64_t)1 << 32;
+    if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void**>(&op.rec_head), n * sizeof(uint64_t));
+    if (e == hipSuccess) e = hipMemsetAsync(op.rec_head, 0, n * sizeof(uint64_t), ctx->stream);
+    if (e == hipSuccess)
+      e = hipMemcpyAsync(op.rec_head, &first, sizeof(first), hipMemcpyHostToDevice, ctx->stream);
+    if (e == hipSuccess) e = hipStreamSynchronize(ctx->stream);
+    if (e != hipSuccess) return hip_fail(ctx, e, "reserve_recurrence");
+    op.rec_words = op.rec_head + kHeadWords;
+    op.rec_tokens = max_tokens;
+    op.rec_D = max_D;
     return POLYGLOT_OK;
   });
 }

@@ -1,0 +1,92 @@
+// Launches of the gated linear recurrence.
+#include "operators.h"
+
+#include <algorithm>
+
+#include "recurrence_dev.h"
+
+namespace pg {
+
+namespace {
+
+bool vector_rows(const void* p, int64_t ld, size_t size) {
+  return reinterpret_cast<uintptr_t>(p) % (4 * size) == 0 && ld % 4 == 0;
+}
+
+// Lanes of a row of threads: as few as hold all channels, so that narrow layers
+// have more rows of tokens; at least what a group takes.
+ScanPlan scan_plan(int64_t tokens, int D, int group, int R) {
+  ScanPlan p{};
+  p.lanes_per_group = group > 1 ? ceil_div(group, 4) : 1;
+  const int64_t lanes = group > 1 ? (int64_t)p.lanes_per_group * (D / group) : ceil_div(D, 4);
+  int log2 = 3;
+  while (log2 < 6 && (1 << log2) < lanes) ++log2;
+  p.lanes_log2 = log2;
+  const int CT = 1 << log2;
+  p.groups_per_tile = CT / p.lanes_per_group;
+  p.tiles = group > 1 ? ceil_div(D / group, p.groups_per_tile) : ceil_div(D, 4 * CT);
+  const int L = (kBlock / CT) * R;
+  p.chunks = std::max(1, (int)((tokens + L - 1) / L));
+  return p;
+}
+
+template <class T, int FORM, bool GRAD>
+hipError_t launch_scan(const RecCall& c, uint64_t* head, uint64_t* words, const Launch& L) {
+  constexpr int R = scan_tokens<T, GRAD>();
+  static_assert(kScanMaxRows * R <= kScanMaxTokens, "places of a chunk");
+  ScanPlan p = scan_plan(c.tokens, c.D, c.group, R);
+  p.head = head;
+  p.words = words;
+  const bool shared = c.group > 1;
+  const bool vec = c.D % 4 == 0 && (shared ? c.group % 4 == 0 : vector_rows(c.gate, c.ld_gate, sizeof(T))) &&
+                   (!c.x || vector_rows(c.x, c.ld_x, sizeof(T))) &&
+                   vector_rows(c.out, c.ld_out, sizeof(T)) &&
+                   (!GRAD || (vector_rows(c.h, c.ld_h, sizeof(T)) &&
+                              vector_rows(c.dh, c.ld_dh, sizeof(T)) &&
+                              (shared || vector_rows(c.dgate, c.ld_dgate, sizeof(T)))));
+  auto k = shared ? (vec ? k_scan<T, FORM, GRAD, true, true, R> : k_scan<T, FORM, GRAD, true, false, R>)
+                  : (vec ? k_scan<T, FORM, GRAD, false, true, R>
+                         : k_scan<T, FORM, GRAD, false, false, R>);
+  return pg_launch(k, dim3(p.chunks * p.tiles), dim3(kBlock), 0, L, c, p);
+}
+
+template <class T, int FORM>
+hipError_t launch_step(const RecCall& c, const Launch& L) {
+  const bool vec = c.D % 4 == 0 && vector_rows(c.x, c.ld_x, sizeof(T)) &&
+                   vector_rows(c.out, c.ld_out, sizeof(T)) && vector_rows(c.init, 0, 4) &&
+                   vector_rows(c.fin, 0, 4) &&
+                   (c.group > 1 || vector_rows(c.gate, c.ld_gate, sizeof(T)));
+  const int64_t total = (int64_t)c.tokens * ceil_div(c.D, 4);
+  const int grid = (int)std::min<int64_t>((total + kBlock - 1) / kBlock, 16 * kCus);
+  return pg_launch(vec ? k_recurrence_step<T, FORM, true> : k_recurrence_step<T, FORM, false>,
+                   dim3(grid), dim3(kBlock), 0, L, c);
+}
+
+}  // namespace
+
+size_t scan_words(int64_t tokens, int D) {
+  // Chunks are shortest where a row has 64 lanes.  Lanes that a group leaves idle at
+  // most double the slots (a group of two channels in a lane of four; 33 lanes of 64).
+  const int64_t L = kBlock / kWave * 8;
+  const size_t slots = 2 * (size_t)D + 4 * kWave;
+  return (size_t)((tokens + L - 1) / L + 1) * slots * 2;
+}
+
+hipError_t launch_recurrence(const RecCall& c, int dtype, int form, bool grad, uint64_t* head,
+                             uint64_t* words, const Launch& L) {
+  constexpr int raw = POLYGLOT_GATE_RAW, sig = POLYGLOT_GATE_SIGMOID;
+  const bool single = !c.offsets && c.tokens == c.nseq;  // every token starts a sequence
+  return by_format(dtype, [&](auto v) {
+    using T = decltype(v);
+    if (single && !grad)
+      return form == raw ? launch_step<T, raw>(c, L) : launch_step<T, sig>(c, L);
+    uint64_t* h = single ? nullptr : head;
+    if (grad)
+      return form == raw ? launch_scan<T, raw, true>(c, h, words, L)
+                         : launch_scan<T, sig, true>(c, h, words, L);
+    return form == raw ? launch_scan<T, raw, false>(c, h, words, L)
+                       : launch_scan<T, sig, false>(c, h, words, L);
+  });
+}
+
+}  // namespace pg
