@@ -271,9 +271,8 @@ int polyglot_kernel_times(polyglot_ctx* ctx, double* ms, int32_t* launches);
  * 32 bits; each output is rounded to its format once (to nearest even).  Calls
  * are asynchronous on the context's stream and may be captured into a HIP
  * graph.  The argument blocks are read before the call returns; fields that
- * are not set must be zero.  Vector loads and stores are used where rows and
- * pointers are aligned to 16 bytes (8 for rows of 16-bit elements); results
- * do not depend on it.  Host-detectable errors: POLYGLOT_ENULL, POLYGLOT_EINVAL,
+ * are not set must be zero.  Results do not depend on strides or alignment.
+ * Host-detectable errors: POLYGLOT_ENULL, POLYGLOT_EINVAL,
  * POLYGLOT_EBATCH (above the reserved workspace), nothing enqueued. */
 
 /* Dropout with a mask that is computed and never stored.
@@ -433,7 +432,9 @@ typedef struct {
   int32_t* token;
   float* lse;
   int64_t ld_logits, ld_out, ld_history, ld_bias, ld_mask;
-  int32_t rows, V, dtype, history_cap, masks;
+  int32_t rows;
+  int32_t V;              /* 1 .. 2^30 */
+  int32_t dtype, history_cap, masks;
 } polyglot_logits_args;
 int polyglot_logits(polyglot_ctx* ctx, const polyglot_logits_args* args);
 

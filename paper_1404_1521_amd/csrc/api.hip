@@ -104,7 +104,8 @@ void free_all(polyglot_ctx* ctx) {
   }
   if (ctx->side) hipStreamDestroy(ctx->side);
   ctx->side = nullptr;
-  if (ctx->op.rec_head) hipFree(ctx->op.rec_head);
+  for (uint64_t* q : {ctx->op.rec_head, ctx->op.log_head})
+    if (q) hipFree(q);
   ctx->op = OpWorkspace{};
   for (void* q : ctx->allocs) hipFree(q);
   ctx->allocs.clear();

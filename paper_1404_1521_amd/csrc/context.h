@@ -34,6 +34,7 @@ struct OpWorkspace {
   int rec_D = 0;
   uint64_t *rec_head = nullptr, *rec_words = nullptr;  // one block
   int log_rows = 0, log_V = 0;
+  uint64_t* log_head = nullptr;  // [log_rows], then the parts' words
 };
 
 }  // namespace pg

@@ -45,11 +45,16 @@ struct Elem<F16> {
   }
 };
 
-// Four elements in a row: 16 bytes of float32 or 8 of a 16-bit format.  VEC: as one
-// aligned word; otherwise element by element, the first n of them.
+// Four elements in a row, in one load or store: 16 bytes of float32 or 8 of a
+// 16-bit format, aligned to the element only (the hardware takes any address; an
+// access that crosses a cache line costs a second one).  Without VEC element by
+// element, the first n of them.
+typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u2_any __attribute__((ext_vector_type(2), aligned(2)));
 template <class T>
 struct Quad {
-  uint2 raw;
+  typedef u2_any any;
+  u2_any raw;
   __device__ __forceinline__ float get(int i) const {
     const uint32_t w = i < 2 ? raw.x : raw.y;
     return Elem<T>::get(T{(uint16_t)(i & 1 ? w >> 16 : w)});
@@ -57,6 +62,7 @@ struct Quad {
 };
 template <>
 struct Quad<float> {
+  typedef f4_any any;
   f4 raw;
   __device__ __forceinline__ float get(int i) const { return raw[i]; }
 };
@@ -82,7 +88,7 @@ template <class T, bool VEC>
 __device__ __forceinline__ Quad<T> load_quad(const T* p, int n) {
   Quad<T> q{};
   if constexpr (VEC) {
-    q.raw = *reinterpret_cast<const decltype(q.raw)*>(p);
+    q.raw = *reinterpret_cast<const typename Quad<T>::any*>(p);
   } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) q.raw[i] = i < n ? p[i] : 0.f;
@@ -90,7 +96,7 @@ __device__ __forceinline__ Quad<T> load_quad(const T* p, int n) {
     uint32_t h[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) h[i] = i < n ? p[i].bits : 0u;
-    q.raw = uint2{h[0] | h[1] << 16, h[2] | h[3] << 16};
+    q.raw = u2_any{h[0] | h[1] << 16, h[2] | h[3] << 16};
   }
   return q;
 }
@@ -98,14 +104,43 @@ __device__ __forceinline__ Quad<T> load_quad(const T* p, int n) {
 template <class T, bool VEC>
 __device__ __forceinline__ void store_quad(T* p, const float (&v)[4], int n) {
   if constexpr (VEC && sizeof(T) == 4) {
-    st4(p, f4{v[0], v[1], v[2], v[3]});
+    *reinterpret_cast<f4_any*>(p) = f4_any{v[0], v[1], v[2], v[3]};
   } else if constexpr (VEC) {
-    *reinterpret_cast<uint2*>(p) = uint2{put2(v[0], v[1], T{}), put2(v[2], v[3], T{})};
+    *reinterpret_cast<u2_any*>(p) = u2_any{put2(v[0], v[1], T{}), put2(v[2], v[3], T{})};
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (i < n) p[i] = Elem<T>::put(settled(v[i]));
   }
 }
+
+// Eight elements in a row, likewise.
+typedef uint32_t u4_any __attribute__((ext_vector_type(4), aligned(2)));
+template <class T>
+struct Oct {
+  u4_any raw;
+  __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const u4_any*>(p); }
+  __device__ __forceinline__ float get(int i) const {
+    const uint32_t w = raw[i / 2];
+    return Elem<T>::get(T{(uint16_t)(i & 1 ? w >> 16 : w)});
+  }
+  static __device__ __forceinline__ void store(T* p, const float (&v)[8]) {
+    *reinterpret_cast<u4_any*>(p) = u4_any{put2(v[0], v[1], T{}), put2(v[2], v[3], T{}),
+                                           put2(v[4], v[5], T{}), put2(v[6], v[7], T{})};
+  }
+};
+template <>
+struct Oct<float> {
+  f4_any lo, hi;
+  __device__ __forceinline__ void load(const float* p) {
+    lo = *reinterpret_cast<const f4_any*>(p);
+    hi = *reinterpret_cast<const f4_any*>(p + 4);
+  }
+  __device__ __forceinline__ float get(int i) const { return i < 4 ? lo[i & 3] : hi[i & 3]; }
+  static __device__ __forceinline__ void store(float* p, const float (&v)[8]) {
+    *reinterpret_cast<f4_any*>(p) = f4_any{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f4_any*>(p + 4) = f4_any{v[4], v[5], v[6], v[7]};
+  }
+};
 
 }  // namespace pg

@@ -1,44 +1,132 @@
 // A vocabulary's scores made ready for a choice: penalties for repeated words,
 // biases, a mask of allowed words; the choice and the row's log-sum-exp.
+//
+// A workgroup takes a part of a row, up to 8,192 words, into registers, counts
+// the row's history in LDS, one counter for each of its words, and applies the
+// rules on the way out: the scores are read once and written once.  The parts of
+// a row are joined by the workgroup that finishes last, from words in memory that
+// carry the launch's tag, in the order of the parts.
 #pragma once
+#include <type_traits>
+
 #include "formats.h"
 #include "operators.h"
 
 namespace pg {
 
-constexpr int kLogitsTile = 8192;          // words whose counts are in LDS at a time
-constexpr uint32_t kSeenOnly = 0x80000000u;  // in the history; the low bits count its made part
+constexpr uint32_t kLogitsSpinLimit = 1u << 22;  // a wait that only a library bug makes
+constexpr uint32_t kInHistory = 0x80000000u;  // of a counter; the low bits count the made part
 
-// The score of word v of a row.  Products and sums are kept apart: a fused
-// multiply-add would round other scores to equal, or equal ones apart.
 struct RowRules {
   float rep, freq, pres;
 };
+// Products and sums are kept apart: a fused multiply-add would round other scores
+// to equal, or equal ones apart.
 __device__ __forceinline__ float ruled(float l, uint32_t seen, const RowRules& k) {
   if (seen) l = l > 0.f ? __fdiv_rn(l, k.rep) : __fmul_rn(l, k.rep);
-  const uint32_t n = seen & ~kSeenOnly;
+  const uint32_t n = seen & ~kInHistory;
   if (n) l = __fsub_rn(l, __fadd_rn(__fmul_rn(k.freq, (float)n), k.pres));
   return l;
 }
 
-// One workgroup per row.
-template <class T>
-__global__ __launch_bounds__(kBlock) void k_logits(LogitsCall c) {
-  __shared__ uint32_t seen[kLogitsTile];
-  __shared__ float red_m[kBlock], red_s[kBlock];
-  __shared__ int red_v[kBlock];
-  const polyglot_logits_args& a = c.a;
-  const int r = blockIdx.x, t = threadIdx.x;
-  const T* in = static_cast<const T*>(a.logits) + (int64_t)r * a.ld_logits;
-  T* out = a.out ? static_cast<T*>(a.out) + (int64_t)r * a.ld_out : nullptr;
-  const RowRules rules{a.repetition ? a.repetition[r] : 1.f, a.frequency ? a.frequency[r] : 0.f,
-                       a.presence ? a.presence[r] : 0.f};
-  const int32_t* hist = a.history ? a.history + (int64_t)r * a.ld_history : nullptr;
-  int len = 0, prompt = 0;
-  if (hist) {
-    len = a.lengths ? min(max(a.lengths[r], 0), a.history_cap) : a.history_cap;
-    prompt = a.prompt ? min(max(a.prompt[r], 0), a.history_cap) : 0;
+__device__ __forceinline__ float exp_fast(float x) {
+  return __builtin_amdgcn_exp2f(1.44269504088896341f * x);
+}
+
+// e^l over a base no smaller than any l of a sum: equal infinities count once, a
+// base of -infinity has no terms.
+__device__ __forceinline__ float exp_over(float l, float base) {
+  if (l == base) return base == -__builtin_inff() ? 0.f : 1.f;
+  return exp_fast(l - base);
+}
+
+// Reductions over a wave in a fixed order, with DPP moves (as wave_incl_scan); the
+// result is in every lane.
+template <class V, class Op>
+__device__ __forceinline__ V wave_reduce(V v, V none, Op op) {
+  const auto moved = [&](auto ctrl, auto rows) {
+    return __builtin_bit_cast(
+        V, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v),
+                                       decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+  };
+  v = op(v, moved(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{}));
+  v = op(v, moved(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{}));
+  v = op(v, moved(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{}));
+  v = op(v, moved(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{}));
+  v = op(v, moved(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{}));
+  v = op(v, moved(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{}));
+  return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+
+// LDS of the reductions.
+struct LogitsLds {
+  float m[kWavesPerBlock], s[kWavesPerBlock];
+  int w[kWavesPerBlock];
+  uint64_t arrived;
+};
+
+constexpr int kNoWord = 0x7fffffff;
+
+// The workgroup's choice: the largest m, and the lowest w of the threads that have
+// it (m -infinity: no word).  Every thread gets it.
+__device__ __forceinline__ void choose(float& m, int& w, LogitsLds& l) {
+  const int wave = threadIdx.x / kWave;
+  const auto larger = [](float a, float b) { return a > b ? a : b; };
+  const auto lower = [](int a, int b) { return a < b ? a : b; };
+  const float wm = wave_reduce(m, -__builtin_inff(), larger);
+  const int ww = wave_reduce(m == wm ? w : kNoWord, kNoWord, lower);
+  if ((threadIdx.x & (kWave - 1)) == 0) l.m[wave] = wm, l.w[wave] = ww;
+  __syncthreads();
+  m = l.m[0];
+  w = l.w[0];
+#pragma unroll
+  for (int i = 1; i < kWavesPerBlock; ++i)
+    if (l.m[i] > m || (l.m[i] == m && l.w[i] < w)) m = l.m[i], w = l.w[i];
+}
+
+__device__ __forceinline__ float total(float s, LogitsLds& l) {
+  s = wave_reduce(s, 0.f, [](float a, float b) { return a + b; });
+  if ((threadIdx.x & (kWave - 1)) == 0) l.s[threadIdx.x / kWave] = s;
+  __syncthreads();
+  s = l.s[0];
+#pragma unroll
+  for (int i = 1; i < kWavesPerBlock; ++i) s += l.s[i];
+  return s;
+}
+
+// A part's or a row's log-sum-exp of sum s over base m.
+__device__ __forceinline__ float log_sum(float m, float s) {
+  if (s != s) return s;
+  return __builtin_isinf(m) ? m : m + 0.69314718055994531f * __builtin_amdgcn_logf(s);
+}
+
+__device__ __forceinline__ void publish_word(uint64_t* w, uint32_t v, uint32_t tag) {
+  __hip_atomic_store(w, (uint64_t)tag << 32 | v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// A word that has been or is being published with this tag.
+__device__ __forceinline__ uint32_t await_word(const uint64_t* w, uint32_t tag, uint32_t* flag) {
+  for (uint32_t spins = 0;; ++spins) {
+    const uint64_t x = __hip_atomic_load(w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if ((uint32_t)(x >> 32) == tag) return (uint32_t)x;
+    if (spins > kLogitsSpinLimit) {
+      atomicOr(flag, kFlagInternal);
+      return 0;
+    }
+    __builtin_amdgcn_s_sleep(1);
   }
+}
+
+// E words per thread, in quads 4 * 256 words apart.
+template <class T, int E>
+__global__ __launch_bounds__(kBlock) void k_logits(LogitsCall c) {
+  constexpr int Q = E / 4;
+  __shared__ __align__(16) uint32_t seen[E * kBlock];
+  __shared__ LogitsLds lds;
+  const polyglot_logits_args& a = c.a;
+  const int t = threadIdx.x;
+  const int r = blockIdx.x / c.tiles, tile = blockIdx.x - r * c.tiles;
+  const int v0 = tile * (E * kBlock);
+  const T* in = static_cast<const T*>(a.logits) + (int64_t)r * a.ld_logits;
   const float* bias = a.bias ? a.bias + (int64_t)r * a.ld_bias : nullptr;
   const uint32_t* mask = nullptr;
   if (a.mask) {
@@ -49,56 +137,130 @@ __global__ __launch_bounds__(kBlock) void k_logits(LogitsCall c) {
     }
     if (m >= 0) mask = a.mask + (int64_t)m * a.ld_mask;
   }
-  float best = -__builtin_inff(), top = -__builtin_inff(), sum = 0.f;
-  int word = -1;
-  for (int v0 = 0; v0 < a.V; v0 += kLogitsTile) {
-    const int n = min(kLogitsTile, a.V - v0);
+  // the part's scores, biases and mask in flight
+  Quad<T> x[Q];
+  Quad<float> bs[Q];
+  uint32_t allow[Q];
+  int n[Q];
+#pragma unroll
+  for (int g = 0; g < Q; ++g) {
+    const int v = v0 + (g * kBlock + t) * 4;
+    n[g] = max(0, min(4, a.V - v));
+    bs[g] = Quad<float>{};
+    allow[g] = 0xfu;
+    if (n[g] == 4) {
+      x[g] = load_quad<T, true>(in + v, 4);
+      if (bias) bs[g] = load_quad<float, true>(bias + v, 4);
+    } else {
+      x[g] = load_quad<T, false>(in + v, n[g]);
+      if (bias) bs[g] = load_quad<float, false>(bias + v, n[g]);
+    }
+    if (mask && n[g] > 0) allow[g] = mask[v >> 5] >> (v & 31);
+  }
+  uint32_t tag = 0;
+  if (c.head && t == 0)  // the row's tag moves on once all its parts are in
+    tag = (uint32_t)(__hip_atomic_load(c.head + r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >> 32);
+  const RowRules rules{a.repetition ? a.repetition[r] : 1.f, a.frequency ? a.frequency[r] : 0.f,
+                       a.presence ? a.presence[r] : 0.f};
+  int len = 0, prompt = 0;
+  if (a.history) {
+    len = a.lengths ? min(max(a.lengths[r], 0), a.history_cap) : a.history_cap;
+    prompt = a.prompt ? min(max(a.prompt[r], 0), a.history_cap) : 0;
+  }
+  if (len > 0) {
+#pragma unroll
+    for (int g = 0; g < Q; ++g)
+      *reinterpret_cast<uint4*>(seen + (g * kBlock + t) * 4) = uint4{0u, 0u, 0u, 0u};
     __syncthreads();
-    for (int i = t; i < n; i += kBlock) seen[i] = 0;
-    __syncthreads();
-    for (int k = t; k < len; k += kBlock) {
-      const int id = hist[k];
-      if (id >= a.V) atomicOr(c.flag, kFlagBadId);
-      const int i = id - v0;
-      if (id >= v0 && i < n) {
-        atomicOr(&seen[i], kSeenOnly);
-        if (k >= prompt) atomicAdd(&seen[i], 1u);
+    const int32_t* hist = a.history + (int64_t)r * a.ld_history;
+    constexpr int kAhead = 4;
+    for (int k0 = t; k0 < len; k0 += kAhead * kBlock) {
+      int id[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) id[j] = k0 + j * kBlock < len ? hist[k0 + j * kBlock] : -1;
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        if (id[j] >= a.V) atomicOr(c.flag, kFlagBadId);
+        const uint32_t i = (uint32_t)(id[j] - v0);
+        if (id[j] >= v0 && i < (uint32_t)(E * kBlock)) {
+          atomicOr(&seen[i], kInHistory);
+          if (k0 + j * kBlock >= prompt) atomicAdd(&seen[i], 1u);
+        }
       }
     }
     __syncthreads();
-    for (int i = t; i < n; i += kBlock) {
-      const int v = v0 + i;
-      float l = ruled(Elem<T>::get(in[v]), seen[i], rules);
-      if (bias) l = __fadd_rn(l, bias[v]);
-      if (mask && !(mask[v >> 5] >> (v & 31) & 1u)) l = -__builtin_inff();
-      if (out) out[v] = Elem<T>::put(l);
-      if (l > best) best = l, word = v;
-      if (l > top) {
-        if (top != -__builtin_inff()) sum *= __expf(top - l);
-        top = l;
-      }
-      if (l != l) sum = l;
-      else if (l != -__builtin_inff()) sum += l == top ? 1.f : __expf(l - top);
+  }
+  T* out = a.out ? static_cast<T*>(a.out) + (int64_t)r * a.ld_out : nullptr;
+  float l[E];
+  float m = -__builtin_inff();
+  int w = kNoWord;
+#pragma unroll
+  for (int g = 0; g < Q; ++g) {
+    const int v = v0 + (g * kBlock + t) * 4;
+    uint4 k{0u, 0u, 0u, 0u};
+    if (len > 0) k = *reinterpret_cast<const uint4*>(seen + (g * kBlock + t) * 4);
+    const uint32_t ks[4] = {k.x, k.y, k.z, k.w};
+    float o[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float s = ruled(x[g].get(j), ks[j], rules);
+      if (bias) s = __fadd_rn(s, bs[g].get(j));
+      if (!(allow[g] >> j & 1u)) s = -__builtin_inff();
+      o[j] = s;
+      l[4 * g + j] = j < n[g] ? s : -__builtin_inff();
+      if (l[4 * g + j] > m) m = l[4 * g + j], w = v + j;
+    }
+    if (out) {
+      if (n[g] == 4) store_quad<T, true>(out + v, o, 4);
+      else store_quad<T, false>(out + v, o, n[g]);
     }
   }
-  red_m[t] = best;
-  red_v[t] = word;
-  red_s[t] = sum;
-  __syncthreads();
-  if (t != 0) return;
-  for (int i = 1; i < kBlock; ++i) {
-    if (red_m[i] > best || (red_m[i] == best && red_v[i] >= 0 && red_v[i] < word)) {
-      best = red_m[i];
-      word = red_v[i];
-    }
-  }
-  if (a.token) a.token[r] = word;
+  if (!c.head) return;
+
+  choose(m, w, lds);
+  float s = 0.f;
   if (a.lse) {
-    float s = 0.f;
-    for (int i = 0; i < kBlock; ++i)
-      s += red_m[i] == best ? red_s[i] : red_s[i] * __expf(red_m[i] - best);
-    // infinities have no finite share of the sum
-    a.lse[r] = s != s ? s : (best == __builtin_inff() || s == 0.f) ? best : best + __logf(s);
+#pragma unroll
+    for (int i = 0; i < E; ++i) s += exp_over(l[i], m);
+    s = total(s, lds);
+  }
+  uint64_t* words = c.words + (int64_t)r * c.stride * 3;
+  if (t == 0) {
+    publish_word(words + tile * 3, __float_as_uint(m), tag);
+    publish_word(words + tile * 3 + 1, (uint32_t)w, tag);
+    publish_word(words + tile * 3 + 2, __float_as_uint(s), tag);
+    lds.arrived = __hip_atomic_fetch_add(c.head + r, (uint64_t)1, __ATOMIC_RELAXED,
+                                         __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if ((uint32_t)lds.arrived != (uint32_t)c.tiles - 1) return;
+
+  // the last part: the row's choice, then its sum over that choice
+  tag = (uint32_t)(lds.arrived >> 32);
+  m = -__builtin_inff();
+  w = kNoWord;
+  for (int j = t; j < c.tiles; j += kBlock) {
+    const float pm = __uint_as_float(await_word(words + j * 3, tag, c.flag));
+    const int pw = (int)await_word(words + j * 3 + 1, tag, c.flag);
+    if (pm > m || (pm == m && pw < w)) m = pm, w = pw;
+  }
+  __syncthreads();
+  choose(m, w, lds);
+  if (a.lse) {
+    s = 0.f;
+    for (int j = t; j < c.tiles; j += kBlock) {
+      const float pm = __uint_as_float(await_word(words + j * 3, tag, c.flag));
+      const float ps = __uint_as_float(await_word(words + j * 3 + 2, tag, c.flag));
+      s += ps * exp_over(pm, m);
+    }
+    s = total(s, lds);
+  }
+  if (t == 0) {
+    if (a.token) a.token[r] = w == kNoWord ? -1 : w;
+    if (a.lse) a.lse[r] = log_sum(m, s);
+    const uint32_t next = tag + 1 ? tag + 1 : 1u;
+    __hip_atomic_store(c.head + r, (uint64_t)next << 32, __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
   }
 }
 

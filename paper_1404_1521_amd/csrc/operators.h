@@ -14,6 +14,8 @@ struct DropoutCall {
   uint32_t* flag;
   uint32_t threshold;  // an element is dropped where its 16 bits are below
   float scale;         // 65536 / (65536 - threshold); 0 where everything is dropped
+  int groups;          // of eight columns, in a row
+  uint32_t groups_inv; // ceil(2^32 / groups)
 };
 
 // The recurrence and its gradient are one scan, s = c s + b, in one of the two
@@ -48,6 +50,10 @@ struct ScanPlan {
 struct LogitsCall {
   polyglot_logits_args a;
   uint32_t* flag;
+  int tiles;             // parts of a row, a workgroup each
+  uint64_t* head;        // [rows] tag << 32 | parts done; null: neither token nor lse
+  uint64_t* words;       // [rows][stride][3] of a part: largest score, its word, sum of exponentials
+  int64_t stride;        // parts that a row has room for
 };
 
 // Calls f with a value of the storage type `dtype` (POLYGLOT_F32, _BF16, _F16).
@@ -65,6 +71,7 @@ hipError_t launch_recurrence(const RecCall& c, int dtype, int form, bool grad, u
                              uint64_t* words, const Launch& L);
 // Words of the scans of up to `tokens` tokens and D channels.
 size_t scan_words(int64_t tokens, int D);
-hipError_t launch_logits(const LogitsCall& c, const Launch& L);
+hipError_t launch_logits(LogitsCall c, const Launch& L);
+constexpr int kLogitsMinTile = 1024;  // words of the shortest part
 
 }  // namespace pg

@@ -8,17 +8,40 @@
 
 namespace pg {
 
+namespace {
+
+template <class T, int U>
+hipError_t dropout_of(const DropoutCall& c, int64_t total, const Launch& L) {
+  static_assert(U * kBlock <= kDropPlaces, "places of a workgroup");
+  const int64_t grid = (total + kBlock * U - 1) / (kBlock * U);
+  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  auto k = c.a.ids ? (c.a.add ? k_dropout<T, true, true, U> : k_dropout<T, false, true, U>)
+                   : (c.a.add ? k_dropout<T, true, false, U> : k_dropout<T, false, false, U>);
+  return pg_launch(k, dim3((uint32_t)grid), dim3(kBlock), 0, L, c);
+}
+
+}  // namespace
+
 hipError_t launch_dropout(const DropoutCall& c, const Launch& L) {
-  const int64_t total = c.a.rows * ((c.a.d + 7) / 8);
-  const int grid = (int)std::min<int64_t>((total + kBlock - 1) / kBlock, 16 * kCus);
+  const int64_t total = c.a.rows * c.groups;
   return by_format(c.a.dtype, [&](auto v) {
-    return pg_launch(k_dropout<decltype(v)>, dim3(grid), dim3(kBlock), 0, L, c);
+    using T = decltype(v);
+    return total >= (int64_t)4 * kBlock * 4 * kCus ? dropout_of<T, 4>(c, total, L)
+                                                   : dropout_of<T, 1>(c, total, L);
   });
 }
 
-hipError_t launch_logits(const LogitsCall& c, const Launch& L) {
+hipError_t launch_logits(LogitsCall c, const Launch& L) {
+  // the longest parts that still give every CU four workgroups
+  int E = 32;
+  while (E > 4 && (int64_t)c.a.rows * ceil_div(c.a.V, E * kBlock) < 4 * kCus) E /= 2;
+  c.tiles = ceil_div(c.a.V, E * kBlock);
+  if ((int64_t)c.a.rows * c.tiles > INT32_MAX) return hipErrorInvalidValue;
   return by_format(c.a.dtype, [&](auto v) {
-    return pg_launch(k_logits<decltype(v)>, dim3(c.a.rows), dim3(kBlock), 0, L, c);
+    using T = decltype(v);
+    auto k = E == 32 ? k_logits<T, 32> : E == 16 ? k_logits<T, 16> : E == 8 ? k_logits<T, 8>
+                                                                          : k_logits<T, 4>;
+    return pg_launch(k, dim3(c.a.rows * c.tiles), dim3(kBlock), 0, L, c);
   });
 }
 

@@ -15,6 +15,11 @@ namespace {
 // Kernel ids of these operators among a context's timing marks.
 constexpr int kOpKernels = POLYGLOT_NKERNELS;
 
+// Most parts of a row of V scores.
+int64_t logits_parts(int V) { return (V + (int64_t)kLogitsMinTile - 1) / kLogitsMinTile; }
+
+constexpr int kLogitsMaxV = 1 << 30;  // places in a row fit an int
+
 constexpr size_t kHeadWords = 64;  // the launch's own words, before those that join its parts
 
 // Runs an entry point's body; nothing that it throws (a message that finds no
@@ -65,7 +70,12 @@ int polyglot_dropout(polyglot_ctx* ctx, const polyglot_dropout_args* args) {
     if (!aligned(a.x, es) || !aligned(a.add, es) || !aligned(a.y, es) ||
         (a.ids && !aligned(a.ids, a.id_bytes)) || !aligned(a.site_dev, 4))
       return fail(ctx, POLYGLOT_EINVAL, "dropout: misaligned pointer");
-    DropoutCall c{a, ctx->ws.flag, (uint32_t)(a.p * 65536.0 + 0.5), 0.f};
+    DropoutCall c{};
+    c.a = a;
+    c.flag = ctx->ws.flag;
+    c.threshold = (uint32_t)(a.p * 65536.0 + 0.5);
+    c.groups = (int)((a.d + 7LL) / 8);
+    c.groups_inv = (uint32_t)(((1ull << 32) + c.groups - 1) / c.groups);
     if (c.threshold < 65536u) c.scale = (float)(65536.0 / (65536u - c.threshold));
     Timed tm(ctx, kOpKernels + POLYGLOT_OPK_DROPOUT);
     const hipError_t e = launch_dropout(c, tm.L);
@@ -238,7 +248,7 @@ int polyglot_logits(polyglot_ctx* ctx, const polyglot_logits_args* args) {
   return entry([&] {
     const polyglot_logits_args& a = *args;
     if (a.rows < 0) return fail(ctx, POLYGLOT_EBATCH, "logits: rows must not be negative");
-    if (a.V < 1 || !format_ok(a.dtype) || a.history_cap < 0)
+    if (a.V < 1 || a.V > kLogitsMaxV || !format_ok(a.dtype) || a.history_cap < 0)
       return fail(ctx, POLYGLOT_EINVAL, "logits: bad vocabulary, storage format or history_cap");
     if (a.rows == 0) return POLYGLOT_OK;
     if (!a.logits) return fail(ctx, POLYGLOT_ENULL, "logits: NULL scores");
@@ -259,9 +269,17 @@ int polyglot_logits(polyglot_ctx* ctx, const polyglot_logits_args* args) {
                            a.bias, a.mask, a.mask_rows, a.token, a.lse};
     for (const void* p : words)
       if (!aligned(p, 4)) return fail(ctx, POLYGLOT_EINVAL, "logits: misaligned pointer");
-    if ((a.token || a.lse) && (a.rows > ctx->op.log_rows || a.V > ctx->op.log_V))
+    OpWorkspace& op = ctx->op;
+    if ((a.token || a.lse) && (!op.log_head || a.rows > op.log_rows || a.V > op.log_V))
       return fail(ctx, POLYGLOT_EBATCH, "logits: above the reserved rows or vocabulary");
-    LogitsCall c{a, ctx->ws.flag};
+    LogitsCall c{};
+    c.a = a;
+    c.flag = ctx->ws.flag;
+    if (a.token || a.lse) {
+      c.head = op.log_head;
+      c.stride = logits_parts(op.log_V);
+      c.words = op.log_head + op.log_rows;
+    }
     Timed tm(ctx, kOpKernels + POLYGLOT_OPK_LOGITS);
     const hipError_t e = launch_logits(c, tm.L);
     return e == hipSuccess ? POLYGLOT_OK : hip_fail(ctx, e, "logits launch");
@@ -273,8 +291,24 @@ int polyglot_reserve_logits(polyglot_ctx* ctx, int32_t max_rows, int32_t max_V) 
   return entry([&] {
     if (max_rows < 0 || max_V < 0)
       return fail(ctx, POLYGLOT_EINVAL, "reserve_logits: bad rows or vocabulary");
-    ctx->op.log_rows = max_rows;
-    ctx->op.log_V = max_V;
+    OpWorkspace& op = ctx->op;
+    hipError_t e = hipStreamSynchronize(ctx->stream);
+    if (e != hipSuccess) return hip_fail(ctx, e, "reserve_logits: sync");
+    if (op.log_head) e = hipFree(op.log_head);
+    op.log_head = nullptr;
+    op.log_rows = op.log_V = 0;
+    // a row's tag is 1 at first, that of words that nothing has written 0
+    const size_t n = (size_t)max_rows * (1 + 3 * logits_parts(max_V)) + 1;
+    const std::vector<uint64_t> first(max_rows, (uint64_t)1 << 32);
+    if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void**>(&op.log_head), n * sizeof(uint64_t));
+    if (e == hipSuccess) e = hipMemsetAsync(op.log_head, 0, n * sizeof(uint64_t), ctx->stream);
+    if (e == hipSuccess && max_rows > 0)
+      e = hipMemcpyAsync(op.log_head, first.data(), first.size() * sizeof(uint64_t),
+                         hipMemcpyHostToDevice, ctx->stream);
+    if (e == hipSuccess) e = hipStreamSynchronize(ctx->stream);
+    if (e != hipSuccess) return hip_fail(ctx, e, "reserve_logits");
+    op.log_rows = max_rows;
+    op.log_V = max_V;
     return POLYGLOT_OK;
   });
 }

@@ -9,10 +9,6 @@ namespace pg {
 
 namespace {
 
-bool vector_rows(const void* p, int64_t ld, size_t size) {
-  return reinterpret_cast<uintptr_t>(p) % (4 * size) == 0 && ld % 4 == 0;
-}
-
 // Lanes of a row of threads: as few as hold all channels, so that narrow layers
 // have more rows of tokens; at least what a group takes.
 ScanPlan scan_plan(int64_t tokens, int D, int group, int R) {
@@ -38,12 +34,7 @@ hipError_t launch_scan(const RecCall& c, uint64_t* head, uint64_t* words, const 
   p.head = head;
   p.words = words;
   const bool shared = c.group > 1;
-  const bool vec = c.D % 4 == 0 && (shared ? c.group % 4 == 0 : vector_rows(c.gate, c.ld_gate, sizeof(T))) &&
-                   (!c.x || vector_rows(c.x, c.ld_x, sizeof(T))) &&
-                   vector_rows(c.out, c.ld_out, sizeof(T)) &&
-                   (!GRAD || (vector_rows(c.h, c.ld_h, sizeof(T)) &&
-                              vector_rows(c.dh, c.ld_dh, sizeof(T)) &&
-                              (shared || vector_rows(c.dgate, c.ld_dgate, sizeof(T)))));
+  const bool vec = shared ? c.group % 4 == 0 : c.D % 4 == 0;  // whole quads
   auto k = shared ? (vec ? k_scan<T, FORM, GRAD, true, true, R> : k_scan<T, FORM, GRAD, true, false, R>)
                   : (vec ? k_scan<T, FORM, GRAD, false, true, R>
                          : k_scan<T, FORM, GRAD, false, false, R>);
@@ -52,10 +43,7 @@ hipError_t launch_scan(const RecCall& c, uint64_t* head, uint64_t* words, const 
 
 template <class T, int FORM>
 hipError_t launch_step(const RecCall& c, const Launch& L) {
-  const bool vec = c.D % 4 == 0 && vector_rows(c.x, c.ld_x, sizeof(T)) &&
-                   vector_rows(c.out, c.ld_out, sizeof(T)) && vector_rows(c.init, 0, 4) &&
-                   vector_rows(c.fin, 0, 4) &&
-                   (c.group > 1 || vector_rows(c.gate, c.ld_gate, sizeof(T)));
+  const bool vec = c.D % 4 == 0;
   const int64_t total = (int64_t)c.tokens * ceil_div(c.D, 4);
   const int grid = (int)std::min<int64_t>((total + kBlock - 1) / kBlock, 16 * kCus);
   return pg_launch(vec ? k_recurrence_step<T, FORM, true> : k_recurrence_step<T, FORM, false>,
