@@ -32,9 +32,10 @@ struct GraphKey {
 struct OpWorkspace {
   int64_t rec_tokens = 0;
   int rec_D = 0;
-  uint64_t *rec_head = nullptr, *rec_words = nullptr;  // one block
+  size_t rec_stride = 0;
+  uint64_t *rec_head = nullptr, *rec_words = nullptr;  // one block: counters, words
   int log_rows = 0, log_V = 0;
-  uint64_t* log_head = nullptr;  // [log_rows], then the parts' words
+  uint64_t *log_head = nullptr, *log_words = nullptr;  // likewise
 };
 
 }  // namespace pg

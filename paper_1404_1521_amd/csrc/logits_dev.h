@@ -33,8 +33,8 @@ __device__ __forceinline__ float exp_fast(float x) {
   return __builtin_amdgcn_exp2f(1.44269504088896341f * x);
 }
 
-// e^l over a base no smaller than any l of a sum: equal infinities count once, a
-// base of -infinity has no terms.
+// e^l over a base no smaller than any l of a sum, where an infinity may be: equal
+// infinities count once, a base of -infinity has no terms.
 __device__ __forceinline__ float exp_over(float l, float base) {
   if (l == base) return base == -__builtin_inff() ? 0.f : 1.f;
   return exp_fast(l - base);
@@ -67,31 +67,25 @@ struct LogitsLds {
 
 constexpr int kNoWord = 0x7fffffff;
 
-// The workgroup's choice: the largest m, and the lowest w of the threads that have
-// it (m -infinity: no word).  Every thread gets it.
-__device__ __forceinline__ void choose(float& m, int& w, LogitsLds& l) {
-  const int wave = threadIdx.x / kWave;
-  const auto larger = [](float a, float b) { return a > b ? a : b; };
-  const auto lower = [](int a, int b) { return a < b ? a : b; };
-  const float wm = wave_reduce(m, -__builtin_inff(), larger);
-  const int ww = wave_reduce(m == wm ? w : kNoWord, kNoWord, lower);
-  if ((threadIdx.x & (kWave - 1)) == 0) l.m[wave] = wm, l.w[wave] = ww;
+// The workgroup's largest m; its lowest w and its sum of s.  Every thread gets them.
+__device__ __forceinline__ float largest(float m, LogitsLds& l) {
+  m = wave_reduce(m, -__builtin_inff(), [](float a, float b) { return fmaxf(a, b); });
+  if ((threadIdx.x & (kWave - 1)) == 0) l.m[threadIdx.x / kWave] = m;
   __syncthreads();
   m = l.m[0];
-  w = l.w[0];
 #pragma unroll
-  for (int i = 1; i < kWavesPerBlock; ++i)
-    if (l.m[i] > m || (l.m[i] == m && l.w[i] < w)) m = l.m[i], w = l.w[i];
+  for (int i = 1; i < kWavesPerBlock; ++i) m = fmaxf(m, l.m[i]);
+  return m;
 }
-
-__device__ __forceinline__ float total(float s, LogitsLds& l) {
+__device__ __forceinline__ void lowest_and_sum(int& w, float& s, LogitsLds& l) {
+  w = wave_reduce(w, kNoWord, [](int a, int b) { return min(a, b); });
   s = wave_reduce(s, 0.f, [](float a, float b) { return a + b; });
-  if ((threadIdx.x & (kWave - 1)) == 0) l.s[threadIdx.x / kWave] = s;
+  if ((threadIdx.x & (kWave - 1)) == 0) l.w[threadIdx.x / kWave] = w, l.s[threadIdx.x / kWave] = s;
   __syncthreads();
+  w = l.w[0];
   s = l.s[0];
 #pragma unroll
-  for (int i = 1; i < kWavesPerBlock; ++i) s += l.s[i];
-  return s;
+  for (int i = 1; i < kWavesPerBlock; ++i) w = min(w, l.w[i]), s += l.s[i];
 }
 
 // A part's or a row's log-sum-exp of sum s over base m.
@@ -116,6 +110,25 @@ __device__ __forceinline__ uint32_t await_word(const uint64_t* w, uint32_t tag, 
   }
 }
 
+// The quad at place v of a row of V: the load stays inside the row, and what lies
+// past its end is shifted out (whole: nothing does).  V < 4: word by word.
+template <class T>
+__device__ __forceinline__ Quad<T> row_quad(const T* row, int v, int V, bool whole) {
+  if (V < 4) return load_quad<T, false>(row + min(v, V), max(0, min(4, V - v)));
+  Quad<T> q = load_quad<T, true>(row + (whole ? v : min(v, V - 4)), 4);
+  if (!whole) {
+    const int off = max(0, min(3, v - (V - 4)));  // elements before v
+    if constexpr (sizeof(T) == 2) {
+      const uint64_t w = ((uint64_t)q.raw.y << 32 | q.raw.x) >> (16 * off);
+      q.raw = u2_any{(uint32_t)w, (uint32_t)(w >> 32)};
+    } else {
+      if (off & 1) q.raw = f4{q.raw[1], q.raw[2], q.raw[3], 0.f};
+      if (off & 2) q.raw = f4{q.raw[2], q.raw[3], 0.f, 0.f};
+    }
+  }
+  return q;
+}
+
 // E words per thread, in quads 4 * 256 words apart.
 template <class T, int E>
 __global__ __launch_bounds__(kBlock) void k_logits(LogitsCall c) {
@@ -125,7 +138,8 @@ __global__ __launch_bounds__(kBlock) void k_logits(LogitsCall c) {
   const polyglot_logits_args& a = c.a;
   const int t = threadIdx.x;
   const int r = blockIdx.x / c.tiles, tile = blockIdx.x - r * c.tiles;
-  const int v0 = tile * (E * kBlock);
+  const int v0 = tile * (E * kBlock) + 4 * t;      // the thread's first word
+  const bool whole = (tile + 1) * (E * kBlock) <= a.V;  // no quad of the part passes the row's end
   const T* in = static_cast<const T*>(a.logits) + (int64_t)r * a.ld_logits;
   const float* bias = a.bias ? a.bias + (int64_t)r * a.ld_bias : nullptr;
   const uint32_t* mask = nullptr;
@@ -137,29 +151,21 @@ __global__ __launch_bounds__(kBlock) void k_logits(LogitsCall c) {
     }
     if (m >= 0) mask = a.mask + (int64_t)m * a.ld_mask;
   }
-  // the part's scores, biases and mask in flight
+  // the part's scores and mask in flight
   Quad<T> x[Q];
-  Quad<float> bs[Q];
   uint32_t allow[Q];
-  int n[Q];
 #pragma unroll
-  for (int g = 0; g < Q; ++g) {
-    const int v = v0 + (g * kBlock + t) * 4;
-    n[g] = max(0, min(4, a.V - v));
-    bs[g] = Quad<float>{};
-    allow[g] = 0xfu;
-    if (n[g] == 4) {
-      x[g] = load_quad<T, true>(in + v, 4);
-      if (bias) bs[g] = load_quad<float, true>(bias + v, 4);
-    } else {
-      x[g] = load_quad<T, false>(in + v, n[g]);
-      if (bias) bs[g] = load_quad<float, false>(bias + v, n[g]);
+  for (int g = 0; g < Q; ++g) x[g] = row_quad<T>(in, v0 + g * 4 * kBlock, a.V, whole);
+  if (mask) {
+#pragma unroll
+    for (int g = 0; g < Q; ++g) {
+      const int v = v0 + g * 4 * kBlock;
+      allow[g] = mask[min(v, a.V - 1) >> 5] >> (v & 31);
     }
-    if (mask && n[g] > 0) allow[g] = mask[v >> 5] >> (v & 31);
   }
   uint32_t tag = 0;
   if (c.head && t == 0)  // the row's tag moves on once all its parts are in
-    tag = (uint32_t)(__hip_atomic_load(c.head + r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >> 32);
+    tag = (uint32_t)(__hip_atomic_load(c.head + r * kHeadLine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >> 32);
   const RowRules rules{a.repetition ? a.repetition[r] : 1.f, a.frequency ? a.frequency[r] : 0.f,
                        a.presence ? a.presence[r] : 0.f};
   int len = 0, prompt = 0;
@@ -168,98 +174,127 @@ __global__ __launch_bounds__(kBlock) void k_logits(LogitsCall c) {
     prompt = a.prompt ? min(max(a.prompt[r], 0), a.history_cap) : 0;
   }
   if (len > 0) {
+    const int32_t* hist = a.history + (int64_t)r * a.ld_history;
+    constexpr int kAhead = 8;
+    int id[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) id[j] = t + j * kBlock < len ? hist[t + j * kBlock] : -1;
 #pragma unroll
     for (int g = 0; g < Q; ++g)
       *reinterpret_cast<uint4*>(seen + (g * kBlock + t) * 4) = uint4{0u, 0u, 0u, 0u};
     __syncthreads();
-    const int32_t* hist = a.history + (int64_t)r * a.ld_history;
-    constexpr int kAhead = 4;
-    for (int k0 = t; k0 < len; k0 += kAhead * kBlock) {
-      int id[kAhead];
-#pragma unroll
-      for (int j = 0; j < kAhead; ++j) id[j] = k0 + j * kBlock < len ? hist[k0 + j * kBlock] : -1;
+    for (int k0 = t;;) {
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
         if (id[j] >= a.V) atomicOr(c.flag, kFlagBadId);
-        const uint32_t i = (uint32_t)(id[j] - v0);
-        if (id[j] >= v0 && i < (uint32_t)(E * kBlock)) {
-          atomicOr(&seen[i], kInHistory);
-          if (k0 + j * kBlock >= prompt) atomicAdd(&seen[i], 1u);
+        const int first = tile * (E * kBlock);
+        if (id[j] >= first && id[j] - first < E * kBlock) {
+          atomicOr(&seen[id[j] - first], kInHistory);
+          if (k0 + j * kBlock >= prompt) atomicAdd(&seen[id[j] - first], 1u);
         }
       }
+      k0 += kAhead * kBlock;
+      if (k0 - t >= len) break;
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) id[j] = k0 + j * kBlock < len ? hist[k0 + j * kBlock] : -1;
     }
     __syncthreads();
   }
-  T* out = a.out ? static_cast<T*>(a.out) + (int64_t)r * a.ld_out : nullptr;
   float l[E];
-  float m = -__builtin_inff();
-  int w = kNoWord;
 #pragma unroll
   for (int g = 0; g < Q; ++g) {
-    const int v = v0 + (g * kBlock + t) * 4;
-    uint4 k{0u, 0u, 0u, 0u};
-    if (len > 0) k = *reinterpret_cast<const uint4*>(seen + (g * kBlock + t) * 4);
-    const uint32_t ks[4] = {k.x, k.y, k.z, k.w};
-    float o[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float s = ruled(x[g].get(j), ks[j], rules);
-      if (bias) s = __fadd_rn(s, bs[g].get(j));
-      if (!(allow[g] >> j & 1u)) s = -__builtin_inff();
-      o[j] = s;
-      l[4 * g + j] = j < n[g] ? s : -__builtin_inff();
-      if (l[4 * g + j] > m) m = l[4 * g + j], w = v + j;
+    for (int j = 0; j < 4; ++j) l[4 * g + j] = x[g].get(j);
+    if (len > 0) {
+      const uint4 k = *reinterpret_cast<const uint4*>(seen + (g * kBlock + t) * 4);
+      if (k.x | k.y | k.z | k.w) {
+        l[4 * g] = ruled(l[4 * g], k.x, rules);
+        l[4 * g + 1] = ruled(l[4 * g + 1], k.y, rules);
+        l[4 * g + 2] = ruled(l[4 * g + 2], k.z, rules);
+        l[4 * g + 3] = ruled(l[4 * g + 3], k.w, rules);
+      }
     }
-    if (out) {
-      if (n[g] == 4) store_quad<T, true>(out + v, o, 4);
-      else store_quad<T, false>(out + v, o, n[g]);
+  }
+  if (bias) {
+    Quad<float> b[Q];
+#pragma unroll
+    for (int g = 0; g < Q; ++g) b[g] = row_quad<float>(bias, v0 + g * 4 * kBlock, a.V, whole);
+#pragma unroll
+    for (int i = 0; i < E; ++i) l[i] = __fadd_rn(l[i], b[i / 4].get(i & 3));
+  }
+  if (mask) {
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (!(allow[i / 4] >> (i & 3) & 1u)) l[i] = -__builtin_inff();
+  }
+  if (a.out) {
+    T* out = static_cast<T*>(a.out) + (int64_t)r * a.ld_out;
+#pragma unroll
+    for (int g = 0; g < Q; ++g) {
+      const int v = v0 + g * 4 * kBlock;
+      const float o[4] = {l[4 * g], l[4 * g + 1], l[4 * g + 2], l[4 * g + 3]};
+      if (whole || v + 4 <= a.V) store_quad<T, true>(out + v, o, 4);
+      else store_quad<T, false>(out + min(v, a.V), o, a.V - v);
     }
   }
   if (!c.head) return;
+  if (!whole) {
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (v0 + (i / 4) * 4 * kBlock + (i & 3) >= a.V) l[i] = -__builtin_inff();
+  }
 
-  choose(m, w, lds);
+  // the part's largest score, its first word, and the sum over that score
+  float own = -__builtin_inff();
+#pragma unroll
+  for (int i = 0; i < E; ++i) own = fmaxf(own, l[i]);
+  const float m = largest(own, lds);
+  int w = kNoWord;
+  if (own == m && m > -__builtin_inff()) {
+#pragma unroll
+    for (int i = E - 1; i >= 0; --i)
+      if (l[i] == m) w = v0 + (i / 4) * 4 * kBlock + (i & 3);
+  }
   float s = 0.f;
   if (a.lse) {
+    if (__builtin_isinf(m)) {
+      for (int i = 0; i < E; ++i) s += exp_over(l[i], m);
+    } else {
 #pragma unroll
-    for (int i = 0; i < E; ++i) s += exp_over(l[i], m);
-    s = total(s, lds);
+      for (int i = 0; i < E; ++i) s += exp_fast(l[i] - m);
+    }
   }
+  lowest_and_sum(w, s, lds);
   uint64_t* words = c.words + (int64_t)r * c.stride * 3;
   if (t == 0) {
     publish_word(words + tile * 3, __float_as_uint(m), tag);
     publish_word(words + tile * 3 + 1, (uint32_t)w, tag);
     publish_word(words + tile * 3 + 2, __float_as_uint(s), tag);
-    lds.arrived = __hip_atomic_fetch_add(c.head + r, (uint64_t)1, __ATOMIC_RELAXED,
+    lds.arrived = __hip_atomic_fetch_add(c.head + r * kHeadLine, (uint64_t)1, __ATOMIC_RELAXED,
                                          __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
   if ((uint32_t)lds.arrived != (uint32_t)c.tiles - 1) return;
 
-  // the last part: the row's choice, then its sum over that choice
+  // the last part joins them, in their order
   tag = (uint32_t)(lds.arrived >> 32);
-  m = -__builtin_inff();
+  float top = -__builtin_inff();
+  for (int j = t; j < c.tiles; j += kBlock)
+    top = fmaxf(top, __uint_as_float(await_word(words + j * 3, tag, c.flag)));
+  top = largest(top, lds);
   w = kNoWord;
+  s = 0.f;
   for (int j = t; j < c.tiles; j += kBlock) {
     const float pm = __uint_as_float(await_word(words + j * 3, tag, c.flag));
-    const int pw = (int)await_word(words + j * 3 + 1, tag, c.flag);
-    if (pm > m || (pm == m && pw < w)) m = pm, w = pw;
+    if (pm == top) w = min(w, (int)await_word(words + j * 3 + 1, tag, c.flag));
+    s += __uint_as_float(await_word(words + j * 3 + 2, tag, c.flag)) * exp_over(pm, top);
   }
-  __syncthreads();
-  choose(m, w, lds);
-  if (a.lse) {
-    s = 0.f;
-    for (int j = t; j < c.tiles; j += kBlock) {
-      const float pm = __uint_as_float(await_word(words + j * 3, tag, c.flag));
-      const float ps = __uint_as_float(await_word(words + j * 3 + 2, tag, c.flag));
-      s += ps * exp_over(pm, m);
-    }
-    s = total(s, lds);
-  }
+  lowest_and_sum(w, s, lds);
   if (t == 0) {
     if (a.token) a.token[r] = w == kNoWord ? -1 : w;
-    if (a.lse) a.lse[r] = log_sum(m, s);
+    if (a.lse) a.lse[r] = log_sum(top, s);
     const uint32_t next = tag + 1 ? tag + 1 : 1u;
-    __hip_atomic_store(c.head + r, (uint64_t)next << 32, __ATOMIC_RELAXED,
+    __hip_atomic_store(c.head + r * kHeadLine, (uint64_t)next << 32, __ATOMIC_RELAXED,
                        __HIP_MEMORY_SCOPE_AGENT);
   }
 }

@@ -9,6 +9,10 @@
 
 namespace pg {
 
+// Words that many workgroups count in lie this many 64-bit words apart: 128 bytes,
+// a cache line.  Atomics on one line take turns at about 17 ns.
+constexpr int64_t kHeadLine = 16;
+
 struct DropoutCall {
   polyglot_dropout_args a;
   uint32_t* flag;
@@ -43,15 +47,16 @@ struct ScanPlan {
   int lanes_log2;        // lanes of a row of threads: four channels each
   int tiles, chunks;     // of the channels and of the tokens; a workgroup for each pair
   int lanes_per_group, groups_per_tile;  // shared gates
-  uint64_t* head;        // {tag << 32 | next chunk, workgroups done}; null: no chunk waits
-  uint64_t* words;       // [chunks * tiles][2][4][lanes]
+  uint64_t* head;        // [tiles][kHeadLine] tag << 32 | next chunk; null: no chunk waits
+  uint64_t* words;       // [tiles][stride], of them [chunks][2][4][lanes]: a tile's words are
+  size_t stride;         // written with its own counter's tags only
 };
 
 struct LogitsCall {
   polyglot_logits_args a;
   uint32_t* flag;
   int tiles;             // parts of a row, a workgroup each
-  uint64_t* head;        // [rows] tag << 32 | parts done; null: neither token nor lse
+  uint64_t* head;        // [rows][kHeadLine] tag << 32 | parts done; null: neither token nor lse
   uint64_t* words;       // [rows][stride][3] of a part: largest score, its word, sum of exponentials
   int64_t stride;        // parts that a row has room for
 };
@@ -65,12 +70,13 @@ hipError_t by_format(int dtype, F f) {
 }
 
 hipError_t launch_dropout(const DropoutCall& c, const Launch& L);
-// head: {.., ..} zeroed once with head[0] = 1 << 32, words: zeroed once; both only for
-// calls of other than one token per sequence, sized by scan_words.
+// head: 1 << 32 in each line's first word at first, words: zeros at first; both only
+// for calls of other than one token per sequence.
 hipError_t launch_recurrence(const RecCall& c, int dtype, int form, bool grad, uint64_t* head,
-                             uint64_t* words, const Launch& L);
-// Words of the scans of up to `tokens` tokens and D channels.
-size_t scan_words(int64_t tokens, int D);
+                             uint64_t* words, size_t stride, const Launch& L);
+// Room of the scans of up to `tokens` tokens and D channels: tiles, and a tile's words.
+int scan_tiles(int D);
+size_t scan_stride(int64_t tokens);
 hipError_t launch_logits(LogitsCall c, const Launch& L);
 constexpr int kLogitsMinTile = 1024;  // words of the shortest part
 

@@ -20,7 +20,24 @@ int64_t logits_parts(int V) { return (V + (int64_t)kLogitsMinTile - 1) / kLogits
 
 constexpr int kLogitsMaxV = 1 << 30;  // places in a row fit an int
 
-constexpr size_t kHeadWords = 64;  // the launch's own words, before those that join its parts
+// A zeroed block of `lines` words of counters, each line's first with tag 1, and
+// `words` more behind them (their tag 0: nothing has written them).
+hipError_t heads(polyglot_ctx* ctx, uint64_t** head, size_t lines, size_t words) {
+  const size_t n = lines + words + 1;
+  std::vector<uint64_t> first(lines, 0);
+  for (size_t i = 0; i < lines; i += kHeadLine) first[i] = (uint64_t)1 << 32;
+  uint64_t* p = nullptr;
+  hipError_t e = hipMalloc(reinterpret_cast<void**>(&p), n * sizeof(uint64_t));
+  if (e != hipSuccess) return e;
+  e = hipMemsetAsync(p, 0, n * sizeof(uint64_t), ctx->stream);
+  if (e == hipSuccess && lines > 0)
+    e = hipMemcpyAsync(p, first.data(), lines * sizeof(uint64_t), hipMemcpyHostToDevice,
+                       ctx->stream);
+  if (e == hipSuccess) e = hipStreamSynchronize(ctx->stream);
+  if (e == hipSuccess) *head = p;
+  else (void)hipFree(p);
+  return e;
+}
 
 // Runs an entry point's body; nothing that it throws (a message that finds no
 // memory) passes the C boundary.
@@ -171,7 +188,8 @@ int polyglot_recurrence(polyglot_ctx* ctx, const polyglot_recurrence_args* args)
     c.fin = a.last;
     c.down = a.reverse != 0;
     Timed tm(ctx, kOpKernels + POLYGLOT_OPK_RECURRENCE);
-    const hipError_t e = launch_recurrence(c, a.dtype, a.form, false, ctx->op.rec_head, ctx->op.rec_words, tm.L);
+    const hipError_t e = launch_recurrence(c, a.dtype, a.form, false, ctx->op.rec_head, ctx->op.rec_words,
+                                           ctx->op.rec_stride, tm.L);
     return e == hipSuccess ? POLYGLOT_OK : hip_fail(ctx, e, "recurrence launch");
   });
 }
@@ -210,7 +228,8 @@ int polyglot_recurrence_grad(polyglot_ctx* ctx, const polyglot_recurrence_grad_a
     c.fin = a.dh0;
     c.down = a.reverse == 0;
     Timed tm(ctx, kOpKernels + POLYGLOT_OPK_RECURRENCE_GRAD);
-    const hipError_t e = launch_recurrence(c, a.dtype, a.form, true, ctx->op.rec_head, ctx->op.rec_words, tm.L);
+    const hipError_t e = launch_recurrence(c, a.dtype, a.form, true, ctx->op.rec_head, ctx->op.rec_words,
+                                           ctx->op.rec_stride, tm.L);
     return e == hipSuccess ? POLYGLOT_OK : hip_fail(ctx, e, "recurrence_grad launch");
   });
 }
@@ -226,17 +245,11 @@ int polyglot_reserve_recurrence(polyglot_ctx* ctx, int64_t max_tokens, int32_t m
     if (op.rec_head) e = hipFree(op.rec_head);
     op.rec_head = op.rec_words = nullptr;
     op.rec_tokens = op.rec_D = 0;
-    // {tag, next chunk} and {workgroups done}, 64 words apart from the chunks' words;
-    // the tag of words that nothing has written is 0, the first launch's is 1
-    const size_t n = kHeadWords + scan_words(max_tokens, max_D);
-    const uint64_t first = (uint64_t)1 << 32;
-    if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void**>(&op.rec_head), n * sizeof(uint64_t));
-    if (e == hipSuccess) e = hipMemsetAsync(op.rec_head, 0, n * sizeof(uint64_t), ctx->stream);
-    if (e == hipSuccess)
-      e = hipMemcpyAsync(op.rec_head, &first, sizeof(first), hipMemcpyHostToDevice, ctx->stream);
-    if (e == hipSuccess) e = hipStreamSynchronize(ctx->stream);
+    const size_t tiles = scan_tiles(max_D), lines = tiles * kHeadLine;
+    op.rec_stride = scan_stride(max_tokens);
+    e = e == hipSuccess ? heads(ctx, &op.rec_head, lines, tiles * op.rec_stride) : e;
     if (e != hipSuccess) return hip_fail(ctx, e, "reserve_recurrence");
-    op.rec_words = op.rec_head + kHeadWords;
+    op.rec_words = op.rec_head + lines;
     op.rec_tokens = max_tokens;
     op.rec_D = max_D;
     return POLYGLOT_OK;
@@ -278,7 +291,7 @@ int polyglot_logits(polyglot_ctx* ctx, const polyglot_logits_args* args) {
     if (a.token || a.lse) {
       c.head = op.log_head;
       c.stride = logits_parts(op.log_V);
-      c.words = op.log_head + op.log_rows;
+      c.words = op.log_words;
     }
     Timed tm(ctx, kOpKernels + POLYGLOT_OPK_LOGITS);
     const hipError_t e = launch_logits(c, tm.L);
@@ -295,18 +308,13 @@ int polyglot_reserve_logits(polyglot_ctx* ctx, int32_t max_rows, int32_t max_V) 
     hipError_t e = hipStreamSynchronize(ctx->stream);
     if (e != hipSuccess) return hip_fail(ctx, e, "reserve_logits: sync");
     if (op.log_head) e = hipFree(op.log_head);
-    op.log_head = nullptr;
+    op.log_head = op.log_words = nullptr;
     op.log_rows = op.log_V = 0;
-    // a row's tag is 1 at first, that of words that nothing has written 0
-    const size_t n = (size_t)max_rows * (1 + 3 * logits_parts(max_V)) + 1;
-    const std::vector<uint64_t> first(max_rows, (uint64_t)1 << 32);
-    if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void**>(&op.log_head), n * sizeof(uint64_t));
-    if (e == hipSuccess) e = hipMemsetAsync(op.log_head, 0, n * sizeof(uint64_t), ctx->stream);
-    if (e == hipSuccess && max_rows > 0)
-      e = hipMemcpyAsync(op.log_head, first.data(), first.size() * sizeof(uint64_t),
-                         hipMemcpyHostToDevice, ctx->stream);
-    if (e == hipSuccess) e = hipStreamSynchronize(ctx->stream);
+    const size_t lines = (size_t)max_rows * kHeadLine;
+    e = e == hipSuccess ? heads(ctx, &op.log_head, lines, 3 * (size_t)max_rows * logits_parts(max_V))
+                        : e;
     if (e != hipSuccess) return hip_fail(ctx, e, "reserve_logits");
+    op.log_words = op.log_head + lines;
     op.log_rows = max_rows;
     op.log_V = max_V;
     return POLYGLOT_OK;

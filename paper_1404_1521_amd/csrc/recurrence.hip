@@ -27,12 +27,14 @@ ScanPlan scan_plan(int64_t tokens, int D, int group, int R) {
 }
 
 template <class T, int FORM, bool GRAD>
-hipError_t launch_scan(const RecCall& c, uint64_t* head, uint64_t* words, const Launch& L) {
+hipError_t launch_scan(const RecCall& c, uint64_t* head, uint64_t* words, size_t stride,
+                       const Launch& L) {
   constexpr int R = scan_tokens<T, GRAD>();
   static_assert(kScanMaxRows * R <= kScanMaxTokens, "places of a chunk");
   ScanPlan p = scan_plan(c.tokens, c.D, c.group, R);
   p.head = head;
   p.words = words;
+  p.stride = stride;
   const bool shared = c.group > 1;
   const bool vec = shared ? c.group % 4 == 0 : c.D % 4 == 0;  // whole quads
   auto k = shared ? (vec ? k_scan<T, FORM, GRAD, true, true, R> : k_scan<T, FORM, GRAD, true, false, R>)
@@ -52,16 +54,17 @@ hipError_t launch_step(const RecCall& c, const Launch& L) {
 
 }  // namespace
 
-size_t scan_words(int64_t tokens, int D) {
-  // Chunks are shortest where a row has 64 lanes.  Lanes that a group leaves idle at
-  // most double the slots (a group of two channels in a lane of four; 33 lanes of 64).
-  const int64_t L = kBlock / kWave * 8;
-  const size_t slots = 2 * (size_t)D + 4 * kWave;
-  return (size_t)((tokens + L - 1) / L + 1) * slots * 2;
+// Lanes that a group leaves idle at most double the slots (a group of two channels in
+// a lane of four; 33 lanes of 64).
+int scan_tiles(int D) { return ceil_div(2 * D, 4 * kWave) + 1; }
+
+size_t scan_stride(int64_t tokens) {
+  const int64_t L = kBlock / kWave * 8;  // chunks are shortest where a row has 64 lanes
+  return (size_t)((tokens + L - 1) / L + 1) * (2 * 4 * kWave);
 }
 
 hipError_t launch_recurrence(const RecCall& c, int dtype, int form, bool grad, uint64_t* head,
-                             uint64_t* words, const Launch& L) {
+                             uint64_t* words, size_t stride, const Launch& L) {
   constexpr int raw = POLYGLOT_GATE_RAW, sig = POLYGLOT_GATE_SIGMOID;
   const bool single = !c.offsets && c.tokens == c.nseq;  // every token starts a sequence
   return by_format(dtype, [&](auto v) {
@@ -70,10 +73,10 @@ hipError_t launch_recurrence(const RecCall& c, int dtype, int form, bool grad, u
       return form == raw ? launch_step<T, raw>(c, L) : launch_step<T, sig>(c, L);
     uint64_t* h = single ? nullptr : head;
     if (grad)
-      return form == raw ? launch_scan<T, raw, true>(c, h, words, L)
-                         : launch_scan<T, sig, true>(c, h, words, L);
-    return form == raw ? launch_scan<T, raw, false>(c, h, words, L)
-                       : launch_scan<T, sig, false>(c, h, words, L);
+      return form == raw ? launch_scan<T, raw, true>(c, h, words, stride, L)
+                         : launch_scan<T, sig, true>(c, h, words, stride, L);
+    return form == raw ? launch_scan<T, raw, false>(c, h, words, stride, L)
+                       : launch_scan<T, sig, false>(c, h, words, stride, L);
   });
 }
 

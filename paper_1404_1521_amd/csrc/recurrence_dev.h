@@ -115,19 +115,27 @@ __global__ __launch_bounds__(kBlock) void k_scan(RecCall c, ScanPlan p) {
   const int CT = 1 << p.lanes_log2, TT = kBlock >> p.lanes_log2;
   const int cl = t & (CT - 1), tl = t >> p.lanes_log2, L = TT * R;
 
-  // Chunks are handed out in the order in which workgroups start, so every chunk
-  // that a look-back waits for is running or done.
+  // The chunks of a tile are handed out in the order in which workgroups start, so
+  // every chunk that a look-back waits for is running or done.  Who takes the last
+  // one makes the counter ready for the next launch.
+  const int tile = blockIdx.x % p.tiles;
+  int chunk = blockIdx.x / p.tiles;
   uint32_t tag = 0;
-  int id = blockIdx.x;
   if (p.head) {
-    if (t == 0)
-      s.ticket = __hip_atomic_fetch_add(p.head, (uint64_t)1, __ATOMIC_RELAXED,
+    if (t == 0) {
+      uint64_t* head = p.head + tile * kHeadLine;
+      s.ticket = __hip_atomic_fetch_add(head, (uint64_t)1, __ATOMIC_RELAXED,
                                         __HIP_MEMORY_SCOPE_AGENT);
+      if ((uint32_t)s.ticket == (uint32_t)p.chunks - 1) {
+        const uint32_t next = (uint32_t)(s.ticket >> 32) + 1;
+        __hip_atomic_store(head, (uint64_t)(next >> 31 ? 1u : next) << 32, __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+      }
+    }
     __syncthreads();
-    id = (int)(uint32_t)s.ticket;
+    chunk = (int)(uint32_t)s.ticket;
     tag = (uint32_t)(s.ticket >> 32) << 1;
   }
-  const int chunk = id / p.tiles, tile = id - chunk * p.tiles;
 
   // this thread's channels [ch, ch + nv) and their gate
   int ch, nv, gate_col = 0, part = 0;
@@ -214,7 +222,7 @@ __global__ __launch_bounds__(kBlock) void k_scan(RecCall c, ScanPlan p) {
   }
   // offsets that do not ascend from 0 to the tokens: each pair is looked at once
   if (c.offsets)
-    for (int64_t i = (int64_t)id * kBlock + t; i <= c.nseq; i += (int64_t)gridDim.x * kBlock) {
+    for (int64_t i = (int64_t)blockIdx.x * kBlock + t; i <= c.nseq; i += (int64_t)gridDim.x * kBlock) {
       const int64_t o = seq_offset(c, (int)i);
       const int64_t next = i < c.nseq ? seq_offset(c, (int)i + 1) : c.tokens;
       if ((i == 0 && o != 0) || next < o || (i == c.nseq && o != c.tokens))
@@ -286,7 +294,8 @@ __global__ __launch_bounds__(kBlock) void k_scan(RecCall c, ScanPlan p) {
   }
   const bool ends = tl == TT - 1 && live && chunk + 1 < p.chunks;
   const bool set = chunk == 0 || pcut || cut;  // the chunk's end does not depend on its beginning
-  uint64_t* words = p.words + ((size_t)id * 8) * CT + cl;  // [2][4][lanes]
+  uint64_t* const tile_words = p.words + tile * p.stride + cl;
+  uint64_t* words = tile_words + (size_t)chunk * 8 * CT;  // [2][4][lanes]
   if (ends && p.head) {
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
@@ -315,7 +324,7 @@ __global__ __launch_bounds__(kBlock) void k_scan(RecCall c, ScanPlan p) {
 #pragma unroll
         for (int k = 0; k < kScanLook; ++k) {
           const int j = base - tl * kScanLook - k;
-          const uint64_t* w = p.words + ((size_t)(j * p.tiles + tile) * 8) * CT + cl;
+          const uint64_t* w = tile_words + (int64_t)j * 8 * CT;
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
             // before the first chunk there is nothing: a state of 0 stands there
@@ -426,19 +435,6 @@ __global__ __launch_bounds__(kBlock) void k_scan(RecCall c, ScanPlan p) {
       }
       if (live && part == 0)
         static_cast<T*>(c.dgate)[n * c.ld_dgate + gate_col] = Elem<T>::put(settled(d.slope(sum)));
-    }
-  }
-
-  // the last workgroup makes the words ready for the next launch
-  if (p.head && t == 0) {
-    uint32_t* n_done = reinterpret_cast<uint32_t*>(p.head + 1);
-    if (__hip_atomic_fetch_add(n_done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
-        gridDim.x - 1) {
-      uint32_t next = (tag >> 1) + 1;
-      if (next >> 31) next = 1;
-      __hip_atomic_store(n_done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __hip_atomic_store(p.head, (uint64_t)next << 32, __ATOMIC_RELAXED,
-                         __HIP_MEMORY_SCOPE_AGENT);
     }
   }
 }

@@ -585,6 +585,23 @@ def test_recurrence_results_do_not_depend_on_the_run(pg, ctx):
         assert all(torch.equal(a, b) for a, b in zip(r, first[2:]))
 
 
+def test_recurrence_widths_take_turns(pg):
+    """Calls that cut their channels into other numbers of tiles share one workspace: what
+    an earlier call left in it must not be taken for this call's."""
+    c = pg.Context(1000, 16, 5, 8, max_batch=1)
+    c.reserve_recurrence(3000, 1100)
+    qs = [Seqs("f32", [2500, 0, 400], D, g, True, seed=D) for D, g in
+          ((64, 1), (1024, 1), (8, 1), (520, 2), (1100, 1))]
+    ref = [q.forward() for q in qs]
+    for _ in range(3):
+        for k in (0, 0, 1, 2, 3, 0, 4, 1, 2, 4, 3):
+            h, E, last, lE = ref[k]
+            got = c.recurrence(qs[k].gate, qs[k].x, qs[k].offsets(), h0=qs[k].h0)
+            near(host(got[0]), h, E + EPS * np.abs(h), k)
+            near(host(got[1]), last, lE + EPS * np.abs(last), k)
+    c.close()
+
+
 def test_recurrence_in_a_graph(pg):
     s = torch.cuda.Stream()
     with torch.cuda.stream(s):
