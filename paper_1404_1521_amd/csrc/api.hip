@@ -104,7 +104,7 @@ void free_all(polyglot_ctx* ctx) {
   }
   if (ctx->side) hipStreamDestroy(ctx->side);
   ctx->side = nullptr;
-  for (uint64_t* q : {ctx->op.rec_head, ctx->op.log_head})
+  for (uint64_t* q : {ctx->op.rec.head, ctx->op.log_head})
     if (q) hipFree(q);
   ctx->op = OpWorkspace{};
   for (void* q : ctx->allocs) hipFree(q);

@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "launch.h"
+#include "operators.h"
 
 namespace pg {
 
@@ -32,10 +33,9 @@ struct GraphKey {
 struct OpWorkspace {
   int64_t rec_tokens = 0;
   int rec_D = 0;
-  size_t rec_stride = 0;
-  uint64_t *rec_head = nullptr, *rec_words = nullptr;  // one block: counters, words
+  ScanSpace rec;
   int log_rows = 0, log_V = 0;
-  uint64_t *log_head = nullptr, *log_words = nullptr;  // likewise
+  uint64_t *log_head = nullptr, *log_words = nullptr;  // one block: counters, words
 };
 
 }  // namespace pg

@@ -47,9 +47,19 @@ struct ScanPlan {
   int lanes_log2;        // lanes of a row of threads: four channels each
   int tiles, chunks;     // of the channels and of the tokens; a workgroup for each pair
   int lanes_per_group, groups_per_tile;  // shared gates
-  uint64_t* head;        // [tiles][kHeadLine] tag << 32 | next chunk; null: no chunk waits
-  uint64_t* words;       // [tiles][stride], of them [chunks][2][4][lanes]: a tile's words are
-  size_t stride;         // written with its own counter's tags only
+  int counters;
+  uint64_t* head;        // [counters >= tiles][kHeadLine] tag << 32 | next chunk; null: no chunk waits
+  int group_log2;        // chunks of a group
+  uint64_t* flags;       // [tiles][chunks + groups]
+  uint64_t* words;       // [tiles] of [chunks][2][4][lanes], [groups][3][4][lanes]
+};
+
+// What a context keeps for its scans: the counters (tag 1 at first), then the flags
+// and words (zeros at first).
+struct ScanSpace {
+  uint64_t* head = nullptr;
+  int counters = 0;
+  size_t flags = 0, words = 0;
 };
 
 struct LogitsCall {
@@ -70,13 +80,11 @@ hipError_t by_format(int dtype, F f) {
 }
 
 hipError_t launch_dropout(const DropoutCall& c, const Launch& L);
-// head: 1 << 32 in each line's first word at first, words: zeros at first; both only
-// for calls of other than one token per sequence.
-hipError_t launch_recurrence(const RecCall& c, int dtype, int form, bool grad, uint64_t* head,
-                             uint64_t* words, size_t stride, const Launch& L);
-// Room of the scans of up to `tokens` tokens and D channels: tiles, and a tile's words.
-int scan_tiles(int D);
-size_t scan_stride(int64_t tokens);
+// `space` matters only to calls of other than one token per sequence.
+hipError_t launch_recurrence(const RecCall& c, int dtype, int form, bool grad,
+                             const ScanSpace& space, const Launch& L);
+// The room that scans of up to `tokens` tokens and D channels need (head stays null).
+ScanSpace scan_space(int64_t tokens, int D);
 hipError_t launch_logits(LogitsCall c, const Launch& L);
 constexpr int kLogitsMinTile = 1024;  // words of the shortest part
 

@@ -121,7 +121,7 @@ int check_recurrence(polyglot_ctx* ctx, const A& a, const std::string& what) {
     return fail(ctx, POLYGLOT_EINVAL, what + ": misaligned offsets");
   // one token per sequence needs no scan; other calls use the reserved workspace
   if ((a.offsets || a.tokens != a.nseq) &&
-      (!ctx->op.rec_head || a.tokens > ctx->op.rec_tokens || a.D > ctx->op.rec_D))
+      (!ctx->op.rec.head || a.tokens > ctx->op.rec_tokens || a.D > ctx->op.rec_D))
     return fail(ctx, POLYGLOT_EBATCH, what + ": above the reserved tokens or channels");
   return POLYGLOT_OK;
 }
@@ -188,8 +188,7 @@ int polyglot_recurrence(polyglot_ctx* ctx, const polyglot_recurrence_args* args)
     c.fin = a.last;
     c.down = a.reverse != 0;
     Timed tm(ctx, kOpKernels + POLYGLOT_OPK_RECURRENCE);
-    const hipError_t e = launch_recurrence(c, a.dtype, a.form, false, ctx->op.rec_head, ctx->op.rec_words,
-                                           ctx->op.rec_stride, tm.L);
+    const hipError_t e = launch_recurrence(c, a.dtype, a.form, false, ctx->op.rec, tm.L);
     return e == hipSuccess ? POLYGLOT_OK : hip_fail(ctx, e, "recurrence launch");
   });
 }
@@ -228,8 +227,7 @@ int polyglot_recurrence_grad(polyglot_ctx* ctx, const polyglot_recurrence_grad_a
     c.fin = a.dh0;
     c.down = a.reverse == 0;
     Timed tm(ctx, kOpKernels + POLYGLOT_OPK_RECURRENCE_GRAD);
-    const hipError_t e = launch_recurrence(c, a.dtype, a.form, true, ctx->op.rec_head, ctx->op.rec_words,
-                                           ctx->op.rec_stride, tm.L);
+    const hipError_t e = launch_recurrence(c, a.dtype, a.form, true, ctx->op.rec, tm.L);
     return e == hipSuccess ? POLYGLOT_OK : hip_fail(ctx, e, "recurrence_grad launch");
   });
 }
@@ -242,14 +240,14 @@ int polyglot_reserve_recurrence(polyglot_ctx* ctx, int64_t max_tokens, int32_t m
     OpWorkspace& op = ctx->op;
     hipError_t e = hipStreamSynchronize(ctx->stream);
     if (e != hipSuccess) return hip_fail(ctx, e, "reserve_recurrence: sync");
-    if (op.rec_head) e = hipFree(op.rec_head);
-    op.rec_head = op.rec_words = nullptr;
+    if (op.rec.head) e = hipFree(op.rec.head);
+    op.rec = ScanSpace{};
     op.rec_tokens = op.rec_D = 0;
-    const size_t tiles = scan_tiles(max_D), lines = tiles * kHeadLine;
-    op.rec_stride = scan_stride(max_tokens);
-    e = e == hipSuccess ? heads(ctx, &op.rec_head, lines, tiles * op.rec_stride) : e;
+    ScanSpace sp = scan_space(max_tokens, max_D);
+    if (e == hipSuccess)
+      e = heads(ctx, &sp.head, (size_t)sp.counters * kHeadLine, sp.flags + sp.words);
     if (e != hipSuccess) return hip_fail(ctx, e, "reserve_recurrence");
-    op.rec_words = op.rec_head + lines;
+    op.rec = sp;
     op.rec_tokens = max_tokens;
     op.rec_D = max_D;
     return POLYGLOT_OK;

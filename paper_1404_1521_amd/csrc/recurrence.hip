@@ -16,30 +16,39 @@ ScanPlan scan_plan(int64_t tokens, int D, int group, int R) {
   p.lanes_per_group = group > 1 ? ceil_div(group, 4) : 1;
   const int64_t lanes = group > 1 ? (int64_t)p.lanes_per_group * (D / group) : ceil_div(D, 4);
   int log2 = 3;
-  while (log2 < 6 && (1 << log2) < lanes) ++log2;
+  while (log2 < 6 && (1 << log2) < lanes &&
+         (log2 < kScanLanesLog2 || (1 << log2) < p.lanes_per_group))
+    ++log2;
   p.lanes_log2 = log2;
   const int CT = 1 << log2;
   p.groups_per_tile = CT / p.lanes_per_group;
   p.tiles = group > 1 ? ceil_div(D / group, p.groups_per_tile) : ceil_div(D, 4 * CT);
-  const int L = (kBlock / CT) * R;
+  const int L = kBlock / CT * R;
   p.chunks = std::max(1, (int)((tokens + L - 1) / L));
+  p.group_log2 = log2 < 6 ? 4 : 3;  // kScanMateSlots
   return p;
 }
 
 template <class T, int FORM, bool GRAD>
-hipError_t launch_scan(const RecCall& c, uint64_t* head, uint64_t* words, size_t stride,
-                       const Launch& L) {
+hipError_t launch_scan(const RecCall& c, const ScanSpace* space, const Launch& L) {
   constexpr int R = scan_tokens<T, GRAD>();
-  static_assert(kScanMaxRows * R <= kScanMaxTokens, "places of a chunk");
+  static_assert(R >= kScanMinTokens, "scan_space");
   ScanPlan p = scan_plan(c.tokens, c.D, c.group, R);
-  p.head = head;
-  p.words = words;
-  p.stride = stride;
+  if (space) {
+    p.counters = space->counters;
+    p.head = space->head;
+    p.flags = space->head + (size_t)space->counters * kHeadLine;
+    p.words = p.flags + space->flags;
+    const size_t groups = (p.chunks >> p.group_log2) + 1;
+    if (p.tiles > space->counters || p.tiles * (p.chunks + groups) > space->flags ||
+        (p.tiles * (8 * (size_t)p.chunks + 12 * groups) << p.lanes_log2) > space->words)
+      return hipErrorInvalidValue;  // not reached within what scan_space bounds
+  }
   const bool shared = c.group > 1;
   const bool vec = shared ? c.group % 4 == 0 : c.D % 4 == 0;  // whole quads
-  auto k = shared ? (vec ? k_scan<T, FORM, GRAD, true, true, R> : k_scan<T, FORM, GRAD, true, false, R>)
-                  : (vec ? k_scan<T, FORM, GRAD, false, true, R>
-                         : k_scan<T, FORM, GRAD, false, false, R>);
+  auto k = shared ? (vec ? k_scan<T, FORM, GRAD, true, true> : k_scan<T, FORM, GRAD, true, false>)
+                  : (vec ? k_scan<T, FORM, GRAD, false, true>
+                         : k_scan<T, FORM, GRAD, false, false>);
   return pg_launch(k, dim3(p.chunks * p.tiles), dim3(kBlock), 0, L, c, p);
 }
 
@@ -54,29 +63,33 @@ hipError_t launch_step(const RecCall& c, const Launch& L) {
 
 }  // namespace
 
-// Lanes that a group leaves idle at most double the slots (a group of two channels in
-// a lane of four; 33 lanes of 64).
-int scan_tiles(int D) { return ceil_div(2 * D, 4 * kWave) + 1; }
-
-size_t scan_stride(int64_t tokens) {
-  const int64_t L = kBlock / kWave * 8;  // chunks are shortest where a row has 64 lanes
-  return (size_t)((tokens + L - 1) / L + 1) * (2 * 4 * kWave);
+ScanSpace scan_space(int64_t tokens, int D) {
+  // Lanes that a group leaves idle at most double the channels' slots (a group of two
+  // channels in a lane of four; 33 lanes of 64), beside one tile's.  Rows of 64 lanes
+  // have the shortest chunks, rows of 8 the narrowest tiles.
+  const int64_t L = kBlock / kWave * kScanMinTokens, chunks = (tokens + L - 1) / L + 1;
+  ScanSpace sp;
+  sp.counters = ceil_div(2 * D, 4 * kScanMinLanes) + 1;
+  const int64_t groups = chunks / 8 + 1;
+  sp.flags = (size_t)(chunks + groups) * sp.counters;
+  sp.words = (size_t)(2 * chunks + 3 * groups) * (2 * (size_t)D + 4 * kWave);
+  return sp;
 }
 
-hipError_t launch_recurrence(const RecCall& c, int dtype, int form, bool grad, uint64_t* head,
-                             uint64_t* words, size_t stride, const Launch& L) {
+hipError_t launch_recurrence(const RecCall& c, int dtype, int form, bool grad,
+                             const ScanSpace& space, const Launch& L) {
   constexpr int raw = POLYGLOT_GATE_RAW, sig = POLYGLOT_GATE_SIGMOID;
   const bool single = !c.offsets && c.tokens == c.nseq;  // every token starts a sequence
   return by_format(dtype, [&](auto v) {
     using T = decltype(v);
     if (single && !grad)
       return form == raw ? launch_step<T, raw>(c, L) : launch_step<T, sig>(c, L);
-    uint64_t* h = single ? nullptr : head;
+    const ScanSpace* sp = single ? nullptr : &space;
     if (grad)
-      return form == raw ? launch_scan<T, raw, true>(c, h, words, stride, L)
-                         : launch_scan<T, sig, true>(c, h, words, stride, L);
-    return form == raw ? launch_scan<T, raw, false>(c, h, words, stride, L)
-                       : launch_scan<T, sig, false>(c, h, words, stride, L);
+      return form == raw ? launch_scan<T, raw, true>(c, sp, L)
+                         : launch_scan<T, sig, true>(c, sp, L);
+    return form == raw ? launch_scan<T, raw, false>(c, sp, L)
+                       : launch_scan<T, sig, false>(c, sp, L);
   });
 }
 
