@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch  # loaded first: the library then binds to torch's HIP runtime
 
@@ -57,11 +58,17 @@ class Config(ctypes.Structure):
 
 
 def _args(name, *fields):
-    """The ctypes mirror of an argument block of include/polyglot.h."""
-    kinds = {"p": ctypes.c_void_p, "i": ctypes.c_int32, "q": ctypes.c_int64,
-             "u": ctypes.c_uint32, "Q": ctypes.c_uint64, "f": ctypes.c_float}
-    return type(name, (ctypes.Structure,), {
-        "_fields_": [(n, kinds[k]) for k, names in fields for n in names.split()]})
+    """The ctypes mirror of an argument block of include/polyglot.h, with ``pack``: all
+    fields in order to the block's bytes, which an entry point takes as it takes a
+    pointer to the block."""
+    kinds = {"p": (ctypes.c_void_p, "P"), "i": (ctypes.c_int32, "i"), "q": (ctypes.c_int64, "q"),
+             "u": (ctypes.c_uint32, "I"), "Q": (ctypes.c_uint64, "Q"), "f": (ctypes.c_float, "f")}
+    each = [(n, kinds[k]) for k, names in fields for n in names.split()]
+    cls = type(name, (ctypes.Structure,), {"_fields_": [(n, c) for n, (c, _) in each]})
+    block = struct.Struct("@" + "".join(f for _, (_, f) in each) + "0q")
+    assert block.size == ctypes.sizeof(cls)
+    cls.pack = block.pack
+    return cls
 
 
 DropoutArgs = _args("DropoutArgs", ("p", "x add y ids site_dev"), ("q", "rows ld_x ld_add ld_y"),
@@ -109,11 +116,11 @@ def load_library():
         "polyglot_last_error": [p],
         "polyglot_set_timing": [p, ctypes.c_int],
         "polyglot_kernel_times": [p, p, p],
-        "polyglot_dropout": [p, ctypes.POINTER(DropoutArgs)],
-        "polyglot_recurrence": [p, ctypes.POINTER(RecurrenceArgs)],
-        "polyglot_recurrence_grad": [p, ctypes.POINTER(RecurrenceGradArgs)],
+        "polyglot_dropout": [p, p],
+        "polyglot_recurrence": [p, p],
+        "polyglot_recurrence_grad": [p, p],
         "polyglot_reserve_recurrence": [p, ctypes.c_int64, i32],
-        "polyglot_logits": [p, ctypes.POINTER(LogitsArgs)],
+        "polyglot_logits": [p, p],
         "polyglot_reserve_logits": [p, i32, i32],
         "polyglot_operator_times": [p, p, p],
     }
@@ -144,10 +151,10 @@ def _row_tensor(t, dtype, name, rows, width):
     consecutive elements, any distance apart."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device (cuda) tensor")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device (cuda) tensor")
     if t.shape != (rows, width):
         raise ValueError(f"{name} must have shape {(rows, width)}, got {tuple(t.shape)}")
     if t.is_contiguous():
@@ -159,9 +166,9 @@ def _row_tensor(t, dtype, name, rows, width):
 
 
 def _vector(t, dtype, name, n):
-    """Pointer of a contiguous device vector of n values (None: NULL)."""
+    """Pointer of a contiguous device vector of n values (None: 0)."""
     if t is None:
-        return None
+        return 0
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda or not t.is_contiguous():
@@ -174,9 +181,9 @@ def _vector(t, dtype, name, n):
 
 
 def _state(t, name, nseq, D):
-    """Pointer of a contiguous float32 device tensor [nseq][D] (None: NULL)."""
+    """Pointer of a contiguous float32 device tensor [nseq][D] (None: 0)."""
     if t is None:
-        return None
+        return 0
     p, ld = _row_tensor(t, torch.float32, name, nseq, D)
     if ld != D:
         raise ValueError(f"{name} must be contiguous")
@@ -184,16 +191,18 @@ def _state(t, name, nseq, D):
 
 
 def _format(t, name):
+    """A tensor's storage format and dtype."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.dtype not in _FORMATS:
+    code = _FORMATS.get(t.dtype)
+    if code is None:
         raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
-    return _FORMATS[t.dtype]
+    return code, t.dtype
 
 
-def _flat(t, name):
+def _flat(t):
     """A [nseq][T][width] tensor as rows of tokens."""
-    return None if t is None else t if t.dim() == 2 else t.view(-1, t.shape[-1])
+    return t if t is None or t.dim() == 2 else t.view(-1, t.shape[-1])
 
 
 NOALLOC_MAX_N = 8192  # POLYGLOT_NOALLOC_MAX_N
@@ -369,26 +378,28 @@ class Context:
         """out[r] = dropout(x[r]) (+ add[r]), or of the rows ids[r] of a table x.  The mask
         is a function of (seed, site + site_dev, first_row + r, column) alone and is never
         stored; dropout_backward computes it again.  float32, bfloat16 or float16."""
-        a = DropoutArgs()
-        a.dtype = _format(x, "x")
+        code, dtype = _format(x, "x")
         if x.dim() != 2:
             raise ValueError("x must have two dimensions")
         rows, d = x.shape
-        a.x, a.ld_x = _row_tensor(x, x.dtype, "x", rows, d)
+        px, ld_x = _row_tensor(x, dtype, "x", rows, d)
+        pids = id_bytes = table_rows = padd = ld_add = 0
         if ids is not None:
             if ids.dtype not in (torch.int32, torch.int64):
                 raise TypeError(f"ids must be int32 or int64, got {ids.dtype}")
-            a.table_rows, rows = rows, ids.shape[0]
-            a.ids, a.id_bytes = _vector(ids, ids.dtype, "ids", rows), ids.element_size()
+            table_rows, rows = rows, ids.shape[0]
+            pids, id_bytes = _vector(ids, ids.dtype, "ids", rows), ids.element_size()
         if add is not None:
-            a.add, a.ld_add = _row_tensor(add, x.dtype, "add", rows, d)
+            padd, ld_add = _row_tensor(add, dtype, "add", rows, d)
         if out is None:
-            out = torch.empty((rows, d), dtype=x.dtype, device=x.device)
-        a.y, a.ld_y = _row_tensor(out, x.dtype, "out", rows, d)
-        a.site_dev = _vector(site_dev, torch.int32, "site_dev", 1)
-        a.rows, a.d, a.p, a.whole_rows = rows, d, p, whole_rows
-        a.seed, a.site, a.first_row = seed, site, first_row
-        self._check(self._lib.polyglot_dropout(self._h, ctypes.byref(a)), "dropout")
+            out = x.new_empty((rows, d))
+        py, ld_y = _row_tensor(out, dtype, "out", rows, d)
+        rc = self._lib.polyglot_dropout(self._h, DropoutArgs.pack(
+            px, padd, py, pids, _vector(site_dev, torch.int32, "site_dev", 1), rows, ld_x, ld_add,
+            ld_y, seed & 0xFFFFFFFFFFFFFFFF, first_row, site & 0xFFFFFFFF, p, d, code, id_bytes,
+            table_rows, whole_rows))
+        if rc != OK:
+            self._check(rc, "dropout")
         return out
 
     def dropout_backward(self, dy, p: float, seed: int, *, site: int = 0, site_dev=None,
@@ -399,23 +410,35 @@ class Context:
                             whole_rows=whole_rows, out=out)
 
     @staticmethod
-    def _sequences(a, x, gate, offsets, form, reverse):
-        """Fills what a recurrence and its gradient share; returns (tokens, D, gates)."""
-        a.dtype = _format(x, "x")
+    def _sequences(x, gate, offsets):
+        """What a recurrence and its gradient share of their inputs' checks: storage format,
+        dtype, token count, channels, gates, and the gate's, x's and the offsets' pointers."""
+        code, dtype = _format(x, "x")
         tokens, D = x.shape
         gates = gate.shape[-1]
         if gates < 1 or D % gates:
             raise ValueError(f"gate has {gates} columns, which do not divide {D} channels")
-        a.gate, a.ld_gate = _row_tensor(gate, x.dtype, "gate", tokens, gates)
-        a.x, a.ld_x = _row_tensor(x, x.dtype, "x", tokens, D)
+        poff = off_bytes = 0
         if offsets is not None:
             if offsets.dtype not in (torch.int32, torch.int64):
                 raise TypeError(f"offsets must be int32 or int64, got {offsets.dtype}")
-            a.offsets = _vector(offsets, offsets.dtype, "offsets", offsets.shape[0])
-            a.offset_bytes = offsets.element_size()
-            a.nseq = offsets.shape[0] - 1
-        a.tokens, a.D, a.group, a.form, a.reverse = tokens, D, D // gates, form, reverse
-        return tokens, D, gates
+            poff = _vector(offsets, offsets.dtype, "offsets", offsets.shape[0])
+            off_bytes = offsets.element_size()
+        return (code, dtype, tokens, D, gates, *_row_tensor(gate, dtype, "gate", tokens, gates),
+                *_row_tensor(x, dtype, "x", tokens, D), poff, off_bytes)
+
+    def _forward(self, what, gate, x, offsets, nseq, h0, form, reverse, out, last):
+        code, dtype, tokens, D, gates, pg_, ld_g, px, ld_x, poff, off_bytes = self._sequences(
+            x, gate, offsets)
+        if last is None:
+            last = x.new_empty((nseq, D), dtype=torch.float32)
+        ph, ld_h = _row_tensor(_flat(out), dtype, "out", tokens, D)
+        rc = self._lib.polyglot_recurrence(self._h, RecurrenceArgs.pack(
+            pg_, px, _state(h0, "h0", nseq, D), poff, ph, _state(last, "last", nseq, D), tokens,
+            ld_g, ld_x, ld_h, nseq, D, D // gates, code, off_bytes, form, reverse))
+        if rc != OK:
+            self._check(rc, what)
+        return out, last
 
     def recurrence(self, gate, x, offsets=None, *, h0=None, form: int = GATE_SIGMOID,
                    reverse: bool = False, out=None, last=None):
@@ -424,60 +447,45 @@ class Context:
         [nseq][T][D] without, or one sequence [T][D].  gate has D columns, or fewer that
         divide D, each for D / columns consecutive channels.  h0 and last are float32
         [nseq][D].  Returns (h, last)."""
-        a = RecurrenceArgs()
-        shape = x.shape
-        a.nseq = shape[0] if x.dim() == 3 else 1
-        x, gate = _flat(x, "x"), _flat(gate, "gate")
-        tokens, D, _ = self._sequences(a, x, gate, offsets, form, reverse)
+        nseq = offsets.shape[0] - 1 if offsets is not None else x.shape[0] if x.dim() == 3 else 1
         if out is None:
-            out = torch.empty(shape, dtype=x.dtype, device=x.device)
-        if last is None:
-            last = torch.empty((a.nseq, D), dtype=torch.float32, device=x.device)
-        a.h, a.ld_h = _row_tensor(_flat(out, "out"), x.dtype, "out", tokens, D)
-        a.h0, a.last = _state(h0, "h0", a.nseq, D), _state(last, "last", a.nseq, D)
-        self._check(self._lib.polyglot_recurrence(self._h, ctypes.byref(a)), "recurrence")
-        return out, last
+            out = x.new_empty(x.shape)
+        return self._forward("recurrence", _flat(gate), _flat(x), offsets, nseq, h0, form, reverse,
+                             out, last)
 
     def recurrence_step(self, gate, x, state=None, *, form: int = GATE_SIGMOID, out=None,
                         last=None):
         """One token x[nseq][D] for each of nseq sequences whose float32 states are
         state[nseq][D].  Returns (h, the new states); last=state updates them in place."""
-        a = RecurrenceArgs()
-        a.nseq = x.shape[0]
-        tokens, D, _ = self._sequences(a, x, gate, None, form, False)
         if out is None:
-            out = torch.empty((tokens, D), dtype=x.dtype, device=x.device)
-        if last is None:
-            last = torch.empty((tokens, D), dtype=torch.float32, device=x.device)
-        a.h, a.ld_h = _row_tensor(out, x.dtype, "out", tokens, D)
-        a.h0, a.last = _state(state, "state", tokens, D), _state(last, "last", tokens, D)
-        self._check(self._lib.polyglot_recurrence(self._h, ctypes.byref(a)), "recurrence_step")
-        return out, last
+            out = x.new_empty(x.shape)
+        return self._forward("recurrence_step", gate, x, None, x.shape[0], state, form, False, out,
+                             last)
 
     def recurrence_backward(self, gate, x, h, dh, offsets=None, *, h0=None, dlast=None,
                             form: int = GATE_SIGMOID, reverse: bool = False, dgate=None, dx=None,
                             dh0=None):
         """The gradient of recurrence, for its inputs, its output h and the gradients dh of h
         and dlast of last.  Returns (dgate, dx, dh0); dh0 is None unless h0 or dh0 is given."""
-        a = RecurrenceGradArgs()
-        shape, gate_shape = x.shape, gate.shape
-        a.nseq = shape[0] if x.dim() == 3 else 1
-        x, gate, h, dh = (_flat(t, n) for t, n in ((x, "x"), (gate, "gate"), (h, "h"), (dh, "dh")))
-        tokens, D, gates = self._sequences(a, x, gate, offsets, form, reverse)
+        nseq = offsets.shape[0] - 1 if offsets is not None else x.shape[0] if x.dim() == 3 else 1
         if dgate is None:
-            dgate = torch.empty(gate_shape, dtype=x.dtype, device=x.device)
+            dgate = x.new_empty(gate.shape)
         if dx is None:
-            dx = torch.empty(shape, dtype=x.dtype, device=x.device)
+            dx = x.new_empty(x.shape)
+        code, dtype, tokens, D, gates, pg_, ld_g, px, ld_x, poff, off_bytes = self._sequences(
+            _flat(x), _flat(gate), offsets)
         if dh0 is None and h0 is not None:
-            dh0 = torch.empty((a.nseq, D), dtype=torch.float32, device=x.device)
-        a.h, a.ld_h = _row_tensor(h, x.dtype, "h", tokens, D)
-        a.dh, a.ld_dh = _row_tensor(dh, x.dtype, "dh", tokens, D)
-        a.dgate, a.ld_dgate = _row_tensor(_flat(dgate, "dgate"), x.dtype, "dgate", tokens, gates)
-        a.dx, a.ld_dx = _row_tensor(_flat(dx, "dx"), x.dtype, "dx", tokens, D)
-        a.h0, a.dlast = _state(h0, "h0", a.nseq, D), _state(dlast, "dlast", a.nseq, D)
-        a.dh0 = _state(dh0, "dh0", a.nseq, D)
-        self._check(self._lib.polyglot_recurrence_grad(self._h, ctypes.byref(a)),
-                    "recurrence_backward")
+            dh0 = x.new_empty((nseq, D), dtype=torch.float32)
+        ph, ld_h = _row_tensor(_flat(h), dtype, "h", tokens, D)
+        pdh, ld_dh = _row_tensor(_flat(dh), dtype, "dh", tokens, D)
+        pdg, ld_dg = _row_tensor(_flat(dgate), dtype, "dgate", tokens, gates)
+        pdx, ld_dx = _row_tensor(_flat(dx), dtype, "dx", tokens, D)
+        rc = self._lib.polyglot_recurrence_grad(self._h, RecurrenceGradArgs.pack(
+            pg_, px, ph, pdh, _state(h0, "h0", nseq, D), _state(dlast, "dlast", nseq, D), poff, pdg,
+            pdx, _state(dh0, "dh0", nseq, D), tokens, ld_g, ld_x, ld_h, ld_dh, ld_dg, ld_dx, nseq,
+            D, D // gates, code, off_bytes, form, reverse))
+        if rc != OK:
+            self._check(rc, "recurrence_backward")
         return dgate, dx, dh0
 
     def logits(self, logits, *, history=None, lengths=None, prompt=None, repetition=None,
@@ -487,38 +495,38 @@ class Context:
         bias[V] or [rows][V], and the mask's bits (int32 words; see polyglot_logits).
         Returns (out, token, lse): the scores in their own dtype (out may be logits itself;
         None with write=False), the int32 choice of each row and its float32 log-sum-exp."""
-        a = LogitsArgs()
-        a.dtype = _format(logits, "logits")
+        code, dtype = _format(logits, "logits")
         if logits.dim() != 2:
             raise ValueError("logits must have two dimensions")
         rows, V = logits.shape
-        a.rows, a.V = rows, V
-        a.logits, a.ld_logits = _row_tensor(logits, logits.dtype, "logits", rows, V)
+        pl, ld_l = _row_tensor(logits, dtype, "logits", rows, V)
+        po = ld_o = ph = ld_h = cap = plen = ppr = pb = ld_b = pm = ld_m = masks = pmr = 0
         if out is None and write:
-            out = torch.empty((rows, V), dtype=logits.dtype, device=logits.device)
+            out = logits.new_empty((rows, V))
         if out is not None:
-            a.out, a.ld_out = _row_tensor(out, logits.dtype, "out", rows, V)
+            po, ld_o = _row_tensor(out, dtype, "out", rows, V)
         if history is not None:
-            a.history_cap = history.shape[1]
-            a.history, a.ld_history = _row_tensor(history, torch.int32, "history", rows,
-                                                  a.history_cap)
-            a.lengths = _vector(lengths, torch.int32, "lengths", rows)
-            a.prompt = _vector(prompt, torch.int32, "prompt", rows)
-        a.repetition = _vector(repetition, torch.float32, "repetition", rows)
-        a.presence = _vector(presence, torch.float32, "presence", rows)
-        a.frequency = _vector(frequency, torch.float32, "frequency", rows)
+            cap = history.shape[1]
+            ph, ld_h = _row_tensor(history, torch.int32, "history", rows, cap)
+            plen = _vector(lengths, torch.int32, "lengths", rows)
+            ppr = _vector(prompt, torch.int32, "prompt", rows)
         if bias is not None and bias.dim() == 1:
-            a.bias = _vector(bias, torch.float32, "bias", V)
+            pb = _vector(bias, torch.float32, "bias", V)
         elif bias is not None:
-            a.bias, a.ld_bias = _row_tensor(bias, torch.float32, "bias", rows, V)
+            pb, ld_b = _row_tensor(bias, torch.float32, "bias", rows, V)
         if mask is not None:
-            a.masks = mask.shape[0]
-            a.mask, a.ld_mask = _row_tensor(mask, torch.int32, "mask", a.masks, (V + 31) // 32)
-            a.mask_rows = _vector(mask_rows, torch.int32, "mask_rows", rows)
-        token = torch.empty(rows, dtype=torch.int32, device=logits.device)
-        lse = torch.empty(rows, dtype=torch.float32, device=logits.device)
-        a.token, a.lse = token.data_ptr(), lse.data_ptr()
-        self._check(self._lib.polyglot_logits(self._h, ctypes.byref(a)), "logits")
+            masks = mask.shape[0]
+            pm, ld_m = _row_tensor(mask, torch.int32, "mask", masks, (V + 31) // 32)
+            pmr = _vector(mask_rows, torch.int32, "mask_rows", rows)
+        token = logits.new_empty(rows, dtype=torch.int32)
+        lse = logits.new_empty(rows, dtype=torch.float32)
+        rc = self._lib.polyglot_logits(self._h, LogitsArgs.pack(
+            pl, po, ph, plen, ppr, _vector(repetition, torch.float32, "repetition", rows),
+            _vector(presence, torch.float32, "presence", rows),
+            _vector(frequency, torch.float32, "frequency", rows), pb, pm, pmr, token.data_ptr(),
+            lse.data_ptr(), ld_l, ld_o, ld_h, ld_b, ld_m, rows, V, code, cap, masks))
+        if rc != OK:
+            self._check(rc, "logits")
         return out, token, lse
 
     def operator_times(self) -> dict:

@@ -29,12 +29,9 @@ ScanPlan scan_plan(int64_t tokens, int D, int group, int R) {
   return p;
 }
 
-template <class T, int FORM, bool GRAD>
-hipError_t launch_scan(const RecCall& c, const ScanSpace* space, const Launch& L) {
-  constexpr int R = scan_tokens<T, GRAD>();
-  static_assert(R >= kScanMinTokens, "scan_space");
-  ScanPlan p = scan_plan(c.tokens, c.D, c.group, R);
-  if (space) {
+template <class T, int FORM, bool GRAD, int R>
+hipError_t launch_cut(const RecCall& c, ScanPlan p, const ScanSpace* space, const Launch& L) {
+  if (space && p.chunks > 1) {  // one chunk waits for nobody
     p.counters = space->counters;
     p.head = space->head;
     p.flags = space->head + (size_t)space->counters * kHeadLine;
@@ -46,10 +43,22 @@ hipError_t launch_scan(const RecCall& c, const ScanSpace* space, const Launch& L
   }
   const bool shared = c.group > 1;
   const bool vec = shared ? c.group % 4 == 0 : c.D % 4 == 0;  // whole quads
-  auto k = shared ? (vec ? k_scan<T, FORM, GRAD, true, true> : k_scan<T, FORM, GRAD, true, false>)
-                  : (vec ? k_scan<T, FORM, GRAD, false, true>
-                         : k_scan<T, FORM, GRAD, false, false>);
+  auto k = shared ? (vec ? k_scan<T, FORM, GRAD, true, true, R>
+                         : k_scan<T, FORM, GRAD, true, false, R>)
+                  : (vec ? k_scan<T, FORM, GRAD, false, true, R>
+                         : k_scan<T, FORM, GRAD, false, false, R>);
   return pg_launch(k, dim3(p.chunks * p.tiles), dim3(kBlock), 0, L, c, p);
+}
+
+template <class T, int FORM, bool GRAD>
+hipError_t launch_scan(const RecCall& c, const ScanSpace* space, const Launch& L) {
+  constexpr int R = scan_tokens<T, GRAD>();
+  static_assert(R >= kScanMinTokens, "scan_space");
+  const ScanPlan p = scan_plan(c.tokens, c.D, c.group, R);
+  if ((int64_t)p.chunks * p.tiles >= kScanFewWorkgroups)
+    return launch_cut<T, FORM, GRAD, R>(c, p, space, L);
+  return launch_cut<T, FORM, GRAD, kScanShortTokens>(
+      c, scan_plan(c.tokens, c.D, c.group, kScanShortTokens), space, L);
 }
 
 template <class T, int FORM>
@@ -73,6 +82,11 @@ ScanSpace scan_space(int64_t tokens, int D) {
   const int64_t groups = chunks / 8 + 1;
   sp.flags = (size_t)(chunks + groups) * sp.counters;
   sp.words = (size_t)(2 * chunks + 3 * groups) * (2 * (size_t)D + 4 * kWave);
+  // the short cut has up to four times the chunks of the few workgroups, and a tile's
+  // last one and its group beside them
+  const size_t few = 4 * kScanFewWorkgroups + 2 * (size_t)sp.counters;
+  sp.flags += 2 * few;
+  sp.words += 20 * few * kWave;
   return sp;
 }
 

@@ -163,6 +163,10 @@ constexpr int scan_tokens() {
   return !GRAD ? 16 : sizeof(T) == 2 ? 12 : 8;
 }
 constexpr int kScanMinTokens = 8;
+// ... and of calls that so have fewer workgroups than there are CUs: their time
+// is latency, and a thread's share of the work is part of it.
+constexpr int kScanShortTokens = 4;
+constexpr int kScanFewWorkgroups = kCus;
 constexpr int kScanMinLanes = 8;  // of a row of threads
 // Lanes of a row of threads where a group of channels does not ask for more: 16 lanes
 // of four channels are whole cache lines of 16-bit elements, and a chunk of 16 rows is
@@ -192,9 +196,8 @@ struct ScanLds {
   uint64_t ticket;
 };
 
-template <class T, int FORM, bool GRAD, bool SHARED, bool VEC>
+template <class T, int FORM, bool GRAD, bool SHARED, bool VEC, int R>
 __global__ __launch_bounds__(kBlock, 2) void k_scan(RecCall c, ScanPlan p) {
-  constexpr int R = scan_tokens<T, GRAD>();
   constexpr bool kUsesX = GRAD && FORM == POLYGLOT_GATE_SIGMOID;
   __shared__ ScanLds<R> s;
   const int t = threadIdx.x;
