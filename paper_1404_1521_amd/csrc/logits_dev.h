@@ -15,16 +15,40 @@
 namespace pg {
 
 constexpr uint32_t kLogitsSpinLimit = 1u << 22;  // a wait that only a library bug makes
-constexpr uint32_t kInHistory = 0x80000000u;  // of a counter; the low bits count the made part
+// A counter of the words that a workgroup holds: its top bit says that the word is in
+// the history, the others count its made part.  16 bits, two counters to a word of LDS,
+// for histories of at most 32,767 ids; 32 bits for longer ones.
+template <bool LONG>
+struct Counters {
+  static constexpr int kBits = LONG ? 32 : 16;
+  static constexpr uint32_t kIn = 1u << (kBits - 1);
+  static constexpr int words(int n) { return LONG ? n : n / 2; }
+  static __device__ __forceinline__ void add(uint32_t* c, int i, bool made) {
+    uint32_t* w = c + (LONG ? i : i >> 1);
+    const int shift = LONG ? 0 : 16 * (i & 1);
+    atomicOr(w, kIn << shift);
+    if (made) atomicAdd(w, 1u << shift);
+  }
+  // The four from i on (i a multiple of four).
+  static __device__ __forceinline__ void quad(const uint32_t* c, int i, uint32_t (&k)[4]) {
+    if constexpr (LONG) {
+      const uint4 q = *reinterpret_cast<const uint4*>(c + i);
+      k[0] = q.x, k[1] = q.y, k[2] = q.z, k[3] = q.w;
+    } else {
+      const uint2 q = *reinterpret_cast<const uint2*>(c + i / 2);
+      k[0] = q.x & 0xffffu, k[1] = q.x >> 16, k[2] = q.y & 0xffffu, k[3] = q.y >> 16;
+    }
+  }
+};
 
 struct RowRules {
   float rep, freq, pres;
 };
 // Products and sums are kept apart: a fused multiply-add would round other scores
 // to equal, or equal ones apart.
-__device__ __forceinline__ float ruled(float l, uint32_t seen, const RowRules& k) {
+__device__ __forceinline__ float ruled(float l, uint32_t seen, uint32_t in, const RowRules& k) {
   if (seen) l = l > 0.f ? __fdiv_rn(l, k.rep) : __fmul_rn(l, k.rep);
-  const uint32_t n = seen & ~kInHistory;
+  const uint32_t n = seen & ~in;
   if (n) l = __fsub_rn(l, __fadd_rn(__fmul_rn(k.freq, (float)n), k.pres));
   return l;
 }
@@ -130,10 +154,12 @@ __device__ __forceinline__ Quad<T> row_quad(const T* row, int v, int V, bool who
 }
 
 // E words per thread, in quads 4 * 256 words apart.
-template <class T, int E>
+template <class T, int E, bool LONG>
 __global__ __launch_bounds__(kBlock) void k_logits(LogitsCall c) {
-  constexpr int Q = E / 4;
-  __shared__ __align__(16) uint32_t seen[E * kBlock];
+  constexpr int Q = E / 4, kWords = E * kBlock;  // the part's words
+  using Count = Counters<LONG>;
+  __shared__ __align__(16) uint32_t seen[Count::words(kWords)];
+  __shared__ uint32_t allowed[kWords / 32];
   __shared__ LogitsLds lds;
   const polyglot_logits_args& a = c.a;
   const int t = threadIdx.x;
@@ -151,18 +177,23 @@ __global__ __launch_bounds__(kBlock) void k_logits(LogitsCall c) {
     }
     if (m >= 0) mask = a.mask + (int64_t)m * a.ld_mask;
   }
-  // the part's scores and mask in flight
+  // the part's scores, its part of the mask and the first of the history in flight: the
+  // history up to what there is room for, what its length leaves out is skipped later
+  constexpr int kAhead = 8;
+  const int32_t* hist = a.history ? a.history + (int64_t)r * a.ld_history : nullptr;
+  int id[kAhead];
+  if (hist) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      id[j] = t + j * kBlock < a.history_cap ? hist[t + j * kBlock] : -1;
+  }
   Quad<T> x[Q];
-  uint32_t allow[Q];
 #pragma unroll
   for (int g = 0; g < Q; ++g) x[g] = row_quad<T>(in, v0 + g * 4 * kBlock, a.V, whole);
-  if (mask) {
-#pragma unroll
-    for (int g = 0; g < Q; ++g) {
-      const int v = v0 + g * 4 * kBlock;
-      allow[g] = mask[min(v, a.V - 1) >> 5] >> (v & 31);
-    }
-  }
+  constexpr int kMaskWords = kWords / 32;
+  static_assert(kMaskWords <= kBlock, "a word of the mask for each thread");
+  uint32_t bits = 0;
+  if (mask && t < kMaskWords) bits = mask[min(tile * kMaskWords + t, (a.V - 1) >> 5)];
   uint32_t tag = 0;
   if (c.head && t == 0)  // the row's tag moves on once all its parts are in
     tag = (uint32_t)(__hip_atomic_load(c.head + r * kHeadLine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >> 32);
@@ -174,24 +205,20 @@ __global__ __launch_bounds__(kBlock) void k_logits(LogitsCall c) {
     prompt = a.prompt ? min(max(a.prompt[r], 0), a.history_cap) : 0;
   }
   if (len > 0) {
-    const int32_t* hist = a.history + (int64_t)r * a.ld_history;
-    constexpr int kAhead = 8;
-    int id[kAhead];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) id[j] = t + j * kBlock < len ? hist[t + j * kBlock] : -1;
-#pragma unroll
-    for (int g = 0; g < Q; ++g)
-      *reinterpret_cast<uint4*>(seen + (g * kBlock + t) * 4) = uint4{0u, 0u, 0u, 0u};
-    __syncthreads();
+    uint4* const z = reinterpret_cast<uint4*>(seen);
+    for (int i = t; i < Count::words(kWords) / 4; i += kBlock) z[i] = uint4{0u, 0u, 0u, 0u};
+  }
+  if (mask && t < kMaskWords) allowed[t] = bits;
+  if (len > 0 || mask) __syncthreads();
+  if (len > 0) {
+    const int first = tile * kWords;
     for (int k0 = t;;) {
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
+        const int k = k0 + j * kBlock;
+        if (k >= len) continue;
         if (id[j] >= a.V) atomicOr(c.flag, kFlagBadId);
-        const int first = tile * (E * kBlock);
-        if (id[j] >= first && id[j] - first < E * kBlock) {
-          atomicOr(&seen[id[j] - first], kInHistory);
-          if (k0 + j * kBlock >= prompt) atomicAdd(&seen[id[j] - first], 1u);
-        }
+        else if (id[j] >= first && id[j] - first < kWords) Count::add(seen, id[j] - first, k >= prompt);
       }
       k0 += kAhead * kBlock;
       if (k0 - t >= len) break;
@@ -206,12 +233,11 @@ __global__ __launch_bounds__(kBlock) void k_logits(LogitsCall c) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) l[4 * g + j] = x[g].get(j);
     if (len > 0) {
-      const uint4 k = *reinterpret_cast<const uint4*>(seen + (g * kBlock + t) * 4);
-      if (k.x | k.y | k.z | k.w) {
-        l[4 * g] = ruled(l[4 * g], k.x, rules);
-        l[4 * g + 1] = ruled(l[4 * g + 1], k.y, rules);
-        l[4 * g + 2] = ruled(l[4 * g + 2], k.z, rules);
-        l[4 * g + 3] = ruled(l[4 * g + 3], k.w, rules);
+      uint32_t k[4];
+      Count::quad(seen, (g * kBlock + t) * 4, k);
+      if (k[0] | k[1] | k[2] | k[3]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) l[4 * g + j] = ruled(l[4 * g + j], k[j], Count::kIn, rules);
       }
     }
   }
@@ -224,8 +250,13 @@ __global__ __launch_bounds__(kBlock) void k_logits(LogitsCall c) {
   }
   if (mask) {
 #pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (!(allow[i / 4] >> (i & 3) & 1u)) l[i] = -__builtin_inff();
+    for (int g = 0; g < Q; ++g) {
+      const int v = (g * kBlock + t) * 4;
+      const uint32_t allow = allowed[v >> 5] >> (v & 31);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (!(allow >> j & 1u)) l[4 * g + j] = -__builtin_inff();
+    }
   }
   if (a.out) {
     T* out = static_cast<T*>(a.out) + (int64_t)r * a.ld_out;
@@ -265,6 +296,13 @@ __global__ __launch_bounds__(kBlock) void k_logits(LogitsCall c) {
     }
   }
   lowest_and_sum(w, s, lds);
+  if (c.tiles == 1) {
+    if (t == 0) {
+      if (a.token) a.token[r] = w == kNoWord ? -1 : w;
+      if (a.lse) a.lse[r] = log_sum(m, s);
+    }
+    return;
+  }
   uint64_t* words = c.words + (int64_t)r * c.stride * 3;
   if (t == 0) {
     publish_word(words + tile * 3, __float_as_uint(m), tag);

@@ -32,15 +32,22 @@ hipError_t launch_dropout(const DropoutCall& c, const Launch& L) {
 }
 
 hipError_t launch_logits(LogitsCall c, const Launch& L) {
-  // the longest parts that still give every CU four workgroups
+  // Long parts read the history and the row's rules fewer times; short ones spread a few
+  // rows over the chip.  The longest that give every CU two workgroups: 256 rows of
+  // 1,000,000 in parts of 2,048 words 456 us, 4,096 328, 8,192 266, 16,384 (fewer
+  // workgroups to a CU) 276; 48 rows of 32,003 in parts of 1,024 9.8, 2,048 9.2, 4,096
+  // 10.2.
   int E = 32;
-  while (E > 4 && (int64_t)c.a.rows * ceil_div(c.a.V, E * kBlock) < 4 * kCus) E /= 2;
+  while (E > 4 && (int64_t)c.a.rows * ceil_div(c.a.V, E * kBlock) < 2 * kCus) E /= 2;
   c.tiles = ceil_div(c.a.V, E * kBlock);
   if ((int64_t)c.a.rows * c.tiles > INT32_MAX) return hipErrorInvalidValue;
   return by_format(c.a.dtype, [&](auto v) {
     using T = decltype(v);
-    auto k = E == 32 ? k_logits<T, 32> : E == 16 ? k_logits<T, 16> : E == 8 ? k_logits<T, 8>
-                                                                          : k_logits<T, 4>;
+    const bool many = c.a.history && c.a.history_cap > 32767;
+    auto k = E == 32   ? (many ? k_logits<T, 32, true> : k_logits<T, 32, false>)
+             : E == 16 ? (many ? k_logits<T, 16, true> : k_logits<T, 16, false>)
+             : E == 8  ? (many ? k_logits<T, 8, true> : k_logits<T, 8, false>)
+                       : (many ? k_logits<T, 4, true> : k_logits<T, 4, false>);
     return pg_launch(k, dim3(c.a.rows * c.tiles), dim3(kBlock), 0, L, c);
   });
 }
