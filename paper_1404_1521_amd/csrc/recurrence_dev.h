@@ -18,6 +18,8 @@
 // What a reset leaves behind is never multiplied by zero but dropped, so that
 // infinities and NaN stay in their sequence.
 #pragma once
+#include <type_traits>
+
 #include "formats.h"
 #include "operators.h"
 
@@ -354,47 +356,55 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(RecCall c, ScanPlan p) {
   bool cut = false;
 #pragma unroll
   for (int v = 0; v < 4; ++v) A[v] = 1.f, B[v] = 0.f;
+  // A chunk in the middle of a sequence has no ends and no missing tokens: it goes
+  // through without a look at either (a branch for each token kept 7 moves per element).
+  const bool plain = !any && count == L;
+  const auto first_pass = [&](auto is_plain) {
+    constexpr bool PLAIN = decltype(is_plain)::value;
 #pragma unroll
-  for (int i = 0; i < R; ++i) {
-    float da[4], rest = 1.f;
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      if (!SHARED || v == 0) {
-        const float g = SHARED ? Elem<T>::get(gs[SHARED ? i : 0]) : gq[SHARED ? 0 : i].get(v);
-        if constexpr (GRAD) {
-          a[i][SHARED ? 0 : v] = keep_gate<FORM>(g);
-          da[v] = decay<FORM>(a[i][SHARED ? 0 : v]).a;
-        } else {
-          gate_pair<FORM>(g, da[v], rest);
-          a[i][SHARED ? 0 : v] = da[v];
-        }
-      } else {
-        da[v] = da[0];
-      }
-      b[i][v] = in[i].get(v);
-      if (!GRAD) b[i][v] *= rest;
-    }
-    if (any) {
-      const int from = s.start[tl * R + i];
-      if (from >= 0) {
-        cut = true;
-        Quad<float> start{};
-        if (c.init) start = load_quad<float, VEC>(c.init + (size_t)from * c.D + own, nv);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          B[v] = 0.f;
-          b[i][v] = __fmaf_rn(GRAD ? 1.f : da[v], start.get(v), b[i][v]);
-        }
-      }
-    }
-    if (tl * R + i < count) {
+    for (int i = 0; i < R; ++i) {
+      float da[4], rest = 1.f;
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        B[v] = GRAD ? da[v] * (b[i][v] + B[v]) : __fmaf_rn(da[v], B[v], b[i][v]);
-        A[v] *= da[v];
+        if (!SHARED || v == 0) {
+          const float g = SHARED ? Elem<T>::get(gs[SHARED ? i : 0]) : gq[SHARED ? 0 : i].get(v);
+          if constexpr (GRAD) {
+            a[i][SHARED ? 0 : v] = keep_gate<FORM>(g);
+            da[v] = decay<FORM>(a[i][SHARED ? 0 : v]).a;
+          } else {
+            gate_pair<FORM>(g, da[v], rest);
+            a[i][SHARED ? 0 : v] = da[v];
+          }
+        } else {
+          da[v] = da[0];
+        }
+        b[i][v] = in[i].get(v);
+        if (!GRAD) b[i][v] *= rest;
+      }
+      if constexpr (!PLAIN) {
+        const int from = s.start[tl * R + i];
+        if (from >= 0) {
+          cut = true;
+          Quad<float> start{};
+          if (c.init) start = load_quad<float, VEC>(c.init + (size_t)from * c.D + own, nv);
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            B[v] = 0.f;
+            b[i][v] = __fmaf_rn(GRAD ? 1.f : da[v], start.get(v), b[i][v]);
+          }
+        }
+      }
+      if (PLAIN || tl * R + i < count) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          B[v] = GRAD ? da[v] * (b[i][v] + B[v]) : __fmaf_rn(da[v], B[v], b[i][v]);
+          A[v] *= da[v];
+        }
       }
     }
-  }
+  };
+  if (plain) first_pass(std::true_type{});
+  else first_pass(std::false_type{});
   // The rows of a wave by doubling: [A, B] of the rows up to this one, closed where a
   // sequence starts in them (then A says nothing).  The waves through LDS.
   const int wave = t / kWave, lane = t & (kWave - 1);
@@ -606,44 +616,49 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(RecCall c, ScanPlan p) {
   if (GRAD)
     dgate = static_cast<T*>(c.dgate) + first * c.ld_dgate + (SHARED ? col : own);
   float sum[GRAD && SHARED ? R : 1];
+  const auto second_pass = [&](auto is_plain) {
+    constexpr bool PLAIN = decltype(is_plain)::value;
 #pragma unroll
-  for (int i = 0; i < R; ++i) {
-    const bool ok = live && tl * R + i < count;
-    int to = -1;
-    if (any) {
-      if (s.start[tl * R + i] >= 0) st[0] = st[1] = st[2] = st[3] = 0.f;
-      to = s.stop[tl * R + i];
-    }
-    Quad<float> h0{};
-    if (GRAD && any && to >= 0 && c.h0) h0 = load_quad<float, VEC>(c.h0 + (size_t)to * c.D + own, nv);
-    float o[4], dg[4];
-    Decay d{};
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      if constexpr (GRAD) {
-        // (settled: computed again and not kept from the first pass)
-        if (!SHARED || v == 0) d = decay<FORM>(settled(a[i][SHARED ? 0 : v]));
-        const float lam = b[i][v] + st[v];
-        float h = hp[i].get(v);
-        if (any && to >= 0) h = h0.get(v);
-        o[v] = d.rest(lam);
-        const float w = kUsesX ? lam * (h - xs[kUsesX ? i : 0].get(v)) : lam * h;
-        dg[v] = SHARED ? (v < nv ? w : 0.f) : d.slope(w);
-        st[v] = d.a * lam;
-      } else {
-        st[v] = __fmaf_rn(a[i][SHARED ? 0 : v], st[v], b[i][v]);
-        o[v] = st[v];
+    for (int i = 0; i < R; ++i) {
+      const bool ok = live && (PLAIN || tl * R + i < count);
+      int to = -1;
+      if constexpr (!PLAIN) {
+        if (s.start[tl * R + i] >= 0) st[0] = st[1] = st[2] = st[3] = 0.f;
+        to = s.stop[tl * R + i];
       }
+      Quad<float> h0{};
+      if (!PLAIN && GRAD && to >= 0 && c.h0) h0 = load_quad<float, VEC>(c.h0 + (size_t)to * c.D + own, nv);
+      float o[4], dg[4];
+      Decay d{};
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        if constexpr (GRAD) {
+          // (settled: computed again and not kept from the first pass)
+          if (!SHARED || v == 0) d = decay<FORM>(settled(a[i][SHARED ? 0 : v]));
+          const float lam = b[i][v] + st[v];
+          float h = hp[i].get(v);
+          if (!PLAIN && to >= 0) h = h0.get(v);
+          o[v] = d.rest(lam);
+          const float w = kUsesX ? lam * (h - xs[kUsesX ? i : 0].get(v)) : lam * h;
+          dg[v] = SHARED ? (v < nv ? w : 0.f) : d.slope(w);
+          st[v] = d.a * lam;
+        } else {
+          st[v] = __fmaf_rn(a[i][SHARED ? 0 : v], st[v], b[i][v]);
+          o[v] = st[v];
+        }
+      }
+      if (ok) {
+        store_quad<T, VEC>(out, o, nv);
+        if (!PLAIN && to >= 0 && c.fin) store_quad<float, VEC>(c.fin + (size_t)to * c.D + own, st, nv);
+        if constexpr (GRAD && !SHARED) store_quad<T, VEC>(dgate, dg, nv);
+      }
+      if constexpr (GRAD && SHARED) sum[i] = (dg[0] + dg[1]) + (dg[2] + dg[3]);
+      out += dir * c.ld_out;
+      if (GRAD && !SHARED) dgate += dir * c.ld_dgate;
     }
-    if (ok) {
-      store_quad<T, VEC>(out, o, nv);
-      if (any && to >= 0 && c.fin) store_quad<float, VEC>(c.fin + (size_t)to * c.D + own, st, nv);
-      if constexpr (GRAD && !SHARED) store_quad<T, VEC>(dgate, dg, nv);
-    }
-    if constexpr (GRAD && SHARED) sum[i] = (dg[0] + dg[1]) + (dg[2] + dg[3]);
-    out += dir * c.ld_out;
-    if (GRAD && !SHARED) dgate += dir * c.ld_dgate;
-  }
+  };
+  if (plain) second_pass(std::true_type{});
+  else second_pass(std::false_type{});
   if constexpr (GRAD && SHARED) {
     // the group's lanes, in a fixed order: lane k holds the sum of [k, k + 2 o) after the
     // step of width o
