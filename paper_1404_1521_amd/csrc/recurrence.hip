@@ -52,7 +52,7 @@ hipError_t launch_cut(const RecCall& c, ScanPlan p, const ScanSpace* space, cons
 
 template <class T, int FORM, bool GRAD>
 hipError_t launch_scan(const RecCall& c, const ScanSpace* space, const Launch& L) {
-  constexpr int R = scan_tokens<T, GRAD>();
+  constexpr int R = scan_tokens<T, FORM, GRAD>();
   static_assert(R >= kScanMinTokens, "scan_space");
   const ScanPlan p = scan_plan(c.tokens, c.D, c.group, R);
   if ((int64_t)p.chunks * p.tiles >= kScanFewWorkgroups)

@@ -156,13 +156,14 @@ __device__ __forceinline__ int first_offset(const RecCall& c, int lo) {
 }
 
 // Tokens of a thread.  More of them are fewer chunks and fewer joining words, and more
-// registers: two workgroups of 256 threads to a CU either way.  65,536 tokens 2,048
-// wide, one sequence, us: forward, bfloat16 8 tokens at three workgroups to a CU 270,
-// 12 276, 16 at two 254; float32 373, 371, 350.  Gradient, bfloat16 8 480, 12 411, 16
-// (spilling) 583; float32 8 571, 12 (spilling) 652.
-template <class T, bool GRAD>
+// registers: two workgroups of 256 threads to a CU, and no spills.  65,536 tokens 2,048
+// wide, one sequence, us.  Forward: bfloat16 12 tokens 277, 16 253; float32 raw 12 352,
+// 16 331; sigmoid 8 364 (three workgroups to a CU), 12 369, 16 (spilling) 401.
+// Gradient: bfloat16 8 418, 10 398, 12 367; float32 8 530, 10 (spilling) 584.
+template <class T, int FORM, bool GRAD>
 constexpr int scan_tokens() {
-  return !GRAD ? 16 : sizeof(T) == 2 ? 12 : 8;
+  if (sizeof(T) == 2) return GRAD ? 12 : 16;
+  return GRAD ? 8 : FORM == POLYGLOT_GATE_RAW ? 16 : 12;
 }
 constexpr int kScanMinTokens = 8;
 // ... and of calls that so have fewer workgroups than there are CUs: their time
