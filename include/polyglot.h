@@ -110,8 +110,8 @@ int polyglot_train_step(polyglot_ctx* ctx, float* E, float* W1, float* b1, float
  * model above, at the pre-step parameters) is written to *loss_host (host
  * memory, caller-owned).  Returns what polyglot_train_step returns for the
  * arguments (nothing is enqueued on such an error and *loss_host is left
- * unchanged); POLYGLOT_EHIP if the synchronisation fails; POLYGLOT_EID if a
- * device error word is raised once the step has run, in which case the step
+ * unchanged); POLYGLOT_EHIP if the synchronisation fails; POLYGLOT_EID (or
+ * POLYGLOT_EOFFSETS, left by a sequence operator) if a device error word is raised once the step has run, in which case the step
  * changed no parameter and *loss_host is NaN.  The error words stay raised
  * (every later step is void) until polyglot_status() clears them. */
 int polyglot_train_step_sync(polyglot_ctx* ctx, float* E, float* W1, float* b1, float* w2,

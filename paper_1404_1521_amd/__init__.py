@@ -200,6 +200,11 @@ def _format(t, name):
     return code, t.dtype
 
 
+def _like(t):
+    """A new contiguous tensor of t's shape and type."""
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
 def _flat(t):
     """A [nseq][T][width] tensor as rows of tokens."""
     return t if t is None or t.dim() == 2 else t.view(-1, t.shape[-1])
@@ -392,7 +397,7 @@ class Context:
         if add is not None:
             padd, ld_add = _row_tensor(add, dtype, "add", rows, d)
         if out is None:
-            out = x.new_empty((rows, d))
+            out = _like(x) if ids is None else x.new_empty((rows, d))
         py, ld_y = _row_tensor(out, dtype, "out", rows, d)
         rc = self._lib.polyglot_dropout(self._h, DropoutArgs.pack(
             px, padd, py, pids, _vector(site_dev, torch.int32, "site_dev", 1), rows, ld_x, ld_add,
@@ -449,7 +454,7 @@ class Context:
         [nseq][D].  Returns (h, last)."""
         nseq = offsets.shape[0] - 1 if offsets is not None else x.shape[0] if x.dim() == 3 else 1
         if out is None:
-            out = x.new_empty(x.shape)
+            out = _like(x)
         return self._forward("recurrence", _flat(gate), _flat(x), offsets, nseq, h0, form, reverse,
                              out, last)
 
@@ -458,7 +463,9 @@ class Context:
         """One token x[nseq][D] for each of nseq sequences whose float32 states are
         state[nseq][D].  Returns (h, the new states); last=state updates them in place."""
         if out is None:
-            out = x.new_empty(x.shape)
+            out = _like(x)
+        if last is None and state is not None:
+            last = _like(state)
         return self._forward("recurrence_step", gate, x, None, x.shape[0], state, form, False, out,
                              last)
 
@@ -469,9 +476,9 @@ class Context:
         and dlast of last.  Returns (dgate, dx, dh0); dh0 is None unless h0 or dh0 is given."""
         nseq = offsets.shape[0] - 1 if offsets is not None else x.shape[0] if x.dim() == 3 else 1
         if dgate is None:
-            dgate = x.new_empty(gate.shape)
+            dgate = _like(gate)
         if dx is None:
-            dx = x.new_empty(x.shape)
+            dx = _like(x)
         code, dtype, tokens, D, gates, pg_, ld_g, px, ld_x, poff, off_bytes = self._sequences(
             _flat(x), _flat(gate), offsets)
         if dh0 is None and h0 is not None:
@@ -502,7 +509,7 @@ class Context:
         pl, ld_l = _row_tensor(logits, dtype, "logits", rows, V)
         po = ld_o = ph = ld_h = cap = plen = ppr = pb = ld_b = pm = ld_m = masks = pmr = 0
         if out is None and write:
-            out = logits.new_empty((rows, V))
+            out = _like(logits)
         if out is not None:
             po, ld_o = _row_tensor(out, dtype, "out", rows, V)
         if history is not None:

@@ -441,6 +441,11 @@ int enqueue_steps(polyglot_ctx* ctx, float* E, float* W1, float* b1, float* w2, 
   return POLYGLOT_OK;
 }
 
+// The code of raised error words.
+int flag_code(uint32_t f) {
+  return f & kFlagBadId ? POLYGLOT_EID : f & kFlagBadOffset ? POLYGLOT_EOFFSETS : POLYGLOT_EHIP;
+}
+
 int check_step_args(polyglot_ctx* ctx, float* E, float* W1, float* b1, float* w2, float* b2,
                     const int32_t* windows, const int32_t* corrupt, int B, float lr) {
   if (!E || !W1 || !b1 || !w2 || !b2 || !windows || !corrupt)
@@ -632,7 +637,7 @@ int polyglot_train_step_sync(polyglot_ctx* ctx, float* E, float* W1, float* b1, 
   if (e != hipSuccess) return hip_fail(ctx, e, "train_step_sync: loss copy");
   *loss_host = loss;
   if (w[0] | w[1] | w[2])
-    return fail(ctx, (w[0] | w[1] | w[2]) & kFlagBadId ? POLYGLOT_EID : POLYGLOT_EHIP,
+    return fail(ctx, flag_code(w[0] | w[1] | w[2]),
                 "train_step_sync: a device error word is raised; the step changed nothing");
   return POLYGLOT_OK;
 }
@@ -956,10 +961,12 @@ int polyglot_status(polyglot_ctx* ctx) {
   if (f) {
     e = hipMemset(ctx->ws.flag, 0, sizeof(w));
     if (e != hipSuccess) return hip_fail(ctx, e, "status: clear flag");
-    if (f & kFlagBadId) return fail(ctx, POLYGLOT_EID, "an id was outside its table");
-    if (f & kFlagBadOffset)
-      return fail(ctx, POLYGLOT_EOFFSETS, "sequence offsets did not ascend from 0 to the tokens");
-    return fail(ctx, POLYGLOT_EHIP, "internal: sort position outside the entry range");
+    const int code = flag_code(f);
+    return fail(ctx, code,
+                code == POLYGLOT_EID ? "an id was outside its table"
+                : code == POLYGLOT_EOFFSETS
+                    ? "sequence offsets did not ascend from 0 to the tokens"
+                    : "internal: a sort position outside the entry range, or a wait without end");
   }
   return POLYGLOT_OK;
 }

@@ -209,25 +209,11 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(RecCall c, ScanPlan p) {
   const int tile = blockIdx.x % p.tiles;
 
   // The chunks of a tile are handed out in the order in which workgroups start, so
-  // every chunk that a look-back waits for is running or done.  Whoever takes a tile's
-  // last one makes the counters ready for the next launch: all of them move on with
-  // every launch, so that a tag is one launch's.
-  if (t == 0) {
-    s.ticket = blockIdx.x / p.tiles;
-    if (p.head) {
-      uint64_t* const head = p.head + tile * kHeadLine;
-      const uint64_t ticket = __hip_atomic_fetch_add(head, (uint64_t)1, __ATOMIC_RELAXED,
-                                                     __HIP_MEMORY_SCOPE_AGENT);
-      s.ticket = ticket;
-      if ((uint32_t)ticket == (uint32_t)p.chunks - 1) {
-        const uint32_t next = max((uint32_t)(ticket >> 32) + 1, 1u);
-        const int last = tile == 0 ? p.counters : tile + 1;
-        for (int i = tile; i < last; i = i == 0 ? p.tiles : i + 1)
-          __hip_atomic_store(p.head + i * kHeadLine, (uint64_t)next << 32, __ATOMIC_RELAXED,
-                             __HIP_MEMORY_SCOPE_AGENT);
-      }
-    }
-  }
+  // every chunk that a look-back waits for is running or done.
+  uint64_t ticket = blockIdx.x / p.tiles;
+  if (t == 0 && p.head)
+    ticket = __hip_atomic_fetch_add(p.head + tile * kHeadLine, (uint64_t)1, __ATOMIC_RELAXED,
+                                    __HIP_MEMORY_SCOPE_AGENT);
 
   // this thread's channels [ch, ch + nv) and their gate
   int ch, nv, gate_col = 0, part = 0;
@@ -244,23 +230,27 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(RecCall c, ScanPlan p) {
   const bool live = nv > 0;
   const int own = live ? ch : 0, col = live ? gate_col : 0;  // idle lanes load something that exists
 
-  // Offsets, a batch at a time with the neighbours of its ends.  Where that is all of
-  // them they are read once; otherwise those near the chunk are searched for.
+  // Offsets, a batch at a time with the neighbours of its ends, asked for at once.
+  // Where that is all of them they are read while the ticket is on its way; otherwise
+  // those near the chunk are searched for.
   const int n_off = c.nseq + 1;
   const bool all = n_off <= kScanBatch;
   const auto load_offsets = [&](int base) {
-    for (int i = t; i < kScanBatch + 2 && base + i - 1 < n_off; i += kBlock)
-      s.off[i] = seq_offset(c, max(base + i - 1, 0));
+    constexpr int kEach = (kScanBatch + 2 + kBlock - 1) / kBlock;
+    int o[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+      o[j] = base + j * kBlock + t <= n_off ? seq_offset(c, max(base + j * kBlock + t - 1, 0)) : 0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+      if (j * kBlock + t < kScanBatch + 2) s.off[j * kBlock + t] = o[j];
   };
   if (all) load_offsets(0);
-  // offsets have to ascend from 0 to the tokens: each is looked at once
-  if (c.offsets)
-    for (int64_t i = (int64_t)blockIdx.x * kBlock + t; i <= c.nseq; i += (int64_t)gridDim.x * kBlock) {
-      const int o = seq_offset(c, (int)i);
-      const int next = i < c.nseq ? seq_offset(c, (int)i + 1) : c.tokens;
-      if ((i == 0 && o != 0) || next < o || (i == c.nseq && o != c.tokens))
-        atomicOr(c.flag, kFlagBadOffset);
-    }
+  for (int i = t; i < L; i += kBlock) s.start[i] = s.stop[i] = -1;
+  if (t == 0) {
+    s.n_empty = s.any = 0;
+    s.ticket = ticket;
+  }
   __syncthreads();
   const uint32_t tag = (uint32_t)(s.ticket >> 32);
   const int chunk = (int)(uint32_t)s.ticket;
@@ -302,14 +292,12 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(RecCall c, ScanPlan p) {
   }
 
   // where sequences start and stop in the chunk
-  for (int i = t; i < L; i += kBlock) s.start[i] = s.stop[i] = -1;
-  if (t == 0) s.n_empty = s.any = 0;
   int base = 0;
   if (!all) {
     base = first_offset(c, lo);
     load_offsets(base);
+    __syncthreads();
   }
-  __syncthreads();
   while (base < n_off) {
     bool more = false;
     for (int j = t; j < kScanBatch && base + j < n_off; j += kBlock) {
@@ -675,6 +663,24 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(RecCall c, ScanPlan p) {
         if (tl * R + i < count)
           dgate[i * dir * c.ld_dgate] =
               Elem<T>::put(settled(decay<FORM>(a[i][0]).slope(sum[i])));
+  }
+
+  // offsets have to ascend from 0 to the tokens: each is looked at once
+  if (c.offsets)
+    for (int64_t i = (int64_t)blockIdx.x * kBlock + t; i <= c.nseq; i += (int64_t)gridDim.x * kBlock) {
+      const int o = seq_offset(c, (int)i);
+      const int next = i < c.nseq ? seq_offset(c, (int)i + 1) : c.tokens;
+      if ((i == 0 && o != 0) || next < o || (i == c.nseq && o != c.tokens))
+        atomicOr(c.flag, kFlagBadOffset);
+    }
+  // Whoever took the tile's last chunk makes the counters ready for the next launch: all
+  // of them move on with every launch, so that a tag is one launch's.
+  if (t == 0 && p.head && chunk == p.chunks - 1) {
+    const uint32_t next = max(tag + 1, 1u);
+    const int last = tile == 0 ? p.counters : tile + 1;
+    for (int i = tile; i < last; i = i == 0 ? p.tiles : i + 1)
+      __hip_atomic_store(p.head + i * kHeadLine, (uint64_t)next << 32, __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
   }
 }
 

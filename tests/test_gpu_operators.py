@@ -149,6 +149,22 @@ def test_dropout_forms(ctx, dtype, rows, d):
     check_dropout(z, host(x), keep, 0.25, dtype, host(add))
 
 
+@pytest.mark.parametrize("dtype,rows,d", [("f32", 1100, 9001), ("bf16", 1_100_000, 5),
+                                          ("f16", 70_001, 123)])
+def test_dropout_of_many_elements(ctx, dtype, rows, d):
+    """Several groups of columns to a thread; rows of more and of fewer groups than a
+    workgroup takes."""
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn(rows, d, device="cuda", generator=gen).to(DT[dtype])
+    keep = torch.from_numpy(kept(rows, d, 0.3, 21)).cuda()
+    y = ctx.dropout(x, 0.3, 21, add=x)
+    limit = int(np.float32(0.3) * 65536.0 + 0.5)
+    ref = torch.where(keep, x.double() * (65536 / (65536 - limit)), 0.0) + x.double()
+    size = 2.5 * x.double().abs()
+    bound = 3.01 * EPS * size + U[dtype] * (ref.abs() + 4 * EPS * size) + TINY[dtype]
+    assert ((y.double() - ref).abs() <= bound).all()
+
+
 @pytest.mark.parametrize("dtype", list(DT))
 @pytest.mark.parametrize("idt", [torch.int32, torch.int64])
 @pytest.mark.parametrize("d", [1, 64, 100, 128, 131])
@@ -399,6 +415,18 @@ def test_recurrence_of_long_sequences(pg, ctx, dtype, D, group, reverse):
     """Longer than any part that a workgroup takes, alone and beside others."""
     Seqs(dtype, [3001], D, group, True, seed=3).check(ctx, pg, reverse)
     Seqs(dtype, [1, 1500, 0, 2, 777, 64, 128, 0], D, group, False, seed=4).check(ctx, pg, reverse)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("sig", [True, False])
+@pytest.mark.parametrize("D,group", [(512, 1), (509, 1), (512, 64), (1020, 255)])
+def test_recurrence_of_many_tokens(pg, ctx, dtype, sig, D, group):
+    """Enough workgroups for the long chunks: sequences that begin and end in every place
+    of them, and one that goes through many."""
+    rng = np.random.default_rng(D + group)
+    lengths = np.concatenate([rng.integers(0, 40, 30), [3200], rng.integers(100, 300, 6), [0, 1]])
+    Seqs(dtype, np.append(lengths, 6001 - lengths.sum()), D, group, sig, state=sig,
+         seed=25).check(ctx, pg, not sig)
 
 
 @pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256,
@@ -765,7 +793,7 @@ class Scores:
 
 
 @pytest.mark.parametrize("dtype", list(DT))
-@pytest.mark.parametrize("rows,V", [(1, 1), (2, 31), (3, 32), (5, 33), (1, 1000), (4, 4099),
+@pytest.mark.parametrize("rows,V", [(1, 1), (3, 2), (4, 3), (1, 4), (2, 5), (2, 31), (3, 32), (5, 33), (1, 1000), (4, 4099),
                                     (2, 8191), (2, 8192), (3, 8193), (2, 32003), (33, 2047),
                                     (1, 100_000)])
 def test_scores(ctx, dtype, rows, V):
@@ -775,7 +803,8 @@ def test_scores(ctx, dtype, rows, V):
     Scores(dtype, rows, V, cap=300, masks=rows + 2, seed=3).check(ctx)
 
 
-@pytest.mark.parametrize("cap", [1, 255, 256, 257, 5000, 20_000])
+@pytest.mark.parametrize("cap", [1, 255, 256, 257, 2047, 2049, 5000, 20_000, 32_767, 32_768,
+                                 50_000])
 def test_scores_with_histories(ctx, cap):
     q = Scores("f32", 3, 9001, cap=cap, seed=4)
     q.check(ctx)
@@ -791,8 +820,9 @@ def test_scores_with_histories(ctx, cap):
     assert torch.equal(out, q.logits)
 
 
-def test_scores_of_one_word_many_times(ctx):
-    q = Scores("f32", 2, 500, cap=6000, seed=5)
+@pytest.mark.parametrize("cap", [6000, 32_767, 70_000])
+def test_scores_of_one_word_many_times(ctx, cap):
+    q = Scores("f32", 2, 500, cap=cap, seed=5)
     q.kw["history"].fill_(17)
     q.kw["history"][:, ::2] = 499
     q.check(ctx)
@@ -895,6 +925,13 @@ def test_scores_with_bad_ids(pg, ctx):
     assert ctx.status() == pg.EID
     assert all(torch.equal(a, b) for a, b in zip(got, free))
     assert all(torch.equal(a, b) for a, b in zip(ref, ctx.logits(q.logits, **q.kw)))
+
+
+def test_scores_of_many_rows(ctx):
+    """Enough rows for the longest parts, in every format."""
+    for dtype in DT:
+        q = Scores(dtype, 64, 70_003, cap=300, masks=64, bias="shared", seed=12)
+        q.check(ctx)
 
 
 def test_scores_in_a_graph(pg):
