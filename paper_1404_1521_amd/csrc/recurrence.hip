@@ -9,15 +9,25 @@ namespace pg {
 
 namespace {
 
-// Lanes of a row of threads: as few as hold all channels, so that narrow layers
-// have more rows of tokens; at least what a group takes.
-ScanPlan scan_plan(int64_t tokens, int D, int group, int R) {
+// Lanes of a row of threads where a group of channels does not ask for more.  16 lanes
+// of four channels are whole cache lines of 16-bit elements.  With 8 a narrow layer has
+// twice the tiles, whose workgroups count themselves in side by side (10 ns each on one
+// counter), and half the chunks to join; 8 lanes are whole lines of float32.  us for 8 and
+// 16 lanes, forward, gradient: 65,537 x 64 float32 21.9, 27.4 and 24.7, 33.6; bfloat16
+// 23.2, 29.5 and 24.1, 32.9; 16,384 x 512 float32 29.2, 38.9 and 31.2, 40.9; bfloat16 23.0,
+// 34.7 and 21.4, 33.9; 65,536 x 2,048 float32 345, 481 and 320, 463; bfloat16 271, 464 and
+// 217, 352 (32 lanes 239, 368).
+int scan_lanes_log2(int D, size_t size) { return D <= 64 || (size == 4 && D <= 512) ? 3 : 4; }
+
+// As few lanes as hold all channels, so that narrow layers have more rows of tokens; at
+// least what a group takes.
+ScanPlan scan_plan(int64_t tokens, int D, int group, int R, size_t size) {
   ScanPlan p{};
   p.lanes_per_group = group > 1 ? ceil_div(group, 4) : 1;
   const int64_t lanes = group > 1 ? (int64_t)p.lanes_per_group * (D / group) : ceil_div(D, 4);
   int log2 = 3;
   while (log2 < 6 && (1 << log2) < lanes &&
-         (log2 < kScanLanesLog2 || (1 << log2) < p.lanes_per_group))
+         (log2 < scan_lanes_log2(D, size) || (1 << log2) < p.lanes_per_group))
     ++log2;
   p.lanes_log2 = log2;
   const int CT = 1 << log2;
@@ -54,11 +64,11 @@ template <class T, int FORM, bool GRAD>
 hipError_t launch_scan(const RecCall& c, const ScanSpace* space, const Launch& L) {
   constexpr int R = scan_tokens<T, FORM, GRAD>();
   static_assert(R >= kScanMinTokens, "scan_space");
-  const ScanPlan p = scan_plan(c.tokens, c.D, c.group, R);
+  const ScanPlan p = scan_plan(c.tokens, c.D, c.group, R, sizeof(T));
   if ((int64_t)p.chunks * p.tiles >= kScanFewWorkgroups)
     return launch_cut<T, FORM, GRAD, R>(c, p, space, L);
   return launch_cut<T, FORM, GRAD, kScanShortTokens>(
-      c, scan_plan(c.tokens, c.D, c.group, kScanShortTokens), space, L);
+      c, scan_plan(c.tokens, c.D, c.group, kScanShortTokens, sizeof(T)), space, L);
 }
 
 template <class T, int FORM>

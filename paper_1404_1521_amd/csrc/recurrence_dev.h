@@ -171,10 +171,13 @@ constexpr int kScanMinTokens = 8;
 constexpr int kScanShortTokens = 4;
 constexpr int kScanFewWorkgroups = kCus;
 constexpr int kScanMinLanes = 8;  // of a row of threads
-// Lanes of a row of threads where a group of channels does not ask for more: 16 lanes
-// of four channels are whole cache lines of 16-bit elements, and a chunk of 16 rows is
-// long.  (The same, 8, 16, 32 and 64 lanes: forward, bfloat16 310, 265, 285, 343.)
-constexpr int kScanLanesLog2 = 4;
+
+// A value of another lane of the row of 16: quad_perm 0xb1 and 0x4e (the neighbour, the
+// other pair), 0x141 the half mirrored, 0x140 the row mirrored.
+template <int CTRL>
+__device__ __forceinline__ float dpp_moved(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
 
 // LDS of a scan.
 constexpr int kLookEnd = 256;     // ScanLds::look: an end lies before the steps
@@ -649,14 +652,29 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(RecCall c, ScanPlan p) {
   if (plain) second_pass(std::true_type{});
   else second_pass(std::false_type{});
   if constexpr (GRAD && SHARED) {
-    // the group's lanes, in a fixed order: lane k holds the sum of [k, k + 2 o) after the
-    // step of width o
-    for (int o = 1; o < p.lanes_per_group; o <<= 1)
+    // The group's lanes, in a fixed order.  Powers of two by exchanges inside rows of 16
+    // lanes (of neighbours, of pairs, halves mirrored, rows mirrored), then of rows;
+    // other counts by doubling, lane k holding the sum of [k, k + 2 o) after the step of
+    // width o.
+    const int lanes = p.lanes_per_group;
+    if ((lanes & (lanes - 1)) == 0) {
 #pragma unroll
       for (int i = 0; i < R; ++i) {
-        const float other = __shfl_down(sum[i], o);
-        if (part + o < p.lanes_per_group) sum[i] += other;
+        if (lanes > 1) sum[i] += dpp_moved<0xb1>(sum[i]);
+        if (lanes > 2) sum[i] += dpp_moved<0x4e>(sum[i]);
+        if (lanes > 4) sum[i] += dpp_moved<0x141>(sum[i]);
+        if (lanes > 8) sum[i] += dpp_moved<0x140>(sum[i]);
+        if (lanes > 16) sum[i] += __shfl_xor(sum[i], 16);
+        if (lanes > 32) sum[i] += __shfl_xor(sum[i], 32);
       }
+    } else {
+      for (int o = 1; o < lanes; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          const float other = __shfl_down(sum[i], o);
+          if (part + o < lanes) sum[i] += other;
+        }
+    }
     if (live && part == 0)
 #pragma unroll
       for (int i = 0; i < R; ++i)
