@@ -3,8 +3,12 @@
 //   y[r][c] = keep(r, c) ? x[r][c] * scale : 0   (+ add[r][c])
 //
 // keep compares 16 bits of a counter-based generator with the threshold
-// round(65536 p).  Eight columns share one counter, so the generator runs
-// once for every eight elements; nothing but x (and add) is read.
+// round(65536 p).  Eight columns share one counter, so the generator runs once
+// for every eight elements; nothing but x (and add) is read.
+//
+// Bound by memory where the tensors are large, by the launch where they are small:
+// 262,144 x 512 float16 96 us (5.6 TB/s read and written), 20,011 x 199 bfloat16
+// with an addition 8.9 us (2.7 TB/s), 5,120 gathered rows of 64 float32 3.3 us.
 #pragma once
 #include "formats.h"
 #include "operators.h"
@@ -37,79 +41,75 @@ __device__ __forceinline__ uint32_t keep_bits(uint4 w, uint32_t threshold) {
 }
 
 // The quotient n / groups of a workgroup's places, n < groups + kDropPlaces.
-constexpr int kDropPlaces = 1024;
+constexpr int kDropPlaces = kBlock;
 __device__ __forceinline__ uint32_t rows_down(uint32_t n, const DropoutCall& c) {
   if (c.groups >= kDropPlaces) return n >= (uint32_t)c.groups ? 1u : 0u;
   return c.groups == 1 ? n : __umulhi(n, c.groups_inv);
 }
 
-// A workgroup takes U * 256 consecutive groups of eight columns, counted through
-// all rows.  Loads go first: their latency passes behind the generator's products.
-template <class T, bool ADD, bool IDS, int U>
+// A workgroup takes 256 consecutive groups of eight columns, counted through all
+// rows, so that rows of every width fill its lanes; only the workgroup's first place
+// takes a 64-bit division.  Loads go first: their latency passes behind the
+// generator's products.  One group to a thread: with two and four, 262,144 x 512
+// float16, repeated on the same tensors, took 99 and 95 us in place of 86 (float32 189
+// and 191 for 184, bfloat16 with an addition 141 and 145 for 132), and 20,011 x 199
+// bfloat16 with an addition 15.9 with four for 8.9.  Only many rows gathered from a
+// large table of 16-bit values are faster with four (262,144 x 512 bfloat16 105 us for
+// 118, float16 96 for 111); 100,003 x 199 of them are not (32 for 28).
+template <class T, bool ADD, bool IDS>
 __global__ __launch_bounds__(kBlock) void k_dropout(DropoutCall c) {
   const polyglot_dropout_args& a = c.a;
-  const int64_t first = (int64_t)blockIdx.x * (kBlock * U);
+  const int64_t first = (int64_t)blockIdx.x * kBlock;
   const int64_t row0 = first / c.groups;
   const uint32_t col0 = (uint32_t)(first - row0 * c.groups);
   const uint32_t site = a.site + (a.site_dev ? *a.site_dev : 0u);
-  int64_t r[U];
-  int col[U], n[U];
-  bool bad[U];
-  const T* x[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const uint32_t place = col0 + threadIdx.x + u * kBlock;
-    const uint32_t q = rows_down(place, c);
-    r[u] = row0 + q;
-    col[u] = (int)(place - q * c.groups) * 8;
-    n[u] = r[u] < a.rows ? min(8, a.d - col[u]) : 0;
-    bad[u] = false;
-    int64_t from = r[u];
-    if (IDS && n[u] > 0) {
-      from = a.id_bytes == 8 ? static_cast<const int64_t*>(a.ids)[r[u]]
-                             : static_cast<const int32_t*>(a.ids)[r[u]];
-      bad[u] = from < 0 || from >= a.table_rows;
-      if (bad[u]) {
-        from = 0;
-        atomicOr(c.flag, kFlagBadId);
-      }
+  const uint32_t place = col0 + threadIdx.x;
+  const uint32_t q = rows_down(place, c);
+  const int64_t r = row0 + q;
+  const int col = (int)(place - q * c.groups) * 8;
+  if (r >= a.rows) return;
+  const int n = min(8, a.d - col);
+  bool bad = false;
+  int64_t from = r;
+  if (IDS) {
+    from = a.id_bytes == 8 ? static_cast<const int64_t*>(a.ids)[r]
+                           : static_cast<const int32_t*>(a.ids)[r];
+    bad = from < 0 || from >= a.table_rows;
+    if (bad) {
+      from = 0;
+      atomicOr(c.flag, kFlagBadId);
     }
-    x[u] = static_cast<const T*>(a.x) + from * a.ld_x + col[u];
   }
-  Oct<T> xv[U], av[U];
+  const T* x = static_cast<const T*>(a.x) + from * a.ld_x + col;
+  const T* add = static_cast<const T*>(a.add) + r * a.ld_add + col;
+  T* y = static_cast<T*>(a.y) + r * a.ld_y + col;
+  Oct<T> xv, av;
+  if (n == 8) {
+    xv.load(x);
+    if (ADD) av.load(add);
+  }
+  const uint64_t row = a.first_row + (uint64_t)r;
+  const uint4 w = philox10(uint4{a.whole_rows ? 0xffffffffu : (uint32_t)col / 8, (uint32_t)row,
+                                 (uint32_t)(row >> 32), site},
+                           (uint32_t)a.seed, (uint32_t)(a.seed >> 32));
+  uint32_t keep = keep_bits(w, c.threshold);
+  if (a.whole_rows) keep = keep & 1u ? 0xffu : 0u;
+  const float spoilt = IDS && bad ? __builtin_nanf("") : 0.f;
+  if (n == 8) {
+    float v[8];
 #pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (n[u] == 8) {
-      xv[u].load(x[u]);
-      if (ADD) av[u].load(static_cast<const T*>(a.add) + r[u] * a.ld_add + col[u]);
+    for (int j = 0; j < 8; ++j) {
+      v[j] = keep >> j & 1u ? settled(xv.get(j) * c.scale) : 0.f;
+      if (ADD) v[j] += av.get(j);
+      if (IDS) v[j] += spoilt;
     }
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const uint64_t row = a.first_row + (uint64_t)r[u];
-    const uint4 w = philox10(uint4{a.whole_rows ? 0xffffffffu : (uint32_t)col[u] / 8, (uint32_t)row,
-                                   (uint32_t)(row >> 32), site},
-                             (uint32_t)a.seed, (uint32_t)(a.seed >> 32));
-    uint32_t keep = keep_bits(w, c.threshold);
-    if (a.whole_rows) keep = keep & 1u ? 0xffu : 0u;
-    const float spoilt = IDS && bad[u] ? __builtin_nanf("") : 0.f;
-    T* y = static_cast<T*>(a.y) + r[u] * a.ld_y + col[u];
-    if (n[u] == 8) {
-      float v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        v[j] = keep >> j & 1u ? settled(xv[u].get(j) * c.scale) : 0.f;
-        if (ADD) v[j] += av[u].get(j);
-        if (IDS) v[j] += spoilt;
-      }
-      Oct<T>::store(y, v);
-    } else {
-      const T* add = static_cast<const T*>(a.add) + r[u] * a.ld_add + col[u];
-      for (int j = 0; j < n[u]; ++j) {
-        float v = keep >> j & 1u ? settled(Elem<T>::get(x[u][j]) * c.scale) : 0.f;
-        if (ADD) v += Elem<T>::get(add[j]);
-        if (IDS) v += spoilt;
-        y[j] = Elem<T>::put(settled(v));
-      }
+    Oct<T>::store(y, v);
+  } else {
+    for (int j = 0; j < n; ++j) {
+      float v = keep >> j & 1u ? settled(Elem<T>::get(x[j]) * c.scale) : 0.f;
+      if (ADD) v += Elem<T>::get(add[j]);
+      if (IDS) v += spoilt;
+      y[j] = Elem<T>::put(settled(v));
     }
   }
 }

@@ -10,25 +10,33 @@ namespace pg {
 
 namespace {
 
-template <class T, int U>
-hipError_t dropout_of(const DropoutCall& c, int64_t total, const Launch& L) {
-  static_assert(U * kBlock <= kDropPlaces, "places of a workgroup");
-  const int64_t grid = (total + kBlock * U - 1) / (kBlock * U);
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
-  auto k = c.a.ids ? (c.a.add ? k_dropout<T, true, true, U> : k_dropout<T, false, true, U>)
-                   : (c.a.add ? k_dropout<T, true, false, U> : k_dropout<T, false, false, U>);
-  return pg_launch(k, dim3((uint32_t)grid), dim3(kBlock), 0, L, c);
+// A launch has fewer than 2^32 threads: larger tensors take several, of whole rows.
+template <class T>
+hipError_t dropout_of(const DropoutCall& call, const Launch& L) {
+  auto k = call.a.ids ? (call.a.add ? k_dropout<T, true, true> : k_dropout<T, false, true>)
+                      : (call.a.add ? k_dropout<T, true, false> : k_dropout<T, false, false>);
+  const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 31) / call.groups);
+  for (int64_t row = 0; row < call.a.rows; row += most) {
+    DropoutCall c = call;
+    c.a.rows = std::min(most, call.a.rows - row);
+    c.a.first_row += row;
+    if (c.a.ids)
+      c.a.ids = static_cast<const char*>(c.a.ids) + row * c.a.id_bytes;
+    else
+      c.a.x = static_cast<const T*>(c.a.x) + row * c.a.ld_x;
+    if (c.a.add) c.a.add = static_cast<const T*>(c.a.add) + row * c.a.ld_add;
+    c.a.y = static_cast<T*>(c.a.y) + row * c.a.ld_y;
+    const int64_t grid = (c.a.rows * c.groups + kBlock - 1) / kBlock;
+    const hipError_t e = pg_launch(k, dim3((uint32_t)grid), dim3(kBlock), 0, L, c);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
 
 hipError_t launch_dropout(const DropoutCall& c, const Launch& L) {
-  const int64_t total = c.a.rows * c.groups;
-  return by_format(c.a.dtype, [&](auto v) {
-    using T = decltype(v);
-    return total >= (int64_t)4 * kBlock * 4 * kCus ? dropout_of<T, 4>(c, total, L)
-                                                   : dropout_of<T, 1>(c, total, L);
-  });
+  return by_format(c.a.dtype, [&](auto v) { return dropout_of<decltype(v)>(c, L); });
 }
 
 hipError_t launch_logits(LogitsCall c, const Launch& L) {

@@ -242,6 +242,22 @@ def test_dropout_rows_past_32_bits(ctx):
     check_dropout(x, a, kept(2, 200, 0.3, 1), 0.3, "f16")
 
 
+def test_dropout_of_more_groups_than_a_launch_has(ctx):
+    # a launch takes 2^31 groups of up to eight columns; rows on both sides of the cut,
+    # and the last ones, against calls of their own rows
+    rows = 2**31 + 5
+    x = torch.ones(rows, 1, device="cuda", dtype=torch.bfloat16)
+    ctx.dropout(x, 0.5, 71, site=3, out=x)
+    torch.cuda.synchronize()
+    for at in (0, 2**31 - 300, 2**31 - 3, rows - 300):
+        n = min(600, rows - at)
+        want = ctx.dropout(torch.ones(n, 1, device="cuda", dtype=torch.bfloat16), 0.5, 71, site=3,
+                           first_row=at)
+        assert torch.equal(x[at:at + n], want), at
+        assert n < 300 or 0 < int((want == 0).sum()) < n
+    assert ctx.status() == 0
+
+
 def test_dropout_in_a_graph(pg):
     """The mask of a replay follows the device word that the program advances."""
     s = torch.cuda.Stream()
