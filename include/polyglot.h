@@ -327,6 +327,9 @@ int polyglot_dropout(polyglot_ctx* ctx, const polyglot_dropout_args* args);
  * token (h0[s] or zeros for an empty one); last may be h0.  reverse != 0 reads
  * every sequence from its last token to its first.  The state is carried in
  * 32 bits from the sequence's start to its end; h holds its roundings to dtype.
+ * h may be x, with the same ld.  Consecutive gates are multiplied with each other:
+ * RAW gates above 1 in size over many tokens may take such a product past 32 bits'
+ * range, and the state with it, where one token after the other would not.
  *
  * With one token per sequence (tokens == nseq, no offsets) this is a model's
  * step for single tokens: one pass over the rows, no workspace.  Other calls

@@ -7,8 +7,8 @@
 // for every eight elements; nothing but x (and add) is read.
 //
 // Bound by memory where the tensors are large, by the launch where they are small:
-// 262,144 x 512 float16 96 us (5.6 TB/s read and written), 20,011 x 199 bfloat16
-// with an addition 8.9 us (2.7 TB/s), 5,120 gathered rows of 64 float32 3.3 us.
+// 262,144 x 512 float16 95 us (5.7 TB/s read and written), 20,011 x 199 bfloat16
+// with an addition 8.8 us (2.7 TB/s), 5,120 gathered rows of 64 float32 3.4 us.
 #pragma once
 #include "formats.h"
 #include "operators.h"
