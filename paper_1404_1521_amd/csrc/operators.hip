@@ -33,6 +33,52 @@ hipError_t dropout_of(const DropoutCall& call, const Launch& L) {
   return hipSuccess;
 }
 
+// p, if it is there, `by` elements on.
+template <class P>
+void advance(P*& p, int64_t by) {
+  if (p) p += by;
+}
+
+// The rows [row, row + rows) of a call.
+template <class T>
+LogitsCall logits_rows(LogitsCall c, int64_t row, int rows) {
+  polyglot_logits_args& a = c.a;
+  a.logits = static_cast<const T*>(a.logits) + row * a.ld_logits;
+  if (a.out) a.out = static_cast<T*>(a.out) + row * a.ld_out;
+  advance(a.history, row * a.ld_history);
+  for (const int32_t** p : {&a.lengths, &a.prompt, &a.mask_rows}) advance(*p, row);
+  for (const float** p : {&a.repetition, &a.presence, &a.frequency}) advance(*p, row);
+  advance(a.bias, row * a.ld_bias);
+  if (!a.mask_rows && a.masks > 1) {  // a mask for each row
+    advance(a.mask, row * a.ld_mask);
+    a.masks = rows;
+  }
+  advance(a.token, row);
+  advance(a.lse, row);
+  advance(c.head, row * kHeadLine);
+  advance(c.words, row * c.stride * 3);
+  a.rows = rows;
+  return c;
+}
+
+// E words to a thread.  A launch has fewer than 2^32 threads: more rows take several.
+template <class T>
+hipError_t logits_of(const LogitsCall& call, int E, const Launch& L) {
+  const bool many = call.a.history && call.a.history_cap > 32767;
+  auto k = E == 32   ? (many ? k_logits<T, 32, true> : k_logits<T, 32, false>)
+           : E == 16 ? (many ? k_logits<T, 16, true> : k_logits<T, 16, false>)
+           : E == 8  ? (many ? k_logits<T, 8, true> : k_logits<T, 8, false>)
+                     : (many ? k_logits<T, 4, true> : k_logits<T, 4, false>);
+  const int most = (int)(((int64_t)1 << 32) / kBlock - 1) / call.tiles;  // V <= 2^30: at least 16
+  for (int64_t row = 0; row < call.a.rows; row += most) {
+    const LogitsCall c =
+        logits_rows<T>(call, row, (int)std::min<int64_t>(most, call.a.rows - row));
+    const hipError_t e = pg_launch(k, dim3(c.a.rows * c.tiles), dim3(kBlock), 0, L, c);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 }  // namespace
 
 hipError_t launch_dropout(const DropoutCall& c, const Launch& L) {
@@ -48,16 +94,7 @@ hipError_t launch_logits(LogitsCall c, const Launch& L) {
   int E = 32;
   while (E > 4 && (int64_t)c.a.rows * ceil_div(c.a.V, E * kBlock) < 2 * kCus) E /= 2;
   c.tiles = ceil_div(c.a.V, E * kBlock);
-  if ((int64_t)c.a.rows * c.tiles > INT32_MAX) return hipErrorInvalidValue;
-  return by_format(c.a.dtype, [&](auto v) {
-    using T = decltype(v);
-    const bool many = c.a.history && c.a.history_cap > 32767;
-    auto k = E == 32   ? (many ? k_logits<T, 32, true> : k_logits<T, 32, false>)
-             : E == 16 ? (many ? k_logits<T, 16, true> : k_logits<T, 16, false>)
-             : E == 8  ? (many ? k_logits<T, 8, true> : k_logits<T, 8, false>)
-                       : (many ? k_logits<T, 4, true> : k_logits<T, 4, false>);
-    return pg_launch(k, dim3(c.a.rows * c.tiles), dim3(kBlock), 0, L, c);
-  });
+  return by_format(c.a.dtype, [&](auto v) { return logits_of<decltype(v)>(c, E, L); });
 }
 
 }  // namespace pg
