@@ -84,14 +84,21 @@ typedef struct {
 
 /* Creates a context on the current HIP device.  `stream` is a hipStream_t
  * (NULL = the legacy default stream).  All workspace is allocated here, once,
- * sized for cfg->max_batch and cfg->max_scatter; no call below allocates.
+ * sized for cfg->max_batch and cfg->max_scatter; of the calls below only
+ * polyglot_reserve_recurrence and polyglot_reserve_logits allocate more.
  * On success *out receives the context; on error *out is left NULL. */
 int polyglot_init(const polyglot_config* cfg, void* stream, polyglot_ctx** out);
 
 /* Waits for the context's stream, frees its workspace and the context. */
 int polyglot_destroy(polyglot_ctx* ctx);
 
-/* Replaces the stream the context enqueues on (hipStream_t, NULL = default). */
+/* Replaces the stream the context enqueues on (hipStream_t, NULL = default).
+ * All calls of a context share its workspace and must run one after the other.
+ * What is enqueued after the change therefore waits for what the old stream holds
+ * (an event; if the old stream no longer exists, for the device).  That leaves the
+ * calls that a graph capture records: where either stream is capturing nothing is
+ * ordered, and the program sees to it that a graph's replay overlaps neither
+ * another replay nor a call of the same context on another stream. */
 int polyglot_set_stream(polyglot_ctx* ctx, void* stream);
 
 /* One SGD step of the window-ranking model (model above; the embedding
@@ -270,7 +277,8 @@ int polyglot_kernel_times(polyglot_ctx* ctx, double* ms, int32_t* launches);
  * length.  Element offsets may pass 2^32.  Arithmetic, sums and states are in
  * 32 bits; each output is rounded to its format once (to nearest even).  Calls
  * are asynchronous on the context's stream and may be captured into a HIP
- * graph.  The argument blocks are read before the call returns; fields that
+ * graph, whose replays must not overlap each other or the context's other calls
+ * (polyglot_set_stream).  The argument blocks are read before the call returns; fields that
  * are not set must be zero.  Results do not depend on strides or alignment.
  * Host-detectable errors: POLYGLOT_ENULL, POLYGLOT_EINVAL,
  * POLYGLOT_EBATCH (above the reserved workspace), nothing enqueued. */

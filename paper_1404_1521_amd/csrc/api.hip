@@ -102,6 +102,8 @@ void free_all(polyglot_ctx* ctx) {
     if (*ev) hipEventDestroy(*ev);
     *ev = nullptr;
   }
+  if (ctx->ev_swap) hipEventDestroy(ctx->ev_swap);
+  ctx->ev_swap = nullptr;
   if (ctx->side) hipStreamDestroy(ctx->side);
   ctx->side = nullptr;
   for (uint64_t* q : {ctx->op.rec.head, ctx->op.log_head})
@@ -441,6 +443,37 @@ int enqueue_steps(polyglot_ctx* ctx, float* E, float* W1, float* b1, float* w2, 
   return POLYGLOT_OK;
 }
 
+// Whether a stream's calls are being captured into a graph; what cannot say so is gone
+// (the program has destroyed it).
+enum class StreamState { kRuns, kCaptures, kGone };
+StreamState stream_state(hipStream_t s) {
+  hipStreamCaptureStatus c = hipStreamCaptureStatusNone;
+  const hipError_t e = hipStreamIsCapturing(s, &c);
+  if (e == hipSuccess)
+    return c == hipStreamCaptureStatusNone ? StreamState::kRuns : StreamState::kCaptures;
+  (void)hipGetLastError();
+  // (the default stream, while a stream that waits for it is captured)
+  return e == hipErrorStreamCaptureImplicit ? StreamState::kCaptures : StreamState::kGone;
+}
+
+// What `next` is given from now on waits for what the calls so far are still doing: the
+// calls of a context share one workspace.  A capture takes no part in that, on either
+// side: its nodes run when their graph is launched.
+hipError_t order_streams(polyglot_ctx* ctx, hipStream_t next) {
+  if (next == ctx->eager || stream_state(next) == StreamState::kCaptures) return hipSuccess;
+  const StreamState last = stream_state(ctx->eager);
+  hipError_t e = hipSuccess;
+  if (last == StreamState::kRuns) {
+    if (!ctx->ev_swap) e = hipEventCreateWithFlags(&ctx->ev_swap, hipEventDisableTiming);
+    if (e == hipSuccess) e = hipEventRecord(ctx->ev_swap, ctx->eager);
+    if (e == hipSuccess) e = hipStreamWaitEvent(next, ctx->ev_swap, 0);
+  } else if (last == StreamState::kGone) {
+    e = hipDeviceSynchronize();
+  }
+  if (e == hipSuccess) ctx->eager = next;
+  return e;
+}
+
 // The code of raised error words.
 int flag_code(uint32_t f) {
   return f & kFlagBadId ? POLYGLOT_EID : f & kFlagBadOffset ? POLYGLOT_EOFFSETS : POLYGLOT_EHIP;
@@ -491,7 +524,7 @@ int polyglot_init(const polyglot_config* cfg, void* stream, polyglot_ctx** out) 
   polyglot_ctx* ctx = new (std::nothrow) polyglot_ctx();
   if (!ctx) return POLYGLOT_EHIP;
   ctx->cfg = c;
-  ctx->stream = static_cast<hipStream_t>(stream);
+  ctx->stream = ctx->eager = static_cast<hipStream_t>(stream);
   ctx->K = c.win * c.d;
   ctx->c = c.win / 2;
   ctx->large = large;
@@ -605,7 +638,10 @@ int polyglot_destroy(polyglot_ctx* ctx) {
 
 int polyglot_set_stream(polyglot_ctx* ctx, void* stream) {
   if (!ctx) return POLYGLOT_ENULL;
-  ctx->stream = static_cast<hipStream_t>(stream);
+  const hipStream_t next = static_cast<hipStream_t>(stream);
+  const hipError_t e = order_streams(ctx, next);
+  if (e != hipSuccess) return hip_fail(ctx, e, "set_stream");
+  ctx->stream = next;
   return POLYGLOT_OK;
 }
 

@@ -50,6 +50,8 @@ struct polyglot_ctx {
   hipStream_t side = nullptr;
   hipEvent_t ev_fork = nullptr, ev_sorted[2] = {nullptr, nullptr},
              ev_done[2] = {nullptr, nullptr};
+  hipStream_t eager = nullptr;   // the stream whose calls run as they are made (not a capture's)
+  hipEvent_t ev_swap = nullptr;  // where it was left for another
   int device = 0;
   int Hp = 0, NT = 0, K = 0, c = 0, cpw = 0;
   bool large = false;  // hidden layer above 64 units: the three-contraction path

@@ -255,10 +255,50 @@ void many_rows() {
   }
 }
 
+// What is enqueued after a change of the stream waits for what was enqueued before it:
+// the calls of a context share its workspace.
+void streams() {
+  polyglot_ctx* ctx = context();
+  const auto stream = [](uintptr_t k) { return reinterpret_cast<hipStream_t>(k); };
+  const auto change = [&](uintptr_t k) { return polyglot_set_stream(ctx, stream(k)); };
+  const auto said = [&](std::vector<std::string> want) {
+    const bool same = order == want;
+    order.clear();
+    return same;
+  };
+  const long before = events;
+  CHECK(change(16) == POLYGLOT_OK && said({"record 0", "wait 16"}));
+  CHECK(change(16) == POLYGLOT_OK && said({}));
+  CHECK(change(32) == POLYGLOT_OK && said({"record 16", "wait 32"}));
+  CHECK(change(0) == POLYGLOT_OK && said({"record 32", "wait 0"}));
+  CHECK(change(16) == POLYGLOT_OK && said({"record 0", "wait 16"}));
+  CHECK(events <= before + 1);
+  // into a graph that is being captured and out of it: its nodes cannot wait for what
+  // is outside, nor what is outside for them
+  capturing = {stream(48)};
+  CHECK(change(48) == POLYGLOT_OK && said({}));
+  CHECK(change(16) == POLYGLOT_OK && said({}));
+  CHECK(change(48) == POLYGLOT_OK && said({}));
+  capturing.clear();  // what ran before the capture is waited for also after it
+  CHECK(change(32) == POLYGLOT_OK && said({"record 16", "wait 32"}));
+  CHECK(change(16) == POLYGLOT_OK && said({"record 32", "wait 16"}));
+  // a stream that is gone: what it held is waited for with everything else
+  gone = {stream(16)};
+  CHECK(change(32) == POLYGLOT_OK && said({"all"}));
+  // the calls go where the last change says
+  polyglot_dropout_args a{};
+  a.x = a.y = room();
+  a.rows = a.d = 1;
+  a.ld_x = a.ld_y = 1;
+  CHECK(polyglot_dropout(ctx, &a) == POLYGLOT_OK && launches.back().stream == stream(32));
+  CHECK(polyglot_set_stream(nullptr, nullptr) == POLYGLOT_ENULL);
+  CHECK(polyglot_destroy(ctx) == POLYGLOT_OK && events == 0);
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
-  const std::map<std::string, void (*)()> all = {{"many_rows", many_rows}};
+  const std::map<std::string, void (*)()> all = {{"many_rows", many_rows}, {"streams", streams}};
   const auto it = argc > 1 ? all.find(argv[1]) : all.end();
   if (it == all.end()) return 2;
   it->second();

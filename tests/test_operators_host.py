@@ -31,3 +31,7 @@ def run(program, what):
 def test_scores_of_more_rows_than_a_launch_has(program):
     """A launch has fewer than 2^32 threads; more rows take several launches."""
     run(program, "many_rows")
+
+
+def test_a_change_of_the_stream_keeps_the_order(program):
+    run(program, "streams")
