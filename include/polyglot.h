@@ -98,7 +98,10 @@ int polyglot_destroy(polyglot_ctx* ctx);
  * (an event; if the old stream no longer exists, for the device).  That leaves the
  * calls that a graph capture records: where either stream is capturing nothing is
  * ordered, and the program sees to it that a graph's replay overlaps neither
- * another replay nor a call of the same context on another stream. */
+ * another replay nor a call of the same context on another stream.  Calls that
+ * overlap all the same may leave outputs unwritten.  Where the sequence operators
+ * notice it, polyglot_status returns POLYGLOT_EHIP; their workspace is then to be
+ * reserved again. */
 int polyglot_set_stream(polyglot_ctx* ctx, void* stream);
 
 /* One SGD step of the window-ranking model (model above; the embedding
@@ -463,7 +466,8 @@ int polyglot_reserve_logits(polyglot_ctx* ctx, int32_t max_rows, int32_t max_V);
 int polyglot_operator_times(polyglot_ctx* ctx, double* ms, int32_t* launches);
 
 /* Synchronises the stream and returns the sticky device error
- * (POLYGLOT_OK, POLYGLOT_EID or POLYGLOT_EOFFSETS), then clears it. */
+ * (POLYGLOT_OK, POLYGLOT_EID, POLYGLOT_EOFFSETS, or POLYGLOT_EHIP for a library
+ * error or calls that overlapped), then clears it. */
 int polyglot_status(polyglot_ctx* ctx);
 
 /* Text of the last error recorded on this context ("" if none). */

@@ -1002,7 +1002,8 @@ int polyglot_status(polyglot_ctx* ctx) {
                 code == POLYGLOT_EID ? "an id was outside its table"
                 : code == POLYGLOT_EOFFSETS
                     ? "sequence offsets did not ascend from 0 to the tokens"
-                    : "internal: a sort position outside the entry range, or a wait without end");
+                    : "internal: a sort position outside the entry range, a wait without end, or "
+                      "calls of one context that overlapped");
   }
   return POLYGLOT_OK;
 }

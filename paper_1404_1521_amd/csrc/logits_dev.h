@@ -318,7 +318,12 @@ __global__ __launch_bounds__(kBlock) void k_logits(LogitsCall c) {
                                          __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
-  if ((uint32_t)lds.arrived != (uint32_t)c.tiles - 1) return;
+  if ((uint32_t)lds.arrived != (uint32_t)c.tiles - 1) {
+    // More parts than the row has: another call, which the program lets overlap with
+    // this one, counted in some of its own.
+    if (t == 0 && (uint32_t)lds.arrived >= (uint32_t)c.tiles) atomicOr(c.flag, kFlagInternal);
+    return;
+  }
 
   // the last part joins them, in their order
   tag = (uint32_t)(lds.arrived >> 32);

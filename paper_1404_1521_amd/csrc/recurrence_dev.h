@@ -270,6 +270,12 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(RecCall c, ScanPlan p) {
   __syncthreads();
   const uint32_t tag = (uint32_t)(s.ticket >> 32);
   const int chunk = (int)(uint32_t)s.ticket;
+  // A ticket past the chunks: another call, which the program lets overlap with this one,
+  // draws from the same counter.  Its place would lie outside of the tile's words.
+  if ((uint32_t)chunk >= (uint32_t)p.chunks) {
+    if (t == 0) atomicOr(c.flag, kFlagInternal);
+    return;
+  }
 
   // The chunk's tokens are the places [0, count) of the scan from q0 on: token
   // t0 + place * dir.

@@ -1,5 +1,7 @@
 """The sequence operators at the limits of what a launch, a tag or a format holds, and
 the variants of their kernels that sizes choose."""
+import ctypes
+
 import pytest
 
 from test_gpu_operators import Scores, Seqs, ctx, dev, host, near, pg  # noqa: F401
@@ -103,3 +105,95 @@ def test_a_change_of_the_stream_into_a_capture(pg):  # noqa: F811
         torch.cuda.synchronize()
     assert c.status() == pg.OK
     c.close()
+
+
+# What the entry points hand to the launches, for calls whose workspace is made here.
+class RecCall(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in
+                "gate x h dh h0 init offsets out dgate fin flag".split()] + \
+               [(n, ctypes.c_int64) for n in "ld_gate ld_x ld_h ld_dh ld_out ld_dgate".split()] + \
+               [(n, ctypes.c_int) for n in "tokens nseq D group offset_bytes down".split()]
+
+
+class ScanSpace(ctypes.Structure):
+    _fields_ = [("head", ctypes.c_void_p), ("counters", ctypes.c_int),
+                ("flags", ctypes.c_size_t), ("words", ctypes.c_size_t)]
+
+
+class Launch(ctypes.Structure):
+    _fields_ = [("stream", ctypes.c_void_p), ("owner", ctypes.c_void_p), ("take", ctypes.c_void_p)]
+
+
+def logits_call(pg):  # noqa: F811
+    class LogitsCall(ctypes.Structure):
+        _fields_ = [("a", pg.LogitsArgs), ("flag", ctypes.c_void_p), ("tiles", ctypes.c_int),
+                    ("head", ctypes.c_void_p), ("words", ctypes.c_void_p),
+                    ("stride", ctypes.c_int64)]
+    return LogitsCall
+
+
+INTERNAL = 2  # kFlagInternal
+LINE = 16     # kHeadLine
+
+
+def test_a_ticket_past_the_chunks(pg, ctx):  # noqa: F811
+    """A tile whose counter another call has moved: its workgroups say so and touch
+    nothing, the other tile is what it is."""
+    lib = pg.load_library()
+    space = lib._ZN2pg10scan_spaceEli
+    space.argtypes, space.restype = [ctypes.c_int64, ctypes.c_int], ScanSpace
+    launch = lib._ZN2pg17launch_recurrenceERKNS_7RecCallEiibRKNS_9ScanSpaceERKNS_6LaunchE
+    launch.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_bool, ctypes.c_void_p,
+                       ctypes.c_void_p]
+    q = Seqs("f32", [600], 64, 1, True, seed=32)
+    off = q.offsets()
+    want, _ = ctx.recurrence(q.gate, q.x, off, h0=q.h0)
+    sp = space(600, 64)
+    n = sp.counters * LINE + sp.flags + sp.words
+    for ticket in (5, 6, 1 << 31, (1 << 32) - 6):  # of five chunks of 128 tokens
+        room = torch.zeros(n, dtype=torch.int64, device="cuda")
+        room[:sp.counters * LINE:LINE] = 1 << 32
+        room[0] += ticket
+        before = room.clone()
+        h = torch.full_like(q.x, 7.0)
+        flag = torch.zeros(3, dtype=torch.int32, device="cuda")
+        sp.head = room.data_ptr()
+        call = RecCall(gate=q.gate.data_ptr(), x=q.x.data_ptr(), h0=q.h0.data_ptr(),
+                       init=q.h0.data_ptr(), offsets=off.data_ptr(), out=h.data_ptr(),
+                       flag=flag.data_ptr(), ld_gate=64, ld_x=64, ld_out=64, tokens=600, nseq=1,
+                       D=64, group=1, offset_bytes=4)
+        on = Launch(stream=torch.cuda.current_stream().cuda_stream)
+        assert launch(ctypes.byref(call), pg.F32, pg.GATE_SIGMOID, False, ctypes.byref(sp),
+                      ctypes.byref(on)) == 0
+        torch.cuda.synchronize()
+        assert flag.tolist() == [INTERNAL, 0, 0]
+        assert (h[:, :32] == 7).all() and torch.equal(h[:, 32:], want[:, 32:])
+        # of the first tile only the counter moved, by its five workgroups
+        assert int(room[0] - before[0]) == 5
+        flags = slice(sp.counters * LINE, sp.counters * LINE + 5 + 1)
+        assert torch.equal(room[flags], before[flags])
+        words = sp.counters * LINE + sp.flags
+        first = slice(words, words + 8 * (8 * 5 + 12 * 1))
+        assert torch.equal(room[first], before[first])
+
+
+def test_more_parts_than_a_row_has(pg, ctx):  # noqa: F811
+    lib = pg.load_library()
+    launch = lib._ZN2pg13launch_logitsENS_10LogitsCallERKNS_6LaunchE
+    LogitsCall = logits_call(pg)
+    launch.argtypes = [LogitsCall, ctypes.c_void_p]
+    V = 2000  # two parts
+    x = torch.randn(2, V, device="cuda")
+    head = torch.zeros(2 * LINE, dtype=torch.int64, device="cuda")
+    head[::LINE] = 1 << 32
+    head[0] += 2
+    words = torch.zeros(2 * 2 * 3, dtype=torch.int64, device="cuda")
+    flag = torch.zeros(3, dtype=torch.int32, device="cuda")
+    token = torch.full((2,), -7, dtype=torch.int32, device="cuda")
+    call = LogitsCall(flag=flag.data_ptr(), head=head.data_ptr(), words=words.data_ptr(), stride=2)
+    call.a = pg.LogitsArgs(logits=x.data_ptr(), token=token.data_ptr(), ld_logits=V, rows=2, V=V)
+    on = Launch(stream=torch.cuda.current_stream().cuda_stream)
+    assert launch(call, ctypes.byref(on)) == 0
+    torch.cuda.synchronize()
+    assert flag.tolist() == [INTERNAL, 0, 0]
+    assert token.tolist() == [-7, int(x[1].argmax())]
