@@ -38,6 +38,12 @@ struct OpWorkspace {
   uint64_t *log_head = nullptr, *log_words = nullptr;  // one block: counters, words
 };
 
+// A kernel's event pairs that are counted and not yet asked for.
+struct KernelTime {
+  double ms = 0.0;
+  int32_t launches = 0;
+};
+
 }  // namespace pg
 
 struct polyglot_ctx {
@@ -72,6 +78,7 @@ struct polyglot_ctx {
   bool capturing = false;
   std::vector<hipEvent_t> ev_pool;
   std::vector<std::pair<int, std::pair<hipEvent_t, hipEvent_t>>> ev_marks;
+  pg::KernelTime times[POLYGLOT_NKERNELS + POLYGLOT_NOPKERNELS];  // by kernel id
 };
 
 namespace pg {
@@ -109,32 +116,29 @@ inline hipEvent_t take_event(polyglot_ctx* ctx) {
   return ev;
 }
 
-// Sums the event pairs of the kernel ids [first, first + n) into ms and
-// launches, and takes them out.
+// Takes all event pairs into the kernels' totals, then moves those of the kernel ids
+// [first, first + n) out to ms and launches; the others' stay for their own question.
 inline int collect_times(polyglot_ctx* ctx, int first, int n, double* ms, int32_t* launches,
                          const char* what) {
   hipError_t e = hipStreamSynchronize(ctx->stream);
   if (e == hipSuccess) e = hipStreamSynchronize(ctx->side);
   if (e != hipSuccess) return hip_fail(ctx, e, what);
-  for (int k = 0; k < n; ++k) {
-    ms[k] = 0.0;
-    launches[k] = 0;
-  }
-  size_t kept = 0;
   for (auto& m : ctx->ev_marks) {
-    if (m.first < first || m.first >= first + n) {
-      ctx->ev_marks[kept++] = m;
-      continue;
-    }
     float t = 0.f;
     if (hipEventElapsedTime(&t, m.second.first, m.second.second) == hipSuccess) {
-      ms[m.first - first] += t;
-      launches[m.first - first] += 1;
+      ctx->times[m.first].ms += t;
+      ctx->times[m.first].launches += 1;
     }
     ctx->ev_pool.push_back(m.second.first);
     ctx->ev_pool.push_back(m.second.second);
   }
-  ctx->ev_marks.resize(kept);
+  ctx->ev_marks.clear();
+  for (int k = 0; k < n; ++k) {
+    KernelTime& t = ctx->times[first + k];
+    ms[k] = t.ms;
+    launches[k] = t.launches;
+    t = KernelTime{};
+  }
   return POLYGLOT_OK;
 }
 

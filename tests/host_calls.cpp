@@ -295,10 +295,49 @@ void streams() {
   CHECK(polyglot_destroy(ctx) == POLYGLOT_OK && events == 0);
 }
 
+// A program that asks for the times of one kind of kernels alone keeps no more event
+// pairs than it makes between two questions; the other kind's times are kept.
+void times() {
+  polyglot_ctx* ctx = context();
+  CHECK(polyglot_set_timing(ctx, 1) == POLYGLOT_OK);
+  polyglot_dropout_args a{};
+  a.x = a.y = room();
+  a.rows = a.d = 1;
+  a.ld_x = a.ld_y = 1;
+  double ms[POLYGLOT_NKERNELS + POLYGLOT_NOPKERNELS];
+  int32_t n[POLYGLOT_NKERNELS + POLYGLOT_NOPKERNELS];
+  long after_one = 0;
+  for (int i = 0; i < 100; ++i) {
+    for (int k = 0; k < 3; ++k) CHECK(polyglot_dropout(ctx, &a) == POLYGLOT_OK);
+    CHECK(polyglot_kernel_times(ctx, ms, n) == POLYGLOT_OK);
+    for (int k = 0; k < POLYGLOT_NKERNELS; ++k) CHECK(n[k] == 0 && ms[k] == 0);
+    if (i == 0) after_one = events;
+  }
+  CHECK(events == after_one);
+  CHECK(polyglot_operator_times(ctx, ms, n) == POLYGLOT_OK);
+  CHECK(n[POLYGLOT_OPK_DROPOUT] == 300 && ms[POLYGLOT_OPK_DROPOUT] == 150.0);
+  CHECK(n[POLYGLOT_OPK_LOGITS] == 0);
+  CHECK(polyglot_operator_times(ctx, ms, n) == POLYGLOT_OK && n[POLYGLOT_OPK_DROPOUT] == 0);
+  // the other way round
+  for (int i = 0; i < 100; ++i) {
+    CHECK(polyglot_score(ctx, room(), room(), room(), room(), room(),
+                         reinterpret_cast<int32_t*>(room()), 1, room()) == POLYGLOT_OK);
+    CHECK(polyglot_operator_times(ctx, ms, n) == POLYGLOT_OK);
+    for (int k = 0; k < POLYGLOT_NOPKERNELS; ++k) CHECK(n[k] == 0);
+    if (i == 0) after_one = events;
+  }
+  CHECK(events == after_one);
+  CHECK(polyglot_kernel_times(ctx, ms, n) == POLYGLOT_OK);
+  int all = 0;
+  for (int k = 0; k < POLYGLOT_NKERNELS; ++k) all += n[k];
+  CHECK(all >= 100 && all % 100 == 0);
+  CHECK(polyglot_destroy(ctx) == POLYGLOT_OK && events == 0);
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
-  const std::map<std::string, void (*)()> all = {{"many_rows", many_rows}, {"streams", streams}};
+  const std::map<std::string, void (*)()> all = {{"many_rows", many_rows}, {"streams", streams}, {"times", times}};
   const auto it = argc > 1 ? all.find(argv[1]) : all.end();
   if (it == all.end()) return 2;
   it->second();

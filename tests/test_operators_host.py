@@ -35,3 +35,7 @@ def test_scores_of_more_rows_than_a_launch_has(program):
 
 def test_a_change_of_the_stream_keeps_the_order(program):
     run(program, "streams")
+
+
+def test_event_pairs_do_not_pile_up(program):
+    run(program, "times")
