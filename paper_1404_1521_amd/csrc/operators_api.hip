@@ -21,18 +21,17 @@ int64_t logits_parts(int V) { return (V + (int64_t)kLogitsMinTile - 1) / kLogits
 constexpr int kLogitsMaxV = 1 << 30;  // places in a row fit an int
 
 // A zeroed block of `lines` words of counters, each line's first with tag 1, and
-// `words` more behind them (their tag 0: nothing has written them).
+// `words` more behind them (their tag 0: nothing has written them).  All of it is made on
+// the device: the counters of many rows are gigabytes.
 hipError_t heads(polyglot_ctx* ctx, uint64_t** head, size_t lines, size_t words) {
   const size_t n = lines + words + 1;
-  std::vector<uint64_t> first(lines, 0);
-  for (size_t i = 0; i < lines; i += kHeadLine) first[i] = (uint64_t)1 << 32;
   uint64_t* p = nullptr;
   hipError_t e = hipMalloc(reinterpret_cast<void**>(&p), n * sizeof(uint64_t));
   if (e != hipSuccess) return e;
   e = hipMemsetAsync(p, 0, n * sizeof(uint64_t), ctx->stream);
-  if (e == hipSuccess && lines > 0)
-    e = hipMemcpyAsync(p, first.data(), lines * sizeof(uint64_t), hipMemcpyHostToDevice,
-                       ctx->stream);
+  if (e == hipSuccess && lines > 0)  // the lowest byte of each line's tag
+    e = hipMemset2DAsync(reinterpret_cast<char*>(p) + 4, kHeadLine * sizeof(uint64_t), 1, 1,
+                         lines / kHeadLine, ctx->stream);
   if (e == hipSuccess) e = hipStreamSynchronize(ctx->stream);
   if (e == hipSuccess) *head = p;
   else (void)hipFree(p);

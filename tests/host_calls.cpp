@@ -334,10 +334,42 @@ void times() {
   CHECK(polyglot_destroy(ctx) == POLYGLOT_OK && events == 0);
 }
 
+// Reserving makes the counters on the device: nothing of their size on the host.  Every
+// line starts with tag 1 and nothing counted, all else is zero.
+void reserve() {
+  polyglot_ctx* ctx = context();
+  const auto newest = [] {  // the largest block
+    std::pair<void*, size_t> b{nullptr, 0};
+    for (const auto& k : blocks)
+      if (k.second > b.second) b = k;
+    return b;
+  };
+  const auto whole = [&](size_t lines, size_t all) {
+    const auto b = newest();
+    const uint64_t* w = static_cast<const uint64_t*>(b.first);
+    CHECK(b.second >= 8 * all);
+    for (size_t i = 0; i < b.second / 8; ++i)
+      if (w[i] != (i % 16 == 0 && i < 16 * lines ? (uint64_t)1 << 32 : 0)) return false;
+    return true;
+  };
+  to_device = 0;
+  const int rows = 1 << 20;
+  CHECK(polyglot_reserve_logits(ctx, rows, 3000) == POLYGLOT_OK);
+  CHECK(whole(rows, (size_t)rows * (16 + 3 * 3)));
+  CHECK(polyglot_reserve_logits(ctx, 0, 0) == POLYGLOT_OK);
+  CHECK(polyglot_reserve_recurrence(ctx, 1000, 1 << 16) == POLYGLOT_OK);
+  const size_t tiles = 2 * (1 << 16) / 32 + 1;  // the narrowest, doubled for a group's idle lanes
+  CHECK(whole(tiles, tiles * 16));
+  CHECK(polyglot_reserve_recurrence(ctx, 0, 0) == POLYGLOT_OK);
+  CHECK(to_device <= 4096);
+  CHECK(polyglot_destroy(ctx) == POLYGLOT_OK && blocks.empty());
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
-  const std::map<std::string, void (*)()> all = {{"many_rows", many_rows}, {"streams", streams}, {"times", times}};
+  const std::map<std::string, void (*)()> all = {{"many_rows", many_rows}, {"streams", streams}, {"times", times},
+                                                        {"reserve", reserve}};
   const auto it = argc > 1 ? all.find(argv[1]) : all.end();
   if (it == all.end()) return 2;
   it->second();

@@ -39,3 +39,7 @@ def test_a_change_of_the_stream_keeps_the_order(program):
 
 def test_event_pairs_do_not_pile_up(program):
     run(program, "times")
+
+
+def test_reserving_takes_no_host_memory_of_its_size(program):
+    run(program, "reserve")
