@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kBlock) void k_dropout(DropoutCall c) {
                            (uint32_t)a.seed, (uint32_t)(a.seed >> 32));
   uint32_t keep = keep_bits(w, c.threshold);
   if (a.whole_rows) keep = keep & 1u ? 0xffu : 0u;
-  const float spoilt = IDS && bad ? __builtin_nanf("") : 0.f;
+  const float spoilt = IDS && bad ? __builtin_nanf("") : -0.f;  // (v + -0 is v, also for -0)
   if (n == 8) {
     float v[8];
 #pragma unroll

@@ -2,6 +2,7 @@
 the variants of their kernels that sizes choose."""
 import ctypes
 
+import numpy as np
 import pytest
 
 from test_gpu_operators import Scores, Seqs, ctx, dev, host, near, pg  # noqa: F401
@@ -197,3 +198,19 @@ def test_more_parts_than_a_row_has(pg, ctx):  # noqa: F811
     torch.cuda.synchronize()
     assert flag.tolist() == [INTERNAL, 0, 0]
     assert token.tolist() == [-7, int(x[1].argmax())]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("d", [5, 64])
+def test_dropout_of_table_rows_keeps_the_sign_of_zero(ctx, dtype, d):  # noqa: F811
+    """Rows taken by their ids are the bits that the same rows give without ids."""
+    rng = np.random.default_rng(d)
+    table = dev(np.where(rng.random((40, d)) < 0.5, -0.0, rng.normal(size=(40, d))), dtype)
+    ids = torch.from_numpy(rng.integers(0, 40, 300).astype(np.int32)).cuda()
+    rows = table[ids.long()]
+    bits = lambda t: t.view(torch.int32 if dtype == "f32" else torch.int16)  # noqa: E731
+    assert torch.equal(bits(ctx.dropout(table, 0.0, 3, ids=ids)), bits(rows))
+    assert torch.equal(bits(ctx.dropout(table, 0.4, 3, ids=ids)), bits(ctx.dropout(rows, 0.4, 3)))
+    add = torch.full_like(rows, -0.0)
+    assert torch.equal(bits(ctx.dropout(table, 0.4, 3, ids=ids, add=add)),
+                       bits(ctx.dropout(rows, 0.4, 3, add=add)))
