@@ -214,3 +214,85 @@ def test_dropout_of_table_rows_keeps_the_sign_of_zero(ctx, dtype, d):  # noqa: F
     add = torch.full_like(rows, -0.0)
     assert torch.equal(bits(ctx.dropout(table, 0.4, 3, ids=ids, add=add)),
                        bits(ctx.dropout(rows, 0.4, 3, add=add)))
+
+
+# The rules by which the launches choose a variant, written out again: a case below says
+# which one it is there for, and fails if a change of the rules moves it to another.
+
+
+def scan_variant(dtype, sig, grad, tokens, D, group):
+    """Lanes of a row of threads and tokens of a thread."""
+    size = 4 if dtype == "f32" else 2
+    per_group = -(-group // 4) if group > 1 else 1
+    lanes = per_group * (D // group) if group > 1 else -(-D // 4)
+    usual = 3 if D <= 64 or (size == 4 and D <= 512) else 4
+    log2 = 3
+    while log2 < 6 and 1 << log2 < lanes and (log2 < usual or 1 << log2 < per_group):
+        log2 += 1
+    row = 1 << log2
+    tiles = -(-(D // group) // (row // per_group)) if group > 1 else -(-D // (4 * row))
+    long = (12 if grad else 16) if size == 2 else 8 if grad else 12 if sig else 16
+    chunks = max(1, -(-tokens // (256 // row * long)))
+    return row, long if chunks * tiles >= 256 else 4
+
+
+LONG_CHUNKS = [(dtype, sig, D, group, row)
+               for dtype in ("f32", "bf16", "f16")
+               for sig, D, group, row in (
+                   (True, 512, 1, 8 if dtype == "f32" else 16),
+                   (False, 512, 1, 8 if dtype == "f32" else 16),
+                   (dtype != "bf16", 509, 1, 8 if dtype == "f32" else 16),
+                   (True, 512, 64, 16), (False, 512, 64, 16), (dtype == "bf16", 510, 5, 8 if dtype == "f32" else 16),
+                   (dtype != "f16", 512, 128, 32), (dtype == "f16", 512, 256, 64))]
+
+
+@pytest.mark.parametrize("dtype,sig,D,group,row", LONG_CHUNKS)
+def test_recurrence_with_long_chunks(pg, ctx, dtype, sig, D, group, row):  # noqa: F811
+    """Threads with the most tokens they take, forward and gradient: sequences that begin and
+    end in every place of a chunk, and one that goes through many."""
+    tokens = 8300
+    most = 16 if dtype != "f32" else 12 if sig else 16
+    assert scan_variant(dtype, sig, False, tokens, D, group) == (row, most)
+    assert scan_variant(dtype, sig, True, tokens, D, group) == (row, 12 if dtype != "f32" else 8)
+    rng = np.random.default_rng([D, group, sig])
+    lengths = np.concatenate([rng.integers(0, 40, 60), [3200], rng.integers(100, 300, 6), [0, 1]])
+    lengths = np.append(lengths, tokens - lengths.sum())
+    Seqs(dtype, lengths, D, group, sig, state=group != 128, seed=33).check(ctx, pg, not sig)
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("empty", [1023, 1024, 1025, 2049, 3000])
+def test_recurrence_of_many_empty_sequences_at_one_place(pg, ctx, empty, reverse):  # noqa: F811
+    """More offsets within reach of a chunk than are read at a time."""
+    none = [0] * empty
+    for lengths in (none + [5] + none + [700] + [1] * 40 + none, [300] + none + [300], none):
+        for state in (True, False):
+            Seqs("f32", lengths, 12, 1, True, state=state, seed=34).check(
+                ctx, pg, reverse, torch.int64 if empty % 2 else torch.int32)
+
+
+@pytest.mark.parametrize("nseq", [1039, 1040, 1104, 4223, 4224, 4225, 4289])
+def test_recurrence_finds_its_first_offset(pg, ctx, nseq):  # noqa: F811
+    """Counts on both sides of those that the search's 65 parts divide."""
+    Seqs("f32", [1] * nseq, 8, 1, True, seed=35).check(ctx, pg, nseq % 2 == 0)
+
+
+def scores_variant(rows, V):
+    words = 32
+    while words > 4 and rows * -(-V // (words * 256)) < 512:
+        words //= 2
+    return words
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("cap", [300, 33_000])
+@pytest.mark.parametrize("rows,V,words", [
+    (48, 32_003, 8), (48, 32_767, 8), (48, 32_769, 8), (64, 35_003, 16), (64, 36_863, 16),
+    (64, 36_865, 16), (64, 65_535, 32), (64, 65_537, 32), (30, 16_384, 4), (64, 20_479, 8)])
+def test_scores_with_every_length_of_a_part(ctx, dtype, cap, rows, V, words):  # noqa: F811
+    """Parts of 1,024 to 8,192 words with counters of 16 and 32 bits; vocabularies just
+    below and just above whole parts."""
+    assert scores_variant(rows, V) == words
+    kind = (rows + V + cap) % 3
+    Scores(dtype, rows, V, cap=cap, masks=(rows, 1, rows + 2)[kind], bias=("shared", "rows")[V % 2],
+           seed=36).check(ctx)
