@@ -161,7 +161,8 @@ __device__ __forceinline__ int first_offset(const RecCall& c, int lo) {
     const bool below = i < l + n && seq_offset(c, i) < lo;
     const int k = __popcll(__ballot(below));  // of ascending offsets the first k are below
     l += k * step;
-    n = min(step - 1, n - k * step);
+    n -= k * step;
+    if (k < kWave) n = min(step - 1, n);  // the next probe is not below
   }
   return l;
 }
