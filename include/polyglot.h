@@ -121,8 +121,9 @@ int polyglot_train_step(polyglot_ctx* ctx, float* E, float* W1, float* b1, float
  * memory, caller-owned).  Returns what polyglot_train_step returns for the
  * arguments (nothing is enqueued on such an error and *loss_host is left
  * unchanged); POLYGLOT_EHIP if the synchronisation fails; POLYGLOT_EID (or
- * POLYGLOT_EOFFSETS, left by a sequence operator) if a device error word is raised once the step has run, in which case the step
- * changed no parameter and *loss_host is NaN.  The error words stay raised
+ * POLYGLOT_EOFFSETS, left by a sequence operator) if a device error word is raised
+ * once the step has run, in which case the step changed no parameter and
+ * *loss_host is NaN.  The error words stay raised
  * (every later step is void) until polyglot_status() clears them. */
 int polyglot_train_step_sync(polyglot_ctx* ctx, float* E, float* W1, float* b1, float* w2,
                              float* b2, const int32_t* windows, const int32_t* corrupt,
@@ -340,7 +341,10 @@ int polyglot_dropout(polyglot_ctx* ctx, const polyglot_dropout_args* args);
  * 32 bits from the sequence's start to its end; h holds its roundings to dtype.
  * h may be x, with the same ld.  Consecutive gates are multiplied with each other:
  * RAW gates above 1 in size over many tokens may take such a product past 32 bits'
- * range, and the state with it, where one token after the other would not.
+ * range, and the state with it, where one token after the other would not.  What is
+ * infinite, a state or a RAW gate, may come out as NaN further on in its sequence and
+ * channel where one token after the other would keep it infinite.
+ * Widths (with shared gates: groups) of whole fours of channels are the fast ones.
  *
  * With one token per sequence (tokens == nseq, no offsets) this is a model's
  * step for single tokens: one pass over the rows, no workspace.  Other calls
@@ -398,7 +402,9 @@ typedef struct {
 int polyglot_recurrence_grad(polyglot_ctx* ctx, const polyglot_recurrence_grad_args* args);
 
 /* Sizes the recurrence's workspace for calls of up to max_tokens tokens and
- * max_D channels.  Waits for the context's stream, frees what an earlier call
+ * max_D channels, of any group and storage format: about 1.2 bytes for each token and
+ * channel, of max_D + 128 channels, and 11 MB (65,536 tokens of 2,048 channels: 185 MB).
+ * Waits for the context's stream, frees what an earlier call
  * reserved and allocates: to be called outside of graph capture, and graphs that
  * were captured with the earlier workspace must not be replayed afterwards. */
 int polyglot_reserve_recurrence(polyglot_ctx* ctx, int64_t max_tokens, int32_t max_D);
@@ -453,7 +459,7 @@ typedef struct {
 int polyglot_logits(polyglot_ctx* ctx, const polyglot_logits_args* args);
 
 /* Sizes the workspace that joins the parts of a row, for calls of up to max_rows
- * rows of max_V scores; otherwise as polyglot_reserve_recurrence. */
+ * rows of max_V scores: 128 bytes a row, and 24 for every 1,024 of its words; otherwise as polyglot_reserve_recurrence. */
 int polyglot_reserve_logits(polyglot_ctx* ctx, int32_t max_rows, int32_t max_V);
 
 /* The operators' kernels under polyglot_set_timing, as polyglot_kernel_times

@@ -8,7 +8,7 @@
 // carry the launch's tag, in the order of the parts.
 //
 // Bound by memory for many rows: 256 rows of 1,000,000 bfloat16 with histories of up to
-// 4,096 ids 234 us (4.4 TB/s of 1.03 GB; copying the scores takes 208); without
+// 4,096 ids 239 us (4.3 TB/s of 1.03 GB; copying the scores takes 208); without
 // histories, which every part of a row reads again, 194.  A few rows: a chain of
 // dependent rounds, the part's loads, the counts, the join's counter and words: one row
 // of 100,000 float32 7.2 us, 48 of 32,003 bfloat16 8.9 us.

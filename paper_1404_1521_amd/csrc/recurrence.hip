@@ -12,11 +12,11 @@ namespace {
 // Lanes of a row of threads where a group of channels does not ask for more.  16 lanes
 // of four channels are whole cache lines of 16-bit elements.  With 8 a narrow layer has
 // twice the tiles, whose workgroups count themselves in side by side (10 ns each on one
-// counter), and half the chunks to join; 8 lanes are whole lines of float32.  us for 8 and
-// 16 lanes, forward, gradient: 65,537 x 64 float32 21.9, 27.4 and 24.7, 33.6; bfloat16
-// 23.2, 29.5 and 24.1, 32.9; 16,384 x 512 float32 29.2, 38.9 and 31.2, 40.9; bfloat16 23.0,
-// 34.7 and 21.4, 33.9; 65,536 x 2,048 float32 345, 481 and 320, 463; bfloat16 271, 464 and
-// 217, 352 (32 lanes 239, 368).
+// counter), and half the chunks to join; 8 lanes are whole lines of float32.  One sequence,
+// sigmoid gates, us for 8 and 16 lanes, forward, gradient: 65,537 x 64 float32 25.7, 34.7
+// and 28.6, 39.9; bfloat16 23.4, 33.1 and 23.8, 32.9; 16,384 x 512 float32 32.4, 50.4 and
+// 35.5, 53.7; bfloat16 27.0, 44.8 and 24.9, 39.4; 65,536 x 2,048 float32 369, 718 and 376,
+// 660; bfloat16 281, 541 and 246, 428 (32 lanes 262, 441).
 int scan_lanes_log2(int D, size_t size) { return D <= 64 || (size == 4 && D <= 512) ? 3 : 4; }
 
 // As few lanes as hold all channels, so that narrow layers have more rows of tokens; at
@@ -52,7 +52,11 @@ hipError_t launch_cut(const RecCall& c, ScanPlan p, const ScanSpace* space, cons
       return hipErrorInvalidValue;  // not reached within what scan_space bounds
   }
   const bool shared = c.group > 1;
-  const bool vec = shared ? c.group % 4 == 0 : c.D % 4 == 0;  // whole quads
+  // Whole quads.  Otherwise every quad, not a row's last alone, is loaded and stored element
+  // by element: sigmoid gates, forward and gradient, 16,384 x 509 bfloat16 42 and 97 us for
+  // 26 and 39 at 512, float32 48 and 89 for 32 and 50; 65,536 x 2,047 bfloat16 627 and 1,219
+  // for 242 and 428 at 2,048, float32 526 and 1,033 for 376 and 660.
+  const bool vec = shared ? c.group % 4 == 0 : c.D % 4 == 0;
   auto k = shared ? (vec ? k_scan<T, FORM, GRAD, true, true, R>
                          : k_scan<T, FORM, GRAD, true, false, R>)
                   : (vec ? k_scan<T, FORM, GRAD, false, true, R>

@@ -21,13 +21,13 @@
 // What bounds it.  Wide layers: memory, and the latency that two workgroups to a CU do
 // not cover (224 registers; a forward wave waits 44% of its cycles, its vector
 // instructions take 22%, 23 of them an element).  65,536 tokens 2,048 wide, bfloat16, 16
-// documents: forward 233 us (3.5 TB/s of the tensors' 806 MB), gradient 420 us (3.8 TB/s
+// documents: forward 231 us (3.5 TB/s of the tensors' 806 MB), gradient 420 us (3.8 TB/s
 // of 1.61 GB); at the 5.17 TB/s of a large copy they take 156 and 312.  Small calls: a
 // chain of dependent rounds, 5.3 us in a workgroup alone: the ticket and the offsets 0.9,
 // the loads' issue 0.6, the marks 1.2, the first pass 0.8, the join 0.8, the second pass
 // 0.7; 2.4 more where chunks wait for each other.  16,384 x 128 float32 in 700 sentences
-// forward 14.7 us, 16,411 x 256 bfloat16 with 8 gates gradient 21.6 us, one sequence of
-// 65,537 x 64 float32 gradient 29 us (at a copy's rate 4.9, 6.6, 16.2).
+// forward 14.7 us, 16,411 x 256 bfloat16 with 8 gates gradient 21.7 us, one sequence of
+// 65,537 x 64 float32 gradient 28 us (at a copy's rate 4.9, 6.6, 16.2).
 #pragma once
 #include <type_traits>
 
@@ -41,7 +41,9 @@ namespace pg {
 // r = 1 / (1 + s^2) and q = s r, the larger one of a and 1 - a is r, the other s q,
 // and the slope q^2: nothing is lost to a subtraction, and a product taken factor
 // by factor keeps its digits where 1 - a alone is below the normal floats.  The
-// hardware's base-2 exponential and reciprocal (one unit in the last place).
+// hardware's base-2 exponential and reciprocal are good to one unit in the last place;
+// the exponential's argument is a rounded product, so that s^2 is off by about |gate|
+// half units more.
 struct Decay {
   float a, q, u, w;
   __device__ __forceinline__ float rest(float v) const { return v * u * w; }
@@ -168,10 +170,13 @@ __device__ __forceinline__ int first_offset(const RecCall& c, int lo) {
 }
 
 // Tokens of a thread.  More of them are fewer chunks and fewer joining words, and more
-// registers: two workgroups of 256 threads to a CU, and no spills.  65,536 tokens 2,048
-// wide, one sequence, us.  Forward: bfloat16 12 tokens 277, 16 253; float32 raw 12 352,
-// 16 331; sigmoid 8 364 (three workgroups to a CU), 12 369, 16 (spilling) 401.
-// Gradient: bfloat16 8 418, 10 398, 12 367; float32 8 530, 10 (spilling) 584.
+// registers: two workgroups of 256 threads to a CU, and no vectors spilled.  65,536 tokens
+// 2,048 wide, one sequence, us.  Forward: bfloat16 sigmoid 12 tokens 278, 16 246; raw 12
+// 262, 16 233; float32 raw 12 362, 16 328; sigmoid 8 (three workgroups to a CU) 367, 12
+// 374, 16 (spilling) 451: 8 and 12 are as good as each other, 25.8 and 25.7 at 65,537 x 64,
+// 33 and 32 to 35 at 16,384 x 512.  Gradient: bfloat16 sigmoid 8 490, 10 465, 12 428; raw 8
+// 360, 10 385, 12 353; float32 sigmoid 8 659, 10 (spilling) 715; raw 8 572, 10 542, which
+// the sigmoid decides for both.
 template <class T, int FORM, bool GRAD>
 constexpr int scan_tokens() {
   if (sizeof(T) == 2) return GRAD ? 12 : 16;
