@@ -462,13 +462,223 @@ int polyglot_logits(polyglot_ctx* ctx, const polyglot_logits_args* args);
  * rows of max_V scores: 128 bytes a row, and 24 for every 1,024 of its words; otherwise as polyglot_reserve_recurrence. */
 int polyglot_reserve_logits(polyglot_ctx* ctx, int32_t max_rows, int32_t max_V);
 
+/* Short causal convolution of every channel on its own, over packed sequences.
+ *
+ *   u_t[c] = bias[c] + sum over k < taps of weight[c][k] x_{t - taps + 1 + k}[c]
+ *   y = u, or with silu u / (1 + e^-u)
+ *
+ * Sequences as in polyglot_recurrence.  What a sequence's first tokens reach back to are
+ * the rows of its state, the taps - 1 inputs before it, the newest one last (zeros if
+ * state is NULL); last[s], if not NULL, receives those after the sequence, of x as it is
+ * and of the state where the sequence is shorter.  With one token per sequence (tokens ==
+ * nseq, no offsets) this is a model's step for single tokens, and last may be state;
+ * otherwise no output may be an input. */
+typedef struct {
+  const void* x;       /* [tokens][D] */
+  const float* weight; /* [D][taps] */
+  const float* bias;   /* [D] or NULL */
+  const void* state;   /* [nseq][taps - 1][D] or NULL */
+  const void* offsets; /* [nseq + 1] int32 or int64, or NULL */
+  void* y;             /* [tokens][D] */
+  void* last;          /* [nseq][taps - 1][D] or NULL */
+  int64_t tokens;      /* 0 .. 2^30 */
+  int64_t ld_x, ld_y;
+  int32_t nseq;        /* >= 1 */
+  int32_t D;           /* 1 .. 2^20 */
+  int32_t taps;        /* 1 .. 8 */
+  int32_t dtype;
+  int32_t offset_bytes; /* 4 or 8 with offsets */
+  int32_t silu;
+} polyglot_convolution_args;
+int polyglot_convolution(polyglot_ctx* ctx, const polyglot_convolution_args* args);
+
+/* The gradient of polyglot_convolution.  With dy the gradient of y, dlast that of last,
+ * g_t = dy_t times the slope of y at u_t, and x going back into the state:
+ *
+ *   dx_t = sum over k of weight[k] g_{t + taps - 1 - k} of the same sequence, plus dlast's row
+ *   dweight[c][k] = sum over t of g_t x_{t - taps + 1 + k},  dbias[c] = sum over t of g_t
+ *
+ * dstate likewise, of the state's rows.  No output may be an input or another output.
+ * Uses the workspace of polyglot_reserve_selective. */
+typedef struct {
+  const void* x;       /* [tokens][D] */
+  const float* weight; /* [D][taps] */
+  const float* bias;   /* [D] or NULL */
+  const void* state;   /* [nseq][taps - 1][D] or NULL */
+  const void* dy;      /* [tokens][D] */
+  const void* dlast;   /* [nseq][taps - 1][D] or NULL */
+  const void* offsets; /* [nseq + 1] or NULL */
+  void* dx;            /* [tokens][D] */
+  float* dweight;      /* [D][taps] */
+  float* dbias;        /* [D] or NULL */
+  void* dstate;        /* [nseq][taps - 1][D] or NULL */
+  int64_t tokens, ld_x, ld_dy, ld_dx;
+  int32_t nseq, D, taps, dtype, offset_bytes, silu;
+} polyglot_convolution_grad_args;
+int polyglot_convolution_grad(polyglot_ctx* ctx, const polyglot_convolution_grad_args* args);
+
+/* Selective state space scan over packed sequences.
+ *
+ *   s_t[c]    = delta_t[c] + delta_bias[c], with softplus log(1 + e^(delta + delta_bias))
+ *   h_t[c][n] = e^(s_t[c] A[c][n]) h_{t-1}[c][n] + s_t[c] x_t[c] B_t[g][n]
+ *   v_t[c]    = sum over n of C_t[g][n] h_t[c][n], plus skip[c] x_t[c]
+ *   y = v, or with z v z / (1 + e^-z)
+ *
+ * for D channels of `states` states each; D / groups consecutive channels share the rows
+ * g of B and C (a head).  Sequences as in polyglot_recurrence; h_{-1} is h0[s] (zeros if
+ * NULL); last[s], if not NULL, receives the state after the sequence (h0[s] or zeros for
+ * an empty one).  States are carried in 32 bits.  marks, if not NULL, receives what
+ * polyglot_selective_grad needs: the states before every token that
+ * POLYGLOT_SELECTIVE_MARK divides.  What is infinite may come out as NaN further on in its
+ * sequence and channel.  States in whole fours, and 8, 16, 32 or 64 of them, are the fast ones.
+ *
+ * With one token per sequence (tokens == nseq, no offsets) and no marks this is a model's
+ * step for single tokens, which needs no workspace and whose last may be h0.  Otherwise no output may be an input, and the call uses the workspace of
+ * polyglot_reserve_selective.  Offsets that do not ascend from 0 to `tokens` raise
+ * POLYGLOT_EOFFSETS; the outputs are then unspecified, and no access leaves the tensors. */
+#define POLYGLOT_SELECTIVE_MARK 16
+typedef struct {
+  const void* x;           /* [tokens][D] */
+  const void* delta;       /* [tokens][D] */
+  const void* B;           /* [tokens][groups * states] */
+  const void* C;           /* [tokens][groups * states] */
+  const void* z;           /* [tokens][D] or NULL */
+  const float* A;          /* [D][states] */
+  const float* skip;       /* [D] or NULL */
+  const float* delta_bias; /* [D] or NULL */
+  const float* h0;         /* [nseq][D][states] or NULL */
+  const void* offsets;     /* [nseq + 1] int32 or int64, or NULL */
+  void* y;                 /* [tokens][D] */
+  float* last;             /* [nseq][D][states] or NULL */
+  float* marks;            /* [tokens / 16, rounded up][D][states rounded up to fours],
+                              aligned to 16 bytes, or NULL */
+  int64_t tokens;          /* 0 .. 2^30 */
+  int64_t ld_x, ld_delta, ld_B, ld_C, ld_z, ld_y;
+  int32_t nseq;            /* >= 1 */
+  int32_t D;               /* 1 .. 2^20 */
+  int32_t states;          /* 1 .. 64 */
+  int32_t groups;          /* dividing D */
+  int32_t dtype;
+  int32_t offset_bytes;    /* 4 or 8 with offsets */
+  int32_t softplus;
+} polyglot_selective_args;
+int polyglot_selective(polyglot_ctx* ctx, const polyglot_selective_args* args);
+
+/* The gradient of polyglot_selective, for the inputs and the marks of that call.  With v' the
+ * gradient of v (dy, or with z dy z / (1 + e^-z)), a = e^(s A), and going from a sequence's
+ * last token to its first, mu after the last one dlast[s]:
+ *
+ *   lambda = v' C + mu,  mu <- a lambda,  q = a lambda h_{t-1},  e = sum over n of lambda B
+ *   dC = sum over the head's channels of v' h,  dB = ... of lambda s x
+ *   dx = s e + skip v',  ddelta = (x e + sum over n of q A) times the slope of s
+ *   dA = sum over t of q s,  dskip = ... of v' x,  ddelta_bias = ... of ddelta
+ *   dz = dy v times the slope of z / (1 + e^-z),  dh0[s] = mu after the sequence's first token
+ *
+ * Sums over tokens and channels are in 32 bits, in an order that the sizes fix.  dz goes with
+ * z.  No output may be an input or another output.  Uses the workspace of
+ * polyglot_reserve_selective. */
+typedef struct {
+  const void* x;
+  const void* delta;
+  const void* B;
+  const void* C;
+  const void* z;           /* or NULL */
+  const void* dy;          /* [tokens][D] */
+  const float* A;
+  const float* skip;       /* or NULL */
+  const float* delta_bias; /* or NULL */
+  const float* h0;         /* or NULL */
+  const float* dlast;      /* [nseq][D][states] or NULL */
+  const float* marks;
+  const void* offsets;     /* or NULL */
+  void* dx;                /* [tokens][D] */
+  void* ddelta;            /* [tokens][D] */
+  void* dB;                /* [tokens][groups * states] */
+  void* dC;                /* [tokens][groups * states] */
+  void* dz;                /* [tokens][D], with z */
+  float* dA;               /* [D][states] */
+  float* dskip;            /* [D] or NULL */
+  float* ddelta_bias;      /* [D] or NULL */
+  float* dh0;              /* [nseq][D][states] or NULL */
+  int64_t tokens;
+  int64_t ld_x, ld_delta, ld_B, ld_C, ld_z, ld_dy, ld_dx, ld_ddelta, ld_dB, ld_dC, ld_dz;
+  int32_t nseq, D, states, groups, dtype, offset_bytes, softplus;
+} polyglot_selective_grad_args;
+int polyglot_selective_grad(polyglot_ctx* ctx, const polyglot_selective_grad_args* args);
+
+/* Sizes the workspace of the selective scan, its gradient and the convolution's gradient for
+ * calls of up to max_tokens tokens, max_D channels and max_states states; otherwise as
+ * polyglot_reserve_recurrence.  Up to 16 states take about 2 bytes for each token and channel
+ * and 128 for each token, up to 32 four times and up to 64 sixteen times as much, and 40 MB. */
+int polyglot_reserve_selective(polyglot_ctx* ctx, int64_t max_tokens, int32_t max_D,
+                               int32_t max_states);
+
+/* The best continuations of groups of beams: of each group's rows b and words v, the `picks`
+ * largest of
+ *
+ *   scores[b][v] + (total[b] - lse[b])      (lse NULL: + total[b])
+ *
+ * in 32 bits, the difference and the sum rounded once each; of equal ones (a zero's sign does
+ * not count) the lower beam's, then the lower word.  NaN and -infinity are never picked.  A
+ * row whose `finished` is not zero has one candidate only, the word `end` with the sum
+ * total[b].  For pick j of group i, best first:
+ *   parent[i][j]  its row, i * beams + b: what polyglot_reorder takes
+ *   token[i][j]   its word
+ *   out[i][j]     its sum
+ * and where nothing is left to pick the row i * beams + j % beams, -1 and -infinity.
+ * groups = 0 does nothing.  Uses the workspace of polyglot_reserve_beam. */
+typedef struct {
+  const void* scores;      /* [groups * beams][V] */
+  const float* total;      /* [groups * beams] */
+  const float* lse;        /* [groups * beams] or NULL */
+  const int32_t* finished; /* [groups * beams] or NULL */
+  int32_t* parent;         /* [groups][picks] */
+  int32_t* token;          /* [groups][picks] */
+  float* out;              /* [groups][picks] */
+  int64_t ld_scores;
+  int32_t groups;
+  int32_t beams;           /* >= 1, beams * V < 2^32 */
+  int32_t V;               /* 1 .. 2^30 */
+  int32_t picks;           /* 1 .. 64 */
+  int32_t end;             /* in [0, V), with finished */
+  int32_t dtype;
+} polyglot_beam_args;
+int polyglot_beam(polyglot_ctx* ctx, const polyglot_beam_args* args);
+
+/* Sizes the workspace of polyglot_beam for calls of up to max_rows rows (beams of all groups)
+ * of max_V scores and max_picks picks: 8 bytes for each pick of every 1,024 words of a row;
+ * otherwise as polyglot_reserve_recurrence. */
+int polyglot_reserve_beam(polyglot_ctx* ctx, int32_t max_rows, int32_t max_V, int32_t max_picks);
+
+/* out[r] = in[ids[r]] for the rows of several tensors at once (the states of a model's layers,
+ * the words said so far, by the beams that go on), bytes as they are.  Rows of row_bytes
+ * bytes lie ld_in and ld_out bytes apart; items is a host array, read before the call returns.
+ * No out may overlap an in or another out.  An id outside [0, in_rows) leaves its row of out
+ * as it was and raises the sticky flag (POLYGLOT_EID).  rows = 0 or count = 0 does nothing. */
+typedef struct {
+  const void* in;
+  void* out;
+  int64_t row_bytes;    /* >= 0 */
+  int64_t ld_in, ld_out;
+  int32_t in_rows;      /* >= 1 */
+  int32_t reserved;     /* 0 */
+} polyglot_row_copy;
+int polyglot_reorder(polyglot_ctx* ctx, const polyglot_row_copy* items, int32_t count,
+                     const int32_t* ids, int32_t rows);
+
 /* The operators' kernels under polyglot_set_timing, as polyglot_kernel_times
  * reports the others. */
 #define POLYGLOT_OPK_DROPOUT 0
 #define POLYGLOT_OPK_RECURRENCE 1
 #define POLYGLOT_OPK_RECURRENCE_GRAD 2
 #define POLYGLOT_OPK_LOGITS 3
-#define POLYGLOT_NOPKERNELS 4
+#define POLYGLOT_OPK_CONVOLUTION 4
+#define POLYGLOT_OPK_CONVOLUTION_GRAD 5
+#define POLYGLOT_OPK_SELECTIVE 6
+#define POLYGLOT_OPK_SELECTIVE_GRAD 7
+#define POLYGLOT_OPK_BEAM 8
+#define POLYGLOT_OPK_REORDER 9
+#define POLYGLOT_NOPKERNELS 10
 int polyglot_operator_times(polyglot_ctx* ctx, double* ms, int32_t* launches);
 
 /* Synchronises the stream and returns the sticky device error

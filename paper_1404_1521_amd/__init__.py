@@ -15,6 +15,7 @@ from __future__ import annotations
 import ctypes
 import os
 import struct
+from typing import NamedTuple
 
 import torch  # loaded first: the library then binds to torch's HIP runtime
 
@@ -38,10 +39,15 @@ EXPORTS = ("polyglot_init", "polyglot_destroy", "polyglot_set_stream", "polyglot
            "polyglot_set_timing", "polyglot_kernel_times",
            "polyglot_dropout", "polyglot_recurrence", "polyglot_recurrence_grad",
            "polyglot_reserve_recurrence", "polyglot_logits", "polyglot_reserve_logits",
-           "polyglot_operator_times")
+           "polyglot_operator_times",
+           "polyglot_convolution", "polyglot_convolution_grad", "polyglot_selective",
+           "polyglot_selective_grad", "polyglot_reserve_selective", "polyglot_beam",
+           "polyglot_reserve_beam", "polyglot_reorder")
 KERNEL_NAMES = ("fwdbwd", "sort", "update", "gather", "scatter", "score", "segfix", "wide_dw1",
                 "wide_g")
-OPERATOR_NAMES = ("dropout", "recurrence", "recurrence_grad", "logits")
+OPERATOR_NAMES = ("dropout", "recurrence", "recurrence_grad", "logits", "convolution",
+                  "convolution_grad", "selective", "selective_grad", "beam", "reorder")
+SELECTIVE_MARK = 16  # POLYGLOT_SELECTIVE_MARK
 
 
 class PolyglotError(RuntimeError):
@@ -87,6 +93,50 @@ LogitsArgs = _args("LogitsArgs",
                    ("q", "ld_logits ld_out ld_history ld_bias ld_mask"),
                    ("i", "rows V dtype history_cap masks"))
 
+ConvolutionArgs = _args("ConvolutionArgs", ("p", "x weight bias state offsets y last"),
+                        ("q", "tokens ld_x ld_y"),
+                        ("i", "nseq D taps dtype offset_bytes silu"))
+ConvolutionGradArgs = _args("ConvolutionGradArgs",
+                            ("p", "x weight bias state dy dlast offsets dx dweight dbias dstate"),
+                            ("q", "tokens ld_x ld_dy ld_dx"),
+                            ("i", "nseq D taps dtype offset_bytes silu"))
+SelectiveArgs = _args("SelectiveArgs",
+                      ("p", "x delta B C z A skip delta_bias h0 offsets y last marks"),
+                      ("q", "tokens ld_x ld_delta ld_B ld_C ld_z ld_y"),
+                      ("i", "nseq D states groups dtype offset_bytes softplus"))
+SelectiveGradArgs = _args("SelectiveGradArgs",
+                          ("p", "x delta B C z dy A skip delta_bias h0 dlast marks offsets dx "
+                                "ddelta dB dC dz dA dskip ddelta_bias dh0"),
+                          ("q", "tokens ld_x ld_delta ld_B ld_C ld_z ld_dy ld_dx ld_ddelta ld_dB "
+                                "ld_dC ld_dz"),
+                          ("i", "nseq D states groups dtype offset_bytes softplus"))
+BeamArgs = _args("BeamArgs", ("p", "scores total lse finished parent token out"),
+                 ("q", "ld_scores"), ("i", "groups beams V picks end dtype"))
+RowCopy = _args("RowCopy", ("p", "in_ out"), ("q", "row_bytes ld_in ld_out"),
+                ("i", "in_rows reserved"))
+
+
+class ConvolutionGrads(NamedTuple):
+    """The gradients of a convolution's inputs; state is None where none was given."""
+    x: torch.Tensor
+    weight: torch.Tensor
+    bias: torch.Tensor | None
+    state: torch.Tensor | None
+
+
+class SelectiveGrads(NamedTuple):
+    """The gradients of a selective scan's inputs, None for those that were not given."""
+    x: torch.Tensor
+    delta: torch.Tensor
+    A: torch.Tensor
+    B: torch.Tensor
+    C: torch.Tensor
+    skip: torch.Tensor | None
+    z: torch.Tensor | None
+    delta_bias: torch.Tensor | None
+    state: torch.Tensor | None
+
+
 _lib = None
 
 
@@ -123,6 +173,14 @@ def load_library():
         "polyglot_logits": [p, p],
         "polyglot_reserve_logits": [p, i32, i32],
         "polyglot_operator_times": [p, p, p],
+        "polyglot_convolution": [p, p],
+        "polyglot_convolution_grad": [p, p],
+        "polyglot_selective": [p, p],
+        "polyglot_selective_grad": [p, p],
+        "polyglot_reserve_selective": [p, ctypes.c_int64, i32, i32],
+        "polyglot_beam": [p, p],
+        "polyglot_reserve_beam": [p, i32, i32, i32],
+        "polyglot_reorder": [p, p, i32, p, i32],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -198,6 +256,30 @@ def _format(t, name):
     if code is None:
         raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
     return code, t.dtype
+
+
+def _offsets(t):
+    """Pointer and size of an offset of a vector of sequence offsets (None: 0, 0)."""
+    if t is None:
+        return 0, 0
+    if t.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"offsets must be int32 or int64, got {t.dtype}")
+    return _vector(t, t.dtype, "offsets", t.shape[0]), t.element_size()
+
+
+def _block(t, dtype, name, shape):
+    """Pointer of a contiguous device tensor of this shape (None: 0)."""
+    if t is None:
+        return 0
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous device (cuda) tensor")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
 
 
 def _like(t):
@@ -535,6 +617,264 @@ class Context:
         if rc != OK:
             self._check(rc, "logits")
         return out, token, lse
+
+    def reserve_selective(self, max_tokens: int, max_width: int, max_states: int) -> None:
+        """Workspace for selective scans and their gradients of up to max_tokens tokens,
+        max_width channels and max_states states, and for the convolution's gradient."""
+        self._check(self._lib.polyglot_reserve_selective(self._h, max_tokens, max_width,
+                                                         max_states), "reserve_selective")
+
+    def reserve_beam(self, max_rows: int, max_vocab: int, max_picks: int) -> None:
+        """Workspace for selections among up to max_rows beams of max_vocab scores."""
+        self._check(self._lib.polyglot_reserve_beam(self._h, max_rows, max_vocab, max_picks),
+                    "reserve_beam")
+
+    @staticmethod
+    def _nseq(x, offsets):
+        return offsets.shape[0] - 1 if offsets is not None else x.shape[0] if x.dim() == 3 else 1
+
+    def _convolution(self, what, x, weight, bias, offsets, nseq, state, silu, out, last):
+        code, dtype = _format(x, "x")
+        tokens, D = x.shape
+        K = weight.shape[-1]
+        poff, off_bytes = _offsets(offsets)
+        if last is None:
+            last = x.new_empty((nseq, K - 1, D))
+        px, ld_x = _row_tensor(x, dtype, "x", tokens, D)
+        py, ld_y = _row_tensor(_flat(out), dtype, "out", tokens, D)
+        rows = (nseq, K - 1, D)
+        rc = self._lib.polyglot_convolution(self._h, ConvolutionArgs.pack(
+            px, _block(weight, torch.float32, "weight", (D, K)),
+            _vector(bias, torch.float32, "bias", D), _block(state, dtype, "state", rows), poff, py,
+            _block(last, dtype, "last", rows), tokens, ld_x, ld_y, nseq, D, K, code, off_bytes,
+            silu))
+        if rc != OK:
+            self._check(rc, what)
+        return out, last
+
+    def convolution(self, x, weight, bias=None, offsets=None, *, state=None, silu: bool = True,
+                    out=None, last=None):
+        """The short causal convolution of every channel, y_t = bias + sum over k of
+        weight[:, k] x_{t - taps + 1 + k} (silu: times its sigmoid), over the sequences of x
+        as in recurrence.  weight[D][taps] and bias[D] are float32; state and last
+        [nseq][taps - 1][D], in x's type, are the inputs before and at the end of each
+        sequence.  Returns (y, last)."""
+        if out is None:
+            out = _like(x)
+        return self._convolution("convolution", _flat(x), weight, bias, offsets,
+                                 self._nseq(x, offsets), state, silu, out, last)
+
+    def convolution_step(self, x, weight, bias=None, state=None, *, silu: bool = True, out=None,
+                         last=None):
+        """One token x[nseq][D] for each of nseq sequences after the inputs in
+        state[nseq][taps - 1][D].  Returns (y, the new states); last=state updates them in
+        place."""
+        if out is None:
+            out = _like(x)
+        return self._convolution("convolution_step", x, weight, bias, None, x.shape[0], state,
+                                 silu, out, last)
+
+    def convolution_backward(self, x, weight, bias, dy, offsets=None, *, state=None, dlast=None,
+                             silu: bool = True, out: ConvolutionGrads | None = None):
+        """The gradient of convolution for the gradients dy of y and dlast of last, into the
+        tensors of out where it has any.  Returns ConvolutionGrads."""
+        code, dtype = _format(x, "x")
+        nseq, shape = self._nseq(x, offsets), x.shape
+        x = _flat(x)
+        tokens, D = x.shape
+        K = weight.shape[-1]
+        rows = (nseq, K - 1, D)
+        dx, dweight, dbias, dstate = out if out is not None else (None,) * 4
+        if dx is None:
+            dx = x.new_empty(shape)
+        if dweight is None:
+            dweight = x.new_empty((D, K), dtype=torch.float32)
+        if dbias is None and bias is not None:
+            dbias = x.new_empty(D, dtype=torch.float32)
+        if dstate is None and state is not None:
+            dstate = x.new_empty(rows)
+        poff, off_bytes = _offsets(offsets)
+        px, ld_x = _row_tensor(x, dtype, "x", tokens, D)
+        pdy, ld_dy = _row_tensor(_flat(dy), dtype, "dy", tokens, D)
+        pdx, ld_dx = _row_tensor(_flat(dx), dtype, "dx", tokens, D)
+        rc = self._lib.polyglot_convolution_grad(self._h, ConvolutionGradArgs.pack(
+            px, _block(weight, torch.float32, "weight", (D, K)),
+            _vector(bias, torch.float32, "bias", D), _block(state, dtype, "state", rows), pdy,
+            _block(dlast, dtype, "dlast", rows), poff, pdx,
+            _block(dweight, torch.float32, "dweight", (D, K)),
+            _vector(dbias, torch.float32, "dbias", D), _block(dstate, dtype, "dstate", rows),
+            tokens, ld_x, ld_dy, ld_dx, nseq, D, K, code, off_bytes, silu))
+        if rc != OK:
+            self._check(rc, "convolution_backward")
+        return ConvolutionGrads(dx, dweight, dbias, dstate)
+
+    @staticmethod
+    def _selective_inputs(x, delta, A, B, C, z):
+        """What a selective scan and its gradient share of their inputs' checks: the shape,
+        and the pointers and row distances of x, delta, B, C and z."""
+        code, dtype = _format(x, "x")
+        tokens, D = x.shape
+        N = A.shape[-1]
+        if A.dim() != 2 or N < 1:
+            raise ValueError(f"A must have shape {(D, 'states')}, got {tuple(A.shape)}")
+        GN = B.shape[-1]
+        if GN < 1 or GN % N:
+            raise ValueError(f"B has {GN} columns, which are not whole heads of {N} states")
+        pz = (0, 0) if z is None else _row_tensor(z, dtype, "z", tokens, D)
+        return (code, dtype, tokens, D, N, GN // N, _row_tensor(x, dtype, "x", tokens, D),
+                _row_tensor(delta, dtype, "delta", tokens, D),
+                _row_tensor(B, dtype, "B", tokens, GN), _row_tensor(C, dtype, "C", tokens, GN), pz)
+
+    def _selective(self, what, x, delta, A, B, C, offsets, nseq, state, skip, z, delta_bias,
+                   softplus, out, last, marks):
+        code, dtype, tokens, D, N, G, px, pd, pb, pc, pz = self._selective_inputs(
+            x, delta, A, B, C, z)
+        poff, off_bytes = _offsets(offsets)
+        shape = (nseq, D, N)
+        if last is None:
+            last = x.new_empty(shape, dtype=torch.float32)
+        room = (-(-tokens // SELECTIVE_MARK), D, -(-N // 4) * 4)
+        if marks is True:
+            marks = x.new_empty(room, dtype=torch.float32)
+        elif marks is False:
+            marks = None
+        py = _row_tensor(_flat(out), dtype, "out", tokens, D)
+        f32 = torch.float32
+        rc = self._lib.polyglot_selective(self._h, SelectiveArgs.pack(
+            px[0], pd[0], pb[0], pc[0], pz[0], _block(A, f32, "A", (D, N)),
+            _vector(skip, f32, "skip", D), _vector(delta_bias, f32, "delta_bias", D),
+            _block(state, f32, "state", shape), poff, py[0], _block(last, f32, "last", shape),
+            _block(marks, f32, "marks", room), tokens, px[1], pd[1], pb[1], pc[1], pz[1], py[1],
+            nseq, D, N, G, code, off_bytes, softplus))
+        if rc != OK:
+            self._check(rc, what)
+        return out, last, marks
+
+    def selective_scan(self, x, delta, A, B, C, offsets=None, *, state=None, skip=None, z=None,
+                       delta_bias=None, softplus: bool = True, out=None, last=None, marks=False):
+        """The selective state space scan h_t = e^(s_t A) h_{t-1} + s_t x_t B_t, v_t = C_t h_t
+        + skip x_t, y = v or, with z, v z sigmoid(z), with s = softplus(delta + delta_bias)
+        (or delta + delta_bias), over the sequences of x as in recurrence.  A[D][states],
+        skip[D], delta_bias[D] and the states[nseq][D][states] are float32; B and C have
+        states columns, or as many for each of several heads of consecutive channels.
+        marks=True keeps what selective_backward needs.  Returns (y, last, marks)."""
+        if out is None:
+            out = _like(x)
+        return self._selective("selective_scan", _flat(x), _flat(delta), A, _flat(B), _flat(C),
+                               offsets, self._nseq(x, offsets), state, skip, _flat(z), delta_bias,
+                               softplus, out, last, marks)
+
+    def selective_step(self, x, delta, A, B, C, state=None, *, skip=None, z=None, delta_bias=None,
+                       softplus: bool = True, out=None, last=None):
+        """One token x[nseq][D] for each of nseq sequences whose states are
+        state[nseq][D][states].  Returns (y, the new states); last=state updates them in
+        place."""
+        if out is None:
+            out = _like(x)
+        return self._selective("selective_step", x, delta, A, B, C, None, x.shape[0], state, skip,
+                               z, delta_bias, softplus, out, last, None)[:2]
+
+    def selective_backward(self, x, delta, A, B, C, dy, marks, offsets=None, *, state=None,
+                           dlast=None, skip=None, z=None, delta_bias=None, softplus: bool = True,
+                           out: SelectiveGrads | None = None):
+        """The gradient of selective_scan, for its inputs, its marks and the gradients dy of y
+        and dlast of last, into the tensors of out where it has any.  Returns SelectiveGrads."""
+        nseq = self._nseq(x, offsets)
+        given = [None] * 9 if out is None else list(out)
+        f32 = torch.float32
+        for i, like in enumerate((x, delta, A, B, C, skip, z, delta_bias, state)):
+            if given[i] is None and like is not None:
+                given[i] = _like(like)
+            elif like is None and i in (5, 6, 7):
+                given[i] = None
+        g = SelectiveGrads(*given)
+        code, dtype, tokens, D, N, G, px, pd, pb, pc, pz = self._selective_inputs(
+            _flat(x), _flat(delta), A, _flat(B), _flat(C), _flat(z))
+        shape = (nseq, D, N)
+        poff, off_bytes = _offsets(offsets)
+        pdy = _row_tensor(_flat(dy), dtype, "dy", tokens, D)
+        gx = _row_tensor(_flat(g.x), dtype, "out.x", tokens, D)
+        gd = _row_tensor(_flat(g.delta), dtype, "out.delta", tokens, D)
+        gb = _row_tensor(_flat(g.B), dtype, "out.B", tokens, G * N)
+        gc = _row_tensor(_flat(g.C), dtype, "out.C", tokens, G * N)
+        gz = (0, 0) if z is None else _row_tensor(_flat(g.z), dtype, "out.z", tokens, D)
+        rc = self._lib.polyglot_selective_grad(self._h, SelectiveGradArgs.pack(
+            px[0], pd[0], pb[0], pc[0], pz[0], pdy[0], _block(A, f32, "A", (D, N)),
+            _vector(skip, f32, "skip", D), _vector(delta_bias, f32, "delta_bias", D),
+            _block(state, f32, "state", shape), _block(dlast, f32, "dlast", shape),
+            _block(marks, f32, "marks", (-(-tokens // SELECTIVE_MARK), D, -(-N // 4) * 4)), poff,
+            gx[0], gd[0], gb[0], gc[0], gz[0], _block(g.A, f32, "out.A", (D, N)),
+            _vector(g.skip, f32, "out.skip", D), _vector(g.delta_bias, f32, "out.delta_bias", D),
+            _block(g.state, f32, "out.state", shape), tokens, px[1], pd[1], pb[1], pc[1], pz[1],
+            pdy[1], gx[1], gd[1], gb[1], gc[1], gz[1], nseq, D, N, G, code, off_bytes, softplus))
+        if rc != OK:
+            self._check(rc, "selective_backward")
+        return g
+
+    def beam(self, scores, total, *, beams: int, picks: int, lse=None, finished=None, end: int = 0,
+             out=None):
+        """For every group of `beams` rows of scores[rows][V], the `picks` largest of
+        scores[r][v] + (total[r] - lse[r]) over its rows and words, of equal ones the first;
+        a row whose finished (int32) is set offers the word `end` with total[r] alone.
+        out: (parent, token, total) to write to.  Returns them, [groups][picks]: the picks'
+        rows of scores (int32, what reorder takes), words (int32, -1 where nothing is left) and
+        sums (float32)."""
+        code, dtype = _format(scores, "scores")
+        if scores.dim() != 2:
+            raise ValueError("scores must have two dimensions")
+        rows, V = scores.shape
+        if beams < 1 or rows % beams:
+            raise ValueError(f"{rows} rows are not whole groups of {beams} beams")
+        shape = (rows // beams, picks)
+        ps, ld = _row_tensor(scores, dtype, "scores", rows, V)
+        if out is None:
+            out = (scores.new_empty(shape, dtype=torch.int32),
+                   scores.new_empty(shape, dtype=torch.int32),
+                   scores.new_empty(shape, dtype=torch.float32))
+        rc = self._lib.polyglot_beam(self._h, BeamArgs.pack(
+            ps, _vector(total, torch.float32, "total", rows),
+            _vector(lse, torch.float32, "lse", rows),
+            _vector(finished, torch.int32, "finished", rows),
+            _block(out[0], torch.int32, "out[0]", shape),
+            _block(out[1], torch.int32, "out[1]", shape),
+            _block(out[2], torch.float32, "out[2]", shape), ld, shape[0], beams, V, picks, end,
+            code))
+        if rc != OK:
+            self._check(rc, "beam")
+        return out
+
+    def reorder(self, tensors, ids, outs=None):
+        """[t[ids] for t in tensors], all of them in one launch, bytes as they are: rows of
+        any shape and type, contiguous within a row; ids int32, of any shape.  outs: tensors
+        to write to, none of which may overlap an input.  Returns the list."""
+        rows = ids.numel()
+        pid = _vector(ids.view(-1), torch.int32, "ids", rows)
+        if outs is None:
+            outs = [t.new_empty((rows, *t.shape[1:])) for t in tensors]
+        if len(outs) != len(tensors):
+            raise ValueError(f"{len(tensors)} tensors, {len(outs)} outputs")
+        items = []
+        for t, o in zip(tensors, outs):
+            if not t.is_cuda or not o.is_cuda:
+                raise ValueError("tensors must be device (cuda) tensors")
+            if t.dim() < 1 or t.dtype is not o.dtype or o.shape != (rows, *t.shape[1:]):
+                raise ValueError(f"an output of {(rows, *t.shape[1:])} {t.dtype} is needed, got "
+                                 f"{tuple(o.shape)} {o.dtype}")
+            size = t.element_size()
+            width = t[0].numel() if t.shape[0] else 0
+            ld = []
+            for v in (t, o):
+                if not v.is_contiguous() and v.shape[0] and not v[0].is_contiguous():
+                    raise ValueError("rows must be contiguous")
+                ld.append(size * (v.stride(0) if v.shape[0] > 1 else width))
+            if not t.shape[0] and rows:
+                raise ValueError("a tensor without rows has none to give")
+            items.append(RowCopy.pack(t.data_ptr(), o.data_ptr(), size * width, *ld,
+                                      max(1, t.shape[0]), 0))
+        rc = self._lib.polyglot_reorder(self._h, b"".join(items), len(items), pid, rows)
+        if rc != OK:
+            self._check(rc, "reorder")
+        return outs
 
     def operator_times(self) -> dict:
         """kernel_times for the sequence operators: {operator: (total ms, launches)}."""

@@ -106,8 +106,9 @@ void free_all(polyglot_ctx* ctx) {
   ctx->ev_swap = nullptr;
   if (ctx->side) hipStreamDestroy(ctx->side);
   ctx->side = nullptr;
-  for (uint64_t* q : {ctx->op.rec.head, ctx->op.log_head})
+  for (uint64_t* q : {ctx->op.rec.head, ctx->op.log_head, ctx->op.beam_keys})
     if (q) hipFree(q);
+  if (ctx->op.sel) hipFree(ctx->op.sel);
   ctx->op = OpWorkspace{};
   for (void* q : ctx->allocs) hipFree(q);
   ctx->allocs.clear();

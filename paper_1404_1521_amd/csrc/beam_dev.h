@@ -1,0 +1,186 @@
+// The best continuations of groups of beams, and the reordering of states that they ask for.
+//
+// A key is a candidate's sum, as an unsigned number that ascends with it, over the
+// complement of its place: larger keys are larger sums, and of equal ones the lower place.
+// No two candidates have the same key, so that the picks do not depend on who finds them.
+//
+// A workgroup takes a part of a row, E words to a thread.  The k-th largest of the 256
+// threads' largest keys is a bound: the k picks are not below it, and only k threads hold
+// keys that are not, k E at most.  Those go to a list, whose k largest, found by counting
+// how many are larger, go out.  A second launch does the same over a group's parts, a
+// batch at a time.
+#pragma once
+#include "logits_dev.h"
+#include "operators.h"
+
+namespace pg {
+
+// -0 counts as +0; what is not to be picked (NaN, -infinity) has no key.
+__device__ __forceinline__ uint64_t beam_key(float v, uint32_t place) {
+  const uint32_t u = __float_as_uint(v + 0.f);
+  if (!(v > -__builtin_inff())) return 0;
+  return (uint64_t)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | ~place;
+}
+__device__ __forceinline__ float beam_value(uint64_t key) {
+  const uint32_t u = (uint32_t)(key >> 32);
+  return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+
+template <int E>
+struct BeamLds {
+  uint64_t top[kBlock];
+  uint64_t list[(kBeamPicks + 1) * E];
+  uint64_t bound;
+  int n;
+};
+
+// The k largest of the workgroup's keys (0: none), E to a thread, to out[k] in their order.
+template <int E>
+__device__ __forceinline__ void pick(const uint64_t (&key)[E], int k, BeamLds<E>& l, uint64_t* out) {
+  const int t = threadIdx.x;
+  uint64_t best = 0;
+#pragma unroll
+  for (int i = 0; i < E; ++i) best = key[i] > best ? key[i] : best;
+  l.top[t] = best;
+  if (t == 0) l.n = 0, l.bound = 0;
+  __syncthreads();
+  int above = 0;
+#pragma unroll 16
+  for (int i = 0; i < kBlock; ++i) above += l.top[i] > best;
+  if (above == k - 1 && best) l.bound = best;  // (one thread: keys differ)
+  __syncthreads();
+  const uint64_t bound = l.bound;
+  if (best >= bound && best) {
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (key[i] && key[i] >= bound) l.list[atomicAdd(&l.n, 1)] = key[i];
+  }
+  __syncthreads();
+  const int n = l.n;
+  for (int i = t; i < n; i += kBlock) {
+    const uint64_t own = l.list[i];
+    int rank = 0;
+    for (int j = 0; j < n && rank < k; ++j) rank += l.list[j] > own;
+    if (rank < k) out[rank] = own;
+  }
+  for (int i = n + t; i < k; i += kBlock) out[i] = 0;
+}
+
+// E words to a thread, in quads 4 * 256 words apart.
+template <class T, int E>
+__global__ __launch_bounds__(kBlock) void k_beam_parts(BeamCall c) {
+  __shared__ BeamLds<E> l;
+  const int t = threadIdx.x;
+  const int64_t r = blockIdx.x / c.parts;
+  const int part = (int)(blockIdx.x - r * c.parts);
+  uint64_t* out = c.keys + (int64_t)blockIdx.x * c.picks;
+  const float total = c.total[r];
+  if (c.finished && c.finished[r]) {  // its one candidate: nothing more is said
+    const bool here = c.end / (E * kBlock) == part;
+    for (int i = t; i < c.picks; i += kBlock)
+      out[i] = i == 0 && here ? beam_key(total, (uint32_t)c.end) : 0;
+    return;
+  }
+  const int v0 = part * (E * kBlock) + 4 * t;
+  const bool whole = (part + 1) * (E * kBlock) <= c.V;
+  const T* in = static_cast<const T*>(c.scores) + r * c.ld;
+  Quad<T> x[E / 4];
+#pragma unroll
+  for (int g = 0; g < E / 4; ++g) x[g] = row_quad<T>(in, v0 + g * 4 * kBlock, c.V, whole);
+  const float base = c.lse ? __fsub_rn(total, c.lse[r]) : total;
+  uint64_t key[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const int v = v0 + (i / 4) * 4 * kBlock + (i & 3);
+    key[i] = whole || v < c.V ? beam_key(__fadd_rn(x[i / 4].get(i & 3), base), (uint32_t)v) : 0;
+  }
+  pick<E>(key, c.picks, l, out);
+}
+
+// A workgroup for each group: its rows' parts, 256 E keys at a time beside the picks so far.
+template <int E>
+__global__ __launch_bounds__(kBlock) void k_beam_join(BeamCall c) {
+  __shared__ BeamLds<E + 1> l;
+  __shared__ uint64_t best[kBeamPicks];
+  const int t = threadIdx.x;
+  const int64_t row0 = (int64_t)blockIdx.x * c.beams;
+  const int64_t each = (int64_t)c.parts * c.picks, all = each * c.beams;
+  const uint64_t* in = c.keys + row0 * each;
+  if (t < kBeamPicks) best[t] = 0;
+  __syncthreads();
+  for (int64_t first = 0; first < all; first += E * kBlock) {
+    uint64_t key[E + 1];
+    bool any = false;
+    const uint64_t last = best[c.picks - 1];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int64_t at = first + i * kBlock + t;
+      key[i] = at < all ? in[at] : 0;
+      if (key[i]) {  // the place in a row becomes the place in the group
+        const uint32_t b = (uint32_t)(at / each);
+        key[i] = (key[i] & 0xffffffff00000000ull) | ~(~(uint32_t)key[i] + b * (uint32_t)c.V);
+        any |= key[i] > last;
+      }
+    }
+    key[E] = t < c.picks ? best[t] : 0;
+    if (!__syncthreads_or(any)) continue;
+    pick<E + 1>(key, c.picks, l, best);
+    __syncthreads();
+  }
+  if (t >= c.picks) return;
+  const int64_t o = (int64_t)blockIdx.x * c.picks + t;
+  const uint64_t key = best[t];
+  const uint32_t place = ~(uint32_t)key;
+  const uint32_t b = key ? place / (uint32_t)c.V : (uint32_t)(t % c.beams);
+  c.parent[o] = (int32_t)(row0 + b);
+  c.token[o] = key ? (int32_t)(place - b * (uint32_t)c.V) : -1;
+  c.out[o] = key ? beam_value(key) : -__builtin_inff();
+}
+
+// out[r] = in[ids[r]] for several tensors: a workgroup copies pieces of rows.
+__global__ __launch_bounds__(kBlock) void k_reorder(ReorderCall c) {
+  int64_t piece = blockIdx.x;
+  const int64_t all = c.first[c.count];
+  for (; piece < all; piece += gridDim.x) {
+    int k = 0;
+    while (k + 1 < c.count && piece >= c.first[k + 1]) ++k;
+    const RowCopy& m = c.item[k];
+    const int64_t local = piece - c.first[k];
+    const int64_t r = local / m.pieces;
+    const int64_t from = (local - r * m.pieces) * kReorderPiece;
+    const int64_t bytes = min((int64_t)kReorderPiece, m.row_bytes - from);
+    const int32_t id = c.ids[r];
+    if ((uint32_t)id >= (uint32_t)m.in_rows) {
+      if (threadIdx.x == 0) atomicOr(c.flag, kFlagBadId);
+      continue;
+    }
+    const char* in = m.in + id * m.ld_in + from;
+    char* out = m.out + r * m.ld_out + from;
+    const int t = threadIdx.x;
+    if (m.unit == 16) {
+      const int n = (int)(bytes / 16);
+      uint4 v[kReorderPiece / (16 * kBlock)];
+#pragma unroll
+      for (int i = 0; i < kReorderPiece / (16 * kBlock); ++i)
+        v[i] = t + i * kBlock < n ? reinterpret_cast<const uint4*>(in)[t + i * kBlock] : uint4{};
+#pragma unroll
+      for (int i = 0; i < kReorderPiece / (16 * kBlock); ++i)
+        if (t + i * kBlock < n) reinterpret_cast<uint4*>(out)[t + i * kBlock] = v[i];
+    } else if (m.unit == 4) {
+      const int n = (int)(bytes / 4);
+#pragma unroll 4
+      for (int i = t; i < n; i += kBlock)
+        reinterpret_cast<uint32_t*>(out)[i] = reinterpret_cast<const uint32_t*>(in)[i];
+    } else if (m.unit == 2) {
+      const int n = (int)(bytes / 2);
+#pragma unroll 4
+      for (int i = t; i < n; i += kBlock)
+        reinterpret_cast<uint16_t*>(out)[i] = reinterpret_cast<const uint16_t*>(in)[i];
+    } else {
+#pragma unroll 4
+      for (int i = t; i < (int)bytes; i += kBlock) out[i] = in[i];
+    }
+  }
+}
+
+}  // namespace pg

@@ -36,6 +36,13 @@ struct OpWorkspace {
   ScanSpace rec;
   int log_rows = 0, log_V = 0;
   uint64_t *log_head = nullptr, *log_words = nullptr;  // one block: counters, words
+  int64_t sel_tokens = 0;
+  int sel_D = 0, sel_states = 0;
+  float* sel = nullptr;  // one block: the scan's parts, the convolution's
+  SelSpace sel_space{};
+  float* conv_part = nullptr;
+  int beam_rows = 0, beam_V = 0, beam_picks = 0;
+  uint64_t* beam_keys = nullptr;
 };
 
 // A kernel's event pairs that are counted and not yet asked for.

@@ -1,5 +1,5 @@
 // Argument blocks and launches of the sequence operators (dropout, gated
-// linear recurrence, scores).
+// linear recurrence, scores; convolution, selective scan, beams, reordering).
 #pragma once
 #include "polyglot.h"
 
@@ -71,6 +71,102 @@ struct LogitsCall {
   int64_t stride;        // parts that a row has room for
 };
 
+// Packed sequences of a call.
+struct Packed {
+  const void* offsets;  // [nseq + 1] of offset_bytes each, or null: tokens / nseq tokens each
+  uint32_t* flag;
+  int offset_bytes, tokens, nseq;
+};
+
+// The selective scan and its gradient (the gradient's in the second half).
+struct SelCall {
+  const void *x, *delta, *B, *C, *z;
+  const float *A, *skip, *bias, *h0;
+  void* y;
+  float *last, *marks;
+  const void* dy;
+  const float* dlast;
+  void *dx, *ddelta, *dB, *dC, *dz;
+  float *dA, *dskip, *dbias, *dh0;
+  int64_t ld_x, ld_delta, ld_B, ld_C, ld_z, ld_y, ld_dy, ld_dx, ld_ddelta, ld_dB, ld_dC, ld_dz;
+  Packed seqs;
+  int D, N, groups, softplus;
+};
+
+constexpr int kSelectiveTile = 16;  // POLYGLOT_SELECTIVE_MARK
+// What a range passes on: nothing (a sequence ends or starts at its end), the state of a
+// sequence that starts in it, or its own carry too.
+constexpr uint32_t kSelNone = 0, kSelClosed = 1, kSelOpen = 2;
+
+// How a selective scan is cut: a workgroup for each range of tokens and block of channels.
+struct SelPlan {
+  int range, ranges;       // tokens of a range
+  int blocks, all_blocks;  // of a head's channels, of all
+  int NM;                  // places of a mark's row
+  float* states;           // [ranges][D][places] what a range passes on
+  float* sums;             // [ranges][D] the sum of its steps
+  uint32_t* info;          // [ranges]
+  float* part_a;           // [ranges][D][places] dA
+  float* part_s;           // [ranges][2][D] dskip and the bias's gradient
+  float* part_bc;          // [blocks][tokens][groups][2][N] dB and dC
+};
+struct SelRoom {  // values of each
+  size_t states, sums, info, part_s, part_bc;
+};
+struct SelSpace {
+  float *states, *sums, *part_a, *part_s, *part_bc;
+  uint32_t* info;
+};
+
+// The short causal convolution and its gradient.
+struct ConvCall {
+  const void *x, *state;
+  const float *weight, *bias;
+  void *y, *last;
+  const void *dy, *dlast;
+  void *dx, *dstate;
+  float *dweight, *dbias;
+  int64_t ld_x, ld_y, ld_dy, ld_dx;
+  Packed seqs;
+  int D, silu;
+  int lanes_log2, blocks;  // lanes of a row of threads, four channels each; rows of blocks
+  int tiles, groups;       // of tokens; the gradient's workgroups for a row of blocks
+  float* part;             // [groups][K + 1][D] sums of the weights' and the bias's gradients
+};
+constexpr int kConvMaxK = 8;
+constexpr int kConvRun = 16;           // tokens of a thread
+constexpr int kConvMinLanes = 8;
+constexpr int kConvWorkgroups = 2048;  // of a gradient, where the tokens give as many
+
+struct BeamCall {
+  const void* scores;
+  const float *total, *lse;
+  const int32_t* finished;
+  int32_t *parent, *token;
+  float* out;
+  uint64_t* keys;  // [rows][parts][picks]
+  int64_t ld;
+  int groups, beams, V, picks, end, parts;
+};
+constexpr int kBeamPicks = 64;   // most
+constexpr int kBeamMinPart = 1024;  // words of the shortest part
+
+constexpr int kReorderItems = 32;            // tensors of a launch
+constexpr int kReorderPiece = 16 * 4 * kBlock;  // bytes of a workgroup's copy
+struct RowCopy {
+  const char* in;
+  char* out;
+  int64_t row_bytes, ld_in, ld_out, pieces;
+  int in_rows, unit;  // bytes that every address and length is a multiple of
+};
+struct ReorderCall {
+  RowCopy item[kReorderItems];
+  int64_t first[kReorderItems + 1];  // piece of each tensor; all pieces behind the last
+  const int32_t* ids;
+  uint32_t* flag;
+  int rows, count;
+};
+
 // Calls f with a value of the storage type `dtype` (POLYGLOT_F32, _BF16, _F16).
 template <class F>
 hipError_t by_format(int dtype, F f) {
@@ -87,5 +183,19 @@ hipError_t launch_recurrence(const RecCall& c, int dtype, int form, bool grad,
 ScanSpace scan_space(int64_t tokens, int D);
 hipError_t launch_logits(LogitsCall c, const Launch& L);
 constexpr int kLogitsMinTile = 1024;  // words of the shortest part
+
+hipError_t launch_selective(const SelCall& c, int dtype, SelSpace space, const Launch& L);
+hipError_t launch_selective_grad(const SelCall& c, int dtype, SelSpace space, const Launch& L);
+hipError_t launch_selective_step(const SelCall& c, int dtype, const Launch& L);
+// The room that selective scans of up to `tokens` tokens, D channels and N states need.
+SelRoom selective_room(int64_t tokens, int D, int N);
+
+hipError_t launch_convolution(ConvCall c, int K, int dtype, const Launch& L);
+hipError_t launch_convolution_step(ConvCall c, int K, int dtype, const Launch& L);
+hipError_t launch_convolution_grad(ConvCall c, int K, int dtype, const Launch& L);
+// Floats of ConvCall::part for gradients of up to D channels.
+size_t convolution_room(int D);
+hipError_t launch_beam(BeamCall c, int dtype, const Launch& L);
+hipError_t launch_reorder(const ReorderCall& c, const Launch& L);
 
 }  // namespace pg

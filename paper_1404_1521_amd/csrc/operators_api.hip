@@ -3,17 +3,12 @@
 #include "polyglot.h"
 
 #include <cmath>
-#include <initializer_list>
 
-#include "context.h"
-#include "operators.h"
+#include "entry.h"
 
 using namespace pg;
 
 namespace {
-
-// Kernel ids of these operators among a context's timing marks.
-constexpr int kOpKernels = POLYGLOT_NKERNELS;
 
 // Most parts of a row of V scores.
 int64_t logits_parts(int V) { return (V + (int64_t)kLogitsMinTile - 1) / kLogitsMinTile; }
@@ -36,30 +31,6 @@ hipError_t heads(polyglot_ctx* ctx, uint64_t** head, size_t lines, size_t words)
   if (e == hipSuccess) *head = p;
   else (void)hipFree(p);
   return e;
-}
-
-// Runs an entry point's body; nothing that it throws (a message that finds no
-// memory) passes the C boundary.
-template <class F>
-int entry(F f) noexcept {
-  try {
-    return f();
-  } catch (...) {
-    return POLYGLOT_EHIP;
-  }
-}
-
-size_t size_of(int dtype) { return dtype == POLYGLOT_F32 ? 4 : 2; }
-
-bool format_ok(int dtype) {
-  return dtype == POLYGLOT_F32 || dtype == POLYGLOT_BF16 || dtype == POLYGLOT_F16;
-}
-
-bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
-
-// Rows of `width` elements `ld` apart whose last byte's offset fits 63 bits.
-bool rows_ok(int64_t ld, int64_t rows, int64_t width) {
-  return ld >= width && (rows == 0 || ld <= (INT64_MAX / 8) / rows);
 }
 
 }  // namespace
@@ -141,25 +112,6 @@ RecCall recurrence_call(polyglot_ctx* ctx, const A& a) {
   c.group = a.group;
   c.offset_bytes = a.offset_bytes;
   return c;
-}
-
-// A tensor of [tokens][width] elements of `size` bytes.
-struct Rows {
-  const void* p;
-  int64_t ld;
-  int width;
-};
-
-int check_rows(polyglot_ctx* ctx, int64_t tokens, size_t size, std::initializer_list<Rows> all,
-               const std::string& what) {
-  if (tokens == 0) return POLYGLOT_OK;
-  for (const Rows& r : all) {
-    if (!r.p) return fail(ctx, POLYGLOT_ENULL, what + ": NULL pointer");
-    if (!rows_ok(r.ld, tokens, r.width))
-      return fail(ctx, POLYGLOT_EINVAL, what + ": rows closer than their width, or too many");
-    if (!aligned(r.p, size)) return fail(ctx, POLYGLOT_EINVAL, what + ": misaligned pointer");
-  }
-  return POLYGLOT_OK;
 }
 
 }  // namespace

@@ -1,0 +1,448 @@
+// The gradient of the selective scan.  With v' the gradient of v and mu what comes back
+// from the token after (dlast after a sequence's last one):
+//   lambda = v' C + mu,  mu <- a lambda,  q = a lambda h_{t-1}
+//   dC = sum_c v' h, dB = sum_c lambda D x, dA = sum_t D q
+//   d(D) = sum_n q A + x e,  dx = D e + skip v',  e = sum_n lambda B
+//
+// The ranges are those of the forward pass, taken from their ends.  A tile starts from the
+// mark that the forward pass left, the states before its first token, goes through its 16
+// tokens in two halves, each once forward, with decays and states kept in registers, and
+// once back.  The sums over the states go over LN lanes by DPP moves; those over the
+// channels over the other lanes, two values at a time by half-wave and row swaps, then over
+// the waves in LDS and over the workgroups in a last launch, always in the same order.
+#pragma once
+#include "selective_dev.h"
+
+namespace pg {
+
+// Eight values of each lane summed over the 64 / LN lanes of the same states: lane l keeps
+// value 4 (l / 32) + 2 (l / 16 % 2) + {0, 1}.
+template <int LN>
+__device__ __forceinline__ void sum_channels(const float (&v)[8], float (&out)[2]) {
+  float u[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 4]),
+                                                    false, false);
+    u[i] = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(u[i]), __float_as_uint(u[i + 2]),
+                                                    false, false);
+    out[i] = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    if constexpr (LN <= 8) out[i] += lane_moved<0x128>(out[i]);  // row_ror:8
+    if constexpr (LN <= 4) out[i] += lane_moved<0x124>(out[i]);  // row_ror:4
+    if constexpr (LN <= 2) out[i] += lane_moved<0x122>(out[i]);  // row_ror:2
+  }
+}
+
+template <class T>
+__device__ __forceinline__ float gated(float dy, const T* z, float& zv, float& sg) {
+  zv = load_one(z);
+  sg = sigmoid(zv);
+  return dy * zv * sg;
+}
+
+// A tile's steps, D x (if x) and v' in LDS.  Tokens past the tile's and channels past the
+// workgroup's: zeros, which change nothing.
+template <class T, int LN, bool X>
+__device__ __forceinline__ void stage_grad(const SelCall& c, const SelPlace<LN>& w, int t0, int count,
+                                           const float (&bias)[4], float* step, float* dx,
+                                           float* dv) {
+  using S = SelShape<LN>;
+  const T* x = static_cast<const T*>(c.x) + w.q0;
+  const T* delta = static_cast<const T*>(c.delta) + w.q0;
+  const T* dy = static_cast<const T*>(c.dy) + w.q0;
+  const T* z = static_cast<const T*>(c.z) + w.q0;
+#pragma unroll
+  for (int e = 0; e < S::EACH; ++e) {
+    const int i = threadIdx.x + e * kBlock, k = i / S::QUADS;
+    if (k >= kSelTile) continue;
+    float d[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f}, g[4] = {0.f, 0.f, 0.f, 0.f};
+    if (k < count && w.qn > 0) {
+      const int64_t row = t0 + (int64_t)k;
+      const Quad<T> raw = some_quad(delta + row * c.ld_delta, w.qn);
+      const Quad<T> gy = some_quad(dy + row * c.ld_dy, w.qn);
+      Quad<T> xv{}, zv{};
+      if (X) xv = some_quad(x + row * c.ld_x, w.qn);
+      if (c.z) zv = some_quad(z + row * c.ld_z, w.qn);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (j >= w.qn) continue;
+        d[j] = step_of(raw.get(j), bias[j], c.softplus);
+        if (X) u[j] = d[j] * xv.get(j);
+        g[j] = gy.get(j);
+        if (c.z) g[j] *= zv.get(j) * sigmoid(zv.get(j));
+      }
+    }
+    st4(step + i * 4, f4{d[0], d[1], d[2], d[3]});
+    if (X) st4(dx + i * 4, f4{u[0], u[1], u[2], u[3]});
+    st4(dv + i * 4, f4{g[0], g[1], g[2], g[3]});
+  }
+}
+
+// What comes back through each range that a sequence runs into, from that sequence's end in
+// it or from nothing.
+template <class T, int LN>
+__global__ __launch_bounds__(kBlock) void k_selective_grad_ends(SelCall c, SelPlan p) {
+  using S = SelShape<LN>;
+  __shared__ SelLds<LN> s;
+  const int t = threadIdx.x;
+  const int range = blockIdx.x / p.all_blocks, block = blockIdx.x % p.all_blocks;
+  const SelPlace<LN> w(c, p, block);
+  const int lo = range * p.range, hi = min(lo + p.range, c.seqs.tokens);
+  const int to = lo < hi ? run_stop(c.seqs, lo, hi) : lo;
+  int seq = -1;  // the sequence that ends at `to`, if one does
+  if (to > lo) {
+    const int i = first_place(c.seqs, to);
+    if (i > 0 && i <= c.seqs.nseq && place_of(c.seqs, i) == to) seq = i - 1;
+  }
+  if (t == 0 && block == 0) p.info[range] = to == lo ? kSelNone : seq >= 0 ? kSelClosed : kSelOpen;
+  if (to == lo) return;
+
+  float A[2][4], mu[2][4], sum[2] = {0.f, 0.f};
+  load_rates(c, w, A);
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    const float* row = seq >= 0 && c.dlast && w.lane_c + r < w.nc
+                           ? c.dlast + ((int64_t)seq * c.D + w.c0 + w.lane_c + r) * c.N
+                           : nullptr;
+    load_states(row, c.N, w.nl, mu[r]);
+  }
+  float bias[4] = {0.f, 0.f, 0.f, 0.f};
+  if (c.bias)
+    for (int k = 0; k < w.qn; ++k) bias[k] = c.bias[w.q0 + k];
+  for (int tile = (to - 1 - lo) / kSelTile; tile >= 0; --tile) {
+    const int t0 = lo + tile * kSelTile, count = min(kSelTile, to - t0);
+    __syncthreads();
+    stage_grad<T, LN, false>(c, w, t0, count, bias, s.step, nullptr, s.dx);
+    stage_states<T, LN>(static_cast<const T*>(c.C), c.ld_C, t0, count, w.head, c.N, s.C);
+    __syncthreads();
+#pragma unroll 4
+    for (int k = kSelTile - 1; k >= 0; --k) {
+      const float2 d = *reinterpret_cast<const float2*>(s.step + k * S::CB + w.lane_c);
+      const float2 g = *reinterpret_cast<const float2*>(s.dx + k * S::CB + w.lane_c);
+      const f4 C = ld4(s.C + k * S::NP + 4 * w.nl);
+      const float dd[2] = {d.x, d.y}, gg[2] = {g.x, g.y};
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        sum[r] += dd[r];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          mu[r][j] = exp2_fast(dd[r] * A[r][j]) * __fmaf_rn(gg[r], C[j], mu[r][j]);
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    if (w.lane_c + r >= w.nc) continue;
+    const int64_t at = (int64_t)range * c.D + w.c0 + w.lane_c + r;
+    st4(p.states + at * S::NP + 4 * w.nl, f4{mu[r][0], mu[r][1], mu[r][2], mu[r][3]});
+    if (w.nl == 0) p.sums[at] = sum[r];
+  }
+}
+
+// LDS of the gradient: what comes in and goes out of each token and channel (D x makes
+// room for e, v' for v), the tile's B and C, the waves' sums for dB and dC.
+template <int LN>
+struct alignas(16) SelGradLds {
+  using S = SelShape<LN>;
+  SelLds<LN> in;
+  float dv[kSelTile * S::CB], dstep[kSelTile * S::CB];
+  float part[kWavesPerBlock][kSelTile][2][S::NP];
+  int list[kBlock];
+};
+
+template <class T, int LN>
+__global__ __launch_bounds__(kBlock, 2) void k_selective_grad(SelCall c, SelPlan p) {
+  using S = SelShape<LN>;
+  constexpr int H = kSelTile / 2;
+  __shared__ SelGradLds<LN> g;
+  SelLds<LN>& s = g.in;
+  const int t = threadIdx.x, lane = t & (kWave - 1), wave = t / kWave;
+  const int range = blockIdx.x / p.all_blocks, block = blockIdx.x % p.all_blocks;
+  const SelPlace<LN> w(c, p, block);
+  const int lo = range * p.range, hi = min(lo + p.range, c.seqs.tokens);
+
+  const auto row_of = [&](const float* base, int i, int r) -> float* {
+    if (!base || w.lane_c + r >= w.nc) return nullptr;
+    return const_cast<float*>(base) + ((int64_t)i * c.D + w.c0 + w.lane_c + r) * c.N;
+  };
+  check_places(c.seqs, range, p.ranges, c.dh0 != nullptr, g.list, [&](int i) {
+    for (int r = 0; r < 2; ++r) {
+      float v[4];
+      load_states(row_of(c.dlast, i, r), c.N, w.nl, v);
+      if (float* to = row_of(c.dh0, i, r)) store_states(to, c.N, w.nl, v);
+    }
+  });
+
+  float A[2][4], dA[2][4], mu[2][4];
+  load_rates(c, w, A);
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) dA[r][j] = mu[r][j] = 0.f;
+  float bias[4] = {0.f, 0.f, 0.f, 0.f}, skip[4] = {0.f, 0.f, 0.f, 0.f};
+  float dskip[4] = {0.f, 0.f, 0.f, 0.f}, dbias[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int k = 0; k < w.qn; ++k) {
+    if (c.bias) bias[k] = c.bias[w.q0 + k];
+    if (c.skip) skip[k] = c.skip[w.q0 + k];
+  }
+
+  const int tiles = lo < hi ? ceil_div(hi - lo, kSelTile) : 0;
+  for (int tile = tiles - 1; tile >= 0; --tile) {
+    const int t0 = lo + tile * kSelTile, count = min(kSelTile, hi - t0);
+    stage_grad<T, LN, true>(c, w, t0, count, bias, s.step, s.dx, g.dv);
+    stage_states<T, LN>(static_cast<const T*>(c.B), c.ld_B, t0, count, w.head, c.N, s.B);
+    stage_states<T, LN>(static_cast<const T*>(c.C), c.ld_C, t0, count, w.head, c.N, s.C);
+    if (t < kWave)
+      mark_places(c.seqs, t0, t0 + count, kSelTile, first_place(c.seqs, t0), s.start, s.stop);
+    __syncthreads();
+    if (tile == tiles - 1 && s.stop[count - 1] < 0 && hi < c.seqs.tokens)
+      carry_into<LN>(c, p, range, -1, w, A, mu);
+
+    // the states before the first half, and before the second one
+    float first[2][4], h[2][4];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      f4 m = kZero4;
+      if (w.lane_c + r < w.nc && 4 * w.nl < c.N)
+        m = ld4(c.marks + ((int64_t)(t0 / kSelTile) * c.D + w.c0 + w.lane_c + r) * p.NM + 4 * w.nl);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) first[r][j] = h[r][j] = m[j];
+    }
+    // one token forward; decays into a
+    const auto forward = [&](int k, float (&a)[2][4]) {
+      const int from = __builtin_amdgcn_readfirstlane(s.start[k]);
+      if (from >= 0) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) load_states(row_of(c.h0, from, r), c.N, w.nl, h[r]);
+      }
+      const float2 d = *reinterpret_cast<const float2*>(s.step + k * S::CB + w.lane_c);
+      const float2 u = *reinterpret_cast<const float2*>(s.dx + k * S::CB + w.lane_c);
+      const f4 B = ld4(s.B + k * S::NP + 4 * w.nl);
+      const float dd[2] = {d.x, d.y}, uu[2] = {u.x, u.y};
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          a[r][j] = exp2_fast(dd[r] * A[r][j]);
+          h[r][j] = __fmaf_rn(a[r][j], h[r][j], uu[r] * B[j]);
+        }
+    };
+    const bool second = count > H;
+    if (second) {
+      for (int k = 0; k < H; ++k) {
+        float a[2][4];
+        forward(k, a);
+      }
+    }
+    for (int half = second; half >= 0; --half) {
+      const int base = half * H;
+      float before[2][4], a[H][2][4], hs[H][2][4];
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) before[r][j] = h[r][j] = half ? h[r][j] : first[r][j];
+#pragma unroll
+      for (int i = 0; i < H; ++i) {
+        forward(base + i, a[i]);
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) hs[i][r][j] = h[r][j];
+      }
+#pragma unroll
+      for (int i = H - 1; i >= 0; --i) {
+        const int k = base + i;
+        const int to = __builtin_amdgcn_readfirstlane(s.stop[k]);
+        if (to >= 0) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) load_states(row_of(c.dlast, to, r), c.N, w.nl, mu[r]);
+        }
+        const int from = __builtin_amdgcn_readfirstlane(s.start[k]);
+        float hp[2][4];
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) hp[r][j] = i ? hs[i ? i - 1 : 0][r][j] : before[r][j];
+        if (from >= 0) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) load_states(row_of(c.h0, from, r), c.N, w.nl, hp[r]);
+        }
+        const float2 d = *reinterpret_cast<const float2*>(s.step + k * S::CB + w.lane_c);
+        const float2 u = *reinterpret_cast<const float2*>(s.dx + k * S::CB + w.lane_c);
+        const float2 dv = *reinterpret_cast<const float2*>(g.dv + k * S::CB + w.lane_c);
+        const f4 B = ld4(s.B + k * S::NP + 4 * w.nl), C = ld4(s.C + k * S::NP + 4 * w.nl);
+        const float dd[2] = {d.x, d.y}, uu[2] = {u.x, u.y}, vv[2] = {dv.x, dv.y};
+        float both[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};  // dB, dC
+        float e[2], ds[2], v[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          e[r] = ds[r] = v[r] = 0.f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float lam = __fmaf_rn(vv[r], C[j], mu[r][j]);
+            both[j] = __fmaf_rn(lam, uu[r], both[j]);
+            both[4 + j] = __fmaf_rn(vv[r], hs[i][r][j], both[4 + j]);
+            e[r] = __fmaf_rn(lam, B[j], e[r]);
+            v[r] = __fmaf_rn(C[j], hs[i][r][j], v[r]);
+            mu[r][j] = lam * a[i][r][j];
+            const float q = mu[r][j] * hp[r][j];
+            ds[r] = __fmaf_rn(q, A[r][j], ds[r]);
+            dA[r][j] = __fmaf_rn(q, dd[r], dA[r][j]);
+          }
+          e[r] = sum_states<LN>(e[r]);
+          ds[r] = sum_states<LN>(ds[r]);
+          v[r] = sum_states<LN>(v[r]);
+        }
+        if (w.nl == 0) {
+          *reinterpret_cast<float2*>(s.dx + k * S::CB + w.lane_c) = float2{e[0], e[1]};
+          *reinterpret_cast<float2*>(g.dstep + k * S::CB + w.lane_c) = float2{ds[0], ds[1]};
+          *reinterpret_cast<float2*>(g.dv + k * S::CB + w.lane_c) = float2{v[0], v[1]};
+        }
+        float pair[2];
+        sum_channels<LN>(both, pair);
+        if (lane % 16 < LN)
+          *reinterpret_cast<float2*>(&g.part[wave][k][lane / 32][4 * w.nl + 2 * (lane / 16 % 2)]) =
+              float2{pair[0], pair[1]};
+        if (from >= 0) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            if (float* row = row_of(c.dh0, from, r)) store_states(row, c.N, w.nl, mu[r]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mu[r][j] = 0.f;
+          }
+        }
+      }
+    }
+    __syncthreads();
+    const T* x = static_cast<const T*>(c.x) + w.q0;
+    const T* delta = static_cast<const T*>(c.delta) + w.q0;
+    const T* dy = static_cast<const T*>(c.dy) + w.q0;
+    const T* z = static_cast<const T*>(c.z) + w.q0;
+#pragma unroll
+    for (int el = 0; el < S::EACH; ++el) {
+      const int i = t + el * kBlock, k = i / S::QUADS;
+      if (k >= count || w.qn <= 0) continue;
+      const int64_t row = t0 + (int64_t)k;
+      const Quad<T> xv = some_quad(x + row * c.ld_x, w.qn);
+      const Quad<T> raw = some_quad(delta + row * c.ld_delta, w.qn);
+      const Quad<T> gy = some_quad(dy + row * c.ld_dy, w.qn);
+      const f4 e = ld4(s.dx + i * 4), st = ld4(s.step + i * 4), ds = ld4(g.dstep + i * 4);
+      const f4 sv = ld4(g.dv + i * 4);
+      Quad<T> zv{};
+      if (c.z) zv = some_quad(z + row * c.ld_z, w.qn);
+      float ox[4], od[4], oz[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float xj = xv.get(j);
+        float gv = gy.get(j);
+        oz[j] = 0.f;
+        if (c.z) {
+          const float zj = zv.get(j), sg = sigmoid(zj);
+          const float v = c.skip ? __fmaf_rn(skip[j], xj, sv[j]) : sv[j];
+          oz[j] = gv * v * (sg * __fmaf_rn(zj, 1.f - sg, 1.f));
+          gv *= zj * sg;
+        }
+        ox[j] = st[j] * e[j];
+        if (c.skip) ox[j] = __fmaf_rn(skip[j], gv, ox[j]);
+        od[j] = __fmaf_rn(xj, e[j], kLn2 * ds[j]);
+        if (c.softplus) od[j] *= sigmoid(raw.get(j) + bias[j]);
+        if (j < w.qn) {
+          dskip[j] = __fmaf_rn(gv, xj, dskip[j]);
+          dbias[j] += od[j];
+        }
+      }
+      put_quad(static_cast<T*>(c.dx) + w.q0 + row * c.ld_dx, ox, w.qn);
+      put_quad(static_cast<T*>(c.ddelta) + w.q0 + row * c.ld_ddelta, od, w.qn);
+      if (c.z) put_quad(static_cast<T*>(c.dz) + w.q0 + row * c.ld_dz, oz, w.qn);
+    }
+    for (int i = t; i < count * 2 * S::NP; i += kBlock) {
+      const int k = i / (2 * S::NP), which = i / S::NP % 2, n = i % S::NP;
+      if (n >= c.N) continue;
+      float v = g.part[0][k][which][n];
+#pragma unroll
+      for (int j = 1; j < kWavesPerBlock; ++j) v += g.part[j][k][which][n];
+      const int64_t row = t0 + (int64_t)k;
+      if (p.blocks == 1) {
+        T* to = which ? static_cast<T*>(c.dC) + row * c.ld_dC : static_cast<T*>(c.dB) + row * c.ld_dB;
+        to[(int64_t)w.head * c.N + n] = Elem<T>::put(settled(v));
+      } else {
+        const int64_t place = (((int64_t)(block % p.blocks) * c.seqs.tokens + row) * c.groups + w.head) * 2;
+        p.part_bc[(place + which) * c.N + n] = v;
+      }
+    }
+  }
+
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+    if (w.lane_c + r < w.nc)
+      st4(p.part_a + ((int64_t)range * c.D + w.c0 + w.lane_c + r) * S::NP + 4 * w.nl,
+          f4{dA[r][0], dA[r][1], dA[r][2], dA[r][3]});
+  // the threads of a quad of channels, in order
+  __syncthreads();
+  constexpr int kBusy = kSelTile * S::QUADS < kBlock ? kSelTile * S::QUADS : kBlock;
+  if (t < kBusy) {
+    st4(s.step + t * 4, f4{dskip[0], dskip[1], dskip[2], dskip[3]});
+    st4(s.dx + t * 4, f4{dbias[0], dbias[1], dbias[2], dbias[3]});
+  }
+  __syncthreads();
+  for (int i = t; i < w.nc; i += kBlock) {
+    float a = 0.f, b = 0.f;
+    for (int j = 0; j < kBusy / S::QUADS; ++j) {
+      a += s.step[j * S::CB + i];
+      b += s.dx[j * S::CB + i];
+    }
+    p.part_s[((int64_t)range * 2) * c.D + w.c0 + i] = a;
+    p.part_s[((int64_t)range * 2 + 1) * c.D + w.c0 + i] = b;
+  }
+}
+
+// The sums over the ranges (dA, dskip, the bias's) and over the workgroups of a head's
+// channels (dB, dC).  64 sums to a workgroup, a quarter of the ranges to each thread.
+template <class T>
+__global__ __launch_bounds__(kBlock) void k_selective_sums(SelCall c, SelPlan p, int NP, int param_blocks) {
+  __shared__ float part[kBlock];
+  const int t = threadIdx.x;
+  if ((int)blockIdx.x < param_blocks) {
+    const int64_t o = (int64_t)blockIdx.x * kWave + t % kWave, n_a = (int64_t)c.D * c.N;
+    const float* from = nullptr;
+    int64_t ld = 0;
+    float* to = nullptr;
+    if (o < n_a) {
+      from = p.part_a + o / c.N * NP + o % c.N;
+      ld = (int64_t)c.D * NP;
+      to = c.dA + o;
+    } else if (o < n_a + 2 * (int64_t)c.D) {
+      const int64_t i = o - n_a;
+      from = p.part_s + i;
+      ld = 2 * (int64_t)c.D;
+      if (i < c.D) to = c.dskip ? c.dskip + i : nullptr;
+      else to = c.dbias ? c.dbias + i - c.D : nullptr;
+    }
+    float v = 0.f;
+    if (from) {
+#pragma unroll 8
+      for (int r = t / kWave; r < p.ranges; r += kWavesPerBlock) v += from[r * ld];
+    }
+    part[t] = v;
+    __syncthreads();
+    if (t < kWave && to) *to = (part[t] + part[t + 64]) + (part[t + 128] + part[t + 192]);
+    return;
+  }
+  const int64_t width = (int64_t)c.groups * 2 * c.N, all = width * c.seqs.tokens;
+  for (int64_t i = ((int64_t)blockIdx.x - param_blocks) * kBlock + t; i < all;
+       i += (int64_t)(gridDim.x - param_blocks) * kBlock) {
+    float v = 0.f;
+#pragma unroll 8
+    for (int b = 0; b < p.blocks; ++b) v += p.part_bc[b * all + i];
+    const int64_t row = i / width;
+    const int rest = (int)(i % width), head = rest / (2 * c.N), which = rest / c.N % 2, n = rest % c.N;
+    T* to = which ? static_cast<T*>(c.dC) + row * c.ld_dC : static_cast<T*>(c.dB) + row * c.ld_dB;
+    to[(int64_t)head * c.N + n] = Elem<T>::put(settled(v));
+  }
+}
+
+}  // namespace pg

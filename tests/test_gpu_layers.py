@@ -1,0 +1,720 @@
+"""The short causal convolution, the selective scan, their gradients, the selection over
+beams and the reordering, against plain implementations in 64 bits (tests/layer_refs.py,
+which also bounds what 32-bit arithmetic may be off), through the public entry points."""
+import math
+import os
+import sys
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import layer_refs as ref  # noqa: E402
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def pg():
+    import paper_1404_1521_amd as pg
+    return pg
+
+
+@pytest.fixture(scope="module")
+def ctx(pg):
+    c = pg.Context(1000, 16, 5, 8, max_batch=1)
+    c.reserve_selective(40_000, 1100, 64)
+    c.reserve_beam(512, 1_000_003, 64)
+    c.reserve_logits(64, 5000)
+    yield c
+    assert c.status() == pg.OK
+    c.close()
+
+
+def normal(gen, *shape, dtype="f32", std=1.0):
+    """Values of the storage type, on the CPU."""
+    return (torch.randn(*shape, generator=gen) * std).to(DT[dtype])
+
+
+def cuda(t):
+    return None if t is None else t.cuda()
+
+
+def wide(t):
+    return None if t is None else t.double().cpu()
+
+
+def strided(t, pad, shift):
+    """t's values in rows t.shape[1] + pad apart that start `shift` elements in."""
+    n, w = t.shape
+    buf = torch.full((n * (w + pad) + shift + 8,), 77.0, dtype=t.dtype, device="cuda")
+    view = buf[shift:shift + n * (w + pad)].view(n, w + pad)[:, :w]
+    view.copy_(t)
+    return view
+
+
+def near(got, want, bound, what):
+    g = wide(got)
+    bad = ~((g - want).abs() <= bound)
+    assert not bad.any(), (what, int(bad.sum()), bad.nonzero()[:4].tolist(), g[bad][:4].tolist(),
+                           want[bad][:4].tolist(), bound.expand_as(want)[bad][:4].tolist())
+
+
+def cuts(rng, tokens, nseq, empties=True):
+    """Offsets of nseq sequences of all lengths, some of one token, some empty."""
+    cut = np.sort(rng.integers(0, tokens + 1, nseq - 1))
+    if empties and nseq > 3:
+        cut[0] = 0
+        cut[-1] = tokens
+        cut[nseq // 2] = cut[nseq // 2 - 1]
+    return np.concatenate([[0], np.sort(cut), [tokens]]).astype(np.int64)
+
+
+# ------------------------------------------------------------------ convolution
+
+CONV = [(1, 1, 1, 4), (5, 3, 2, 2), (70, 63, 9, 3), (300, 64, 1, 4), (517, 100, 40, 4), (130, 255, 3, 3),
+        (1029, 260, 17, 5), (64, 1000, 64, 4), (200, 33, 150, 4), (90, 17, 5, 1), (77, 20, 6, 8),
+        (600, 5, 4, 7), (1300, 8, 90, 6)]
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("tokens,D,nseq,K", CONV)
+def test_convolution(ctx, dtype, tokens, D, nseq, K):
+    gen = torch.Generator().manual_seed(tokens + D)
+    rng = np.random.default_rng([tokens, D])
+    x, dy = normal(gen, tokens, D, dtype=dtype), normal(gen, tokens, D, dtype=dtype)
+    w, b = normal(gen, D, K, std=0.5), normal(gen, D)
+    state, dlast = (normal(gen, nseq, K - 1, D, dtype=dtype) for _ in range(2))
+    off = cuts(rng, tokens, nseq)
+    for form in range(4):
+        silu, has, idt = form % 2 == 0, form < 2, torch.int32 if form < 3 else torch.int64
+        bb, st, dl = (b, state, dlast) if has else (None, None, None)
+        o = torch.from_numpy(off).to(idt).cuda()
+        y, last, err = ref.conv(wide(x), wide(w), wide(bb), off, wide(st), silu)
+        xs = strided(cuda(x), 3, 1) if form == 1 else cuda(x)
+        gy, gl = ctx.convolution(xs, cuda(w), cuda(bb), o, state=cuda(st), silu=silu)
+        near(gy, y, ref.rounded(err, y, dtype), ("y", form))
+        assert torch.equal(wide(gl), last), form
+        want, errs = ref.conv_grad(wide(x), wide(w), wide(bb), wide(dy), off, wide(st), wide(dl), silu)
+        dys = strided(cuda(dy), 5, 3) if form == 1 else cuda(dy)
+        g = ctx.convolution_backward(xs, cuda(w), cuda(bb), dys, o, state=cuda(st), dlast=cuda(dl),
+                                     silu=silu)
+        near(g.x, want[0], ref.rounded(errs[0], want[0], dtype), ("dx", form))
+        near(g.weight, want[1], ref.rounded(errs[1], want[1], "f32"), ("dw", form))
+        if has:
+            near(g.bias, want[2], ref.rounded(errs[2], want[2], "f32"), ("db", form))
+            near(g.state, want[3], ref.rounded(errs[3], want[3], dtype), ("dstate", form))
+        else:
+            assert g.bias is None and g.state is None
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("nseq,D,K", [(1, 1, 4), (7, 33, 2), (64, 512, 4), (300, 130, 3), (5, 9, 1),
+                                      (3, 2050, 8)])
+def test_convolution_steps(ctx, dtype, nseq, D, K):
+    """One token after the other gives what the whole sequences give, bit for bit."""
+    gen = torch.Generator().manual_seed(nseq)
+    T = 5
+    x = normal(gen, nseq, T, D, dtype=dtype).cuda()
+    w, b = normal(gen, D, K, std=0.5).cuda(), normal(gen, D).cuda()
+    state = normal(gen, nseq, K - 1, D, dtype=dtype).cuda()
+    y, last = ctx.convolution(x, w, b, state=state)
+    assert y.shape == x.shape
+    rows = state.clone()
+    for t in range(T):
+        out, new = ctx.convolution_step(x[:, t].contiguous(), w, b, rows,
+                                        last=rows if t % 2 else None)
+        assert torch.equal(out, y[:, t]), t
+        rows = new
+    assert torch.equal(rows, last)
+    out, _ = ctx.convolution_step(strided(x[:, 0], 3, 1), w, b, state)
+    assert torch.equal(out, y[:, 0])
+
+
+def test_convolution_keeps_to_its_rows(ctx):
+    gen = torch.Generator().manual_seed(3)
+    x = normal(gen, 100, 37).cuda()
+    w = normal(gen, 37, 4).cuda()
+    out = strided(torch.zeros_like(x), 3, 2)
+    guard = out._base.clone()
+    ctx.convolution(x, w, None, out=out)
+    y, _ = ctx.convolution(x, w, None)
+    assert torch.equal(out, y)
+    out.zero_()
+    assert torch.equal(out._base, guard)
+
+
+def test_convolution_lets_nothing_out_of_a_sequence(ctx):
+    """Infinities and NaN reach the next taps - 1 tokens of their sequence and channel."""
+    gen = torch.Generator().manual_seed(4)
+    x = normal(gen, 60, 8)
+    off = torch.tensor([0, 20, 40, 60], dtype=torch.int32)
+    w = normal(gen, 8, 4)
+    x[19, 2], x[30, 5] = math.inf, math.nan
+    y, _ = ctx.convolution(x.cuda(), w.cuda(), None, off.cuda(), silu=False)
+    hit = ~torch.isfinite(y.cpu())
+    want = torch.zeros_like(hit)
+    want[19, 2] = True
+    want[30:34, 5] = True
+    assert torch.equal(hit, want)
+
+
+# ------------------------------------------------------------------ selective scan
+
+# tokens, D, N, groups, nseq
+SCAN = [(1, 1, 1, 1, 1), (17, 3, 5, 1, 2), (16, 8, 4, 2, 1), (100, 130, 16, 1, 7), (333, 64, 16, 4, 30),
+        (257, 20, 64, 1, 3), (90, 70, 33, 2, 4), (64, 260, 8, 1, 64), (200, 5, 16, 5, 1), (150, 12, 2, 3, 100),
+        (700, 33, 16, 1, 1), (1000, 9, 7, 3, 5)]
+
+
+def scan_inputs(gen, tokens, D, N, groups, nseq, dtype, state=True, gated=True, skip=True, bias=True):
+    n = lambda *s, **k: normal(gen, *s, dtype=dtype, **k)
+    s = {"x": n(tokens, D), "delta": n(tokens, D), "B": n(tokens, groups * N), "C": n(tokens, groups * N),
+         "A": -torch.exp(normal(gen, D, N)), "z": n(tokens, D) if gated else None,
+         "skip": normal(gen, D) if skip else None, "bias": normal(gen, D) - 1.5 if bias else None,
+         "h0": normal(gen, nseq, D, N) if state else None, "dy": n(tokens, D),
+         "dlast": normal(gen, nseq, D, N) if state else None}
+    return s
+
+
+def scan_reference(s, off, soft, cut, grad=True):
+    w = {k: wide(v) for k, v in s.items()}
+    return ref.selective(w["x"], w["delta"], w["A"], w["B"], w["C"], off, w["h0"], w["skip"], w["z"],
+                         w["bias"], soft, cut, (w["dy"], w["dlast"]) if grad else None)
+
+
+def scan_call(ctx, s, o, soft, x=None, **kw):
+    c = {k: cuda(v) for k, v in s.items()}
+    form = dict(state=c["h0"], skip=c["skip"], z=c["z"], delta_bias=c["bias"], softplus=soft)
+    ins = (c["x"] if x is None else x, c["delta"], c["A"], c["B"], c["C"])
+    y, last, marks = ctx.selective_scan(*ins, o, marks=True, **form, **kw)
+    g = ctx.selective_backward(*ins, c["dy"], marks, o, dlast=c["dlast"], **form)
+    got = {"y": y, "last": last, "x": g.x, "delta": g.delta, "A": g.A, "B": g.B, "C": g.C}
+    for k in ("skip", "z", "delta_bias", "state"):
+        if getattr(g, k) is not None:
+            got[k] = getattr(g, k)
+    return got
+
+
+F32_OUT = ("last", "A", "skip", "delta_bias", "state")
+
+
+def check_scan(got, want, err, dtype, what):
+    for k, v in got.items():
+        near(v, want[k], ref.rounded(err[k], want[k], "f32" if k in F32_OUT else dtype), (k, what))
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("tokens,D,N,groups,nseq", SCAN)
+def test_selective(ctx, dtype, tokens, D, N, groups, nseq):
+    rng = np.random.default_rng([tokens, D, N])
+    off = cuts(rng, tokens, nseq)
+    for form in range(3):
+        gen = torch.Generator().manual_seed(tokens + D + form)
+        s = scan_inputs(gen, tokens, D, N, groups, nseq, dtype, state=form != 1, gated=form != 2,
+                        skip=form != 1, bias=form != 2)
+        soft = form != 1
+        if not soft:  # the step itself: not below zero
+            s["delta"] = s["delta"].abs() * 0.25
+            s["bias"] = s["bias"].abs() * 0.1
+        o = torch.from_numpy(off).to(torch.int64 if form == 2 else torch.int32).cuda()
+        # a range's decay is the exponential of a sum: at most all tokens of the call
+        want, err = scan_reference(s, off, soft, tokens)
+        check_scan(scan_call(ctx, s, o, soft), want, err, dtype, form)
+
+
+def test_selective_of_equal_sequences(ctx):
+    """[nseq][T][D] without offsets is the same as packed, bit for bit; strided rows too."""
+    gen = torch.Generator().manual_seed(8)
+    nseq, T, D, N = 6, 37, 50, 16
+    s = scan_inputs(gen, nseq * T, D, N, 2, nseq, "bf16")
+    o = torch.arange(0, nseq * T + 1, T, dtype=torch.int32).cuda()
+    a = scan_call(ctx, s, o, True)
+    t3 = {k: v if v is None or k in ("A", "skip", "bias", "h0", "dlast") else v.view(nseq, T, -1)
+          for k, v in s.items()}
+    b = scan_call(ctx, t3, None, True)
+    for k in a:
+        assert torch.equal(a[k].view(-1), b[k].reshape(-1)), k
+    c = scan_call(ctx, s, o, True, x=strided(s["x"].cuda(), 3, 1))
+    for k in a:
+        assert torch.equal(a[k], c[k]), k
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("nseq,D,N,groups", [(1, 1, 1, 1), (7, 33, 16, 1), (64, 256, 16, 2), (3, 70, 64, 7),
+                                             (130, 20, 5, 4), (2, 1030, 32, 1), (1, 96, 8, 96)])
+def test_selective_steps(ctx, dtype, nseq, D, N, groups):
+    """Token by token against the formulas, the states in place every other time."""
+    gen = torch.Generator().manual_seed(nseq + D)
+    T = 4
+    s = scan_inputs(gen, nseq * T, D, N, groups, nseq, dtype)
+    off = list(range(0, nseq * T + 1, T))
+    want, err = scan_reference(s, off, True, 0, grad=False)
+    c = {k: cuda(v) for k, v in s.items()}
+    state = c["h0"].clone()
+    tok = lambda v, t: v.view(nseq, T, -1)[:, t].contiguous()
+    for t in range(T):
+        y, new = ctx.selective_step(tok(c["x"], t), tok(c["delta"], t), c["A"], tok(c["B"], t),
+                                    tok(c["C"], t), state, skip=c["skip"], z=tok(c["z"], t),
+                                    delta_bias=c["bias"], last=state if t % 2 else None)
+        r = want["y"].view(nseq, T, D)[:, t]
+        near(y, r, ref.rounded(err["y"].view(nseq, T, D)[:, t], r, dtype), t)
+        state = new
+    near(state, want["last"], ref.rounded(err["last"], want["last"], "f32"), "last")
+    # without states, a gate, a skip or a bias; marks take the way of whole sequences
+    y, last = ctx.selective_step(tok(c["x"], 0), tok(c["delta"], 0), c["A"], tok(c["B"], 0), tok(c["C"], 0))
+    y2, last2, marks = ctx.selective_scan(tok(c["x"], 0).unsqueeze(1), tok(c["delta"], 0).unsqueeze(1), c["A"],
+                                          tok(c["B"], 0).unsqueeze(1), tok(c["C"], 0).unsqueeze(1), marks=True)
+    assert marks is not None
+    bare = {k: (v if k == "A" else wide(tok(v, 0).cpu())) for k, v in c.items() if k in ("x", "delta", "B", "C")}
+    w, e = ref.selective(bare["x"], bare["delta"], wide(c["A"]), bare["B"], bare["C"], list(range(nseq + 1)), None,
+                         None, None, None, True, 0)
+    for got in (y, y2.squeeze(1)):
+        near(got, w["y"], ref.rounded(e["y"], w["y"], dtype), "bare")
+    for got in (last, last2):
+        near(got, w["last"], ref.rounded(e["last"], w["last"], "f32"), "bare last")
+
+
+@pytest.mark.parametrize("tokens,D,N,nseq", [(9000, 40, 16, 1), (9001, 16, 4, 3), (3000, 300, 16, 40),
+                                             (2500, 24, 40, 2)])
+def test_selective_over_many_ranges(ctx, tokens, D, N, nseq):
+    """Sequences that run through many ranges, slow decays; in two runs the same bits."""
+    gen = torch.Generator().manual_seed(tokens)
+    s = scan_inputs(gen, tokens, D, N, 1, nseq, "f32")
+    s["A"] = -torch.exp(normal(gen, D, N) - 1)
+    s["bias"] = normal(gen, D) - 4
+    off = cuts(np.random.default_rng(tokens), tokens, nseq, empties=False)
+    o = torch.from_numpy(off).cuda()
+    want, err = scan_reference(s, off, True, tokens)
+    a = scan_call(ctx, s, o, True)
+    check_scan(a, want, err, "f32", "ranges")
+    b = scan_call(ctx, s, o, True)
+    for k in a:
+        assert torch.equal(a[k], b[k]), k
+
+
+def test_selective_of_no_tokens(ctx):
+    gen = torch.Generator().manual_seed(5)
+    h0, D, N = normal(gen, 3, 20, 16).cuda(), 20, 16
+    e = torch.empty(0, D, device="cuda")
+    bc = torch.empty(0, N, device="cuda")
+    A = -torch.ones(D, N, device="cuda")
+    o = torch.zeros(4, dtype=torch.int32, device="cuda")
+    y, last, marks = ctx.selective_scan(e, e, A, bc, bc, o, state=h0, marks=True)
+    assert y.shape == (0, D) and torch.equal(last, h0)
+    g = ctx.selective_backward(e, e, A, bc, bc, e, marks, o, state=h0, dlast=2 * h0, skip=A[:, 0].contiguous())
+    assert torch.equal(g.state, 2 * h0) and not g.A.any() and not g.skip.any()
+    w = normal(gen, D, 4).cuda()
+    st = normal(gen, 3, 3, D).cuda()
+    y, last = ctx.convolution(e, w, None, o, state=st)
+    assert torch.equal(last, st)
+    g = ctx.convolution_backward(e, w, None, e, o, state=st, dlast=2 * st)
+    assert torch.equal(g.state, 2 * st) and not g.weight.any()
+
+
+def test_selective_lets_nothing_out_of_a_sequence(ctx):
+    """What is not finite stays in its sequence; x's and delta's in their channel."""
+    gen = torch.Generator().manual_seed(6)
+    n, D = 400, 24
+    s = scan_inputs(gen, n, D, 16, 1, 4, "f32")
+    o = torch.tensor([0, 100, 200, 300, 400], dtype=torch.int32).cuda()
+    clean = scan_call(ctx, s, o, True)
+    for name, value in (("x", math.nan), ("x", math.inf), ("delta", math.nan), ("B", math.inf), ("dy", math.nan)):
+        d = {k: None if v is None else v.clone() for k, v in s.items()}
+        d[name][150, 3] = value
+        got = scan_call(ctx, d, o, True)
+        for k in ("y", "x", "delta", "z", "B", "C"):
+            same = torch.ones(n, dtype=torch.bool)
+            same[100:200] = False
+            assert torch.equal(got[k].cpu()[same], clean[k].cpu()[same]), (name, k)
+            if name in ("x", "delta") and k == "y":
+                keep = torch.ones(D, dtype=torch.bool)
+                keep[3] = False
+                assert torch.equal(got[k].cpu()[:, keep], clean[k].cpu()[:, keep]), name
+        assert torch.equal(got["last"][[0, 2, 3]], clean["last"][[0, 2, 3]])
+        assert not torch.isfinite(got["x"].cpu()[150, 3]) or name == "x" or name == "B"
+
+
+def test_selective_far_steps(ctx):
+    """Steps from far below zero to far above: the softplus at both ends, decays to zero."""
+    D, N = 6, 16
+    delta = torch.tensor([-100.0, -60.0, -20.0, -8.0, -1e-3, 0.0, 1e-3, 8.0, 20.0, 60.0, 100.0, 0.5])
+    gen = torch.Generator().manual_seed(7)
+    s = scan_inputs(gen, 12, D, N, 1, 1, "f32", bias=False)
+    s["delta"] = delta.view(12, 1).repeat(1, D).contiguous()
+    o = torch.tensor([0, 12], dtype=torch.int32).cuda()
+    want, err = scan_reference(s, [0, 12], True, 0)
+    # below e^-87 a value leaves the normal numbers: nothing is promised there
+    for k in err:
+        err[k] = err[k] + 1e-36
+    check_scan(scan_call(ctx, s, o, True), want, err, "f32", "far")
+
+
+# ------------------------------------------------------------------ beams
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("groups,beams,V,picks", [(1, 1, 1, 1), (1, 4, 100_000, 4), (3, 5, 1000, 10),
+                                                  (32, 8, 3203, 16), (2, 16, 4097, 64), (5, 3, 7, 64),
+                                                  (1, 64, 300, 64), (70, 1, 50, 2), (2, 2, 1_000_003, 33)])
+def test_beam(ctx, dtype, groups, beams, V, picks):
+    gen = torch.Generator().manual_seed(V + beams)
+    rows = groups * beams
+    scores = normal(gen, rows, V, dtype=dtype, std=2.0)
+    total, lse = normal(gen, rows) - 20, normal(gen, rows) + 8
+    over = (torch.rand(rows, generator=gen) < 0.3).to(torch.int32)
+    end = V // 3
+    if rows > 2:
+        total[1] = -math.inf  # a beam that is not there yet
+        if V > 100:
+            scores[0, 5], scores[0, 17] = math.nan, -math.inf
+    s = scores.float().numpy()
+    for kw in ({}, {"lse": lse}, {"lse": lse, "finished": over, "end": end}):
+        n = {k: v.numpy() if torch.is_tensor(v) else v for k, v in kw.items()}
+        want = ref.beam(s, total.numpy(), n.get("lse"), beams, picks, n.get("finished"), n.get("end", 0))
+        got = ctx.beam(cuda(scores), cuda(total), beams=beams, picks=picks,
+                       **{k: cuda(v) if torch.is_tensor(v) else v for k, v in kw.items()})
+        for g, w in zip(got, want):
+            assert np.array_equal(g.cpu().numpy(), w), (kw.keys(), g.cpu().numpy()[:2], w[:2])
+    got = ctx.beam(strided(cuda(scores), 5, 3), cuda(total), beams=beams, picks=picks)
+    want = ref.beam(s, total.numpy(), None, beams, picks)
+    for g, w in zip(got, want):
+        assert np.array_equal(g.cpu().numpy(), w)
+
+
+@pytest.mark.parametrize("kind", ["equal", "rising", "falling", "two", "zeros", "empty", "infinite"])
+def test_beam_ties_and_orders(ctx, kind):
+    """Equal scores go to the lowest place, a zero's sign does not count."""
+    groups, beams, V, picks = 2, 3, 20_000, 64
+    rows = groups * beams
+    s = np.zeros((rows, V), np.float32)
+    if kind == "rising":
+        s[:] = np.arange(V, dtype=np.float32)
+    elif kind == "falling":
+        s[:] = -np.arange(V, dtype=np.float32)
+    elif kind == "two":
+        s[:, 1::7] = 1.0
+    elif kind == "zeros":
+        s[:, ::2] = -0.0
+    elif kind == "empty":
+        s[:] = -np.inf
+        s[3, 77] = -1.0
+    elif kind == "infinite":
+        s[:, 5] = np.inf
+        s[:, 6] = np.finfo(np.float32).max
+        s[:, 7] = np.nan
+    total = np.zeros(rows, np.float32)
+    want = ref.beam(s, total, None, beams, picks)
+    got = ctx.beam(torch.from_numpy(s).cuda(), torch.from_numpy(total).cuda(), beams=beams, picks=picks)
+    for g, w in zip(got, want):
+        assert np.array_equal(g.cpu().numpy(), w), kind
+
+
+@pytest.mark.parametrize("rows,in_rows", [(1, 1), (5, 3), (256, 256), (300, 40)])
+def test_reorder(ctx, rows, in_rows):
+    gen = torch.Generator().manual_seed(rows)
+    ids = torch.randint(0, in_rows, (rows,), generator=gen).to(torch.int32)
+    shapes = [((256, 16), torch.float32), ((3, 255), torch.bfloat16), ((201,), torch.int32), ((1,), torch.uint8),
+              ((7, 3), torch.float16), ((9001,), torch.float32), ((), torch.int64), ((0,), torch.float32),
+              ((33,), torch.uint8)] * 5  # more tensors than a launch takes
+    ts = [(torch.rand(in_rows, *s, generator=gen) * 100).to(d).cuda() for s, d in shapes]
+    for t, o in zip(ts, ctx.reorder(ts, ids.cuda())):
+        assert torch.equal(o, t[ids.long().cuda()])
+    # rows apart, and starts that no vector is aligned to
+    t = strided(normal(gen, in_rows, 37).cuda(), 2, 1)
+    o = strided(torch.zeros(rows, 37, device="cuda"), 5, 3)
+    guard = o._base.clone()
+    ctx.reorder([t], ids.cuda(), [o])
+    assert torch.equal(o, t[ids.long().cuda()])
+    o.zero_()
+    assert torch.equal(o._base, guard)
+
+
+def test_reorder_of_rows_that_are_not_there(pg, ctx):
+    t = torch.arange(12.0, device="cuda").view(4, 3)
+    out = torch.full((3, 3), -1.0, device="cuda")
+    ctx.reorder([t], torch.tensor([3, 4, -1], dtype=torch.int32, device="cuda"), [out])
+    assert ctx.status() == pg.EID and ctx.status() == pg.OK
+    assert torch.equal(out, torch.tensor([[9.0, 10, 11], [-1, -1, -1], [-1, -1, -1]], device="cuda"))
+
+
+# ------------------------------------------------------------------ together
+
+
+class Layer:
+    """A language model of one selective layer on a word table; products are torch's."""
+
+    def __init__(self, ctx, V=301, d=24, N=8, K=4):
+        gen = torch.Generator().manual_seed(11)
+        self.ctx, self.V, self.d, self.N, self.K = ctx, V, d, N, K
+        n = lambda *s: normal(gen, *s, std=s[-1] ** -0.5).cuda()
+        self.E, self.w, self.b = 3 * n(V, d), 2 * n(d, K), n(d)
+        self.Wd, self.WB, self.WC, self.Wz, self.O = n(d, d), 2 * n(N, d), 2 * n(N, d), n(d, d), 6 * n(V, d)
+        self.A = -torch.arange(1, N + 1, device="cuda").float().repeat(d, 1).contiguous()
+        self.skip, self.bias = torch.ones(d, device="cuda"), torch.full((d,), -1.0, device="cuda")
+
+    def prompt(self, words, offsets):
+        e = self.E[words.long()]
+        u, taps = self.ctx.convolution(e, self.w, self.b, offsets)
+        y, h, _ = self.ctx.selective_scan(u, u @ self.Wd.t(), self.A, u @ self.WB.t(), u @ self.WC.t(), offsets,
+                                          skip=self.skip, z=e @ self.Wz.t(), delta_bias=self.bias)
+        return y @ self.O.t(), taps, h
+
+    def next(self, words, taps, h):
+        e = self.E[words.long()]
+        u, taps = self.ctx.convolution_step(e, self.w, self.b, taps)
+        y, h = self.ctx.selective_step(u, u @ self.Wd.t(), self.A, u @ self.WB.t(), u @ self.WC.t(), h,
+                                       skip=self.skip, z=e @ self.Wz.t(), delta_bias=self.bias)
+        return y @ self.O.t(), taps, h
+
+    def scores64(self, words):
+        """The scores after the last of these words, in 64 bits on the CPU."""
+        e = wide(self.E)[words]
+        off = [0, len(words)]
+        u, _, _ = ref.conv(e, wide(self.w), wide(self.b), off, None, True)
+        out, _ = ref.selective(u, u @ wide(self.Wd).t(), wide(self.A), u @ wide(self.WB).t(), u @ wide(self.WC).t(),
+                               off, None, wide(self.skip), e @ wide(self.Wz).t(), wide(self.bias), True, 0)
+        return out["y"][-1] @ wide(self.O).t()
+
+
+def test_prompt_then_beams(pg, ctx):
+    """Prompts of two lengths read in one packed call, then a beam search word by word with the
+    states reordered, against a search in 64 bits that reads every continuation anew."""
+    m = Layer(ctx)
+    beams, steps, prompts = 3, 5, [[5, 9, 200, 31, 7], [44, 3]]
+    words = torch.tensor(sum(prompts, []), dtype=torch.int32, device="cuda")
+    offsets = torch.tensor([0, 5, 7], dtype=torch.int32, device="cuda")
+    scores, taps, h = m.prompt(words, offsets)
+    last = scores[offsets[1:].long() - 1].contiguous()
+    _, _, lse = ctx.logits(last, write=False)
+    total = torch.zeros(2, device="cuda")
+    parent, token, total = ctx.beam(last, total, beams=1, picks=beams, lse=lse)
+    said = torch.full((2 * beams, steps), -1, dtype=torch.int32, device="cuda")
+    taps, h = ctx.reorder([taps, h], parent)
+    said[:, 0] = token.view(-1)
+    for k in range(1, steps):
+        scores, taps, h = m.next(said[:, k - 1], taps, h)
+        _, _, lse = ctx.logits(scores, write=False)
+        parent, token, total = ctx.beam(scores, total.view(-1), beams=beams, picks=beams, lse=lse)
+        taps, h, said = ctx.reorder([taps, h, said], parent)
+        said[:, k] = token.view(-1)
+    assert ctx.status() == pg.OK
+    for i, p in enumerate(prompts):
+        live = [([], 0.0)]
+        for k in range(steps):
+            every = []
+            for seq, tot in live:
+                s = m.scores64(p + seq)
+                l = s - torch.logsumexp(s, 0)
+                every += [(tot + float(l[v]), seq + [v]) for v in range(m.V)]
+            every.sort(key=lambda c: -c[0])
+            # the search is only told apart where the margin is wider than 32 bits' errors
+            assert every[beams - 1][0] - every[beams][0] > 1e-4
+            live = [(seq, tot) for tot, seq in every[:beams]]
+        got = said[i * beams:(i + 1) * beams].tolist()
+        assert got == [seq for seq, _ in live]
+        assert np.allclose(total[i].tolist(), [t for _, t in live], atol=1e-4)
+
+
+def test_steps_continue_prompts(ctx):
+    """A sequence read at once, and the same one cut into a prompt and single tokens."""
+    m = Layer(ctx)
+    words = torch.tensor([3, 1, 4, 1, 5, 9, 2, 6, 5, 3], dtype=torch.int32, device="cuda")
+    whole, taps_all, h_all = m.prompt(words, torch.tensor([0, 10], dtype=torch.int32, device="cuda"))
+    scores, taps, h = m.prompt(words[:6], torch.tensor([0, 6], dtype=torch.int32, device="cuda"))
+    for t in range(6, 10):
+        scores, taps, h = m.next(words[t:t + 1], taps, h)
+        assert torch.allclose(scores[0], whole[t], rtol=1e-4, atol=1e-4)
+    assert torch.equal(taps, taps_all) and torch.allclose(h, h_all, rtol=1e-4, atol=1e-5)
+
+
+def test_a_training_step_against_autograd(ctx):
+    """Convolution, scan and both gradients chained, against autograd of the formulas in 64
+    bits.  The chain's float32 products and sums are of at most 64 terms each in 40 tokens:
+    1e-4 of a gradient's largest value is some thousand float32 roundings."""
+    m = Layer(ctx)
+    gen = torch.Generator().manual_seed(12)
+    off = [0, 13, 14, 40]
+    o = torch.tensor(off, dtype=torch.int32, device="cuda")
+    e, dy = normal(gen, 40, m.d), normal(gen, 40, m.d)
+    names = ("e", "w", "b", "Wd", "WB", "WC", "Wz", "A", "skip", "bias")
+    leaf = {k: wide(getattr(m, k, e)).requires_grad_() for k in names}
+    L = leaf
+    ys = []
+    for a, z in zip(off, off[1:]):
+        x = torch.cat([torch.zeros(m.K - 1, m.d, dtype=torch.float64), L["e"][a:z]])
+        u = L["b"] + sum(x[k:k + z - a] * L["w"][:, k] for k in range(m.K))
+        u = u * torch.sigmoid(u)
+        s = torch.nn.functional.softplus(u @ L["Wd"].t() + L["bias"])
+        B, C, g = u @ L["WB"].t(), u @ L["WC"].t(), L["e"][a:z] @ L["Wz"].t()
+        h = torch.zeros(m.d, m.N, dtype=torch.float64)
+        for t in range(z - a):
+            h = torch.exp(s[t][:, None] * L["A"]) * h + (s[t] * u[t])[:, None] * B[t]
+            ys.append(((h * C[t]).sum(1) + L["skip"] * u[t]) * g[t] * torch.sigmoid(g[t]))
+    (torch.stack(ys) * wide(dy)).sum().backward()
+
+    ec = e.cuda()
+    u, _ = ctx.convolution(ec, m.w, m.b, o)
+    ins = (u, u @ m.Wd.t(), m.A, u @ m.WB.t(), u @ m.WC.t())
+    z = ec @ m.Wz.t()
+    form = dict(skip=m.skip, z=z, delta_bias=m.bias)
+    _, _, marks = ctx.selective_scan(*ins, o, marks=True, **form)
+    g = ctx.selective_backward(*ins, dy.cuda(), marks, o, **form)
+    du = g.x + g.delta @ m.Wd + g.B @ m.WB + g.C @ m.WC
+    c = ctx.convolution_backward(ec, m.w, m.b, du, o)
+    got = {"e": c.x + g.z @ m.Wz, "w": c.weight, "b": c.bias, "Wd": g.delta.t() @ u, "WB": g.B.t() @ u,
+           "WC": g.C.t() @ u, "Wz": g.z.t() @ ec, "A": g.A, "skip": g.skip, "bias": g.delta_bias}
+    for k, v in got.items():
+        want = leaf[k].grad
+        assert (wide(v) - want).abs().max() <= 1e-4 * want.abs().max(), k
+
+
+def test_captured_and_replayed(pg):
+    """All of it in a graph, replayed with other inputs and eager work in between."""
+    stream = torch.cuda.Stream()
+    gen = torch.Generator().manual_seed(13)
+    D, N, K, n, nseq = 70, 16, 4, 500, 5
+    o = torch.from_numpy(cuts(np.random.default_rng(1), n, nseq)).to(torch.int32).cuda()
+    names = ("x", "delta", "B", "C", "z", "dy", "dlast", "h0")
+    c = {k: cuda(v) for k, v in scan_inputs(gen, n, D, N, 1, nseq, "bf16").items()}
+    w, b = normal(gen, D, K).cuda(), normal(gen, D).cuda()
+    scores, total = normal(gen, 8, 5000).cuda(), normal(gen, 8).cuda()
+    with torch.cuda.stream(stream):
+        ctx = pg.Context(1000, 16, 5, 8, max_batch=1, stream=stream)
+        ctx.reserve_selective(n, D, N)
+        ctx.reserve_beam(8, 5000, 8)
+
+        def work():
+            u, taps = ctx.convolution(c["x"], w, b, o)
+            form = dict(state=c["h0"], skip=c["skip"], z=c["z"], delta_bias=c["bias"])
+            ins = (u, c["delta"], c["A"], c["B"], c["C"])
+            y, last, marks = ctx.selective_scan(*ins, o, marks=True, **form)
+            g = ctx.selective_backward(*ins, c["dy"], marks, o, dlast=c["dlast"], **form)
+            cg = ctx.convolution_backward(c["x"], w, b, g.x, o)
+            parent, token, out = ctx.beam(scores, total, beams=4, picks=4)
+            moved = ctx.reorder([scores, total], parent)
+            return [u, taps, y, last, *g, *cg[:3], parent, token, out, *moved]
+
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            held = work()
+        for turn in range(4):
+            for k in names:
+                c[k].copy_(torch.randn(c[k].shape, generator=gen))
+            scores.copy_(torch.randn(scores.shape, generator=gen))
+            graph.replay()
+            torch.cuda.synchronize()
+            first = [t.clone() for t in held]
+            for a, e in zip(first, work()):
+                assert torch.equal(a, e), turn
+            torch.cuda.synchronize()
+        assert ctx.status() == pg.OK
+        ctx.close()
+
+
+# ------------------------------------------------------------------ limits, refusals
+
+
+def test_offsets_past_32_bits(ctx):
+    """Rows so far apart that elements lie behind the 2^32nd."""
+    gen = torch.Generator().manual_seed(14)
+    n, D, N, ld = 1100, 16, 4, 4_000_000
+    s = scan_inputs(gen, n, D, N, 1, 2, "bf16", gated=False)
+    base = torch.empty(n * ld, dtype=torch.bfloat16, device="cuda")
+    far = base.view(n, ld)[:, 5:5 + D]
+    far.copy_(s["x"].cuda())
+    o = torch.tensor([0, 600, n], dtype=torch.int32, device="cuda")
+    near_, far_ = scan_call(ctx, s, o, True), scan_call(ctx, s, o, True, x=far)
+    for k in near_:
+        assert torch.equal(near_[k], far_[k]), k
+    w = normal(gen, D, 4).cuda()
+    for a, b in zip(ctx.convolution(s["x"].cuda(), w, None, o), ctx.convolution(far, w, None, o)):
+        assert torch.equal(a, b)
+    dy = s["dy"].cuda()
+    for a, b in zip(ctx.convolution_backward(s["x"].cuda(), w, None, dy, o)[:2],
+                    ctx.convolution_backward(far, w, None, dy, o)[:2]):
+        assert torch.equal(a, b)
+    ids = torch.tensor([n - 1, 0], dtype=torch.int32, device="cuda")
+    assert torch.equal(ctx.reorder([far], ids)[0], far[ids.long()])
+
+
+def test_refusals(pg, ctx):
+    f = lambda *s: torch.zeros(*s, device="cuda")
+    n, D, N = 4, 6, 4
+    x, A, B, w = f(n, D), f(D, N), f(n, N), f(D, 4)
+    o = torch.tensor([0, 1, 4], dtype=torch.int32, device="cuda")
+    st = f(2, D, N)
+
+    def refused(code, call, *a, **k):
+        with pytest.raises(pg.PolyglotError) as e:
+            call(*a, **k)
+        assert e.value.rc == code, e.value
+
+    marks = f(1, D, N)
+    refused(pg.EINVAL, ctx.selective_scan, x, x, A, B, B, o, out=x)
+    refused(pg.EINVAL, ctx.selective_scan, x, x, A, B, B, o, state=st, last=st)
+    refused(pg.EINVAL, ctx.selective_scan, x, x, f(D, 65), f(n, 65), f(n, 65), o)
+    refused(pg.EINVAL, ctx.selective_scan, x, x, A, f(n, 4 * N), f(n, 4 * N), o)  # 4 heads of 6 channels
+    refused(pg.EBATCH, ctx.selective_scan, f(n, 2000), f(n, 2000), f(2000, N), B, B, o)
+    refused(pg.EINVAL, ctx.selective_backward, x, x, A, B, B, x, marks, o,
+            out=pg.SelectiveGrads(x, *[None] * 8))
+    refused(pg.EINVAL, ctx.selective_backward, x, x, A, B, B, x, f(n * D + 1)[1:].view(1, D, N)
+            if n * D == D * N else f(D * N + 1)[1:].view(1, D, N), o)
+    with pytest.raises(ValueError):
+        ctx.selective_scan(x, x, A, f(n, 6), f(n, 6), o)
+    with pytest.raises(ValueError):
+        ctx.selective_scan(x, f(n, D + 1), A, B, B, o)
+    with pytest.raises(TypeError):
+        ctx.selective_scan(x, x.half(), A, B, B, o)
+    with pytest.raises(TypeError):
+        ctx.selective_scan(x, x, A.half(), B, B, o)
+    with pytest.raises(ValueError):
+        ctx.selective_scan(x, x, A, B, B, o, state=f(3, D, N))
+    with pytest.raises(ValueError):
+        ctx.selective_backward(x, x, A, B, B, x, f(2, D, N), o)
+    refused(pg.EINVAL, ctx.convolution, x, w, None, o, out=x)
+    cs = f(2, 3, D)
+    refused(pg.EINVAL, ctx.convolution, x, w, None, o, state=cs, last=cs)
+    refused(pg.EINVAL, ctx.convolution, x, f(D, 9), None, o)
+    refused(pg.EINVAL, ctx.convolution_backward, x, w, None, x, o, out=pg.ConvolutionGrads(x, None, None, None))
+    with pytest.raises(ValueError):
+        ctx.convolution(x, f(D + 1, 4), None, o)
+    s, t = f(8, 10), f(8)
+    refused(pg.EINVAL, ctx.beam, s, t, beams=4, picks=0)
+    refused(pg.EINVAL, ctx.beam, s, t, beams=4, picks=65)
+    refused(pg.EINVAL, ctx.beam, s, t, beams=4, picks=4, finished=t.int(), end=10)
+    refused(pg.EBATCH, ctx.beam, f(600, 10), f(600), beams=4, picks=4)
+    with pytest.raises(ValueError):
+        ctx.beam(s, t, beams=3, picks=4)
+    ids = torch.zeros(8, dtype=torch.int32, device="cuda")
+    refused(pg.EINVAL, ctx.reorder, [s], ids, [s])
+    out = f(8, 10)
+    refused(pg.EINVAL, ctx.reorder, [s, s], ids, [out, out])
+    with pytest.raises(ValueError):
+        ctx.reorder([s], ids, [f(7, 10)])
+    with pytest.raises(TypeError):
+        ctx.reorder([s], ids.long())
+    assert ctx.status() == pg.OK
+
+
+@pytest.mark.parametrize("bad", [[0, 50, 20, 100], [0, 10, 20, 90], [1, 10, 20, 100], [0, -5, 20, 100],
+                                 [0, 10, 2_000_000_000, 100]])
+@pytest.mark.parametrize("idt", [torch.int32, torch.int64])
+def test_offsets_that_do_not_ascend(pg, ctx, bad, idt):
+    """The flag, and no access outside of the tensors (offsets are held to the tokens)."""
+    gen = torch.Generator().manual_seed(15)
+    s = scan_inputs(gen, 100, 10, 8, 1, 3, "f32")
+    o = torch.tensor(bad, dtype=idt, device="cuda")
+    scan_call(ctx, s, o, True)
+    assert ctx.status() == pg.EOFFSETS and ctx.status() == pg.OK
+    w = normal(gen, 10, 4).cuda()
+    st = normal(gen, 3, 3, 10).cuda()
+    ctx.convolution(s["x"].cuda(), w, None, o, state=st)
+    assert ctx.status() == pg.EOFFSETS
+    ctx.convolution_backward(s["x"].cuda(), w, None, s["dy"].cuda(), o, state=st, dlast=st)
+    assert ctx.status() == pg.EOFFSETS and ctx.status() == pg.OK
