@@ -531,6 +531,7 @@ int polyglot_convolution_grad(polyglot_ctx* ctx, const polyglot_convolution_grad
  * polyglot_selective_grad needs: the states before every token that
  * POLYGLOT_SELECTIVE_MARK divides.  What is infinite may come out as NaN further on in its
  * sequence and channel.  States in whole fours, and 8, 16, 32 or 64 of them, are the fast ones.
+ * Rows lie less than 2^25 elements apart.
  *
  * With one token per sequence (tokens == nseq, no offsets) and no marks this is a model's
  * step for single tokens, which needs no workspace and whose last may be h0.  Otherwise no output may be an input, and the call uses the workspace of

@@ -15,7 +15,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libpolyglot.so")
 SOURCES = ["kernels.hip", "api.hip", "operators.hip", "recurrence.hip", "operators_api.hip",
-           "convolution.hip", "selective.hip", "beam.hip", "layers_api.hip"]
+           "selective_grad_f32.hip", "selective_grad_bf16.hip", "selective_grad_f16.hip",
+           "selective.hip", "convolution.hip", "beam.hip", "layers_api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",

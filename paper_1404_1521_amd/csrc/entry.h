@@ -42,11 +42,11 @@ struct Rows {
 };
 
 inline int check_rows(polyglot_ctx* ctx, int64_t tokens, size_t size, std::initializer_list<Rows> all,
-               const std::string& what) {
+                      const std::string& what, int64_t most_ld = INT64_MAX) {
   if (tokens == 0) return POLYGLOT_OK;
   for (const Rows& r : all) {
     if (!r.p) return fail(ctx, POLYGLOT_ENULL, what + ": NULL pointer");
-    if (!rows_ok(r.ld, tokens, r.width))
+    if (!rows_ok(r.ld, tokens, r.width) || r.ld > most_ld)
       return fail(ctx, POLYGLOT_EINVAL, what + ": rows closer than their width, or too many");
     if (!aligned(r.p, size)) return fail(ctx, POLYGLOT_EINVAL, what + ": misaligned pointer");
   }

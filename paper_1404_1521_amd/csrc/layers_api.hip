@@ -10,6 +10,7 @@ namespace {
 
 constexpr int64_t kMaxTokens = 1 << 30;
 constexpr int kMaxChannels = 1 << 20, kMaxStates = 64;
+constexpr int64_t kMaxRowDistance = (1 << 25) - 1;  // a tile's offsets fit 32 bits
 constexpr int64_t kMaxBeamParts = 1 << 23;  // workgroups of the selection
 
 int64_t beam_parts(int64_t V) { return (V + kBeamMinPart - 1) / kBeamMinPart; }
@@ -199,7 +200,7 @@ int polyglot_selective(polyglot_ctx* ctx, const polyglot_selective_args* args) {
     rc = check_rows(ctx, a.tokens, size_of(a.dtype),
                     {{a.x, a.ld_x, a.D}, {a.delta, a.ld_delta, a.D}, {a.B, a.ld_B, GN}, {a.C, a.ld_C, GN},
                      {a.y, a.ld_y, a.D}, a.z ? Rows{a.z, a.ld_z, a.D} : Rows{a.x, a.ld_x, a.D}},
-                    "selective");
+                    "selective", kMaxRowDistance);
     if (rc) return rc;
     if (!aligned(a.last, 4)) return fail(ctx, POLYGLOT_EINVAL, "selective: misaligned state");
     if (!apart({a.y, a.last, a.marks}, {a.x, a.delta, a.B, a.C, a.z, a.A, a.skip, a.delta_bias,
@@ -236,7 +237,7 @@ int polyglot_selective_grad(polyglot_ctx* ctx, const polyglot_selective_grad_arg
                     {x, {a.delta, a.ld_delta, a.D}, {a.B, a.ld_B, GN}, {a.C, a.ld_C, GN}, {a.dy, a.ld_dy, a.D},
                      a.z ? Rows{a.z, a.ld_z, a.D} : x, {a.dx, a.ld_dx, a.D}, {a.ddelta, a.ld_ddelta, a.D},
                      {a.dB, a.ld_dB, GN}, {a.dC, a.ld_dC, GN}, a.z ? Rows{a.dz, a.ld_dz, a.D} : x},
-                    "selective_grad");
+                    "selective_grad", kMaxRowDistance);
     if (rc) return rc;
     if (!a.dA || (a.tokens > 0 && !a.marks))
       return fail(ctx, POLYGLOT_ENULL, "selective_grad: NULL dA or marks");

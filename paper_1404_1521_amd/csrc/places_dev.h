@@ -63,6 +63,53 @@ __device__ __forceinline__ int mark_places(const Packed& s, int lo, int hi, int 
   return next;
 }
 
+// The sequences' offsets near the tiles that a wave goes through, one to a lane: where none
+// of them lies in a tile, which is the usual case in long sequences, nothing is read.
+struct UpCursor {   // tiles in ascending order: the offsets from `at`, the first >= lo, on
+  int at, o;
+  __device__ __forceinline__ void read(const Packed& s, int first) {
+    at = first;
+    o = at + lane_id() <= s.nseq ? place_of(s, at + lane_id()) : INT32_MAX;
+  }
+};
+struct DownCursor {  // in descending order: the offsets below `at`, the first > hi
+  int at, o;
+  __device__ __forceinline__ void read(const Packed& s, int first) {
+    at = first;
+    o = at - 1 - lane_id() >= 0 ? place_of(s, at - 1 - lane_id()) : -1;
+  }
+};
+
+// The places of a tile and, as bits, where in it sequences start and stop.  By a whole wave;
+// up to 32 places.
+struct TileMarks {
+  int start[32], stop[32];
+  uint32_t starts, stops;
+};
+__device__ __forceinline__ void mark_bits(TileMarks& m) {
+  const int l = lane_id() & 31;
+  const uint32_t a = (uint32_t)__ballot(m.start[l] >= 0), b = (uint32_t)__ballot(m.stop[l] >= 0);
+  m.starts = a;
+  m.stops = b;
+}
+__device__ __forceinline__ void mark_tile(const Packed& s, int lo, int hi, UpCursor& c, TileMarks& m) {
+  if (__ballot(c.o <= hi) == 0) {
+    m.starts = m.stops = 0;
+    return;
+  }
+  c.read(s, mark_places(s, lo, hi, 32, c.at, m.start, m.stop));
+  mark_bits(m);
+}
+__device__ __forceinline__ void mark_tile(const Packed& s, int lo, int hi, DownCursor& c, TileMarks& m) {
+  if (__ballot(c.o >= lo) == 0) {
+    m.starts = m.stops = 0;
+    return;
+  }
+  mark_places(s, lo, hi, 32, first_place(s, lo), m.start, m.stop);
+  mark_bits(m);
+  c.read(s, first_place(s, lo + 1));
+}
+
 // A workgroup's share of the sequences, the `part`-th of `parts`: raises the flag where
 // the offsets do not ascend from 0 to the tokens, and calls copy(i) with every thread for
 // each empty sequence i.

@@ -23,33 +23,36 @@ constexpr int kSelTile = kSelectiveTile;  // tokens of a tile, and between two m
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// e^x, x <= 0: the product with log2 e and what its rounding lost.
+// e^-|x|: the product with log2 e and what its rounding lost.  (From 2^-150 on it is zero
+// for all that follows; |x| stays finite there.)
 __device__ __forceinline__ float exp_neg(float x) {
-  const float t = x * kLog2e;
-  const float r = __fmaf_rn(x, kLog2e, -t);
+  const float m = __builtin_fminf(__builtin_fabsf(x), 104.f);
+  const float t = m * -kLog2e;
+  const float r = __fmaf_rn(m, -kLog2e, -t);
   const float e = exp2_fast(t);
   return __fmaf_rn(e, r * kLn2, e);
 }
 
-// log(1 + e^v) and its slope.  log(1 + e) = 2 atanh(e / (2 + e)); the argument is at most
-// 1/3, and the Maclaurin series' first term left out, s^17 / 17, is below 2^-29 of s.
+// log(1 + e^v) = max(v, 0) + log(1 + e), e = e^-|v|, and log(1 + e) = 2 atanh(e / (2 + e));
+// the argument is at most 1/3, and the Maclaurin series' first term left out, s^17 / 17, is
+// below 2^-29 of s.
 __device__ __forceinline__ float softplus(float v) {
-  const float e = exp_neg(-__builtin_fabsf(v));
+  const float e = exp_neg(v);
   const float s = e * __builtin_amdgcn_rcpf(2.f + e), q = s * s;
-  float p = 1.f / 15.f;
-  p = __fmaf_rn(p, q, 1.f / 13.f);
-  p = __fmaf_rn(p, q, 1.f / 11.f);
-  p = __fmaf_rn(p, q, 1.f / 9.f);
-  p = __fmaf_rn(p, q, 1.f / 7.f);
-  p = __fmaf_rn(p, q, 1.f / 5.f);
-  p = __fmaf_rn(p, q, 1.f / 3.f);
-  const float l = 2.f * __fmaf_rn(s * q, p, s);
-  return v > 0.f ? v + l : (v != v ? v : l);
+  float p = 2.f / 15.f;
+  p = __fmaf_rn(p, q, 2.f / 13.f);
+  p = __fmaf_rn(p, q, 2.f / 11.f);
+  p = __fmaf_rn(p, q, 2.f / 9.f);
+  p = __fmaf_rn(p, q, 2.f / 7.f);
+  p = __fmaf_rn(p, q, 2.f / 5.f);
+  p = __fmaf_rn(p, q, 2.f / 3.f);
+  const float l = __fmaf_rn(s * q, p, s + s);
+  return __fmaf_rn(v + __builtin_fabsf(v), 0.5f, l);  // (NaN stays)
 }
 __device__ __forceinline__ float sigmoid(float v) {
-  const float e = exp_neg(-__builtin_fabsf(v));
+  const float e = exp_neg(v);
   const float r = __builtin_amdgcn_rcpf(1.f + e);
-  return v >= 0.f ? r : e * r;  // (NaN stays)
+  return v >= 0.f ? r : e * r;
 }
 
 // A value of another lane of the row of 16 (DPP).
@@ -78,6 +81,7 @@ struct SelShape {
   static constexpr int NP = 4 * LN;               // states, with the empty places
   static constexpr int QUADS = CB / 4;            // of a token's row
   static constexpr int EACH = (kSelTile * QUADS + kBlock - 1) / kBlock;  // of a thread
+  static constexpr int STEP = kBlock / QUADS;     // tokens between two of a thread's
   static_assert(kBlock % QUADS == 0, "a thread keeps its channels from token to token");
 };
 
@@ -87,6 +91,7 @@ struct SelPlace {
   using S = SelShape<LN>;
   int head, c0, nc;  // the head, the workgroup's first channel, its channels
   int quad, qn, q0;  // a thread's quad of channels in a row, how many are there, the first
+  int k0;            // the first of a tile's tokens that the thread brings in
   int lane_c, nl;    // a lane's channels (of the workgroup) and states
   __device__ __forceinline__ SelPlace(const SelCall& c, const SelPlan& p, int block) {
     const int t = threadIdx.x, Dg = c.D / c.groups;
@@ -95,6 +100,7 @@ struct SelPlace {
     c0 = head * Dg + b * S::CB;
     nc = min(S::CB, Dg - b * S::CB);
     quad = t % S::QUADS;
+    k0 = t / S::QUADS;
     qn = max(0, min(4, nc - 4 * quad));
     q0 = qn ? c0 + 4 * quad : c0;
     const int lane = t & (kWave - 1);
@@ -112,6 +118,20 @@ __device__ __forceinline__ void put_quad(T* p, const float (&v)[4], int n) {
   if (n == 4) store_quad<T, true>(p, v, 4);
   else store_quad<T, false>(p, v, n);
 }
+// A thread's place in a tile of a tensor: an offset of 32 bits (rows are less than 2^25
+// elements apart) behind the tile's row, which is the same for the whole wave.
+struct RowSpot {
+  uint32_t off;
+  template <class T>
+  static __device__ __forceinline__ RowSpot of(const T*, int64_t ld, int k0, int q0) {
+    return RowSpot{((uint32_t)k0 * (uint32_t)ld + (uint32_t)q0) * (uint32_t)sizeof(T)};
+  }
+  template <class T>
+  __device__ __forceinline__ T* at(T* base, int64_t ld, int64_t row) const {
+    return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(base + row * ld) + off);
+  }
+};
+
 template <class T>
 __device__ __forceinline__ float load_one(const T* p) { return Elem<T>::get(*p); }
 
@@ -125,6 +145,20 @@ __device__ __forceinline__ void store_states(float* row, int N, int nl, const fl
   for (int j = 0; j < 4; ++j)
     if (4 * nl + j < N) row[4 * nl + j] = h[j];
 }
+
+// A tile's quads of a tensor on their way to a thread.
+template <class T, class S>
+struct QuadTile {
+  Quad<T> q[S::EACH];
+  __device__ __forceinline__ void load(const T* base, int64_t ld, RowSpot spot, int t0, int count, int k0,
+                                       int qn) {
+#pragma unroll
+    for (int e = 0; e < S::EACH; ++e) {
+      q[e] = Quad<T>{};
+      if (k0 + e * S::STEP < count && qn > 0) q[e] = some_quad(spot.at(base, ld, t0 + e * S::STEP), qn);
+    }
+  }
+};
 
 // A tile's rows of B or C in 32 bits, empty places zero.
 template <class T, int LN>
@@ -187,7 +221,7 @@ struct alignas(16) SelLds {
   using S = SelShape<LN>;
   float step[kSelTile * S::CB], dx[kSelTile * S::CB];
   float B[kSelTile * S::NP], C[kSelTile * S::NP];
-  int start[kSelTile], stop[kSelTile];
+  TileMarks marks;
   int from;
 };
 
@@ -252,30 +286,35 @@ __global__ __launch_bounds__(kBlock) void k_selective_ends(SelCall c, SelPlan p)
   float bias[4] = {0.f, 0.f, 0.f, 0.f};
   if (c.bias)
     for (int k = 0; k < w.qn; ++k) bias[k] = c.bias[w.q0 + k];
-  const T* x = static_cast<const T*>(c.x) + w.q0;
-  const T* delta = static_cast<const T*>(c.delta) + w.q0;
+  const T* x = static_cast<const T*>(c.x);
+  const T* delta = static_cast<const T*>(c.delta);
+  const RowSpot xs = RowSpot::of(x, c.ld_x, w.k0, w.q0), ds = RowSpot::of(x, c.ld_delta, w.k0, w.q0);
+  QuadTile<T, S> xn, dn;  // the next tile's
+  const auto fetch = [&](int t0) {
+    const int count = min(kSelTile, hi - t0);
+    xn.load(x, c.ld_x, xs, t0, count, w.k0, w.qn);
+    dn.load(delta, c.ld_delta, ds, t0, count, w.k0, w.qn);
+  };
+  fetch(from);
 
   for (int t0 = from; t0 < hi; t0 += kSelTile) {
     const int count = min(kSelTile, hi - t0);
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < S::EACH; ++e) {
-      const int i = t + e * kBlock, k = i / S::QUADS;
+      const int i = t + e * kBlock, k = w.k0 + e * S::STEP;
       if (k >= kSelTile) continue;
-      float d[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f};
-      if (k < count && w.qn > 0) {
-        const Quad<T> xv = some_quad(x + (t0 + (int64_t)k) * c.ld_x, w.qn);
-        const Quad<T> dv = some_quad(delta + (t0 + (int64_t)k) * c.ld_delta, w.qn);
-        for (int j = 0; j < 4; ++j) {
-          if (j >= w.qn) continue;
-          d[j] = step_of(dv.get(j), bias[j], c.softplus);
-          u[j] = d[j] * xv.get(j);
-        }
+      float d[4], u[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        d[j] = k < count && j < w.qn ? step_of(dn.q[e].get(j), bias[j], c.softplus) : 0.f;
+        u[j] = d[j] * xn.q[e].get(j);
       }
       st4(s.step + i * 4, f4{d[0], d[1], d[2], d[3]});
       st4(s.dx + i * 4, f4{u[0], u[1], u[2], u[3]});
     }
     stage_states<T, LN>(static_cast<const T*>(c.B), c.ld_B, t0, count, w.head, c.N, s.B);
+    if (t0 + kSelTile < hi) fetch(t0 + kSelTile);
     __syncthreads();
 #pragma unroll 4
     for (int k = 0; k < kSelTile; ++k) {  // (tokens past the range: no step, nothing added)
@@ -326,6 +365,20 @@ __global__ __launch_bounds__(kBlock) void k_selective(SelCall c, SelPlan p) {
   });
   if (lo >= hi) return;
 
+  const T* x = static_cast<const T*>(c.x);
+  const T* delta = static_cast<const T*>(c.delta);
+  const T* z = static_cast<const T*>(c.z);
+  T* y = static_cast<T*>(c.y);
+  const RowSpot xs = RowSpot::of(x, c.ld_x, w.k0, w.q0), ds = RowSpot::of(x, c.ld_delta, w.k0, w.q0);
+  const RowSpot zs = RowSpot::of(x, c.ld_z, w.k0, w.q0), ys = RowSpot::of(x, c.ld_y, w.k0, w.q0);
+  QuadTile<T, S> xn, dn, zn;  // the next tile's
+  const auto fetch = [&](int t0) {
+    const int count = min(kSelTile, hi - t0);
+    xn.load(x, c.ld_x, xs, t0, count, w.k0, w.qn);
+    dn.load(delta, c.ld_delta, ds, t0, count, w.k0, w.qn);
+    if (c.z) zn.load(z, c.ld_z, zs, t0, count, w.k0, w.qn);
+  };
+  fetch(lo);
   float A[2][4], h[2][4];
   load_rates(c, w, A);
   float bias[4] = {0.f, 0.f, 0.f, 0.f}, skip[4] = {0.f, 0.f, 0.f, 0.f};
@@ -333,40 +386,35 @@ __global__ __launch_bounds__(kBlock) void k_selective(SelCall c, SelPlan p) {
     if (c.bias) bias[k] = c.bias[w.q0 + k];
     if (c.skip) skip[k] = c.skip[w.q0 + k];
   }
-  const T* x = static_cast<const T*>(c.x) + w.q0;
-  const T* delta = static_cast<const T*>(c.delta) + w.q0;
-  const T* z = static_cast<const T*>(c.z) + w.q0;
-  T* y = static_cast<T*>(c.y) + w.q0;
+  UpCursor cursor{};
+  if (t < kWave) cursor.read(c.seqs, first_place(c.seqs, lo));
 
-  int cursor = 0;
-  if (t < kWave) cursor = first_place(c.seqs, lo);
   for (int t0 = lo; t0 < hi; t0 += kSelTile) {
     const int count = min(kSelTile, hi - t0);
-    Quad<T> xv[S::EACH];
+    const QuadTile<T, S> xv = xn, zv = zn;
 #pragma unroll
     for (int e = 0; e < S::EACH; ++e) {
-      const int i = t + e * kBlock, k = i / S::QUADS;
+      const int i = t + e * kBlock, k = w.k0 + e * S::STEP;
       if (k >= kSelTile) continue;
-      float d[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f};
-      xv[e] = Quad<T>{};
-      if (k < count && w.qn > 0) {
-        xv[e] = some_quad(x + (t0 + (int64_t)k) * c.ld_x, w.qn);
-        const Quad<T> dv = some_quad(delta + (t0 + (int64_t)k) * c.ld_delta, w.qn);
-        for (int j = 0; j < 4; ++j) {
-          if (j >= w.qn) continue;
-          d[j] = step_of(dv.get(j), bias[j], c.softplus);
-          u[j] = d[j] * xv[e].get(j);
-        }
+      const bool there = k < count;
+      float d[4], u[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        d[j] = there && j < w.qn ? step_of(dn.q[e].get(j), bias[j], c.softplus) : 0.f;
+        u[j] = d[j] * xv.q[e].get(j);
       }
       st4(s.step + i * 4, f4{d[0], d[1], d[2], d[3]});
       st4(s.dx + i * 4, f4{u[0], u[1], u[2], u[3]});
     }
     stage_states<T, LN>(static_cast<const T*>(c.B), c.ld_B, t0, count, w.head, c.N, s.B);
     stage_states<T, LN>(static_cast<const T*>(c.C), c.ld_C, t0, count, w.head, c.N, s.C);
-    if (t < kWave) cursor = mark_places(c.seqs, t0, t0 + count, kSelTile, cursor, s.start, s.stop);
+    if (t < kWave) mark_tile(c.seqs, t0, t0 + count, cursor, s.marks);
     __syncthreads();
+    const uint32_t starts = __builtin_amdgcn_readfirstlane(s.marks.starts);
+    const uint32_t stops = __builtin_amdgcn_readfirstlane(s.marks.stops);
+    if (t0 + kSelTile < hi) fetch(t0 + kSelTile);
     if (t0 == lo) {
-      if (s.start[0] < 0 && lo > 0) {
+      if (!(starts & 1) && lo > 0) {
         carry_into<LN>(c, p, range, 1, w, A, h);
       } else {
 #pragma unroll
@@ -383,12 +431,7 @@ __global__ __launch_bounds__(kBlock) void k_selective(SelCall c, SelPlan p) {
         st4(c.marks + at * p.NM + 4 * w.nl, f4{h[r][0], h[r][1], h[r][2], h[r][3]});
       }
     }
-    for (int k = 0; k < count; ++k) {
-      const int from = __builtin_amdgcn_readfirstlane(s.start[k]);
-      if (from >= 0) {
-#pragma unroll
-        for (int r = 0; r < 2; ++r) load_states(row_of(c.h0, from, r), c.N, w.nl, h[r]);
-      }
+    const auto token = [&](int k) {
       const float2 d = *reinterpret_cast<const float2*>(s.step + k * S::CB + w.lane_c);
       const float2 u = *reinterpret_cast<const float2*>(s.dx + k * S::CB + w.lane_c);
       const f4 B = ld4(s.B + k * S::NP + 4 * w.nl), C = ld4(s.C + k * S::NP + 4 * w.nl);
@@ -405,29 +448,42 @@ __global__ __launch_bounds__(kBlock) void k_selective(SelCall c, SelPlan p) {
         out[r] = sum_states<LN>(v);
       }
       if (w.nl == 0) *reinterpret_cast<float2*>(sy + k * S::CB + w.lane_c) = float2{out[0], out[1]};
-      const int to = __builtin_amdgcn_readfirstlane(s.stop[k]);
-      if (to >= 0 && c.last) {
+    };
+    if ((starts | stops) == 0) {  // (tokens past the range have no step and add nothing)
+#pragma unroll 4
+      for (int k = 0; k < kSelTile; ++k) token(k);
+    } else {
+      for (int k = 0; k < count; ++k) {
+        if (starts >> k & 1) {
+          const int from = __builtin_amdgcn_readfirstlane(s.marks.start[k]);
 #pragma unroll
-        for (int r = 0; r < 2; ++r)
-          if (float* row = row_of(c.last, to, r)) store_states(row, c.N, w.nl, h[r]);
+          for (int r = 0; r < 2; ++r) load_states(row_of(c.h0, from, r), c.N, w.nl, h[r]);
+        }
+        token(k);
+        if ((stops >> k & 1) && c.last) {
+          const int to = __builtin_amdgcn_readfirstlane(s.marks.stop[k]);
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+            if (float* row = row_of(c.last, to, r)) store_states(row, c.N, w.nl, h[r]);
+        }
       }
     }
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < S::EACH; ++e) {
-      const int i = t + e * kBlock, k = i / S::QUADS;
+      const int i = t + e * kBlock, k = w.k0 + e * S::STEP;
       if (k >= count || w.qn <= 0) continue;
       const f4 q = ld4(sy + i * 4);
-      float v[4];
+      float v[4] = {q[0], q[1], q[2], q[3]};
+      if (c.skip) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = __fmaf_rn(skip[j], xv[e].get(j), q[j]);
-      if (!c.skip) v[0] = q[0], v[1] = q[1], v[2] = q[2], v[3] = q[3];
-      if (c.z) {
-        const Quad<T> zv = some_quad(z + (t0 + (int64_t)k) * c.ld_z, w.qn);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] *= zv.get(j) * sigmoid(zv.get(j));
+        for (int j = 0; j < 4; ++j) v[j] = __fmaf_rn(skip[j], xv.q[e].get(j), q[j]);
       }
-      put_quad(y + (t0 + (int64_t)k) * c.ld_y, v, w.qn);
+      if (c.z) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] *= zv.q[e].get(j) * sigmoid(zv.q[e].get(j));
+      }
+      put_quad(ys.at(y, c.ld_y, t0 + e * S::STEP), v, w.qn);
     }
   }
 }

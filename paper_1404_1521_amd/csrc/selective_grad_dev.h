@@ -37,44 +37,46 @@ __device__ __forceinline__ void sum_channels(const float (&v)[8], float (&out)[2
   }
 }
 
-template <class T>
-__device__ __forceinline__ float gated(float dy, const T* z, float& zv, float& sg) {
-  zv = load_one(z);
-  sg = sigmoid(zv);
-  return dy * zv * sg;
-}
+// A value that is computed at this place: the compiler otherwise moves a sum to where it is
+// read and keeps all its terms until then, which took 64 registers more.
+__device__ __forceinline__ void here(float& v) { asm volatile("" : "+v"(v)); }
+
+// Where a thread finds its quads of the gradient's inputs.
+struct GradSpots {
+  RowSpot x, delta, dy, z;
+  template <class T, class W>
+  static __device__ __forceinline__ GradSpots of(const SelCall& c, const T* type, const W& w) {
+    return GradSpots{RowSpot::of(type, c.ld_x, w.k0, w.q0), RowSpot::of(type, c.ld_delta, w.k0, w.q0),
+                     RowSpot::of(type, c.ld_dy, w.k0, w.q0), RowSpot::of(type, c.ld_z, w.k0, w.q0)};
+  }
+};
 
 // A tile's steps, D x (if x) and v' in LDS.  Tokens past the tile's and channels past the
 // workgroup's: zeros, which change nothing.
 template <class T, int LN, bool X>
-__device__ __forceinline__ void stage_grad(const SelCall& c, const SelPlace<LN>& w, int t0, int count,
-                                           const float (&bias)[4], float* step, float* dx,
-                                           float* dv) {
+__device__ __forceinline__ void stage_grad(const SelCall& c, const SelPlace<LN>& w, const GradSpots& at,
+                                           int t0, int count, const float (&bias)[4], float* step,
+                                           float* dx, float* dv) {
   using S = SelShape<LN>;
-  const T* x = static_cast<const T*>(c.x) + w.q0;
-  const T* delta = static_cast<const T*>(c.delta) + w.q0;
-  const T* dy = static_cast<const T*>(c.dy) + w.q0;
-  const T* z = static_cast<const T*>(c.z) + w.q0;
+  QuadTile<T, S> raw, gy, xv, zv;
+  raw.load(static_cast<const T*>(c.delta), c.ld_delta, at.delta, t0, count, w.k0, w.qn);
+  gy.load(static_cast<const T*>(c.dy), c.ld_dy, at.dy, t0, count, w.k0, w.qn);
+  if (X) xv.load(static_cast<const T*>(c.x), c.ld_x, at.x, t0, count, w.k0, w.qn);
+  if (c.z) zv.load(static_cast<const T*>(c.z), c.ld_z, at.z, t0, count, w.k0, w.qn);
 #pragma unroll
   for (int e = 0; e < S::EACH; ++e) {
-    const int i = threadIdx.x + e * kBlock, k = i / S::QUADS;
+    const int i = threadIdx.x + e * kBlock, k = w.k0 + e * S::STEP;
     if (k >= kSelTile) continue;
-    float d[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f}, g[4] = {0.f, 0.f, 0.f, 0.f};
-    if (k < count && w.qn > 0) {
-      const int64_t row = t0 + (int64_t)k;
-      const Quad<T> raw = some_quad(delta + row * c.ld_delta, w.qn);
-      const Quad<T> gy = some_quad(dy + row * c.ld_dy, w.qn);
-      Quad<T> xv{}, zv{};
-      if (X) xv = some_quad(x + row * c.ld_x, w.qn);
-      if (c.z) zv = some_quad(z + row * c.ld_z, w.qn);
+    float d[4], u[4], g[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (j >= w.qn) continue;
-        d[j] = step_of(raw.get(j), bias[j], c.softplus);
-        if (X) u[j] = d[j] * xv.get(j);
-        g[j] = gy.get(j);
-        if (c.z) g[j] *= zv.get(j) * sigmoid(zv.get(j));
-      }
+    for (int j = 0; j < 4; ++j) {
+      d[j] = k < count && j < w.qn ? step_of(raw.q[e].get(j), bias[j], c.softplus) : 0.f;
+      if (X) u[j] = d[j] * xv.q[e].get(j);
+      g[j] = gy.q[e].get(j);
+    }
+    if (c.z) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) g[j] *= zv.q[e].get(j) * sigmoid(zv.q[e].get(j));
     }
     st4(step + i * 4, f4{d[0], d[1], d[2], d[3]});
     if (X) st4(dx + i * 4, f4{u[0], u[1], u[2], u[3]});
@@ -113,10 +115,11 @@ __global__ __launch_bounds__(kBlock) void k_selective_grad_ends(SelCall c, SelPl
   float bias[4] = {0.f, 0.f, 0.f, 0.f};
   if (c.bias)
     for (int k = 0; k < w.qn; ++k) bias[k] = c.bias[w.q0 + k];
+  const GradSpots at = GradSpots::of(c, static_cast<const T*>(nullptr), w);
   for (int tile = (to - 1 - lo) / kSelTile; tile >= 0; --tile) {
     const int t0 = lo + tile * kSelTile, count = min(kSelTile, to - t0);
     __syncthreads();
-    stage_grad<T, LN, false>(c, w, t0, count, bias, s.step, nullptr, s.dx);
+    stage_grad<T, LN, false>(c, w, at, t0, count, bias, s.step, nullptr, s.dx);
     stage_states<T, LN>(static_cast<const T*>(c.C), c.ld_C, t0, count, w.head, c.N, s.C);
     __syncthreads();
 #pragma unroll 4
@@ -191,15 +194,19 @@ __global__ __launch_bounds__(kBlock, 2) void k_selective_grad(SelCall c, SelPlan
   }
 
   const int tiles = lo < hi ? ceil_div(hi - lo, kSelTile) : 0;
+  DownCursor cursor{};
+  if (t < kWave) cursor.read(c.seqs, first_place(c.seqs, hi + 1));
+  const GradSpots at = GradSpots::of(c, static_cast<const T*>(nullptr), w);
   for (int tile = tiles - 1; tile >= 0; --tile) {
     const int t0 = lo + tile * kSelTile, count = min(kSelTile, hi - t0);
-    stage_grad<T, LN, true>(c, w, t0, count, bias, s.step, s.dx, g.dv);
+    stage_grad<T, LN, true>(c, w, at, t0, count, bias, s.step, s.dx, g.dv);
     stage_states<T, LN>(static_cast<const T*>(c.B), c.ld_B, t0, count, w.head, c.N, s.B);
     stage_states<T, LN>(static_cast<const T*>(c.C), c.ld_C, t0, count, w.head, c.N, s.C);
-    if (t < kWave)
-      mark_places(c.seqs, t0, t0 + count, kSelTile, first_place(c.seqs, t0), s.start, s.stop);
+    if (t < kWave) mark_tile(c.seqs, t0, t0 + count, cursor, s.marks);
     __syncthreads();
-    if (tile == tiles - 1 && s.stop[count - 1] < 0 && hi < c.seqs.tokens)
+    const uint32_t starts = __builtin_amdgcn_readfirstlane(s.marks.starts);
+    const uint32_t stops = __builtin_amdgcn_readfirstlane(s.marks.stops);
+    if (tile == tiles - 1 && !(stops >> (count - 1) & 1) && hi < c.seqs.tokens)
       carry_into<LN>(c, p, range, -1, w, A, mu);
 
     // the states before the first half, and before the second one
@@ -212,136 +219,160 @@ __global__ __launch_bounds__(kBlock, 2) void k_selective_grad(SelCall c, SelPlan
 #pragma unroll
       for (int j = 0; j < 4; ++j) first[r][j] = h[r][j] = m[j];
     }
-    // one token forward; decays into a
-    const auto forward = [&](int k, float (&a)[2][4]) {
-      const int from = __builtin_amdgcn_readfirstlane(s.start[k]);
-      if (from >= 0) {
-#pragma unroll
-        for (int r = 0; r < 2; ++r) load_states(row_of(c.h0, from, r), c.N, w.nl, h[r]);
-      }
-      const float2 d = *reinterpret_cast<const float2*>(s.step + k * S::CB + w.lane_c);
-      const float2 u = *reinterpret_cast<const float2*>(s.dx + k * S::CB + w.lane_c);
-      const f4 B = ld4(s.B + k * S::NP + 4 * w.nl);
-      const float dd[2] = {d.x, d.y}, uu[2] = {u.x, u.y};
-#pragma unroll
-      for (int r = 0; r < 2; ++r)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          a[r][j] = exp2_fast(dd[r] * A[r][j]);
-          h[r][j] = __fmaf_rn(a[r][j], h[r][j], uu[r] * B[j]);
+    const auto halves = [&](auto is_plain) {
+      constexpr bool PLAIN = decltype(is_plain)::value;  // no sequence starts or stops here
+      // What a token brings, on its way from LDS while the token before is worked on.
+      struct Token {
+        float2 d, u, dv;
+        f4 B, C;
+      };
+      const auto fetch = [&](int k, bool back) {
+        Token o;
+        o.d = *reinterpret_cast<const float2*>(s.step + k * S::CB + w.lane_c);
+        o.u = *reinterpret_cast<const float2*>(s.dx + k * S::CB + w.lane_c);
+        o.B = ld4(s.B + k * S::NP + 4 * w.nl);
+        if (back) {
+          o.dv = *reinterpret_cast<const float2*>(g.dv + k * S::CB + w.lane_c);
+          o.C = ld4(s.C + k * S::NP + 4 * w.nl);
         }
-    };
-    const bool second = count > H;
-    if (second) {
-      for (int k = 0; k < H; ++k) {
-        float a[2][4];
-        forward(k, a);
-      }
-    }
-    for (int half = second; half >= 0; --half) {
-      const int base = half * H;
-      float before[2][4], a[H][2][4], hs[H][2][4];
+        return o;
+      };
+      const auto forward = [&](int k, const Token& o) {
+        if (!PLAIN && (starts >> k & 1)) {
+          const int from = __builtin_amdgcn_readfirstlane(s.marks.start[k]);
 #pragma unroll
-      for (int r = 0; r < 2; ++r)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) before[r][j] = h[r][j] = half ? h[r][j] : first[r][j];
-#pragma unroll
-      for (int i = 0; i < H; ++i) {
-        forward(base + i, a[i]);
+          for (int r = 0; r < 2; ++r) load_states(row_of(c.h0, from, r), c.N, w.nl, h[r]);
+        }
+        const float dd[2] = {o.d.x, o.d.y}, uu[2] = {o.u.x, o.u.y};
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) hs[i][r][j] = h[r][j];
-      }
-#pragma unroll
-      for (int i = H - 1; i >= 0; --i) {
-        const int k = base + i;
-        const int to = __builtin_amdgcn_readfirstlane(s.stop[k]);
-        if (to >= 0) {
-#pragma unroll
-          for (int r = 0; r < 2; ++r) load_states(row_of(c.dlast, to, r), c.N, w.nl, mu[r]);
+          for (int j = 0; j < 4; ++j)
+            h[r][j] = __fmaf_rn(exp2_fast(dd[r] * A[r][j]), h[r][j], uu[r] * o.B[j]);
+      };
+      const bool second = count > H;
+      if (second) {
+        Token now = fetch(0, false);
+#pragma unroll 2
+        for (int k = 0; k < H; ++k) {
+          const Token next = fetch(k + 1, false);
+          forward(k, now);
+          __builtin_amdgcn_sched_barrier(0);
+          now = next;
         }
-        const int from = __builtin_amdgcn_readfirstlane(s.start[k]);
-        float hp[2][4];
+      }
+      for (int half = second; half >= 0; --half) {
+        const int base = half * H;
+        float before[2][4], hs[H][2][4];
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) hp[r][j] = i ? hs[i ? i - 1 : 0][r][j] : before[r][j];
-        if (from >= 0) {
+          for (int j = 0; j < 4; ++j) before[r][j] = h[r][j] = half ? h[r][j] : first[r][j];
+        Token now = fetch(base, false);
 #pragma unroll
-          for (int r = 0; r < 2; ++r) load_states(row_of(c.h0, from, r), c.N, w.nl, hp[r]);
+        for (int i = 0; i < H; ++i) {
+          const Token next = fetch(base + min(i + 1, H - 1), i == H - 1);
+          forward(base + i, now);
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) hs[i][r][j] = h[r][j];
+          __builtin_amdgcn_sched_barrier(0);
+          now = next;
         }
-        const float2 d = *reinterpret_cast<const float2*>(s.step + k * S::CB + w.lane_c);
-        const float2 u = *reinterpret_cast<const float2*>(s.dx + k * S::CB + w.lane_c);
-        const float2 dv = *reinterpret_cast<const float2*>(g.dv + k * S::CB + w.lane_c);
-        const f4 B = ld4(s.B + k * S::NP + 4 * w.nl), C = ld4(s.C + k * S::NP + 4 * w.nl);
-        const float dd[2] = {d.x, d.y}, uu[2] = {u.x, u.y}, vv[2] = {dv.x, dv.y};
-        float both[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};  // dB, dC
-        float e[2], ds[2], v[2];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          e[r] = ds[r] = v[r] = 0.f;
+        for (int i = H - 1; i >= 0; --i) {
+          const int k = base + i;
+          const Token next = fetch(base + max(i - 1, 0), true);
+          if (!PLAIN && (stops >> k & 1)) {
+            const int to = __builtin_amdgcn_readfirstlane(s.marks.stop[k]);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float lam = __fmaf_rn(vv[r], C[j], mu[r][j]);
-            both[j] = __fmaf_rn(lam, uu[r], both[j]);
-            both[4 + j] = __fmaf_rn(vv[r], hs[i][r][j], both[4 + j]);
-            e[r] = __fmaf_rn(lam, B[j], e[r]);
-            v[r] = __fmaf_rn(C[j], hs[i][r][j], v[r]);
-            mu[r][j] = lam * a[i][r][j];
-            const float q = mu[r][j] * hp[r][j];
-            ds[r] = __fmaf_rn(q, A[r][j], ds[r]);
-            dA[r][j] = __fmaf_rn(q, dd[r], dA[r][j]);
+            for (int r = 0; r < 2; ++r) load_states(row_of(c.dlast, to, r), c.N, w.nl, mu[r]);
           }
-          e[r] = sum_states<LN>(e[r]);
-          ds[r] = sum_states<LN>(ds[r]);
-          v[r] = sum_states<LN>(v[r]);
-        }
-        if (w.nl == 0) {
-          *reinterpret_cast<float2*>(s.dx + k * S::CB + w.lane_c) = float2{e[0], e[1]};
-          *reinterpret_cast<float2*>(g.dstep + k * S::CB + w.lane_c) = float2{ds[0], ds[1]};
-          *reinterpret_cast<float2*>(g.dv + k * S::CB + w.lane_c) = float2{v[0], v[1]};
-        }
-        float pair[2];
-        sum_channels<LN>(both, pair);
-        if (lane % 16 < LN)
-          *reinterpret_cast<float2*>(&g.part[wave][k][lane / 32][4 * w.nl + 2 * (lane / 16 % 2)]) =
-              float2{pair[0], pair[1]};
-        if (from >= 0) {
+          const bool starts_here = !PLAIN && (starts >> k & 1);
+          int from = 0;
+          float hp[2][4];
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) hp[r][j] = i ? hs[i ? i - 1 : 0][r][j] : before[r][j];
+          if (starts_here) {
+            from = __builtin_amdgcn_readfirstlane(s.marks.start[k]);
+#pragma unroll
+            for (int r = 0; r < 2; ++r) load_states(row_of(c.h0, from, r), c.N, w.nl, hp[r]);
+          }
+          // (here: the decays are computed again, not kept from the way forward)
+          here(now.d.x), here(now.d.y);
+          const float dd[2] = {now.d.x, now.d.y}, uu[2] = {now.u.x, now.u.y};
+          const float vv[2] = {now.dv.x, now.dv.y};
+          const f4 B = now.B, C = now.C;
+          float both[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};  // dB, dC
+          float e[2], ds[2], v[2];
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            if (float* row = row_of(c.dh0, from, r)) store_states(row, c.N, w.nl, mu[r]);
+            e[r] = ds[r] = v[r] = 0.f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mu[r][j] = 0.f;
+            for (int j = 0; j < 4; ++j) {
+              const float lam = __fmaf_rn(vv[r], C[j], mu[r][j]);
+              both[j] = __fmaf_rn(lam, uu[r], both[j]);
+              both[4 + j] = __fmaf_rn(vv[r], hs[i][r][j], both[4 + j]);
+              e[r] = __fmaf_rn(lam, B[j], e[r]);
+              v[r] = __fmaf_rn(C[j], hs[i][r][j], v[r]);
+              mu[r][j] = lam * exp2_fast(dd[r] * A[r][j]);
+              const float q = mu[r][j] * hp[r][j];
+              ds[r] = __fmaf_rn(q, A[r][j], ds[r]);
+              dA[r][j] = __fmaf_rn(q, dd[r], dA[r][j]);
+              here(dA[r][j]);
+            }
+            e[r] = sum_states<LN>(e[r]);
+            ds[r] = sum_states<LN>(ds[r]);
+            v[r] = sum_states<LN>(v[r]);
           }
+          if (w.nl == 0) {
+            *reinterpret_cast<float2*>(s.dx + k * S::CB + w.lane_c) = float2{e[0], e[1]};
+            *reinterpret_cast<float2*>(g.dstep + k * S::CB + w.lane_c) = float2{ds[0], ds[1]};
+            *reinterpret_cast<float2*>(g.dv + k * S::CB + w.lane_c) = float2{v[0], v[1]};
+          }
+          float pair[2];
+          sum_channels<LN>(both, pair);
+          if (lane % 16 < LN)
+            *reinterpret_cast<float2*>(&g.part[wave][k][lane / 32][4 * w.nl + 2 * (lane / 16 % 2)]) =
+                float2{pair[0], pair[1]};
+          if (starts_here) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              if (float* row = row_of(c.dh0, from, r)) store_states(row, c.N, w.nl, mu[r]);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) mu[r][j] = 0.f;
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          now = next;
         }
       }
-    }
+    };
+    if ((starts | stops) == 0) halves(std::true_type{});
+    else halves(std::false_type{});
     __syncthreads();
-    const T* x = static_cast<const T*>(c.x) + w.q0;
-    const T* delta = static_cast<const T*>(c.delta) + w.q0;
-    const T* dy = static_cast<const T*>(c.dy) + w.q0;
-    const T* z = static_cast<const T*>(c.z) + w.q0;
+    QuadTile<T, S> raw, gy, xv, zv;
+    raw.load(static_cast<const T*>(c.delta), c.ld_delta, at.delta, t0, count, w.k0, w.qn);
+    gy.load(static_cast<const T*>(c.dy), c.ld_dy, at.dy, t0, count, w.k0, w.qn);
+    xv.load(static_cast<const T*>(c.x), c.ld_x, at.x, t0, count, w.k0, w.qn);
+    if (c.z) zv.load(static_cast<const T*>(c.z), c.ld_z, at.z, t0, count, w.k0, w.qn);
 #pragma unroll
     for (int el = 0; el < S::EACH; ++el) {
-      const int i = t + el * kBlock, k = i / S::QUADS;
+      const int i = t + el * kBlock, k = w.k0 + el * S::STEP;
       if (k >= count || w.qn <= 0) continue;
-      const int64_t row = t0 + (int64_t)k;
-      const Quad<T> xv = some_quad(x + row * c.ld_x, w.qn);
-      const Quad<T> raw = some_quad(delta + row * c.ld_delta, w.qn);
-      const Quad<T> gy = some_quad(dy + row * c.ld_dy, w.qn);
       const f4 e = ld4(s.dx + i * 4), st = ld4(s.step + i * 4), ds = ld4(g.dstep + i * 4);
       const f4 sv = ld4(g.dv + i * 4);
-      Quad<T> zv{};
-      if (c.z) zv = some_quad(z + row * c.ld_z, w.qn);
       float ox[4], od[4], oz[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float xj = xv.get(j);
-        float gv = gy.get(j);
+        const float xj = xv.q[el].get(j);
+        float gv = gy.q[el].get(j);
         oz[j] = 0.f;
         if (c.z) {
-          const float zj = zv.get(j), sg = sigmoid(zj);
+          const float zj = zv.q[el].get(j), sg = sigmoid(zj);
           const float v = c.skip ? __fmaf_rn(skip[j], xj, sv[j]) : sv[j];
           oz[j] = gv * v * (sg * __fmaf_rn(zj, 1.f - sg, 1.f));
           gv *= zj * sg;
@@ -349,15 +380,19 @@ __global__ __launch_bounds__(kBlock, 2) void k_selective_grad(SelCall c, SelPlan
         ox[j] = st[j] * e[j];
         if (c.skip) ox[j] = __fmaf_rn(skip[j], gv, ox[j]);
         od[j] = __fmaf_rn(xj, e[j], kLn2 * ds[j]);
-        if (c.softplus) od[j] *= sigmoid(raw.get(j) + bias[j]);
+        if (c.softplus) od[j] *= sigmoid(raw.q[el].get(j) + bias[j]);
         if (j < w.qn) {
           dskip[j] = __fmaf_rn(gv, xj, dskip[j]);
           dbias[j] += od[j];
         }
       }
-      put_quad(static_cast<T*>(c.dx) + w.q0 + row * c.ld_dx, ox, w.qn);
-      put_quad(static_cast<T*>(c.ddelta) + w.q0 + row * c.ld_ddelta, od, w.qn);
-      if (c.z) put_quad(static_cast<T*>(c.dz) + w.q0 + row * c.ld_dz, oz, w.qn);
+      const auto put = [&](void* base, int64_t ld, const float (&v)[4]) {
+        T* to = static_cast<T*>(base);
+        put_quad(RowSpot::of(to, ld, w.k0, w.q0).at(to, ld, t0 + el * S::STEP), v, w.qn);
+      };
+      put(c.dx, c.ld_dx, ox);
+      put(c.ddelta, c.ld_ddelta, od);
+      if (c.z) put(c.dz, c.ld_dz, oz);
     }
     for (int i = t; i < count * 2 * S::NP; i += kBlock) {
       const int k = i / (2 * S::NP), which = i / S::NP % 2, n = i % S::NP;

@@ -1,0 +1,8 @@
+// The selective scan's gradient in one format.
+#include "selective_grad_launch.h"
+
+namespace pg {
+
+template hipError_t selective_grad<F16>(const SelCall&, const SelPlan&, const Launch&);
+
+}  // namespace pg
