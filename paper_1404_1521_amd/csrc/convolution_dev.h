@@ -124,7 +124,7 @@ __global__ __launch_bounds__(kBlock) void k_convolution(ConvCall c) {
   const ConvPlace w(c, block);
   const int tokens = (kBlock >> c.lanes_log2) * R;
   const int lo = tile * tokens;
-  check_places(c.seqs, tile, c.tiles, c.last != nullptr && K > 1, l.list,
+  check_places(c.seqs, tile, c.tiles, kBlock, c.last != nullptr && K > 1, l.list,
                [&](int i) { conv_copy<T>(c, K, i, c.state, c.last, w); });
   if (lo >= c.seqs.tokens) return;
   const int t0 = lo + w.tl * R, count = max(0, min(R, c.seqs.tokens - t0));
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(kBlock) void k_convolution_grad(ConvCall c) {
   const int group = blockIdx.x / c.blocks, block = blockIdx.x % c.blocks;
   const ConvPlace w(c, block);
   const int CT = 1 << c.lanes_log2, TL = kBlock >> c.lanes_log2, tokens = TL * R;
-  check_places(c.seqs, group, c.groups, c.dstate != nullptr && K > 1, l.list,
+  check_places(c.seqs, group, c.groups, kBlock, c.dstate != nullptr && K > 1, l.list,
                [&](int i) { conv_copy<T>(c, K, i, c.dlast, c.dstate, w); });
   float wt[K][4], bias[4], dw[K][4], db[4] = {0.f, 0.f, 0.f, 0.f};
   conv_weights<K>(c, w, wt, bias);

@@ -98,6 +98,11 @@ constexpr int kSelectiveTile = 16;  // POLYGLOT_SELECTIVE_MARK
 // sequence that starts in it, or its own carry too.
 constexpr uint32_t kSelNone = 0, kSelClosed = 1, kSelOpen = 2;
 
+// A kernel's lanes to a channel (four states each), its waves and its channels.
+__host__ __device__ constexpr int sel_lanes(int N) { return N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
+__host__ __device__ constexpr int sel_waves(int lanes) { return lanes == 2 ? 2 : 4; }
+__host__ __device__ constexpr int sel_channels(int lanes) { return sel_waves(lanes) * 2 * kWave / lanes; }
+
 // How a selective scan is cut: a workgroup for each range of tokens and block of channels.
 struct SelPlan {
   int range, ranges;       // tokens of a range

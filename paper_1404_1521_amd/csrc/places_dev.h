@@ -114,10 +114,10 @@ __device__ __forceinline__ void mark_tile(const Packed& s, int lo, int hi, DownC
 // the offsets do not ascend from 0 to the tokens, and calls copy(i) with every thread for
 // each empty sequence i.
 template <class F>
-__device__ __forceinline__ void check_places(const Packed& s, int part, int parts, bool copies,
-                                             int* list, F copy) {
+__device__ __forceinline__ void check_places(const Packed& s, int part, int parts, int threads,
+                                             bool copies, int* list, F copy) {
   const int t = threadIdx.x;
-  for (int64_t base = (int64_t)part * kBlock; base < s.nseq; base += (int64_t)parts * kBlock) {
+  for (int64_t base = (int64_t)part * threads; base < s.nseq; base += (int64_t)parts * threads) {
     const int i = (int)base + t;
     bool empty = false;
     if (i < s.nseq) {
@@ -137,8 +137,8 @@ __device__ __forceinline__ void check_places(const Packed& s, int part, int part
     if (!__syncthreads_or(empty)) continue;
     list[t] = empty ? i : -1;
     __syncthreads();
-    for (int j = 0; j < kBlock; ++j)
-      if (list[j] >= 0) copy(list[j]);
+    for (int j = 0; j < threads; ++j)
+      if (list[j] >= 0) copy(__builtin_amdgcn_readfirstlane(list[j]));
     __syncthreads();
   }
 }

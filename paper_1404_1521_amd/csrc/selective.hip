@@ -7,13 +7,14 @@ namespace pg {
 namespace {
 
 template <class T, int LN>
-hipError_t forward(const SelCall& c, SelPlan p, const Launch& L) {
+hipError_t forward(const SelCall& c, const SelPlan& p, const Launch& L) {
+  const dim3 block(SelShape<LN>::THREADS);
   const dim3 grid((uint32_t)p.ranges * p.all_blocks);
   if (p.ranges > 1) {
-    const hipError_t e = pg_launch(k_selective_ends<T, LN>, grid, dim3(kBlock), 0, L, c, p);
+    const hipError_t e = pg_launch(k_selective_ends<T, LN>, grid, block, 0, L, SelArgs{c, p});
     if (e != hipSuccess) return e;
   }
-  return pg_launch(k_selective<T, LN>, grid, dim3(kBlock), 0, L, c, p);
+  return pg_launch(k_selective<T, LN>, grid, block, 0, L, SelArgs{c, p});
 }
 
 template <class T, int LN>
@@ -26,7 +27,7 @@ hipError_t step(const SelCall& c, const Launch& L) {
 // Channels times ranges of any call of up to D channels: one range, or as many as give
 // the workgroups of up to CB channels.
 int64_t range_channels(int D, int N) {
-  return std::max<int64_t>(D, (int64_t)kSelWorkgroups * (512 / sel_lanes(N)));
+  return std::max<int64_t>(D, (int64_t)kSelWorkgroups * sel_channels(sel_lanes(N)));
 }
 
 }  // namespace
@@ -42,7 +43,7 @@ SelRoom selective_room(int64_t tokens, int D, int N) {
   r.info = (size_t)std::max<int64_t>(kSelWorkgroups, 1);
   r.part_s = 2 * (size_t)rc;
   // blocks of a head's channels, where there are two or more: at most twice D / CB
-  r.part_bc = (size_t)tokens * 2 * N * (2 * (size_t)D / (512 / LN) + 2);
+  r.part_bc = (size_t)tokens * 2 * N * (2 * (size_t)D / sel_channels(LN) + 2);
   return r;
 }
 

@@ -3,10 +3,10 @@
 //   v_t[c] = sum_n C_t[n] h_t[c][n] + skip[c] x_t[c],     y = v or v z sigmoid(z)
 //
 // A wave holds all states of a few channels: LN lanes of four states each for a channel,
-// two channels to a lane.  A state costs an exponential (a quarter of the vector rate)
-// and four operations a token; what a token brings for a channel (its step D, D x) or a
-// state (B, C) comes from LDS, where the workgroup has put a tile of 16 tokens, converted
-// once.  The sum over the states goes over LN lanes by DPP moves.
+// two channels to a lane.  A state costs an exponential (twice an operation's time) and four
+// operations a token; what a token brings for a channel (its step D, D x) or a state (B, C)
+// comes from LDS, where the workgroup has put a tile of 16 tokens, converted once.  The sum
+// over the states goes over LN lanes by DPP moves.
 //
 // The tokens are cut into ranges, a workgroup for each range and block of channels.  A
 // first launch takes every range that a sequence runs out of from the sequence's start in
@@ -71,42 +71,63 @@ __device__ __forceinline__ float sum_states(float v) {
   return v;
 }
 
+// The kernels' arguments, one block.  They are more than the scalar registers hold: `again`
+// hides where the block lies, so that a phase of a tile loads those it needs from the scalar
+// cache.  (Kept all the way they went to lanes of vector registers and came back one vector
+// instruction each, a third of a tile's staging.)
+struct SelArgs {
+  SelCall c;
+  SelPlan p;
+};
+typedef const __attribute__((address_space(4))) SelArgs* SelArgsPtr;
+__device__ __forceinline__ SelArgsPtr sel_args() {
+  return (SelArgsPtr)__builtin_amdgcn_kernarg_segment_ptr();
+}
+__device__ __forceinline__ const SelArgs& again(SelArgsPtr p) {
+  asm volatile("" : "+s"(p));
+  return *(const SelArgs*)p;
+}
+
 // Lanes, channels and places of a workgroup with LN lanes to a channel.
 template <int LN>
 struct SelShape {
-  static constexpr int RC = 2;                    // channels of a lane
-  static constexpr int CL = kWave / LN;           // lanes of a state
-  static constexpr int CW = CL * RC;              // channels of a wave
-  static constexpr int CB = CW * kWavesPerBlock;  // ... of a workgroup
-  static constexpr int NP = 4 * LN;               // states, with the empty places
-  static constexpr int QUADS = CB / 4;            // of a token's row
-  static constexpr int EACH = (kSelTile * QUADS + kBlock - 1) / kBlock;  // of a thread
-  static constexpr int STEP = kBlock / QUADS;     // tokens between two of a thread's
-  static_assert(kBlock % QUADS == 0, "a thread keeps its channels from token to token");
+  static constexpr int W = sel_waves(LN), THREADS = W * kWave;
+  static constexpr int RC = 2;             // channels of a lane
+  static constexpr int CL = kWave / LN;    // lanes of a state
+  static constexpr int CW = CL * RC;       // channels of a wave
+  static constexpr int CB = CW * W;        // ... of a workgroup
+  static constexpr int NP = 4 * LN;        // states, with the empty places
+  static constexpr int QUADS = CB / 4;     // of a token's row
+  static constexpr int EACH = (kSelTile * QUADS + THREADS - 1) / THREADS;  // of a thread
+  static constexpr int STEP = THREADS / QUADS;  // tokens between two of a thread's
+  static constexpr int STATES = (2 * kSelTile * LN + THREADS - 1) / THREADS;  // quads of B and C
+  static_assert(CB == sel_channels(LN) && THREADS % QUADS == 0, "a thread keeps its channels");
 };
 
-// What a workgroup works on.
+// What a workgroup, a thread and a lane work on.
 template <int LN>
 struct SelPlace {
   using S = SelShape<LN>;
   int head, c0, nc;  // the head, the workgroup's first channel, its channels
-  int quad, qn, q0;  // a thread's quad of channels in a row, how many are there, the first
-  int k0;            // the first of a tile's tokens that the thread brings in
+  int qn, q0, k0;    // a thread's quad of channels: how many are there, the first; its first token
   int lane_c, nl;    // a lane's channels (of the workgroup) and states
+  uint32_t rate;     // the byte offset of the lane's states in a row of A, or of a sequence
   __device__ __forceinline__ SelPlace(const SelCall& c, const SelPlan& p, int block) {
     const int t = threadIdx.x, Dg = c.D / c.groups;
     head = block / p.blocks;
     const int b = block - head * p.blocks;
     c0 = head * Dg + b * S::CB;
     nc = min(S::CB, Dg - b * S::CB);
-    quad = t % S::QUADS;
+    const int quad = t % S::QUADS;
     k0 = t / S::QUADS;
     qn = max(0, min(4, nc - 4 * quad));
     q0 = qn ? c0 + 4 * quad : c0;
     const int lane = t & (kWave - 1);
     nl = lane % LN;
     lane_c = t / kWave * S::CW + lane / LN * S::RC;
+    rate = ((uint32_t)(c0 + lane_c) * c.N + 4 * nl) * 4;
   }
+  __device__ __forceinline__ bool has(int r) const { return lane_c + r < nc; }
 };
 
 template <class T>
@@ -118,6 +139,18 @@ __device__ __forceinline__ void put_quad(T* p, const float (&v)[4], int n) {
   if (n == 4) store_quad<T, true>(p, v, 4);
   else store_quad<T, false>(p, v, n);
 }
+template <class T>
+__device__ __forceinline__ float load_one(const T* p) { return Elem<T>::get(*p); }
+// Four of a channel's values from q0 on (none there: zero).
+__device__ __forceinline__ void load_four(const float* p, int q0, int qn, float (&v)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = 0.f;
+  if (!p || qn == 0) return;
+  const Quad<float> q = some_quad(p + q0, qn);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = q.get(j);
+}
+
 // A thread's place in a tile of a tensor: an offset of 32 bits (rows are less than 2^25
 // elements apart) behind the tile's row, which is the same for the whole wave.
 struct RowSpot {
@@ -132,86 +165,186 @@ struct RowSpot {
   }
 };
 
-template <class T>
-__device__ __forceinline__ float load_one(const T* p) { return Elem<T>::get(*p); }
-
-// The states' rows: a lane's four of channel c (none past N: zero), and back.
-__device__ __forceinline__ void load_states(const float* row, int N, int nl, float (&h)[4]) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) h[j] = row && 4 * nl + j < N ? row[4 * nl + j] : 0.f;
-}
-__device__ __forceinline__ void store_states(float* row, int N, int nl, const float (&h)[4]) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (4 * nl + j < N) row[4 * nl + j] = h[j];
-}
-
-// A tile's quads of a tensor on their way to a thread.
-template <class T, class S>
-struct QuadTile {
-  Quad<T> q[S::EACH];
-  __device__ __forceinline__ void load(const T* base, int64_t ld, RowSpot spot, int t0, int count, int k0,
-                                       int qn) {
-#pragma unroll
-    for (int e = 0; e < S::EACH; ++e) {
-      q[e] = Quad<T>{};
-      if (k0 + e * S::STEP < count && qn > 0) q[e] = some_quad(spot.at(base, ld, t0 + e * S::STEP), qn);
-    }
-  }
-};
-
-// A tile's rows of B or C in 32 bits, empty places zero.
-template <class T, int LN>
-__device__ __forceinline__ void stage_states(const T* base, int64_t ld, int lo, int count, int head,
-                                             int N, float* to) {
-  constexpr int NP = 4 * LN;
-  for (int i = threadIdx.x; i < kSelTile * NP; i += kBlock) {
-    const int t = i / NP, n = i % NP;
-    to[i] = t < count && n < N ? load_one(base + (lo + (int64_t)t) * ld + (int64_t)head * N + n) : 0.f;
-  }
-}
-
-// The step of a token: what comes in, its bias, softplus.
-__device__ __forceinline__ float step_of(float v, float bias, int soft) {
-  v += bias;
-  return soft ? softplus(v) : v;
-}
-
-// The carry into a range from those before it (up: the gradient's, from those after it):
-// the nearest one that does not pass its own carry on, then each one's whole decay and
-// what it adds.
+// A lane's four states of channel r, in A or in a sequence's states (row: the same for the
+// whole wave); none past N: zero, and back.
 template <int LN>
-__device__ __forceinline__ void carry_into(const SelCall& c, const SelPlan& p, int range, int dir,
-                                           const SelPlace<LN>& w, const float (&A)[2][4],
-                                           float (&h)[2][4]) {
-  using S = SelShape<LN>;
-  int j = range - dir;
-  while (j - dir >= 0 && j - dir < p.ranges && p.info[j] == kSelOpen) j -= dir;
+__device__ __forceinline__ void load_states(const float* row, const SelPlace<LN>& w, int r, int N,
+                                            float (&h)[4]) {
 #pragma unroll
-  for (int r = 0; r < S::RC; ++r)
+  for (int j = 0; j < 4; ++j) h[j] = 0.f;
+  const int n = N - 4 * w.nl;
+  if (!row || !w.has(r) || n <= 0) return;
+  const float* p = reinterpret_cast<const float*>(reinterpret_cast<uintptr_t>(row + r * N) + w.rate);
+  const Quad<float> q = some_quad(p, min(n, 4));
 #pragma unroll
-    for (int k = 0; k < 4; ++k) h[r][k] = 0.f;
-  for (; j != range; j += dir) {
+  for (int j = 0; j < 4; ++j) h[j] = q.get(j);
+}
+template <int LN>
+__device__ __forceinline__ void store_states(float* row, const SelPlace<LN>& w, int r, int N,
+                                             const float (&h)[4]) {
+  const int n = N - 4 * w.nl;
+  if (!row || !w.has(r) || n <= 0) return;
+  float* p = reinterpret_cast<float*>(reinterpret_cast<uintptr_t>(row + r * N) + w.rate);
+  if (n >= 4) {
+    *reinterpret_cast<f4_any*>(p) = f4_any{h[0], h[1], h[2], h[3]};
+  } else {
 #pragma unroll
-    for (int r = 0; r < S::RC; ++r) {
-      if (w.lane_c + r >= w.nc) continue;
-      const int64_t at = (int64_t)j * c.D + w.c0 + w.lane_c + r;
-      const float d = p.sums[at];
-      const f4 s = ld4(p.states + at * S::NP + 4 * w.nl);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) h[r][k] = __fmaf_rn(exp2_fast(d * A[r][k]), h[r][k], s[k]);
-    }
+    for (int j = 0; j < 3; ++j)
+      if (j < n) p[j] = h[j];
   }
+}
+// The row of sequence i in [nseq][D][N].
+template <class F>
+__device__ __forceinline__ F* state_row(F* base, int i, const SelCall& c) {
+  return base ? base + (int64_t)i * c.D * c.N : nullptr;
 }
 
 template <int LN>
 __device__ __forceinline__ void load_rates(const SelCall& c, const SelPlace<LN>& w, float (&A)[2][4]) {
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
-    const float* row = w.lane_c + r < w.nc ? c.A + (int64_t)(w.c0 + w.lane_c + r) * c.N : nullptr;
-    load_states(row, c.N, w.nl, A[r]);
+    load_states(c.A, w, r, c.N, A[r]);
 #pragma unroll
     for (int k = 0; k < 4; ++k) A[r][k] *= kLog2e;
+  }
+}
+
+// A tile's quads of a tensor on their way to a thread.  whole: all of them are there.
+template <class T, class S>
+struct QuadTile {
+  Quad<T> q[S::EACH];
+  template <class W>
+  __device__ __forceinline__ void load(const void* base, int64_t ld, RowSpot spot, int t0, int count, bool whole,
+                                       const W& w) {
+    const T* p = static_cast<const T*>(base);
+    if (whole) {
+#pragma unroll
+      for (int e = 0; e < S::EACH; ++e) q[e] = load_quad<T, true>(spot.at(p, ld, t0 + e * S::STEP), 4);
+    } else {
+#pragma unroll
+      for (int e = 0; e < S::EACH; ++e) {
+        q[e] = Quad<T>{};
+        if (w.k0 + e * S::STEP < count && w.qn > 0) q[e] = some_quad(spot.at(p, ld, t0 + e * S::STEP), w.qn);
+      }
+    }
+  }
+};
+// All quads of a tile are there: no thread is idle, no token or channel missing.
+template <class S, class W>
+__device__ __forceinline__ bool whole_tile(const W& w, int count) {
+  return kSelTile * S::QUADS >= S::THREADS && count == kSelTile && w.nc == S::CB;
+}
+
+// A tile's rows of B and C (one of them null: of the other alone) on their way to LDS.
+template <class T, int LN>
+struct StateTile {
+  using S = SelShape<LN>;
+  Quad<T> q[S::STATES];
+  __device__ __forceinline__ void load(const void* B, int64_t ld_B, const void* C, int64_t ld_C, int t0, int count,
+                                       int head, int N) {
+#pragma unroll
+    for (int e = 0; e < S::STATES; ++e) {
+      const int i = threadIdx.x + e * S::THREADS, k = i / LN % kSelTile, n0 = 4 * (i % LN);
+      const bool second = i >= kSelTile * LN;
+      const T* base = static_cast<const T*>(second ? C : B);
+      q[e] = Quad<T>{};
+      const int n = min(4, N - n0);
+      if (base && i < 2 * kSelTile * LN && k < count && n > 0)
+        q[e] = some_quad(base + (t0 + (int64_t)k) * (second ? ld_C : ld_B) + (int64_t)head * N + n0, n);
+    }
+  }
+  __device__ __forceinline__ void put(float* B, float* C) const {
+#pragma unroll
+    for (int e = 0; e < S::STATES; ++e) {
+      const int i = threadIdx.x + e * S::THREADS, at = i % (kSelTile * LN) * 4;
+      if (i >= 2 * kSelTile * LN) continue;
+      st4((i >= kSelTile * LN ? C : B) + at, f4{q[e].get(0), q[e].get(1), q[e].get(2), q[e].get(3)});
+    }
+  }
+};
+
+// A thread's steps of a tile: what comes in, its bias, softplus; none where no token or
+// channel is.
+template <class T, int LN>
+__device__ __forceinline__ void tile_steps(const QuadTile<T, SelShape<LN>>& raw, const float (&bias)[4],
+                                           bool soft, const SelPlace<LN>& w, int count, bool whole,
+                                           float (&d)[SelShape<LN>::EACH][4]) {
+  using S = SelShape<LN>;
+#pragma unroll
+  for (int e = 0; e < S::EACH; ++e)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) d[e][j] = raw.q[e].get(j) + bias[j];
+  if (soft) {
+#pragma unroll
+    for (int e = 0; e < S::EACH; ++e)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) d[e][j] = softplus(d[e][j]);
+  }
+  if (!whole) {
+#pragma unroll
+    for (int e = 0; e < S::EACH; ++e)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (w.k0 + e * S::STEP >= count || j >= w.qn) d[e][j] = 0.f;
+  }
+}
+// The place of a thread's quad in a tile's [tokens][channels]; -1 for a thread without one.
+template <class S>
+__device__ __forceinline__ int quad_place(int e) {
+  const int i = threadIdx.x + e * S::THREADS;
+  return kSelTile * S::QUADS >= S::THREADS || i < kSelTile * S::QUADS ? i * 4 : -1;
+}
+
+// The carry into a range from those before it (dir -1: the gradient's, from those after it):
+// the nearest one that does not pass its own carry on, then each one's whole decay and
+// what it adds, four of them at a time.
+template <int LN>
+__device__ __forceinline__ void carry_into(const SelCall& c, const SelPlan& p, int range, int dir,
+                                           const SelPlace<LN>& w, const float (&A)[2][4],
+                                           float (&h)[2][4]) {
+  using S = SelShape<LN>;
+  int many = 0;  // ranges to take in
+  for (;;) {
+    const int j = range - dir * (many + 1 + lane_id());
+    const bool there = j >= 0 && j < p.ranges;
+    const uint64_t end = __ballot(!there || p.info[there ? j : 0] != kSelOpen);
+    if (end) {
+      many += __builtin_ctzll(end);
+      const int last = range - dir * (many + 1);
+      if (last >= 0 && last < p.ranges) ++many;
+      break;
+    }
+    many += kWave;
+  }
+#pragma unroll
+  for (int r = 0; r < S::RC; ++r)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) h[r][k] = 0.f;
+  constexpr int BATCH = 4;
+  const int own = w.has(0) ? w.lane_c : 0, two = w.has(1) ? 1 : 0;
+  for (int m = many; m > 0; m -= BATCH) {
+    float d[BATCH][2];
+    f4 s[BATCH][2];
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      const int j = range - dir * max(m - b, 1);
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int64_t at = (int64_t)j * c.D + w.c0 + own + r * two;
+        d[b][r] = p.sums[at];
+        s[b][r] = ld4(p.states + at * S::NP + 4 * w.nl);
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      if (m - b < 1) continue;
+      const bool furthest = m - b == many;  // nothing comes into it
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          h[r][k] = furthest ? s[b][r][k] : __fmaf_rn(exp2_fast(d[b][r] * A[r][k]), h[r][k], s[b][r][k]);
+    }
   }
 }
 
@@ -224,6 +357,20 @@ struct alignas(16) SelLds {
   TileMarks marks;
   int from;
 };
+
+// What a range passes on, to the workspace.
+template <int LN>
+__device__ __forceinline__ void pass_on(const SelCall& c, const SelPlan& p, int range, const SelPlace<LN>& w,
+                                        const float (&h)[2][4], const float (&sum)[2]) {
+  using S = SelShape<LN>;
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    if (!w.has(r)) continue;
+    const int64_t at = (int64_t)range * c.D + w.c0 + w.lane_c + r;
+    st4(p.states + at * S::NP + 4 * w.nl, f4{h[r][0], h[r][1], h[r][2], h[r][3]});
+    if (w.nl == 0) p.sums[at] = sum[r];
+  }
+}
 
 // ---------------------------------------------------------------- forward
 
@@ -245,83 +392,78 @@ __device__ __forceinline__ int run_stop(const Packed& s, int lo, int hi) {
 }
 
 template <class T, int LN>
-__global__ __launch_bounds__(kBlock) void k_selective_ends(SelCall c, SelPlan p) {
+__global__ __launch_bounds__(SelShape<LN>::THREADS) void k_selective_ends(SelArgs) {
   using S = SelShape<LN>;
   __shared__ SelLds<LN> s;
+  const SelArgsPtr args = sel_args();
+  const SelArgs& first = again(args);
   const int t = threadIdx.x;
-  const int range = blockIdx.x / p.all_blocks, block = blockIdx.x % p.all_blocks;
-  const SelPlace<LN> w(c, p, block);
-  const int lo = range * p.range, hi = min(lo + p.range, c.seqs.tokens);
+  const int range = blockIdx.x / first.p.all_blocks, block = blockIdx.x % first.p.all_blocks;
+  const SelPlace<LN> w(first.c, first.p, block);
+  const int lo = range * first.p.range, hi = min(lo + first.p.range, first.c.seqs.tokens);
   if (t < kWave) {
-    const int at = run_start(c.seqs, lo, hi);
+    const int at = run_start(first.c.seqs, lo, hi);
     if (t == 0) s.from = at;
   }
   __syncthreads();
   const int from = s.from;
   // A sequence that starts in the range, or one that runs through all of it.
-  const bool open = from == lo && lo > 0;
   int seq = -1;  // ... whose state before its first token counts, if it starts here
-  bool starts = !open;
-  if (open) {
-    const int i = first_place(c.seqs, lo);
-    starts = i <= c.seqs.nseq && place_of(c.seqs, i) == lo;
+  bool starts = from > lo || lo == 0;
+  if (!starts) {
+    const int i = first_place(first.c.seqs, lo);
+    starts = i <= first.c.seqs.nseq && place_of(first.c.seqs, i) == lo;
   }
-  if (starts && from < hi) {  // the last offset <= from
-    seq = first_place(c.seqs, from + 1) - 1;
-    seq = max(0, min(seq, c.seqs.nseq - 1));
-  }
-  if (t == 0 && block == 0)
-    p.info[range] = from == hi ? kSelNone : starts ? kSelClosed : kSelOpen;
+  if (starts && from < hi)  // the last offset <= from
+    seq = max(0, min(first_place(first.c.seqs, from + 1) - 1, first.c.seqs.nseq - 1));
+  if (t == 0 && block == 0) first.p.info[range] = from == hi ? kSelNone : starts ? kSelClosed : kSelOpen;
   if (from == hi) return;
 
-  float A[2][4], h[2][4], sum[2] = {0.f, 0.f};
-  load_rates(c, w, A);
-#pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    const float* row = seq >= 0 && c.h0 && w.lane_c + r < w.nc
-                           ? c.h0 + ((int64_t)seq * c.D + w.c0 + w.lane_c + r) * c.N
-                           : nullptr;
-    load_states(row, c.N, w.nl, h[r]);
-  }
-  float bias[4] = {0.f, 0.f, 0.f, 0.f};
-  if (c.bias)
-    for (int k = 0; k < w.qn; ++k) bias[k] = c.bias[w.q0 + k];
-  const T* x = static_cast<const T*>(c.x);
-  const T* delta = static_cast<const T*>(c.delta);
-  const RowSpot xs = RowSpot::of(x, c.ld_x, w.k0, w.q0), ds = RowSpot::of(x, c.ld_delta, w.k0, w.q0);
+  const RowSpot xs = RowSpot::of((const T*)nullptr, first.c.ld_x, w.k0, w.q0);
+  const RowSpot ds = RowSpot::of((const T*)nullptr, first.c.ld_delta, w.k0, w.q0);
   QuadTile<T, S> xn, dn;  // the next tile's
+  StateTile<T, LN> bn;
   const auto fetch = [&](int t0) {
+    const SelCall& c = again(args).c;
     const int count = min(kSelTile, hi - t0);
-    xn.load(x, c.ld_x, xs, t0, count, w.k0, w.qn);
-    dn.load(delta, c.ld_delta, ds, t0, count, w.k0, w.qn);
+    const bool whole = whole_tile<S>(w, count);
+    dn.load(c.delta, c.ld_delta, ds, t0, count, whole, w);
+    xn.load(c.x, c.ld_x, xs, t0, count, whole, w);
+    bn.load(c.B, c.ld_B, nullptr, 0, t0, count, w.head, c.N);
   };
   fetch(from);
+  float A[2][4], h[2][4], sum[2] = {0.f, 0.f}, bias[4];
+  load_rates(first.c, w, A);
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+    load_states(seq >= 0 ? state_row(first.c.h0, seq, first.c) : nullptr, w, r, first.c.N, h[r]);
+  load_four(first.c.bias, w.q0, w.qn, bias);
+  const bool soft = first.c.softplus;
 
   for (int t0 = from; t0 < hi; t0 += kSelTile) {
     const int count = min(kSelTile, hi - t0);
     __syncthreads();
+    float d[S::EACH][4];
+    tile_steps<T, LN>(dn, bias, soft, w, count, whole_tile<S>(w, count), d);
 #pragma unroll
     for (int e = 0; e < S::EACH; ++e) {
-      const int i = t + e * kBlock, k = w.k0 + e * S::STEP;
-      if (k >= kSelTile) continue;
-      float d[4], u[4];
+      const int at = quad_place<S>(e);
+      if (at < 0) continue;
+      f4 u;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        d[j] = k < count && j < w.qn ? step_of(dn.q[e].get(j), bias[j], c.softplus) : 0.f;
-        u[j] = d[j] * xn.q[e].get(j);
-      }
-      st4(s.step + i * 4, f4{d[0], d[1], d[2], d[3]});
-      st4(s.dx + i * 4, f4{u[0], u[1], u[2], u[3]});
+      for (int j = 0; j < 4; ++j) u[j] = d[e][j] * xn.q[e].get(j);
+      st4(s.step + at, f4{d[e][0], d[e][1], d[e][2], d[e][3]});
+      st4(s.dx + at, u);
     }
-    stage_states<T, LN>(static_cast<const T*>(c.B), c.ld_B, t0, count, w.head, c.N, s.B);
+    bn.put(s.B, s.C);
     if (t0 + kSelTile < hi) fetch(t0 + kSelTile);
     __syncthreads();
 #pragma unroll 4
     for (int k = 0; k < kSelTile; ++k) {  // (tokens past the range: no step, nothing added)
-      const float2 d = *reinterpret_cast<const float2*>(s.step + k * S::CB + w.lane_c);
-      const float2 u = *reinterpret_cast<const float2*>(s.dx + k * S::CB + w.lane_c);
+      const float2 d2 = *reinterpret_cast<const float2*>(s.step + k * S::CB + w.lane_c);
+      const float2 u2 = *reinterpret_cast<const float2*>(s.dx + k * S::CB + w.lane_c);
       const f4 B = ld4(s.B + k * S::NP + 4 * w.nl);
-      const float dd[2] = {d.x, d.y}, uu[2] = {u.x, u.y};
+      const float dd[2] = {d2.x, d2.y}, uu[2] = {u2.x, u2.y};
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         sum[r] += dd[r];
@@ -331,91 +473,83 @@ __global__ __launch_bounds__(kBlock) void k_selective_ends(SelCall c, SelPlan p)
       }
     }
   }
-#pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    if (w.lane_c + r >= w.nc) continue;
-    const int64_t at = (int64_t)range * c.D + w.c0 + w.lane_c + r;
-    st4(p.states + at * S::NP + 4 * w.nl, f4{h[r][0], h[r][1], h[r][2], h[r][3]});
-    if (w.nl == 0) p.sums[at] = sum[r];
-  }
+  const SelArgs& last = again(args);
+  pass_on(last.c, last.p, range, w, h, sum);
 }
 
 template <class T, int LN>
-__global__ __launch_bounds__(kBlock) void k_selective(SelCall c, SelPlan p) {
+__global__ __launch_bounds__(SelShape<LN>::THREADS) void k_selective(SelArgs) {
   using S = SelShape<LN>;
   __shared__ SelLds<LN> s;
   __shared__ __align__(16) float sy[kSelTile * S::CB];
-  __shared__ int list[kBlock];
+  __shared__ int list[S::THREADS];
+  const SelArgsPtr args = sel_args();
+  const SelArgs& first = again(args);
   const int t = threadIdx.x;
-  const int range = blockIdx.x / p.all_blocks, block = blockIdx.x % p.all_blocks;
-  const SelPlace<LN> w(c, p, block);
-  const int lo = range * p.range, hi = min(lo + p.range, c.seqs.tokens);
+  const int range = blockIdx.x / first.p.all_blocks, block = blockIdx.x % first.p.all_blocks;
+  const SelPlace<LN> w(first.c, first.p, block);
+  const int lo = range * first.p.range, hi = min(lo + first.p.range, first.c.seqs.tokens);
 
-  // a lane's states of sequence i, before it or after it
-  const auto row_of = [&](const float* base, int i, int r) -> float* {
-    if (!base || w.lane_c + r >= w.nc) return nullptr;
-    return const_cast<float*>(base) + ((int64_t)i * c.D + w.c0 + w.lane_c + r) * c.N;
-  };
-  check_places(c.seqs, range, p.ranges, c.last != nullptr, list, [&](int i) {
+  check_places(first.c.seqs, range, first.p.ranges, S::THREADS, first.c.last != nullptr, list, [&](int i) {
+    const SelCall& c = again(args).c;
     for (int r = 0; r < 2; ++r) {
       float v[4];
-      load_states(row_of(c.h0, i, r), c.N, w.nl, v);
-      if (float* to = row_of(c.last, i, r)) store_states(to, c.N, w.nl, v);
+      load_states(state_row(c.h0, i, c), w, r, c.N, v);
+      store_states(state_row(c.last, i, c), w, r, c.N, v);
     }
   });
   if (lo >= hi) return;
 
-  const T* x = static_cast<const T*>(c.x);
-  const T* delta = static_cast<const T*>(c.delta);
-  const T* z = static_cast<const T*>(c.z);
-  T* y = static_cast<T*>(c.y);
-  const RowSpot xs = RowSpot::of(x, c.ld_x, w.k0, w.q0), ds = RowSpot::of(x, c.ld_delta, w.k0, w.q0);
-  const RowSpot zs = RowSpot::of(x, c.ld_z, w.k0, w.q0), ys = RowSpot::of(x, c.ld_y, w.k0, w.q0);
+  const T* none = nullptr;
+  const RowSpot xs = RowSpot::of(none, first.c.ld_x, w.k0, w.q0), ds = RowSpot::of(none, first.c.ld_delta, w.k0, w.q0);
+  const RowSpot zs = RowSpot::of(none, first.c.ld_z, w.k0, w.q0), ys = RowSpot::of(none, first.c.ld_y, w.k0, w.q0);
+  const bool gated = first.c.z != nullptr, soft = first.c.softplus;
   QuadTile<T, S> xn, dn, zn;  // the next tile's
+  StateTile<T, LN> bn;
   const auto fetch = [&](int t0) {
+    const SelCall& c = again(args).c;
     const int count = min(kSelTile, hi - t0);
-    xn.load(x, c.ld_x, xs, t0, count, w.k0, w.qn);
-    dn.load(delta, c.ld_delta, ds, t0, count, w.k0, w.qn);
-    if (c.z) zn.load(z, c.ld_z, zs, t0, count, w.k0, w.qn);
+    const bool whole = whole_tile<S>(w, count);
+    dn.load(c.delta, c.ld_delta, ds, t0, count, whole, w);
+    xn.load(c.x, c.ld_x, xs, t0, count, whole, w);
+    bn.load(c.B, c.ld_B, c.C, c.ld_C, t0, count, w.head, c.N);
+    if (gated) zn.load(c.z, c.ld_z, zs, t0, count, whole, w);
   };
   fetch(lo);
-  float A[2][4], h[2][4];
-  load_rates(c, w, A);
-  float bias[4] = {0.f, 0.f, 0.f, 0.f}, skip[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int k = 0; k < w.qn; ++k) {
-    if (c.bias) bias[k] = c.bias[w.q0 + k];
-    if (c.skip) skip[k] = c.skip[w.q0 + k];
-  }
+  float A[2][4], h[2][4], bias[4], skip[4];
+  load_rates(first.c, w, A);
+  load_four(first.c.bias, w.q0, w.qn, bias);
+  load_four(first.c.skip, w.q0, w.qn, skip);
+  const bool skips = first.c.skip != nullptr;
   UpCursor cursor{};
-  if (t < kWave) cursor.read(c.seqs, first_place(c.seqs, lo));
+  if (t < kWave) cursor.read(first.c.seqs, first_place(first.c.seqs, lo));
 
   for (int t0 = lo; t0 < hi; t0 += kSelTile) {
     const int count = min(kSelTile, hi - t0);
+    const bool whole = whole_tile<S>(w, count);
     const QuadTile<T, S> xv = xn, zv = zn;
+    float d[S::EACH][4];
+    tile_steps<T, LN>(dn, bias, soft, w, count, whole, d);
 #pragma unroll
     for (int e = 0; e < S::EACH; ++e) {
-      const int i = t + e * kBlock, k = w.k0 + e * S::STEP;
-      if (k >= kSelTile) continue;
-      const bool there = k < count;
-      float d[4], u[4];
+      const int at = quad_place<S>(e);
+      if (at < 0) continue;
+      f4 u;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        d[j] = there && j < w.qn ? step_of(dn.q[e].get(j), bias[j], c.softplus) : 0.f;
-        u[j] = d[j] * xv.q[e].get(j);
-      }
-      st4(s.step + i * 4, f4{d[0], d[1], d[2], d[3]});
-      st4(s.dx + i * 4, f4{u[0], u[1], u[2], u[3]});
+      for (int j = 0; j < 4; ++j) u[j] = d[e][j] * xv.q[e].get(j);
+      st4(s.step + at, f4{d[e][0], d[e][1], d[e][2], d[e][3]});
+      st4(s.dx + at, u);
     }
-    stage_states<T, LN>(static_cast<const T*>(c.B), c.ld_B, t0, count, w.head, c.N, s.B);
-    stage_states<T, LN>(static_cast<const T*>(c.C), c.ld_C, t0, count, w.head, c.N, s.C);
-    if (t < kWave) mark_tile(c.seqs, t0, t0 + count, cursor, s.marks);
+    bn.put(s.B, s.C);
+    if (t < kWave) mark_tile(again(args).c.seqs, t0, t0 + count, cursor, s.marks);
     __syncthreads();
     const uint32_t starts = __builtin_amdgcn_readfirstlane(s.marks.starts);
     const uint32_t stops = __builtin_amdgcn_readfirstlane(s.marks.stops);
     if (t0 + kSelTile < hi) fetch(t0 + kSelTile);
+    const SelArgs& a = again(args);
     if (t0 == lo) {
       if (!(starts & 1) && lo > 0) {
-        carry_into<LN>(c, p, range, 1, w, A, h);
+        carry_into<LN>(a.c, a.p, range, 1, w, A, h);
       } else {
 #pragma unroll
         for (int r = 0; r < 2; ++r)
@@ -423,19 +557,19 @@ __global__ __launch_bounds__(kBlock) void k_selective(SelCall c, SelPlan p) {
           for (int j = 0; j < 4; ++j) h[r][j] = 0.f;
       }
     }
-    if (c.marks) {
+    if (a.c.marks) {
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        if (w.lane_c + r >= w.nc || 4 * w.nl >= c.N) continue;
-        const int64_t at = (int64_t)(t0 / kSelTile) * c.D + w.c0 + w.lane_c + r;
-        st4(c.marks + at * p.NM + 4 * w.nl, f4{h[r][0], h[r][1], h[r][2], h[r][3]});
+        if (!w.has(r) || 4 * w.nl >= a.c.N) continue;
+        const int64_t at = (int64_t)(t0 / kSelTile) * a.c.D + w.c0 + w.lane_c + r;
+        st4(a.c.marks + at * a.p.NM + 4 * w.nl, f4{h[r][0], h[r][1], h[r][2], h[r][3]});
       }
     }
     const auto token = [&](int k) {
-      const float2 d = *reinterpret_cast<const float2*>(s.step + k * S::CB + w.lane_c);
-      const float2 u = *reinterpret_cast<const float2*>(s.dx + k * S::CB + w.lane_c);
+      const float2 d2 = *reinterpret_cast<const float2*>(s.step + k * S::CB + w.lane_c);
+      const float2 u2 = *reinterpret_cast<const float2*>(s.dx + k * S::CB + w.lane_c);
       const f4 B = ld4(s.B + k * S::NP + 4 * w.nl), C = ld4(s.C + k * S::NP + 4 * w.nl);
-      const float dd[2] = {d.x, d.y}, uu[2] = {u.x, u.y};
+      const float dd[2] = {d2.x, d2.y}, uu[2] = {u2.x, u2.y};
       float out[2];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
@@ -455,35 +589,35 @@ __global__ __launch_bounds__(kBlock) void k_selective(SelCall c, SelPlan p) {
     } else {
       for (int k = 0; k < count; ++k) {
         if (starts >> k & 1) {
-          const int from = __builtin_amdgcn_readfirstlane(s.marks.start[k]);
+          const float* row = state_row(a.c.h0, __builtin_amdgcn_readfirstlane(s.marks.start[k]), a.c);
 #pragma unroll
-          for (int r = 0; r < 2; ++r) load_states(row_of(c.h0, from, r), c.N, w.nl, h[r]);
+          for (int r = 0; r < 2; ++r) load_states(row, w, r, a.c.N, h[r]);
         }
         token(k);
-        if ((stops >> k & 1) && c.last) {
-          const int to = __builtin_amdgcn_readfirstlane(s.marks.stop[k]);
+        if (stops >> k & 1) {
+          float* row = state_row(a.c.last, __builtin_amdgcn_readfirstlane(s.marks.stop[k]), a.c);
 #pragma unroll
-          for (int r = 0; r < 2; ++r)
-            if (float* row = row_of(c.last, to, r)) store_states(row, c.N, w.nl, h[r]);
+          for (int r = 0; r < 2; ++r) store_states(row, w, r, a.c.N, h[r]);
         }
       }
     }
     __syncthreads();
+    const SelCall& c = again(args).c;
 #pragma unroll
     for (int e = 0; e < S::EACH; ++e) {
-      const int i = t + e * kBlock, k = w.k0 + e * S::STEP;
-      if (k >= count || w.qn <= 0) continue;
-      const f4 q = ld4(sy + i * 4);
+      const int at = quad_place<S>(e);
+      if (at < 0 || (!whole && (w.k0 + e * S::STEP >= count || w.qn == 0))) continue;
+      const f4 q = ld4(sy + at);
       float v[4] = {q[0], q[1], q[2], q[3]};
-      if (c.skip) {
+      if (skips) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = __fmaf_rn(skip[j], xv.q[e].get(j), q[j]);
       }
-      if (c.z) {
+      if (gated) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] *= zv.q[e].get(j) * sigmoid(zv.q[e].get(j));
       }
-      put_quad(ys.at(y, c.ld_y, t0 + e * S::STEP), v, w.qn);
+      put_quad(ys.at(static_cast<T*>(c.y), c.ld_y, t0 + e * S::STEP), v, w.qn);
     }
   }
 }
@@ -498,37 +632,35 @@ __global__ __launch_bounds__(kBlock) void k_selective_step(SelCall c, int blocks
     const int64_t row = i / blocks;
     const int ch = (int)(i - row * blocks) * CB + threadIdx.x / LN;
     const bool live = ch < c.D;
-    const int own = live ? ch : 0, head = own / (c.D / c.groups);
-    const int64_t at = (row * c.D + own) * c.N;
-    const T* B = static_cast<const T*>(c.B) + row * c.ld_B + (int64_t)head * c.N;
-    const T* C = static_cast<const T*>(c.C) + row * c.ld_C + (int64_t)head * c.N;
-    const float x = load_one(static_cast<const T*>(c.x) + row * c.ld_x + own);
-    const float raw = load_one(static_cast<const T*>(c.delta) + row * c.ld_delta + own);
-    float A[4], h[4], Bv[4], Cv[4];
-    load_states(c.A + (int64_t)own * c.N, c.N, nl, A);
-    load_states(c.h0 ? c.h0 + at : nullptr, c.N, nl, h);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int n = 4 * nl + j;
-      Bv[j] = n < c.N ? load_one(B + n) : 0.f;
-      Cv[j] = n < c.N ? load_one(C + n) : 0.f;
+    const int own = live ? ch : 0, head = own / (c.D / c.groups), n = min(4, c.N - 4 * nl);
+    const int64_t at = (row * c.D + own) * c.N + 4 * nl;
+    const int64_t bc = (int64_t)head * c.N + 4 * nl;
+    Quad<float> A{}, h{};
+    Quad<T> B{}, C{};
+    if (n > 0) {
+      if (c.h0) h = some_quad(c.h0 + at, n);
+      A = some_quad(c.A + (int64_t)own * c.N + 4 * nl, n);
+      B = some_quad(static_cast<const T*>(c.B) + row * c.ld_B + bc, n);
+      C = some_quad(static_cast<const T*>(c.C) + row * c.ld_C + bc, n);
     }
-    const float d = step_of(raw, c.bias ? c.bias[own] : 0.f, c.softplus), u = d * x;
-    float v = 0.f;
+    const float x = load_one(static_cast<const T*>(c.x) + row * c.ld_x + own);
+    const float z = c.z ? load_one(static_cast<const T*>(c.z) + row * c.ld_z + own) : 0.f;
+    float d = load_one(static_cast<const T*>(c.delta) + row * c.ld_delta + own);
+    if (c.bias) d += c.bias[own];
+    if (c.softplus) d = softplus(d);
+    const float u = d * x;
+    float v = 0.f, out[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      h[j] = __fmaf_rn(exp2_fast(d * (A[j] * kLog2e)), h[j], u * Bv[j]);
-      v = __fmaf_rn(Cv[j], h[j], v);
+      out[j] = __fmaf_rn(exp2_fast(d * (A.get(j) * kLog2e)), h.get(j), u * B.get(j));
+      v = __fmaf_rn(C.get(j), out[j], v);
     }
     v = sum_states<LN>(v);
     if (!live) continue;
-    if (c.last) store_states(c.last + at, c.N, nl, h);
+    if (c.last && n > 0) put_quad(c.last + at, out, n);
     if (nl == 0) {
       if (c.skip) v = __fmaf_rn(c.skip[own], x, v);
-      if (c.z) {
-        const float z = load_one(static_cast<const T*>(c.z) + row * c.ld_z + own);
-        v *= z * sigmoid(z);
-      }
+      if (c.z) v *= z * sigmoid(z);
       static_cast<T*>(c.y)[row * c.ld_y + own] = Elem<T>::put(settled(v));
     }
   }

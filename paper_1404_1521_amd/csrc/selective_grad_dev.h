@@ -41,86 +41,89 @@ __device__ __forceinline__ void sum_channels(const float (&v)[8], float (&out)[2
 // read and keeps all its terms until then, which took 64 registers more.
 __device__ __forceinline__ void here(float& v) { asm volatile("" : "+v"(v)); }
 
-// Where a thread finds its quads of the gradient's inputs.
-struct GradSpots {
-  RowSpot x, delta, dy, z;
-  template <class T, class W>
-  static __device__ __forceinline__ GradSpots of(const SelCall& c, const T* type, const W& w) {
-    return GradSpots{RowSpot::of(type, c.ld_x, w.k0, w.q0), RowSpot::of(type, c.ld_delta, w.k0, w.q0),
-                     RowSpot::of(type, c.ld_dy, w.k0, w.q0), RowSpot::of(type, c.ld_z, w.k0, w.q0)};
-  }
-};
-
-// A tile's steps, D x (if x) and v' in LDS.  Tokens past the tile's and channels past the
-// workgroup's: zeros, which change nothing.
-template <class T, int LN, bool X>
-__device__ __forceinline__ void stage_grad(const SelCall& c, const SelPlace<LN>& w, const GradSpots& at,
-                                           int t0, int count, const float (&bias)[4], float* step,
-                                           float* dx, float* dv) {
+// A tile of the gradient's inputs on its way to a thread.
+template <class T, int LN>
+struct GradTile {
   using S = SelShape<LN>;
   QuadTile<T, S> raw, gy, xv, zv;
-  raw.load(static_cast<const T*>(c.delta), c.ld_delta, at.delta, t0, count, w.k0, w.qn);
-  gy.load(static_cast<const T*>(c.dy), c.ld_dy, at.dy, t0, count, w.k0, w.qn);
-  if (X) xv.load(static_cast<const T*>(c.x), c.ld_x, at.x, t0, count, w.k0, w.qn);
-  if (c.z) zv.load(static_cast<const T*>(c.z), c.ld_z, at.z, t0, count, w.k0, w.qn);
-#pragma unroll
-  for (int e = 0; e < S::EACH; ++e) {
-    const int i = threadIdx.x + e * kBlock, k = w.k0 + e * S::STEP;
-    if (k >= kSelTile) continue;
-    float d[4], u[4], g[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      d[j] = k < count && j < w.qn ? step_of(raw.q[e].get(j), bias[j], c.softplus) : 0.f;
-      if (X) u[j] = d[j] * xv.q[e].get(j);
-      g[j] = gy.q[e].get(j);
-    }
-    if (c.z) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) g[j] *= zv.q[e].get(j) * sigmoid(zv.q[e].get(j));
-    }
-    st4(step + i * 4, f4{d[0], d[1], d[2], d[3]});
-    if (X) st4(dx + i * 4, f4{u[0], u[1], u[2], u[3]});
-    st4(dv + i * 4, f4{g[0], g[1], g[2], g[3]});
+  StateTile<T, LN> states;
+  // Without X, of what the first launch reads: neither x nor B.
+  template <bool X>
+  __device__ __forceinline__ void load(const SelCall& c, const SelPlace<LN>& w, int t0, int count) {
+    const T* none = nullptr;
+    const bool whole = whole_tile<S>(w, count);
+    raw.load(c.delta, c.ld_delta, RowSpot::of(none, c.ld_delta, w.k0, w.q0), t0, count, whole, w);
+    gy.load(c.dy, c.ld_dy, RowSpot::of(none, c.ld_dy, w.k0, w.q0), t0, count, whole, w);
+    if (X) xv.load(c.x, c.ld_x, RowSpot::of(none, c.ld_x, w.k0, w.q0), t0, count, whole, w);
+    if (c.z) zv.load(c.z, c.ld_z, RowSpot::of(none, c.ld_z, w.k0, w.q0), t0, count, whole, w);
+    states.load(X ? c.B : nullptr, c.ld_B, c.C, c.ld_C, t0, count, w.head, c.N);
   }
-}
+  // The tile's steps, D x and v' to LDS.  Tokens past the tile's and channels past the
+  // workgroup's: zeros, which change nothing.
+  template <bool X>
+  __device__ __forceinline__ void put(const SelCall& c, const SelPlace<LN>& w, int count, float* step,
+                                      float* dx, float* dv) const {
+    float bias[4], d[S::EACH][4];
+    load_four(c.bias, w.q0, w.qn, bias);
+    tile_steps<T, LN>(raw, bias, c.softplus, w, count, whole_tile<S>(w, count), d);
+    const bool gated = c.z != nullptr;
+#pragma unroll
+    for (int e = 0; e < S::EACH; ++e) {
+      const int at = quad_place<S>(e);
+      if (at < 0) continue;
+      f4 u, v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (X) u[j] = d[e][j] * xv.q[e].get(j);
+        v[j] = gy.q[e].get(j);
+      }
+      if (gated) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] *= zv.q[e].get(j) * sigmoid(zv.q[e].get(j));
+      }
+      st4(step + at, f4{d[e][0], d[e][1], d[e][2], d[e][3]});
+      if (X) st4(dx + at, u);
+      st4(dv + at, v);
+    }
+  }
+};
 
 // What comes back through each range that a sequence runs into, from that sequence's end in
 // it or from nothing.
 template <class T, int LN>
-__global__ __launch_bounds__(kBlock) void k_selective_grad_ends(SelCall c, SelPlan p) {
+__global__ __launch_bounds__(SelShape<LN>::THREADS) void k_selective_grad_ends(SelArgs) {
   using S = SelShape<LN>;
   __shared__ SelLds<LN> s;
+  const SelArgsPtr args = sel_args();
+  const SelArgs& first = again(args);
   const int t = threadIdx.x;
-  const int range = blockIdx.x / p.all_blocks, block = blockIdx.x % p.all_blocks;
-  const SelPlace<LN> w(c, p, block);
-  const int lo = range * p.range, hi = min(lo + p.range, c.seqs.tokens);
-  const int to = lo < hi ? run_stop(c.seqs, lo, hi) : lo;
+  const int range = blockIdx.x / first.p.all_blocks, block = blockIdx.x % first.p.all_blocks;
+  const SelPlace<LN> w(first.c, first.p, block);
+  const int lo = range * first.p.range, hi = min(lo + first.p.range, first.c.seqs.tokens);
+  const int to = lo < hi ? run_stop(first.c.seqs, lo, hi) : lo;
   int seq = -1;  // the sequence that ends at `to`, if one does
   if (to > lo) {
-    const int i = first_place(c.seqs, to);
-    if (i > 0 && i <= c.seqs.nseq && place_of(c.seqs, i) == to) seq = i - 1;
+    const int i = first_place(first.c.seqs, to);
+    if (i > 0 && i <= first.c.seqs.nseq && place_of(first.c.seqs, i) == to) seq = i - 1;
   }
-  if (t == 0 && block == 0) p.info[range] = to == lo ? kSelNone : seq >= 0 ? kSelClosed : kSelOpen;
+  if (t == 0 && block == 0) first.p.info[range] = to == lo ? kSelNone : seq >= 0 ? kSelClosed : kSelOpen;
   if (to == lo) return;
 
+  int tile = (to - 1 - lo) / kSelTile;
+  GradTile<T, LN> in;
+  in.template load<false>(first.c, w, lo + tile * kSelTile, min(kSelTile, to - lo - tile * kSelTile));
   float A[2][4], mu[2][4], sum[2] = {0.f, 0.f};
-  load_rates(c, w, A);
+  load_rates(first.c, w, A);
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    const float* row = seq >= 0 && c.dlast && w.lane_c + r < w.nc
-                           ? c.dlast + ((int64_t)seq * c.D + w.c0 + w.lane_c + r) * c.N
-                           : nullptr;
-    load_states(row, c.N, w.nl, mu[r]);
-  }
-  float bias[4] = {0.f, 0.f, 0.f, 0.f};
-  if (c.bias)
-    for (int k = 0; k < w.qn; ++k) bias[k] = c.bias[w.q0 + k];
-  const GradSpots at = GradSpots::of(c, static_cast<const T*>(nullptr), w);
-  for (int tile = (to - 1 - lo) / kSelTile; tile >= 0; --tile) {
-    const int t0 = lo + tile * kSelTile, count = min(kSelTile, to - t0);
+  for (int r = 0; r < 2; ++r)
+    load_states(seq >= 0 ? state_row(first.c.dlast, seq, first.c) : nullptr, w, r, first.c.N, mu[r]);
+  for (; tile >= 0; --tile) {
+    const int t0 = lo + tile * kSelTile;
+    const SelCall& c = again(args).c;
     __syncthreads();
-    stage_grad<T, LN, false>(c, w, at, t0, count, bias, s.step, nullptr, s.dx);
-    stage_states<T, LN>(static_cast<const T*>(c.C), c.ld_C, t0, count, w.head, c.N, s.C);
+    in.template put<false>(c, w, min(kSelTile, to - t0), s.step, nullptr, s.dx);
+    in.states.put(s.B, s.C);
+    if (tile > 0) in.template load<false>(c, w, t0 - kSelTile, kSelTile);
     __syncthreads();
 #pragma unroll 4
     for (int k = kSelTile - 1; k >= 0; --k) {
@@ -137,13 +140,8 @@ __global__ __launch_bounds__(kBlock) void k_selective_grad_ends(SelCall c, SelPl
       }
     }
   }
-#pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    if (w.lane_c + r >= w.nc) continue;
-    const int64_t at = (int64_t)range * c.D + w.c0 + w.lane_c + r;
-    st4(p.states + at * S::NP + 4 * w.nl, f4{mu[r][0], mu[r][1], mu[r][2], mu[r][3]});
-    if (w.nl == 0) p.sums[at] = sum[r];
-  }
+  const SelArgs& last = again(args);
+  pass_on(last.c, last.p, range, w, mu, sum);
 }
 
 // LDS of the gradient: what comes in and goes out of each token and channel (D x makes
@@ -153,74 +151,81 @@ struct alignas(16) SelGradLds {
   using S = SelShape<LN>;
   SelLds<LN> in;
   float dv[kSelTile * S::CB], dstep[kSelTile * S::CB];
-  float part[kWavesPerBlock][kSelTile][2][S::NP];
-  int list[kBlock];
+  float part[S::W][kSelTile][2][S::NP];
+  int list[S::THREADS];
 };
 
 template <class T, int LN>
-__global__ __launch_bounds__(kBlock, 2) void k_selective_grad(SelCall c, SelPlan p) {
+__global__ __launch_bounds__(SelShape<LN>::THREADS, 2) void k_selective_grad(SelArgs) {
   using S = SelShape<LN>;
   constexpr int H = kSelTile / 2;
   __shared__ SelGradLds<LN> g;
   SelLds<LN>& s = g.in;
+  const SelArgsPtr args = sel_args();
+  const SelArgs& first = again(args);
   const int t = threadIdx.x, lane = t & (kWave - 1), wave = t / kWave;
-  const int range = blockIdx.x / p.all_blocks, block = blockIdx.x % p.all_blocks;
-  const SelPlace<LN> w(c, p, block);
-  const int lo = range * p.range, hi = min(lo + p.range, c.seqs.tokens);
+  const int range = blockIdx.x / first.p.all_blocks, block = blockIdx.x % first.p.all_blocks;
+  const SelPlace<LN> w(first.c, first.p, block);
+  const int lo = range * first.p.range, hi = min(lo + first.p.range, first.c.seqs.tokens);
 
-  const auto row_of = [&](const float* base, int i, int r) -> float* {
-    if (!base || w.lane_c + r >= w.nc) return nullptr;
-    return const_cast<float*>(base) + ((int64_t)i * c.D + w.c0 + w.lane_c + r) * c.N;
-  };
-  check_places(c.seqs, range, p.ranges, c.dh0 != nullptr, g.list, [&](int i) {
+  check_places(first.c.seqs, range, first.p.ranges, S::THREADS, first.c.dh0 != nullptr, g.list, [&](int i) {
+    const SelCall& c = again(args).c;
     for (int r = 0; r < 2; ++r) {
       float v[4];
-      load_states(row_of(c.dlast, i, r), c.N, w.nl, v);
-      if (float* to = row_of(c.dh0, i, r)) store_states(to, c.N, w.nl, v);
+      load_states(state_row(c.dlast, i, c), w, r, c.N, v);
+      store_states(state_row(c.dh0, i, c), w, r, c.N, v);
     }
   });
 
   float A[2][4], dA[2][4], mu[2][4];
-  load_rates(c, w, A);
+  load_rates(first.c, w, A);
 #pragma unroll
   for (int r = 0; r < 2; ++r)
 #pragma unroll
     for (int j = 0; j < 4; ++j) dA[r][j] = mu[r][j] = 0.f;
-  float bias[4] = {0.f, 0.f, 0.f, 0.f}, skip[4] = {0.f, 0.f, 0.f, 0.f};
   float dskip[4] = {0.f, 0.f, 0.f, 0.f}, dbias[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int k = 0; k < w.qn; ++k) {
-    if (c.bias) bias[k] = c.bias[w.q0 + k];
-    if (c.skip) skip[k] = c.skip[w.q0 + k];
-  }
-
+  const bool last_range = hi >= first.c.seqs.tokens;
   const int tiles = lo < hi ? ceil_div(hi - lo, kSelTile) : 0;
   DownCursor cursor{};
-  if (t < kWave) cursor.read(c.seqs, first_place(c.seqs, hi + 1));
-  const GradSpots at = GradSpots::of(c, static_cast<const T*>(nullptr), w);
+  if (t < kWave) cursor.read(first.c.seqs, first_place(first.c.seqs, hi + 1));
+
   for (int tile = tiles - 1; tile >= 0; --tile) {
     const int t0 = lo + tile * kSelTile, count = min(kSelTile, hi - t0);
-    stage_grad<T, LN, true>(c, w, at, t0, count, bias, s.step, s.dx, g.dv);
-    stage_states<T, LN>(static_cast<const T*>(c.B), c.ld_B, t0, count, w.head, c.N, s.B);
-    stage_states<T, LN>(static_cast<const T*>(c.C), c.ld_C, t0, count, w.head, c.N, s.C);
-    if (t < kWave) mark_tile(c.seqs, t0, t0 + count, cursor, s.marks);
+    {
+      const SelCall& c = again(args).c;
+      GradTile<T, LN> in;
+      in.template load<true>(c, w, t0, count);
+      in.template put<true>(c, w, count, s.step, s.dx, g.dv);
+      in.states.put(s.B, s.C);
+      if (t < kWave) mark_tile(c.seqs, t0, t0 + count, cursor, s.marks);
+    }
     __syncthreads();
     const uint32_t starts = __builtin_amdgcn_readfirstlane(s.marks.starts);
     const uint32_t stops = __builtin_amdgcn_readfirstlane(s.marks.stops);
-    if (tile == tiles - 1 && !(stops >> (count - 1) & 1) && hi < c.seqs.tokens)
-      carry_into<LN>(c, p, range, -1, w, A, mu);
-
     // the states before the first half, and before the second one
-    float first[2][4], h[2][4];
+    float first_h[2][4], h[2][4];
+    {
+      const SelArgs& a = again(args);
+      if (tile == tiles - 1 && !(stops >> (count - 1) & 1) && !last_range)
+        carry_into<LN>(a.c, a.p, range, -1, w, A, mu);
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      f4 m = kZero4;
-      if (w.lane_c + r < w.nc && 4 * w.nl < c.N)
-        m = ld4(c.marks + ((int64_t)(t0 / kSelTile) * c.D + w.c0 + w.lane_c + r) * p.NM + 4 * w.nl);
+      for (int r = 0; r < 2; ++r) {
+        f4 m = kZero4;
+        if (w.has(r) && 4 * w.nl < a.c.N)
+          m = ld4(a.c.marks + ((int64_t)(t0 / kSelTile) * a.c.D + w.c0 + w.lane_c + r) * a.p.NM + 4 * w.nl);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) first[r][j] = h[r][j] = m[j];
+        for (int j = 0; j < 4; ++j) first_h[r][j] = h[r][j] = m[j];
+      }
     }
     const auto halves = [&](auto is_plain) {
       constexpr bool PLAIN = decltype(is_plain)::value;  // no sequence starts or stops here
+      // The states of the sequence that starts or stops at token k, of one of the tensors.
+      const auto states_at = [&](const int* places, int k, const float* SelCall::* of, float (&v)[2][4]) {
+        const SelCall& c = again(args).c;
+        const float* row = state_row(c.*of, __builtin_amdgcn_readfirstlane(places[k]), c);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) load_states(row, w, r, c.N, v[r]);
+      };
       // What a token brings, on its way from LDS while the token before is worked on.
       struct Token {
         float2 d, u, dv;
@@ -238,11 +243,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_selective_grad(SelCall c, SelPlan
         return o;
       };
       const auto forward = [&](int k, const Token& o) {
-        if (!PLAIN && (starts >> k & 1)) {
-          const int from = __builtin_amdgcn_readfirstlane(s.marks.start[k]);
-#pragma unroll
-          for (int r = 0; r < 2; ++r) load_states(row_of(c.h0, from, r), c.N, w.nl, h[r]);
-        }
+        if (!PLAIN && (starts >> k & 1)) states_at(s.marks.start, k, &SelCall::h0, h);
         const float dd[2] = {o.d.x, o.d.y}, uu[2] = {o.u.x, o.u.y};
 #pragma unroll
         for (int r = 0; r < 2; ++r)
@@ -267,7 +268,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_selective_grad(SelCall c, SelPlan
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) before[r][j] = h[r][j] = half ? h[r][j] : first[r][j];
+          for (int j = 0; j < 4; ++j) before[r][j] = h[r][j] = half ? h[r][j] : first_h[r][j];
         Token now = fetch(base, false);
 #pragma unroll
         for (int i = 0; i < H; ++i) {
@@ -284,23 +285,14 @@ __global__ __launch_bounds__(kBlock, 2) void k_selective_grad(SelCall c, SelPlan
         for (int i = H - 1; i >= 0; --i) {
           const int k = base + i;
           const Token next = fetch(base + max(i - 1, 0), true);
-          if (!PLAIN && (stops >> k & 1)) {
-            const int to = __builtin_amdgcn_readfirstlane(s.marks.stop[k]);
-#pragma unroll
-            for (int r = 0; r < 2; ++r) load_states(row_of(c.dlast, to, r), c.N, w.nl, mu[r]);
-          }
+          if (!PLAIN && (stops >> k & 1)) states_at(s.marks.stop, k, &SelCall::dlast, mu);
           const bool starts_here = !PLAIN && (starts >> k & 1);
-          int from = 0;
           float hp[2][4];
 #pragma unroll
           for (int r = 0; r < 2; ++r)
 #pragma unroll
             for (int j = 0; j < 4; ++j) hp[r][j] = i ? hs[i ? i - 1 : 0][r][j] : before[r][j];
-          if (starts_here) {
-            from = __builtin_amdgcn_readfirstlane(s.marks.start[k]);
-#pragma unroll
-            for (int r = 0; r < 2; ++r) load_states(row_of(c.h0, from, r), c.N, w.nl, hp[r]);
-          }
+          if (starts_here) states_at(s.marks.start, k, &SelCall::h0, hp);
           // (here: the decays are computed again, not kept from the way forward)
           here(now.d.x), here(now.d.y);
           const float dd[2] = {now.d.x, now.d.y}, uu[2] = {now.u.x, now.u.y};
@@ -339,9 +331,11 @@ __global__ __launch_bounds__(kBlock, 2) void k_selective_grad(SelCall c, SelPlan
             *reinterpret_cast<float2*>(&g.part[wave][k][lane / 32][4 * w.nl + 2 * (lane / 16 % 2)]) =
                 float2{pair[0], pair[1]};
           if (starts_here) {
+            const SelCall& c = again(args).c;
+            float* row = state_row(c.dh0, __builtin_amdgcn_readfirstlane(s.marks.start[k]), c);
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-              if (float* row = row_of(c.dh0, from, r)) store_states(row, c.N, w.nl, mu[r]);
+              store_states(row, w, r, c.N, mu[r]);
 #pragma unroll
               for (int j = 0; j < 4; ++j) mu[r][j] = 0.f;
             }
@@ -354,84 +348,103 @@ __global__ __launch_bounds__(kBlock, 2) void k_selective_grad(SelCall c, SelPlan
     if ((starts | stops) == 0) halves(std::true_type{});
     else halves(std::false_type{});
     __syncthreads();
+
+    const SelArgs& a = again(args);
+    const SelCall& c = a.c;
+    const bool whole = whole_tile<S>(w, count), gated = c.z != nullptr, skips = c.skip != nullptr;
+    const bool soft = c.softplus;
+    const T* none = nullptr;
     QuadTile<T, S> raw, gy, xv, zv;
-    raw.load(static_cast<const T*>(c.delta), c.ld_delta, at.delta, t0, count, w.k0, w.qn);
-    gy.load(static_cast<const T*>(c.dy), c.ld_dy, at.dy, t0, count, w.k0, w.qn);
-    xv.load(static_cast<const T*>(c.x), c.ld_x, at.x, t0, count, w.k0, w.qn);
-    if (c.z) zv.load(static_cast<const T*>(c.z), c.ld_z, at.z, t0, count, w.k0, w.qn);
+    gy.load(c.dy, c.ld_dy, RowSpot::of(none, c.ld_dy, w.k0, w.q0), t0, count, whole, w);
+    xv.load(c.x, c.ld_x, RowSpot::of(none, c.ld_x, w.k0, w.q0), t0, count, whole, w);
+    if (gated) zv.load(c.z, c.ld_z, RowSpot::of(none, c.ld_z, w.k0, w.q0), t0, count, whole, w);
+    if (soft) raw.load(c.delta, c.ld_delta, RowSpot::of(none, c.ld_delta, w.k0, w.q0), t0, count, whole, w);
+    float bias[4], skip[4];
+    load_four(c.bias, w.q0, w.qn, bias);
+    load_four(c.skip, w.q0, w.qn, skip);
 #pragma unroll
     for (int el = 0; el < S::EACH; ++el) {
-      const int i = t + el * kBlock, k = w.k0 + el * S::STEP;
-      if (k >= count || w.qn <= 0) continue;
-      const f4 e = ld4(s.dx + i * 4), st = ld4(s.step + i * 4), ds = ld4(g.dstep + i * 4);
-      const f4 sv = ld4(g.dv + i * 4);
-      float ox[4], od[4], oz[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float xj = xv.q[el].get(j);
-        float gv = gy.q[el].get(j);
-        oz[j] = 0.f;
-        if (c.z) {
-          const float zj = zv.q[el].get(j), sg = sigmoid(zj);
-          const float v = c.skip ? __fmaf_rn(skip[j], xj, sv[j]) : sv[j];
-          oz[j] = gv * v * (sg * __fmaf_rn(zj, 1.f - sg, 1.f));
-          gv *= zj * sg;
-        }
-        ox[j] = st[j] * e[j];
-        if (c.skip) ox[j] = __fmaf_rn(skip[j], gv, ox[j]);
-        od[j] = __fmaf_rn(xj, e[j], kLn2 * ds[j]);
-        if (c.softplus) od[j] *= sigmoid(raw.q[el].get(j) + bias[j]);
-        if (j < w.qn) {
-          dskip[j] = __fmaf_rn(gv, xj, dskip[j]);
-          dbias[j] += od[j];
-        }
-      }
+      const int at = quad_place<S>(el);
+      if (at < 0 || (!whole && (w.k0 + el * S::STEP >= count || w.qn == 0))) continue;
+      const f4 e = ld4(s.dx + at), st = ld4(s.step + at), ds = ld4(g.dstep + at);
+      const int64_t row = t0 + el * S::STEP;
       const auto put = [&](void* base, int64_t ld, const float (&v)[4]) {
         T* to = static_cast<T*>(base);
-        put_quad(RowSpot::of(to, ld, w.k0, w.q0).at(to, ld, t0 + el * S::STEP), v, w.qn);
+        put_quad(RowSpot::of(to, ld, w.k0, w.q0).at(to, ld, row), v, w.qn);
       };
-      put(c.dx, c.ld_dx, ox);
-      put(c.ddelta, c.ld_ddelta, od);
-      if (c.z) put(c.dz, c.ld_dz, oz);
+      float gv[4], out[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) gv[j] = gy.q[el].get(j);
+      if (gated) {
+        const f4 sv = ld4(g.dv + at);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float zj = zv.q[el].get(j), sg = sigmoid(zj);
+          const float v = __fmaf_rn(skip[j], skips ? xv.q[el].get(j) : 0.f, sv[j]);
+          out[j] = gv[j] * v * (sg * __fmaf_rn(zj, 1.f - sg, 1.f));
+          gv[j] *= zj * sg;
+        }
+        put(c.dz, c.ld_dz, out);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) out[j] = st[j] * e[j];
+      if (skips) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          out[j] = __fmaf_rn(skip[j], gv[j], out[j]);
+          dskip[j] = __fmaf_rn(gv[j], xv.q[el].get(j), dskip[j]);
+        }
+      }
+      put(c.dx, c.ld_dx, out);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) out[j] = __fmaf_rn(xv.q[el].get(j), e[j], kLn2 * ds[j]);
+      if (soft) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) out[j] *= sigmoid(raw.q[el].get(j) + bias[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) dbias[j] += out[j];
+      put(c.ddelta, c.ld_ddelta, out);
     }
-    for (int i = t; i < count * 2 * S::NP; i += kBlock) {
+    for (int i = t; i < count * 2 * S::NP; i += S::THREADS) {
       const int k = i / (2 * S::NP), which = i / S::NP % 2, n = i % S::NP;
       if (n >= c.N) continue;
       float v = g.part[0][k][which][n];
 #pragma unroll
-      for (int j = 1; j < kWavesPerBlock; ++j) v += g.part[j][k][which][n];
+      for (int j = 1; j < S::W; ++j) v += g.part[j][k][which][n];
       const int64_t row = t0 + (int64_t)k;
-      if (p.blocks == 1) {
+      if (a.p.blocks == 1) {
         T* to = which ? static_cast<T*>(c.dC) + row * c.ld_dC : static_cast<T*>(c.dB) + row * c.ld_dB;
         to[(int64_t)w.head * c.N + n] = Elem<T>::put(settled(v));
       } else {
-        const int64_t place = (((int64_t)(block % p.blocks) * c.seqs.tokens + row) * c.groups + w.head) * 2;
-        p.part_bc[(place + which) * c.N + n] = v;
+        const int64_t place = (((int64_t)(block % a.p.blocks) * c.seqs.tokens + row) * c.groups + w.head) * 2;
+        a.p.part_bc[(place + which) * c.N + n] = v;
       }
     }
   }
 
+  const SelArgs& a = again(args);
 #pragma unroll
   for (int r = 0; r < 2; ++r)
-    if (w.lane_c + r < w.nc)
-      st4(p.part_a + ((int64_t)range * c.D + w.c0 + w.lane_c + r) * S::NP + 4 * w.nl,
+    if (w.has(r))
+      st4(a.p.part_a + ((int64_t)range * a.c.D + w.c0 + w.lane_c + r) * S::NP + 4 * w.nl,
           f4{dA[r][0], dA[r][1], dA[r][2], dA[r][3]});
   // the threads of a quad of channels, in order
   __syncthreads();
-  constexpr int kBusy = kSelTile * S::QUADS < kBlock ? kSelTile * S::QUADS : kBlock;
+  constexpr int kBusy = kSelTile * S::QUADS < S::THREADS ? kSelTile * S::QUADS : S::THREADS;
   if (t < kBusy) {
     st4(s.step + t * 4, f4{dskip[0], dskip[1], dskip[2], dskip[3]});
     st4(s.dx + t * 4, f4{dbias[0], dbias[1], dbias[2], dbias[3]});
   }
   __syncthreads();
-  for (int i = t; i < w.nc; i += kBlock) {
-    float a = 0.f, b = 0.f;
+  for (int i = t; i < w.nc; i += S::THREADS) {
+    float u = 0.f, v = 0.f;
     for (int j = 0; j < kBusy / S::QUADS; ++j) {
-      a += s.step[j * S::CB + i];
-      b += s.dx[j * S::CB + i];
+      u += s.step[j * S::CB + i];
+      v += s.dx[j * S::CB + i];
     }
-    p.part_s[((int64_t)range * 2) * c.D + w.c0 + i] = a;
-    p.part_s[((int64_t)range * 2 + 1) * c.D + w.c0 + i] = b;
+    a.p.part_s[((int64_t)range * 2) * a.c.D + w.c0 + i] = u;
+    a.p.part_s[((int64_t)range * 2 + 1) * a.c.D + w.c0 + i] = v;
   }
 }
 

@@ -7,10 +7,10 @@ namespace pg {
 
 template <class T, int LN>
 hipError_t grad_of_lanes(const SelCall& c, const SelPlan& p, const Launch& L) {
-  const dim3 grid((uint32_t)p.ranges * p.all_blocks);
+  const dim3 grid((uint32_t)p.ranges * p.all_blocks), block(SelShape<LN>::THREADS);
   hipError_t e = hipSuccess;
-  if (p.ranges > 1) e = pg_launch(k_selective_grad_ends<T, LN>, grid, dim3(kBlock), 0, L, c, p);
-  if (e == hipSuccess) e = pg_launch(k_selective_grad<T, LN>, grid, dim3(kBlock), 0, L, c, p);
+  if (p.ranges > 1) e = pg_launch(k_selective_grad_ends<T, LN>, grid, block, 0, L, SelArgs{c, p});
+  if (e == hipSuccess) e = pg_launch(k_selective_grad<T, LN>, grid, block, 0, L, SelArgs{c, p});
   if (e != hipSuccess) return e;
   const int params = (int)(((int64_t)c.D * (c.N + 2) + kWave - 1) / kWave);
   const int64_t rest = p.blocks == 1 ? 0 : (int64_t)c.groups * 2 * c.N * c.seqs.tokens;

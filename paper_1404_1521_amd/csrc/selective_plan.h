@@ -7,9 +7,6 @@
 
 namespace pg {
 
-// Lanes of a channel: four states each.
-inline int sel_lanes(int N) { return N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
-
 template <class F>
 hipError_t by_lanes(int N, F f) {
   switch (sel_lanes(N)) {
@@ -25,7 +22,7 @@ constexpr int kSelWorkgroups = 4 * kCus;  // that the ranges are to give
 // How a call is cut, in the workspace.
 inline SelPlan selective_plan(int64_t tokens, int D, int N, int groups, const SelSpace& space) {
   SelPlan p{};
-  const int CB = 512 / sel_lanes(N);
+  const int CB = sel_channels(sel_lanes(N));
   p.blocks = ceil_div(D / groups, CB);
   p.all_blocks = p.blocks * groups;
   const int64_t tiles = std::max<int64_t>(1, (tokens + kSelectiveTile - 1) / kSelectiveTile);
