@@ -60,6 +60,10 @@ template <int CTRL>
 __device__ __forceinline__ float lane_moved(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
 }
+// A value that is computed at this place.  The compiler otherwise moves a sum to where it is
+// read: the last step of a sum over lanes into the branch that stores it, where it takes an
+// instruction more, a gradient's sum behind the loop, with all its terms in registers.
+__device__ __forceinline__ void here(float& v) { asm volatile("" : "+v"(v)); }
 // The sum over the LN lanes of a channel, in all of them: neighbours, pairs, the half row
 // mirrored, the row mirrored.
 template <int LN>
@@ -68,6 +72,7 @@ __device__ __forceinline__ float sum_states(float v) {
   if constexpr (LN > 2) v += lane_moved<0x4e>(v);
   if constexpr (LN > 4) v += lane_moved<0x141>(v);
   if constexpr (LN > 8) v += lane_moved<0x140>(v);
+  here(v);
   return v;
 }
 
@@ -478,7 +483,7 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS) void k_selective_ends(SelArg
 }
 
 template <class T, int LN>
-__global__ __launch_bounds__(SelShape<LN>::THREADS) void k_selective(SelArgs) {
+__global__ __launch_bounds__(SelShape<LN>::THREADS, 4) void k_selective(SelArgs) {
   using S = SelShape<LN>;
   __shared__ SelLds<LN> s;
   __shared__ __align__(16) float sy[kSelTile * S::CB];
@@ -504,7 +509,7 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS) void k_selective(SelArgs) {
   const RowSpot xs = RowSpot::of(none, first.c.ld_x, w.k0, w.q0), ds = RowSpot::of(none, first.c.ld_delta, w.k0, w.q0);
   const RowSpot zs = RowSpot::of(none, first.c.ld_z, w.k0, w.q0), ys = RowSpot::of(none, first.c.ld_y, w.k0, w.q0);
   const bool gated = first.c.z != nullptr, soft = first.c.softplus;
-  QuadTile<T, S> xn, dn, zn;  // the next tile's
+  QuadTile<T, S> xn, dn, zv;  // the next tile's, and this one's z
   StateTile<T, LN> bn;
   const auto fetch = [&](int t0) {
     const SelCall& c = again(args).c;
@@ -513,7 +518,6 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS) void k_selective(SelArgs) {
     dn.load(c.delta, c.ld_delta, ds, t0, count, whole, w);
     xn.load(c.x, c.ld_x, xs, t0, count, whole, w);
     bn.load(c.B, c.ld_B, c.C, c.ld_C, t0, count, w.head, c.N);
-    if (gated) zn.load(c.z, c.ld_z, zs, t0, count, whole, w);
   };
   fetch(lo);
   float A[2][4], h[2][4], bias[4], skip[4];
@@ -527,7 +531,7 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS) void k_selective(SelArgs) {
   for (int t0 = lo; t0 < hi; t0 += kSelTile) {
     const int count = min(kSelTile, hi - t0);
     const bool whole = whole_tile<S>(w, count);
-    const QuadTile<T, S> xv = xn, zv = zn;
+    const QuadTile<T, S> xv = xn;
     float d[S::EACH][4];
     tile_steps<T, LN>(dn, bias, soft, w, count, whole, d);
 #pragma unroll
@@ -545,8 +549,9 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS) void k_selective(SelArgs) {
     __syncthreads();
     const uint32_t starts = __builtin_amdgcn_readfirstlane(s.marks.starts);
     const uint32_t stops = __builtin_amdgcn_readfirstlane(s.marks.stops);
-    if (t0 + kSelTile < hi) fetch(t0 + kSelTile);
     const SelArgs& a = again(args);
+    if (gated) zv.load(a.c.z, a.c.ld_z, zs, t0, count, whole, w);
+    if (t0 + kSelTile < hi) fetch(t0 + kSelTile);
     if (t0 == lo) {
       if (!(starts & 1) && lo > 0) {
         carry_into<LN>(a.c, a.p, range, 1, w, A, h);
@@ -584,7 +589,7 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS) void k_selective(SelArgs) {
       if (w.nl == 0) *reinterpret_cast<float2*>(sy + k * S::CB + w.lane_c) = float2{out[0], out[1]};
     };
     if ((starts | stops) == 0) {  // (tokens past the range have no step and add nothing)
-#pragma unroll 4
+#pragma unroll 2
       for (int k = 0; k < kSelTile; ++k) token(k);
     } else {
       for (int k = 0; k < count; ++k) {

@@ -34,12 +34,9 @@ __device__ __forceinline__ void sum_channels(const float (&v)[8], float (&out)[2
     if constexpr (LN <= 8) out[i] += lane_moved<0x128>(out[i]);  // row_ror:8
     if constexpr (LN <= 4) out[i] += lane_moved<0x124>(out[i]);  // row_ror:4
     if constexpr (LN <= 2) out[i] += lane_moved<0x122>(out[i]);  // row_ror:2
+    here(out[i]);
   }
 }
-
-// A value that is computed at this place: the compiler otherwise moves a sum to where it is
-// read and keeps all its terms until then, which took 64 registers more.
-__device__ __forceinline__ void here(float& v) { asm volatile("" : "+v"(v)); }
 
 // A tile of the gradient's inputs on its way to a thread.
 template <class T, int LN>
