@@ -485,7 +485,7 @@ typedef struct {
   int64_t ld_x, ld_y;
   int32_t nseq;        /* >= 1 */
   int32_t D;           /* 1 .. 2^20 */
-  int32_t taps;        /* 1 .. 8 */
+  int32_t taps;        /* 1 .. 4 */
   int32_t dtype;
   int32_t offset_bytes; /* 4 or 8 with offsets */
   int32_t silu;

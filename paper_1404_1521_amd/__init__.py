@@ -848,29 +848,39 @@ class Context:
         any shape and type, contiguous within a row; ids int32, of any shape.  outs: tensors
         to write to, none of which may overlap an input.  Returns the list."""
         rows = ids.numel()
-        pid = _vector(ids.view(-1), torch.int32, "ids", rows)
+        pid = _vector(ids if ids.dim() == 1 else ids.view(-1), torch.int32, "ids", rows)
         if outs is None:
-            outs = [t.new_empty((rows, *t.shape[1:])) for t in tensors]
-        if len(outs) != len(tensors):
-            raise ValueError(f"{len(tensors)} tensors, {len(outs)} outputs")
+            outs = [torch.empty_like(t) if t.shape[:1] == (rows,) and t.is_contiguous()
+                    else t.new_empty((rows, *t.shape[1:])) for t in tensors]
+        else:
+            if len(outs) != len(tensors):
+                raise ValueError(f"{len(tensors)} tensors, {len(outs)} outputs")
+            for t, o in zip(tensors, outs):
+                if not o.is_cuda or t.dtype is not o.dtype or o.shape != (rows, *t.shape[1:]):
+                    raise ValueError(f"an output of {(rows, *t.shape[1:])} {t.dtype} on the device "
+                                     f"is needed, got {tuple(o.shape)} {o.dtype}")
         items = []
         for t, o in zip(tensors, outs):
-            if not t.is_cuda or not o.is_cuda:
-                raise ValueError("tensors must be device (cuda) tensors")
-            if t.dim() < 1 or t.dtype is not o.dtype or o.shape != (rows, *t.shape[1:]):
-                raise ValueError(f"an output of {(rows, *t.shape[1:])} {t.dtype} is needed, got "
-                                 f"{tuple(o.shape)} {o.dtype}")
-            size = t.element_size()
-            width = t[0].numel() if t.shape[0] else 0
-            ld = []
-            for v in (t, o):
-                if not v.is_contiguous() and v.shape[0] and not v[0].is_contiguous():
+            if not t.is_cuda or t.dim() < 1:
+                raise ValueError("tensors must be device (cuda) tensors of rows")
+            have = t.shape[0]
+            if not have:
+                if rows:
+                    raise ValueError("a tensor without rows has none to give")
+                continue
+            if t.is_contiguous():
+                width = ld_t = t.nbytes // have
+            else:
+                width, ld_t = t[0].nbytes, t.stride(0) * t.element_size()
+                if not t[0].is_contiguous():
                     raise ValueError("rows must be contiguous")
-                ld.append(size * (v.stride(0) if v.shape[0] > 1 else width))
-            if not t.shape[0] and rows:
-                raise ValueError("a tensor without rows has none to give")
-            items.append(RowCopy.pack(t.data_ptr(), o.data_ptr(), size * width, *ld,
-                                      max(1, t.shape[0]), 0))
+            ld_o = width
+            if not o.is_contiguous():
+                if rows and not o[0].is_contiguous():
+                    raise ValueError("rows must be contiguous")
+                ld_o = o.stride(0) * o.element_size()
+            items.append(RowCopy.pack(t.data_ptr(), o.data_ptr(), width, max(ld_t, width),
+                                      max(ld_o, width), have, 0))
         rc = self._lib.polyglot_reorder(self._h, b"".join(items), len(items), pid, rows)
         if rc != OK:
             self._check(rc, "reorder")

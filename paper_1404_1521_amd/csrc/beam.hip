@@ -9,7 +9,8 @@ namespace pg {
 
 namespace {
 
-constexpr int kJoinEach = 8;  // keys of a thread in a batch of the join
+constexpr int kJoinEach = 7;  // keys of a thread in a batch of the join, beside a pick so far
+static_assert((kJoinEach + 1) * kBeamPicks <= kBeamList, "the join's list");
 
 template <class T>
 hipError_t parts_of(const BeamCall& c, int E, const Launch& L) {
@@ -23,6 +24,7 @@ hipError_t parts_of(const BeamCall& c, int E, const Launch& L) {
 hipError_t launch_beam(BeamCall c, int dtype, const Launch& L) {
   // Long parts are fewer picks to join; short ones spread a few rows over the chip.
   int E = 32;
+  while (E * c.picks > kBeamList) E /= 2;
   const int64_t rows = (int64_t)c.groups * c.beams;
   while (E > 4 && rows * ceil_div(c.V, E * kBlock) < 2 * kCus) E /= 2;
   c.parts = ceil_div(c.V, E * kBlock);

@@ -4,11 +4,11 @@
 // complement of its place: larger keys are larger sums, and of equal ones the lower place.
 // No two candidates have the same key, so that the picks do not depend on who finds them.
 //
-// A workgroup takes a part of a row, E words to a thread.  The k-th largest of the 256
-// threads' largest keys is a bound: the k picks are not below it, and only k threads hold
-// keys that are not, k E at most.  Those go to a list, whose k largest, found by counting
-// how many are larger, go out.  A second launch does the same over a group's parts, a
-// batch at a time.
+// A workgroup takes a part of a row, E words to a thread.  The k-th largest of a wave's 64
+// lanes' largest keys is a bound: the wave's k largest are not below it, and only k lanes hold
+// keys that are not, k E at most.  Those of the four waves go to a list, whose k largest, found
+// by counting how many are larger, go out.  A second launch does the same over a group's parts,
+// a batch at a time.
 #pragma once
 #include "logits_dev.h"
 #include "operators.h"
@@ -26,54 +26,56 @@ __device__ __forceinline__ float beam_value(uint64_t key) {
   return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
 }
 
-template <int E>
+constexpr int kBeamList = 512;  // most keys of a wave's list: k E
+
 struct BeamLds {
-  uint64_t top[kBlock];
-  uint64_t list[(kBeamPicks + 1) * E];
-  uint64_t bound;
+  uint64_t list[kWavesPerBlock * kBeamList];
   int n;
 };
 
-// The k largest of the workgroup's keys (0: none), E to a thread, to out[k] in their order.
-template <int E>
-__device__ __forceinline__ void pick(const uint64_t (&key)[E], int k, BeamLds<E>& l, uint64_t* out) {
-  const int t = threadIdx.x;
-  uint64_t best = 0;
-#pragma unroll
-  for (int i = 0; i < E; ++i) best = key[i] > best ? key[i] : best;
-  l.top[t] = best;
-  if (t == 0) l.n = 0, l.bound = 0;
-  __syncthreads();
+__device__ __forceinline__ uint64_t lane_key(uint64_t v, int lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+  const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane);
+  return (uint64_t)hi << 32 | lo;
+}
+
+// The k-th largest of a wave's keys `best` (0 where there are fewer).
+__device__ __forceinline__ uint64_t wave_bound(uint64_t best, int k) {
   int above = 0;
 #pragma unroll 16
-  for (int i = 0; i < kBlock; ++i) above += l.top[i] > best;
-  if (above == k - 1 && best) l.bound = best;  // (one thread: keys differ)
-  __syncthreads();
-  const uint64_t bound = l.bound;
-  if (best >= bound && best) {
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (key[i] && key[i] >= bound) l.list[atomicAdd(&l.n, 1)] = key[i];
-  }
-  __syncthreads();
+  for (int i = 0; i < kWave; ++i) above += lane_key(best, i) > best;
+  const uint64_t at = __ballot(above == k - 1 && best);  // one lane: keys differ
+  return at ? lane_key(best, __builtin_ctzll(at)) : 0;
+}
+
+// The k largest of the list, to out[k] in their order (0: none).  By the workgroup, behind a
+// barrier.
+__device__ __forceinline__ void rank_list(const BeamLds& l, int k, uint64_t* out) {
   const int n = l.n;
-  for (int i = t; i < n; i += kBlock) {
+  for (int i = threadIdx.x; i < n; i += kBlock) {
     const uint64_t own = l.list[i];
     int rank = 0;
-    for (int j = 0; j < n && rank < k; ++j) rank += l.list[j] > own;
+    int j = 0;
+    for (; j + 8 <= n && rank < k; j += 8) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) rank += l.list[j + e] > own;
+    }
+    for (; j < n; ++j) rank += l.list[j] > own;
     if (rank < k) out[rank] = own;
   }
-  for (int i = n + t; i < k; i += kBlock) out[i] = 0;
+  for (int i = n + threadIdx.x; i < k; i += kBlock) out[i] = 0;
 }
 
 // E words to a thread, in quads 4 * 256 words apart.
 template <class T, int E>
 __global__ __launch_bounds__(kBlock) void k_beam_parts(BeamCall c) {
-  __shared__ BeamLds<E> l;
+  __shared__ BeamLds l;
   const int t = threadIdx.x;
   const int64_t r = blockIdx.x / c.parts;
   const int part = (int)(blockIdx.x - r * c.parts);
   uint64_t* out = c.keys + (int64_t)blockIdx.x * c.picks;
+  const int v0 = part * (E * kBlock) + 4 * t;
+  const bool whole = (part + 1) * (E * kBlock) <= c.V;
   const float total = c.total[r];
   if (c.finished && c.finished[r]) {  // its one candidate: nothing more is said
     const bool here = c.end / (E * kBlock) == part;
@@ -81,50 +83,75 @@ __global__ __launch_bounds__(kBlock) void k_beam_parts(BeamCall c) {
       out[i] = i == 0 && here ? beam_key(total, (uint32_t)c.end) : 0;
     return;
   }
-  const int v0 = part * (E * kBlock) + 4 * t;
-  const bool whole = (part + 1) * (E * kBlock) <= c.V;
   const T* in = static_cast<const T*>(c.scores) + r * c.ld;
   Quad<T> x[E / 4];
 #pragma unroll
   for (int g = 0; g < E / 4; ++g) x[g] = row_quad<T>(in, v0 + g * 4 * kBlock, c.V, whole);
   const float base = c.lse ? __fsub_rn(total, c.lse[r]) : total;
-  uint64_t key[E];
+  if (t == 0) l.n = 0;
+  // the sums, the largest of them, and the first place that has it
+  float v[E], top = -__builtin_inff();
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    const int v = v0 + (i / 4) * 4 * kBlock + (i & 3);
-    key[i] = whole || v < c.V ? beam_key(__fadd_rn(x[i / 4].get(i & 3), base), (uint32_t)v) : 0;
+    v[i] = __fadd_rn(x[i / 4].get(i & 3), base);
+    if (!whole && v0 + (i / 4) * 4 * kBlock + (i & 3) >= c.V) v[i] = -__builtin_inff();
+    top = fmaxf(top, v[i]);  // (not a NaN)
   }
-  pick<E>(key, c.picks, l, out);
+  int first = 0;
+#pragma unroll
+  for (int i = E - 1; i >= 0; --i)
+    if (v[i] == top) first = (i / 4) * 4 * kBlock + (i & 3);
+  const uint64_t best = beam_key(top, (uint32_t)(v0 + first));
+  const uint64_t bound = wave_bound(best, c.picks);
+  __syncthreads();
+  if (best >= bound && best) {
+    const float low = bound ? beam_value(bound) : -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      if (!(v[i] >= low)) continue;
+      const uint64_t key = beam_key(v[i], (uint32_t)(v0 + (i / 4) * 4 * kBlock + (i & 3)));
+      if (key && key >= bound) l.list[atomicAdd(&l.n, 1)] = key;
+    }
+  }
+  __syncthreads();
+  rank_list(l, c.picks, out);
 }
 
 // A workgroup for each group: its rows' parts, 256 E keys at a time beside the picks so far.
 template <int E>
 __global__ __launch_bounds__(kBlock) void k_beam_join(BeamCall c) {
-  __shared__ BeamLds<E + 1> l;
+  __shared__ BeamLds l;
   __shared__ uint64_t best[kBeamPicks];
   const int t = threadIdx.x;
   const int64_t row0 = (int64_t)blockIdx.x * c.beams;
   const int64_t each = (int64_t)c.parts * c.picks, all = each * c.beams;
   const uint64_t* in = c.keys + row0 * each;
   if (t < kBeamPicks) best[t] = 0;
-  __syncthreads();
   for (int64_t first = 0; first < all; first += E * kBlock) {
-    uint64_t key[E + 1];
-    bool any = false;
-    const uint64_t last = best[c.picks - 1];
+    uint64_t key[E + 1], top = 0;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       const int64_t at = first + i * kBlock + t;
       key[i] = at < all ? in[at] : 0;
       if (key[i]) {  // the place in a row becomes the place in the group
-        const uint32_t b = (uint32_t)(at / each);
+        const uint32_t b = (uint32_t)((uint64_t)at < (1ull << 32) ? (uint32_t)at / (uint32_t)each : at / each);
         key[i] = (key[i] & 0xffffffff00000000ull) | ~(~(uint32_t)key[i] + b * (uint32_t)c.V);
-        any |= key[i] > last;
       }
+      top = key[i] > top ? key[i] : top;
     }
+    if (t == 0) l.n = 0;
+    __syncthreads();
+    if (!__syncthreads_or(top > best[c.picks - 1])) continue;
     key[E] = t < c.picks ? best[t] : 0;
-    if (!__syncthreads_or(any)) continue;
-    pick<E + 1>(key, c.picks, l, best);
+    top = key[E] > top ? key[E] : top;
+    const uint64_t bound = wave_bound(top, c.picks);
+    if (top >= bound && top) {
+#pragma unroll
+      for (int i = 0; i <= E; ++i)
+        if (key[i] && key[i] >= bound) l.list[atomicAdd(&l.n, 1)] = key[i];
+    }
+    __syncthreads();
+    rank_list(l, c.picks, best);
     __syncthreads();
   }
   if (t >= c.picks) return;

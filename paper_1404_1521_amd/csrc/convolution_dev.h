@@ -2,267 +2,336 @@
 //   u_t[c] = bias[c] + sum_{k < K} w[c][k] x_{t-K+1+k}[c],   y = u or u sigmoid(u)
 // where a sequence's first tokens reach back into its state, the K - 1 inputs before it.
 //
-// A thread takes four channels of a run of consecutive tokens and keeps the last K - 1
-// inputs in registers: every tensor is read once and written once, but for the K - 1
-// tokens before a run (the gradient: behind it, too), which the caches hold.
-// The gradient walks forward as well: a token's g = dy act'(u) goes into K sums, for itself
-// and the K - 1 inputs before it; the oldest of them is complete and leaves.
+// A row of lanes takes a chunk of consecutive tokens, four or eight channels to a lane, and
+// goes through it in steps of eight tokens with the last K - 1 inputs in registers and the
+// next step's inputs on their way: every tensor is read once and written once, but for the
+// K - 1 tokens before a chunk (the gradient: behind it, too).  Which sequence it is in and
+// where that ends, it keeps; no two waves wait for each other.  The gradient walks forward as
+// well: a token's g = dy act'(u) goes into K sums, for itself and the K - 1 inputs before it;
+// the oldest of them is complete and leaves.
 #pragma once
+#include <type_traits>
+
 #include "selective_dev.h"
 
 namespace pg {
 
-constexpr int kConvRoom = kBlock / kConvMinLanes * kConvRun + kConvMaxK;  // marked places
-
-struct ConvLds {
-  int start[kConvRoom], stop[kConvRoom];
-  int before[kWave];  // the sequence of the token before each 64th of the tile
-  int list[kBlock];
-};
-
-// The places of a tile of `tokens` tokens (a multiple of 64), and K - 1 more, by wave 0.
-__device__ __forceinline__ void conv_places(const Packed& s, int lo, int tokens, int more,
-                                            ConvLds& l) {
-  const int lane = lane_id();
-  const int hi = (int)min((int64_t)lo + tokens + more, (int64_t)s.tokens);
-  const int cursor = first_place(s, lo);
-  mark_places(s, lo, hi, tokens + more, cursor, l.start, l.stop);
-  const int seg = tokens / kWave;
-  int m = -1;
-  for (int j = 0; j < seg; ++j) m = max(m, l.start[lane * seg + j]);
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const int o = __shfl_up(m, d);
-    if (lane >= d) m = max(m, o);
+// f(0), ..., f(N - 1), each by itself: loads held in registers are indexed by constants.
+template <int N, class F>
+__device__ __forceinline__ void each(F f) {
+  if constexpr (N > 0) {
+    each<N - 1>(f);
+    f(std::integral_constant<int, N - 1>{});
   }
-  const int o = __shfl_up(m, 1);
-  l.before[lane] = min(s.nseq - 1, max(0, max(lane ? o : -1, cursor - 1)));
 }
 
-// A thread's tile, run and channels.
+// The sequence that a row of lanes is in, and where that ends.
+struct ConvWalk {
+  int seq, end;
+  // The one that token t lies in: the last offset <= t, found by the row's lanes side by side.
+  __device__ __forceinline__ ConvWalk(const Packed& s, int t, int lanes_log2) {
+    const int lanes = 1 << lanes_log2, l = lane_id() & (lanes - 1), row = lane_id() >> lanes_log2;
+    int at = 0, n = s.nseq + 1;  // the first offset > t is in [at, at + n]
+    while (__ballot(n > 0)) {
+      const int step = ceil_div(n, lanes + 1);
+      const int i = at + (l + 1) * step - 1;
+      const bool below = n > 0 && i < at + n && place_of(s, i) <= t;
+      const uint64_t all = __ballot(below) >> (row << lanes_log2);
+      const int k = __popcll(lanes == kWave ? all : all & ((1ull << lanes) - 1));
+      at += k * step;
+      n -= k * step;
+      if (k < lanes) n = min(max(step - 1, 0), n);
+    }
+    seq = min(max(at - 1, 0), s.nseq - 1);
+    end = place_of(s, seq + 1);
+  }
+  // To the next sequence that has tokens, if token t is its first.
+  __device__ __forceinline__ bool next(const Packed& s, int t) {
+    if (t != end) return false;
+    do {
+      end = ++seq < s.nseq ? place_of(s, seq + 1) : INT32_MAX;
+    } while (end <= t);
+    seq = min(seq, s.nseq - 1);
+    return true;
+  }
+};
+
+// V channels in 8 or 16 bytes, any alignment; at a row's end the first n of them.
+template <class T, int V>
+struct Strip {
+  typedef std::conditional_t<V * sizeof(T) == 16, u4_any, u2_any> Raw;
+  Raw raw;
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(raw[i]);
+    else return Elem<T>::get(T{(uint16_t)(i & 1 ? raw[i / 2] >> 16 : raw[i / 2])});
+  }
+  __device__ __forceinline__ void load(const T* p, int n) {
+    raw = Raw{};
+    if (n == V) {
+      raw = *reinterpret_cast<const Raw*>(p);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V - 1; ++i) {
+        if (i >= n) continue;
+        if constexpr (sizeof(T) == 4) raw[i] = __float_as_uint(p[i]);
+        else raw[i / 2] |= (uint32_t)p[i].bits << (16 * (i & 1));
+      }
+    }
+  }
+  static __device__ __forceinline__ void store(T* p, const float (&v)[V], int n) {
+    if (n == V) {
+      if constexpr (V == 4) store_quad<T, true>(p, v, 4);
+      else Oct<T>::store(p, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V - 1; ++i)
+        if (i < n) p[i] = Elem<T>::put(settled(v[i]));
+    }
+  }
+};
+
+// A thread's chunk and channels.
+template <int V>
 struct ConvPlace {
   int cl, tl, ch, nv;
   __device__ __forceinline__ ConvPlace(const ConvCall& c, int block) {
     const int CT = 1 << c.lanes_log2;
     cl = threadIdx.x & (CT - 1);
     tl = threadIdx.x >> c.lanes_log2;
-    ch = (block * CT + cl) * 4;
-    nv = max(0, min(4, c.D - ch));
+    ch = (block * CT + cl) * V;
+    nv = max(0, min(V, c.D - ch));
     if (nv == 0) ch = 0;
   }
 };
 
-template <class T>
+// A row of a sequence's state (none: zeros).
+template <class T, int V>
 __device__ __forceinline__ void conv_state(const ConvCall& c, const void* state, int K, int seq, int row,
-                                           const ConvPlace& w, float (&v)[4]) {
-  Quad<T> q{};
-  if (state && w.nv > 0)
-    q = some_quad(static_cast<const T*>(state) + ((int64_t)seq * (K - 1) + row) * c.D + w.ch, w.nv);
+                                           const ConvPlace<V>& w, float (&v)[V]) {
+  Strip<T, V> q;
+  q.load(static_cast<const T*>(state) + ((int64_t)seq * (K - 1) + row) * c.D + w.ch, state ? w.nv : 0);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) v[j] = q.get(j);
+  for (int j = 0; j < V; ++j) v[j] = q.get(j);
 }
 
 // Copies an empty sequence's rows, the workgroup's channels of them.
-template <class T>
+template <class T, int V>
 __device__ __forceinline__ void conv_copy(const ConvCall& c, int K, int seq, const void* from, void* to,
-                                          const ConvPlace& w) {
+                                          const ConvPlace<V>& w) {
   if (w.nv <= 0) return;
   for (int row = w.tl; row < K - 1; row += kBlock >> c.lanes_log2) {
-    float v[4];
+    float v[V];
     conv_state<T>(c, from, K, seq, row, w, v);
-    put_quad(static_cast<T*>(to) + ((int64_t)seq * (K - 1) + row) * c.D + w.ch, v, w.nv);
+    Strip<T, V>::store(static_cast<T*>(to) + ((int64_t)seq * (K - 1) + row) * c.D + w.ch, v, w.nv);
   }
 }
 
-template <int K>
-__device__ __forceinline__ void conv_weights(const ConvCall& c, const ConvPlace& w, float (&wt)[K][4],
-                                             float (&bias)[4]) {
+template <int K, int V>
+__device__ __forceinline__ void conv_weights(const ConvCall& c, const ConvPlace<V>& w, float (&wt)[K][V],
+                                             float (&bias)[V]) {
+  struct __attribute__((packed, aligned(4))) Taps {
+    float k[K];
+  };
+  const Taps* rows = reinterpret_cast<const Taps*>(c.weight) + w.ch;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const bool there = j < w.nv;
-    bias[j] = there && c.bias ? c.bias[w.ch + j] : 0.f;
+  for (int j = 0; j < V; ++j) {
+    Taps q{};
+    if (j < w.nv) q = rows[j];
 #pragma unroll
-    for (int k = 0; k < K; ++k) wt[k][j] = there ? c.weight[(int64_t)(w.ch + j) * K + k] : 0.f;
+    for (int k = 0; k < K; ++k) wt[k][j] = q.k[k];
+    bias[j] = j < w.nv && c.bias ? c.bias[w.ch + j] : 0.f;
   }
 }
 
 // The inputs before token t of sequence seq, `place` tokens into it.
-template <class T, int K>
-__device__ __forceinline__ void conv_window(const ConvCall& c, const ConvPlace& w, int t, int seq, int place,
-                                            float (&win)[K][4]) {
+template <class T, int K, int V>
+__device__ __forceinline__ void conv_window(const ConvCall& c, const ConvPlace<V>& w, int t, int seq, int place,
+                                            float (&win)[K][V]) {
 #pragma unroll
   for (int k = 0; k < K - 1; ++k) {
     const int back = K - 1 - k;
     if (place >= back) {
-      Quad<T> q{};
-      if (w.nv > 0) q = some_quad(static_cast<const T*>(c.x) + (t - (int64_t)back) * c.ld_x + w.ch, w.nv);
+      Strip<T, V> q;
+      q.load(static_cast<const T*>(c.x) + (t - (int64_t)back) * c.ld_x + w.ch, w.nv);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) win[k][j] = q.get(j);
+      for (int j = 0; j < V; ++j) win[k][j] = q.get(j);
     } else {
       conv_state<T>(c, c.state, K, seq, K - 1 + place - back, w, win[k]);
     }
   }
 }
 
-template <int K>
-__device__ __forceinline__ void conv_sum(const float (&wt)[K][4], const float (&bias)[4],
-                                         const float (&win)[K][4], float (&u)[4]) {
+template <int K, int V>
+__device__ __forceinline__ void conv_sum(const float (&wt)[K][V], const float (&bias)[V],
+                                         const float (&win)[K][V], float (&u)[V]) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (int j = 0; j < V; ++j) {
     u[j] = bias[j];
 #pragma unroll
     for (int k = 0; k < K; ++k) u[j] = __fmaf_rn(wt[k][j], win[k][j], u[j]);
   }
 }
+template <int K, int V>
+__device__ __forceinline__ void conv_shift(float (&win)[K][V]) {
+#pragma unroll
+  for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+    for (int j = 0; j < V; ++j) win[k][j] = win[k + 1][j];
+}
 
-template <class T, int K>
+template <class T, int K, int V>
 __global__ __launch_bounds__(kBlock) void k_convolution(ConvCall c) {
-  constexpr int R = kConvRun;
-  __shared__ ConvLds l;
-  const int t = threadIdx.x;
-  const int tile = blockIdx.x / c.blocks, block = blockIdx.x % c.blocks;
-  const ConvPlace w(c, block);
-  const int tokens = (kBlock >> c.lanes_log2) * R;
-  const int lo = tile * tokens;
-  check_places(c.seqs, tile, c.tiles, kBlock, c.last != nullptr && K > 1, l.list,
+  constexpr int R = kConvStep;
+  __shared__ int list[kBlock];
+  const int group = blockIdx.x / c.blocks, block = blockIdx.x % c.blocks;
+  const ConvPlace<V> w(c, block);
+  check_places(c.seqs, group, c.groups, kBlock, c.last != nullptr && K > 1, list,
                [&](int i) { conv_copy<T>(c, K, i, c.state, c.last, w); });
-  if (lo >= c.seqs.tokens) return;
-  const int t0 = lo + w.tl * R, count = max(0, min(R, c.seqs.tokens - t0));
+  const int64_t chunk = (int64_t)group * (kBlock >> c.lanes_log2) + w.tl;
+  const int t0 = (int)min(chunk * c.chunk, (int64_t)c.seqs.tokens);
+  const int t1 = (int)min((int64_t)t0 + c.chunk, (int64_t)c.seqs.tokens);
   const T* x = static_cast<const T*>(c.x) + w.ch;
-  Quad<T> xv[R];
+  T* y = static_cast<T*>(c.y) + w.ch;
+  Strip<T, V> xv[R];
+  const auto fetch = [&](int at) {
 #pragma unroll
-  for (int i = 0; i < R; ++i) {
-    xv[i] = Quad<T>{};
-    if (i < count && w.nv > 0) xv[i] = some_quad(x + (t0 + (int64_t)i) * c.ld_x, w.nv);
-  }
-  float wt[K][4], bias[4], win[K][4];
+    for (int i = 0; i < R; ++i) xv[i].load(x + (at + (int64_t)i) * c.ld_x, at + i < t1 ? w.nv : 0);
+  };
+  fetch(t0);
+  float wt[K][V], bias[V], win[K][V];
   conv_weights<K>(c, w, wt, bias);
-  if (t < kWave) conv_places(c.seqs, lo, tokens, 0, l);
-  __syncthreads();
-  if (count == 0 || w.nv == 0) return;
-  int seq = l.before[w.tl * R / (tokens / kWave)];
-  if (l.start[t0 - lo] < 0) conv_window<T, K>(c, w, t0, seq, max(0, t0 - place_of(c.seqs, seq)), win);
+  ConvWalk walk(c.seqs, min(t0, c.seqs.tokens - 1), c.lanes_log2);
+  if (t0 >= t1 || w.nv == 0) return;
+  conv_window<T, K>(c, w, t0, walk.seq, max(0, t0 - place_of(c.seqs, walk.seq)), win);
+  const auto token = [&](const Strip<T, V>& in, T* to) {
 #pragma unroll
-  for (int i = 0; i < R; ++i) {
-    if (i >= count) continue;
-    const int from = l.start[t0 - lo + i];
-    if (from >= 0) {
-      seq = from;
-      conv_window<T, K>(c, w, t0 + i, seq, 0, win);
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) win[K - 1][j] = xv[i].get(j);
-    float u[4];
+    for (int j = 0; j < V; ++j) win[K - 1][j] = in.get(j);
+    float u[V];
     conv_sum<K>(wt, bias, win, u);
     if (c.silu) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) u[j] *= sigmoid(u[j]);
+      for (int j = 0; j < V; ++j) u[j] *= sigmoid(u[j]);
     }
-    put_quad(static_cast<T*>(c.y) + (t0 + (int64_t)i) * c.ld_y + w.ch, u, w.nv);
-    if (c.last && l.stop[t0 - lo + i] >= 0) {
+    Strip<T, V>::store(to, u, w.nv);
+  };
+  for (int at = t0; at < t1; at += R) {
+    if (walk.end > at + R && at + R <= t1) {  // the usual step, in the middle of a sequence
+      Strip<T, V> now[R];
 #pragma unroll
-      for (int k = 1; k < K; ++k)
-        put_quad(static_cast<T*>(c.last) + ((int64_t)seq * (K - 1) + k - 1) * c.D + w.ch, win[k], w.nv);
+      for (int i = 0; i < R; ++i) now[i] = xv[i];
+      if (at + R < t1) fetch(at + R);
+      each<R>([&](auto step) {
+        constexpr int i = decltype(step)::value;
+        token(now[i], y + (at + (int64_t)i) * c.ld_y);
+        conv_shift<K>(win);
+      });
+      continue;
     }
+    for (int k = at; k < min(at + R, t1); ++k) {
+      if (walk.next(c.seqs, k)) conv_window<T, K>(c, w, k, walk.seq, 0, win);
+      Strip<T, V> in;
+      in.load(x + (int64_t)k * c.ld_x, w.nv);
+      token(in, y + (int64_t)k * c.ld_y);
+      if (c.last && k + 1 == walk.end) {
 #pragma unroll
-    for (int k = 0; k < K - 1; ++k)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) win[k][j] = win[k + 1][j];
+        for (int j = 1; j < K; ++j)
+          Strip<T, V>::store(static_cast<T*>(c.last) + ((int64_t)walk.seq * (K - 1) + j - 1) * c.D + w.ch, win[j],
+                             w.nv);
+      }
+      conv_shift<K>(win);
+    }
+    if (at + R < t1) fetch(at + R);
   }
 }
 
 // One token for each sequence; a thread reads all that it needs before it writes.
-template <class T, int K>
+template <class T, int K, int V>
 __global__ __launch_bounds__(kBlock) void k_convolution_step(ConvCall c) {
-  const int quads = ceil_div(c.D, 4);
-  const int64_t all = (int64_t)c.seqs.nseq * quads;
+  const int strips = ceil_div(c.D, V);
+  const int64_t all = (int64_t)c.seqs.nseq * strips;
   for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < all; i += (int64_t)gridDim.x * kBlock) {
-    const int row = (int)(i / quads);
-    ConvPlace w(c, 0);
-    w.ch = (int)(i % quads) * 4;
-    w.nv = min(4, c.D - w.ch);
-    float wt[K][4], bias[4], win[K][4], u[4];
+    const int row = (int)(i / strips);
+    ConvPlace<V> w(c, 0);
+    w.ch = (int)(i % strips) * V;
+    w.nv = min(V, c.D - w.ch);
+    float wt[K][V], bias[V], win[K][V], u[V];
 #pragma unroll
     for (int k = 0; k < K - 1; ++k) conv_state<T>(c, c.state, K, row, k, w, win[k]);
-    const Quad<T> xv = some_quad(static_cast<const T*>(c.x) + row * c.ld_x + w.ch, w.nv);
+    Strip<T, V> xv;
+    xv.load(static_cast<const T*>(c.x) + row * c.ld_x + w.ch, w.nv);
     conv_weights<K>(c, w, wt, bias);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) win[K - 1][j] = xv.get(j);
+    for (int j = 0; j < V; ++j) win[K - 1][j] = xv.get(j);
     conv_sum<K>(wt, bias, win, u);
     if (c.silu) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) u[j] *= sigmoid(u[j]);
+      for (int j = 0; j < V; ++j) u[j] *= sigmoid(u[j]);
     }
-    put_quad(static_cast<T*>(c.y) + row * c.ld_y + w.ch, u, w.nv);
+    Strip<T, V>::store(static_cast<T*>(c.y) + row * c.ld_y + w.ch, u, w.nv);
     if (c.last) {
 #pragma unroll
       for (int k = 1; k < K; ++k)
-        put_quad(static_cast<T*>(c.last) + ((int64_t)row * (K - 1) + k - 1) * c.D + w.ch, win[k], w.nv);
+        Strip<T, V>::store(static_cast<T*>(c.last) + ((int64_t)row * (K - 1) + k - 1) * c.D + w.ch, win[k], w.nv);
     }
   }
 }
 
-template <class T, int K>
+template <class T, int K, int V>
 __global__ __launch_bounds__(kBlock) void k_convolution_grad(ConvCall c) {
-  constexpr int R = kConvRun;
-  __shared__ ConvLds l;
-  __shared__ __align__(16) float red[kBlock * 4];
+  constexpr int R = kConvStep;
+  __shared__ int list[kBlock];
+  __shared__ __align__(16) float red[kBlock * V];
   const int t = threadIdx.x;
   const int group = blockIdx.x / c.blocks, block = blockIdx.x % c.blocks;
-  const ConvPlace w(c, block);
-  const int CT = 1 << c.lanes_log2, TL = kBlock >> c.lanes_log2, tokens = TL * R;
-  check_places(c.seqs, group, c.groups, kBlock, c.dstate != nullptr && K > 1, l.list,
+  const ConvPlace<V> w(c, block);
+  const int CT = 1 << c.lanes_log2, TL = kBlock >> c.lanes_log2;
+  check_places(c.seqs, group, c.groups, kBlock, c.dstate != nullptr && K > 1, list,
                [&](int i) { conv_copy<T>(c, K, i, c.dlast, c.dstate, w); });
-  float wt[K][4], bias[4], dw[K][4], db[4] = {0.f, 0.f, 0.f, 0.f};
+  const int64_t chunk = (int64_t)group * TL + w.tl;
+  const int t0 = (int)min(chunk * c.chunk, (int64_t)c.seqs.tokens);
+  const int t1 = (int)min((int64_t)t0 + c.chunk, (int64_t)c.seqs.tokens);
+  const int end = (int)min((int64_t)t1 + K - 1, (int64_t)c.seqs.tokens);  // looked at
+  const T* x = static_cast<const T*>(c.x) + w.ch;
+  const T* dy = static_cast<const T*>(c.dy) + w.ch;
+  T* dx = static_cast<T*>(c.dx) + w.ch;
+  Strip<T, V> xv[R], gv[R];
+  const auto fetch = [&](int at) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      xv[i].load(x + (at + (int64_t)i) * c.ld_x, at + i < end ? w.nv : 0);
+      gv[i].load(dy + (at + (int64_t)i) * c.ld_dy, at + i < end ? w.nv : 0);
+    }
+  };
+  fetch(t0);
+  float wt[K][V], bias[V], dw[K][V], db[V], win[K][V], acc[K][V];
   conv_weights<K>(c, w, wt, bias);
 #pragma unroll
-  for (int k = 0; k < K; ++k)
+  for (int j = 0; j < V; ++j) {
+    db[j] = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) dw[k][j] = 0.f;
-
-  for (int tile = group; tile < c.tiles; tile += c.groups) {
-    const int lo = tile * tokens;
-    __syncthreads();
-    if (t < kWave) conv_places(c.seqs, lo, tokens, K - 1, l);
-    __syncthreads();
-    const int t0 = lo + w.tl * R;
-    if (t0 >= c.seqs.tokens || w.nv == 0) continue;
-    const int end = (int)min((int64_t)t0 + R + K - 1, (int64_t)c.seqs.tokens);  // looked at
-    float win[K][4], acc[K][4];
+    for (int k = 0; k < K; ++k) dw[k][j] = acc[k][j] = 0.f;
+  }
+  ConvWalk walk(c.seqs, min(t0, max(0, c.seqs.tokens - 1)), c.lanes_log2);
+  if (t0 < t1 && w.nv > 0) {
+    int begin = min(place_of(c.seqs, walk.seq), t0);  // of the sequence
+    conv_window<T, K>(c, w, t0, walk.seq, t0 - begin, win);
+    // A token's g into the sums: own, of the chunk (not of those looked at behind it).
+    const auto take = [&](const Strip<T, V>& xi, const Strip<T, V>& gi, bool own) {
+      float g[V];
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[k][j] = 0.f;
-    int seq = l.before[w.tl * R / (tokens / kWave)], place = 0;
-    if (l.start[t0 - lo] < 0) {
-      place = max(0, t0 - place_of(c.seqs, seq));
-      conv_window<T, K>(c, w, t0, seq, place, win);
-    }
-    for (int at = t0; at < end; ++at) {
-      const int from = l.start[at - lo];
-      if (from >= 0) {
-        if (at >= t0 + R) break;  // the run's last sequence has ended
-        seq = from;
-        place = 0;
-        conv_window<T, K>(c, w, at, seq, 0, win);
-      }
-      const Quad<T> xv = some_quad(static_cast<const T*>(c.x) + (int64_t)at * c.ld_x + w.ch, w.nv);
-      const Quad<T> gv = some_quad(static_cast<const T*>(c.dy) + (int64_t)at * c.ld_dy + w.ch, w.nv);
-      float g[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) win[K - 1][j] = xv.get(j), g[j] = gv.get(j);
+      for (int j = 0; j < V; ++j) win[K - 1][j] = xi.get(j), g[j] = gi.get(j);
       if (c.silu) {
-        float u[4];
+        float u[V];
         conv_sum<K>(wt, bias, win, u);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < V; ++j) {
           const float s = sigmoid(u[j]);
           g[j] *= s * __fmaf_rn(u[j], 1.f - s, 1.f);
         }
       }
-      if (at < t0 + R) {
+      if (own) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < V; ++j) {
           db[j] += g[j];
 #pragma unroll
           for (int k = 0; k < K; ++k) dw[k][j] = __fmaf_rn(g[j], win[k][j], dw[k][j]);
@@ -271,79 +340,111 @@ __global__ __launch_bounds__(kBlock) void k_convolution_grad(ConvCall c) {
 #pragma unroll
       for (int b = 0; b < K; ++b)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[b][j] = __fmaf_rn(wt[K - 1 - b][j], g[j], acc[b][j]);
-      // What is complete leaves: the input b tokens back, or that row of the state.
-      const auto emit = [&](int b, const float (&v)[4]) {
-        if (place >= b) {
-          const int s = at - b;
-          if (s >= t0 && s < t0 + R) put_quad(static_cast<T*>(c.dx) + (int64_t)s * c.ld_dx + w.ch, v, w.nv);
-        } else if (c.dstate && at - place >= t0 && at - place < t0 + R) {
-          put_quad(static_cast<T*>(c.dstate) + ((int64_t)seq * (K - 1) + K - 1 + place - b) * c.D + w.ch, v,
-                   w.nv);
-        }
-      };
-      if (l.stop[at - lo] >= 0) {
+        for (int j = 0; j < V; ++j) acc[b][j] = __fmaf_rn(wt[K - 1 - b][j], g[j], acc[b][j]);
+    };
+    const auto move_on = [&] {
+      conv_shift<K>(win);
 #pragma unroll
-        for (int b = K - 1; b >= 0; --b) {
-          float v[4] = {acc[b][0], acc[b][1], acc[b][2], acc[b][3]};
-          if (b < K - 1 && c.dlast) {
-            float d[4];
-            conv_state<T>(c, c.dlast, K, seq, K - 2 - b, w, d);
+      for (int j = 0; j < V; ++j) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] += d[j];
-          }
-          emit(b, v);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[b][j] = 0.f;
-        }
-      } else {
-        emit(K - 1, acc[K - 1]);
-#pragma unroll
-        for (int b = K - 1; b > 0; --b)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[b][j] = acc[b - 1][j];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[0][j] = 0.f;
+        for (int b = K - 1; b > 0; --b) acc[b][j] = acc[b - 1][j];
+        acc[0][j] = 0.f;
       }
+    };
+    for (int at = t0; at < end; at += R) {
+      // the usual step: tokens of the chunk, whose sequence goes on behind them
+      if (walk.end > at + R && at + R <= t1) {
+        Strip<T, V> xn[R], gn[R];
 #pragma unroll
-      for (int k = 0; k < K - 1; ++k)
+        for (int i = 0; i < R; ++i) xn[i] = xv[i], gn[i] = gv[i];
+        if (at + R < end) fetch(at + R);
+        each<R>([&](auto step) {
+          constexpr int i = decltype(step)::value;
+          take(xn[i], gn[i], true);
+          const int k = at + i, s = k - (K - 1);
+          if (s >= max(t0, begin)) Strip<T, V>::store(dx + (int64_t)s * c.ld_dx, acc[K - 1], w.nv);
+          else if (s < begin && begin >= t0 && c.dstate)
+            Strip<T, V>::store(static_cast<T*>(c.dstate) + ((int64_t)walk.seq * (K - 1) + k - begin) * c.D + w.ch,
+                               acc[K - 1], w.nv);
+          move_on();
+        });
+        continue;
+      }
+      for (int k = at; k < min(at + R, end); ++k) {
+        if (walk.next(c.seqs, k)) {
+          if (k >= t1) {  // the chunk's last sequence has ended
+            at = end;
+            break;
+          }
+          begin = k;
+          conv_window<T, K>(c, w, k, walk.seq, 0, win);
+        }
+        Strip<T, V> xi, gi;
+        xi.load(x + (int64_t)k * c.ld_x, w.nv);
+        gi.load(dy + (int64_t)k * c.ld_dy, w.nv);
+        take(xi, gi, k < t1);
+        // What is complete leaves: the input b tokens back, or that row of the state.
+        const auto emit = [&](int b, const float (&v)[V]) {
+          const int s = k - b;
+          if (s >= begin) {
+            if (s >= t0 && s < t1) Strip<T, V>::store(dx + (int64_t)s * c.ld_dx, v, w.nv);
+          } else if (c.dstate && begin >= t0 && begin < t1) {
+            Strip<T, V>::store(
+                static_cast<T*>(c.dstate) + ((int64_t)walk.seq * (K - 1) + K - 1 + s - begin) * c.D + w.ch, v, w.nv);
+          }
+        };
+        if (k + 1 == walk.end) {  // all of them, with dlast's rows
+          for (int b = K - 1; b >= 0; --b) {
+            if (b < K - 1 && c.dlast) {
+              float d[V];
+              conv_state<T>(c, c.dlast, K, walk.seq, K - 2 - b, w, d);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) win[k][j] = win[k + 1][j];
-      ++place;
+              for (int j = 0; j < V; ++j) acc[K - 1][j] += d[j];
+            }
+            emit(b, acc[K - 1]);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+#pragma unroll
+              for (int i = K - 1; i > 0; --i) acc[i][j] = acc[i - 1][j];
+              acc[0][j] = 0.f;
+            }
+          }
+          conv_shift<K>(win);
+        } else {
+          emit(K - 1, acc[K - 1]);
+          move_on();
+        }
+      }
+      if (at + R < end) fetch(at + R);
     }
   }
 
-  // the workgroup's runs, in order
+  // the workgroup's chunks, in order
 #pragma unroll
   for (int k = 0; k <= K; ++k) {
     __syncthreads();
-    if (k < K) st4(red + t * 4, f4{dw[k < K ? k : 0][0], dw[k < K ? k : 0][1], dw[k < K ? k : 0][2], dw[k < K ? k : 0][3]});
-    else st4(red + t * 4, f4{db[0], db[1], db[2], db[3]});
+#pragma unroll
+    for (int j = 0; j < V; j += 4) {
+      const float* v = k < K ? dw[k < K ? k : 0] : db;
+      st4(red + t * V + j, f4{v[j], v[j + 1], v[j + 2], v[j + 3]});
+    }
     __syncthreads();
-    const int ch = block * 4 * CT + t;
-    if (t < 4 * CT && ch < c.D) {
+    for (int i = t; i < V * CT; i += kBlock) {
+      const int ch = block * V * CT + i;
+      if (ch >= c.D) continue;
       float v = 0.f;
-      for (int j = 0; j < TL; ++j) v += red[j * 4 * CT + t];
+      for (int j = 0; j < TL; ++j) v += red[j * V * CT + i];
       c.part[((int64_t)group * (K + 1) + k) * c.D + ch] = v;
     }
   }
 }
 
-// dw and the bias's gradient from the groups' sums: 64 of them to a workgroup, a quarter of
-// the groups to each thread.
+// dw and the bias's gradient from the groups' sums: 16 of them to a workgroup, a sixteenth
+// of the groups to each thread.
 __global__ __launch_bounds__(kBlock) void k_convolution_sums(ConvCall c, int K) {
-  __shared__ float part[kBlock];
-  const int t = threadIdx.x;
-  const int64_t o = (int64_t)blockIdx.x * kWave + t % kWave, all = (int64_t)(K + 1) * c.D;
-  float v = 0.f;
-  if (o < all) {
-#pragma unroll 8
-    for (int g = t / kWave; g < c.groups; g += kWavesPerBlock) v += c.part[g * all + o];
-  }
-  part[t] = v;
-  __syncthreads();
-  if (t >= kWave || o >= all) return;
-  v = (part[t] + part[t + 64]) + (part[t + 128] + part[t + 192]);
+  const int64_t o = (int64_t)blockIdx.x * kSumOutputs + threadIdx.x % kSumOutputs, all = (int64_t)(K + 1) * c.D;
+  const float v = sum_parts(c.part + o, all, c.groups, o < all);
+  if (threadIdx.x >= kSumOutputs || o >= all) return;
   const int64_t k = o / c.D, ch = o % c.D;
   if (k < K) c.dweight[ch * K + k] = v;
   else if (c.dbias) c.dbias[ch] = v;

@@ -61,7 +61,7 @@ template <class A>
 int check_convolution(polyglot_ctx* ctx, const A& a, const std::string& what) {
   const int rc = check_packed(ctx, a, what);
   if (rc) return rc;
-  if (a.taps < 1 || a.taps > kConvMaxK) return fail(ctx, POLYGLOT_EINVAL, what + ": 1 to 8 taps");
+  if (a.taps < 1 || a.taps > kConvMaxK) return fail(ctx, POLYGLOT_EINVAL, what + ": 1 to 4 taps");
   if (!a.weight) return fail(ctx, POLYGLOT_ENULL, what + ": NULL weight");
   if (!all_aligned({a.weight, a.bias}, 4) || !aligned(a.state, size_of(a.dtype)))
     return fail(ctx, POLYGLOT_EINVAL, what + ": misaligned weight, bias or state");

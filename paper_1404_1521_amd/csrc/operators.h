@@ -134,14 +134,13 @@ struct ConvCall {
   int64_t ld_x, ld_y, ld_dy, ld_dx;
   Packed seqs;
   int D, silu;
-  int lanes_log2, blocks;  // lanes of a row of threads, four channels each; rows of blocks
-  int tiles, groups;       // of tokens; the gradient's workgroups for a row of blocks
+  int lanes_log2, blocks;  // lanes of a row of threads; rows of blocks
+  int chunk, groups;       // tokens of a row of threads; workgroups for a row of blocks
   float* part;             // [groups][K + 1][D] sums of the weights' and the bias's gradients
 };
-constexpr int kConvMaxK = 8;
-constexpr int kConvRun = 16;           // tokens of a thread
-constexpr int kConvMinLanes = 8;
-constexpr int kConvWorkgroups = 2048;  // of a gradient, where the tokens give as many
+constexpr int kConvMaxK = 4;
+constexpr int kConvStep = 8;           // tokens that a row of threads reads ahead
+constexpr int kConvWorkgroups = 1024;  // where the tokens give as many
 
 struct BeamCall {
   const void* scores;

@@ -135,6 +135,28 @@ struct SelPlace {
   __device__ __forceinline__ bool has(int r) const { return lane_c + r < nc; }
 };
 
+// The sum of n values `ld` apart, by a workgroup for kSumOutputs sums side by side: each
+// thread takes every sixteenth value, and the sixteen sums are added in their order.  The
+// first kSumOutputs threads have the results.
+constexpr int kSumOutputs = 16;
+__device__ __forceinline__ float sum_parts(const float* from, int64_t ld, int n, bool there) {
+  constexpr int kSlices = kBlock / kSumOutputs;
+  __shared__ float part[kBlock];
+  float v = 0.f;
+  if (there) {
+#pragma unroll 8
+    for (int i = threadIdx.x / kSumOutputs; i < n; i += kSlices) v += from[i * ld];
+  }
+  part[threadIdx.x] = v;
+  __syncthreads();
+  v = 0.f;
+  if (threadIdx.x < kSumOutputs) {
+#pragma unroll
+    for (int i = 0; i < kSlices; ++i) v += part[i * kSumOutputs + threadIdx.x];
+  }
+  return v;
+}
+
 template <class T>
 __device__ __forceinline__ Quad<T> some_quad(const T* p, int n) {
   return n == 4 ? load_quad<T, true>(p, 4) : load_quad<T, false>(p, n);
@@ -360,7 +382,6 @@ struct alignas(16) SelLds {
   float step[kSelTile * S::CB], dx[kSelTile * S::CB];
   float B[kSelTile * S::NP], C[kSelTile * S::NP];
   TileMarks marks;
-  int from;
 };
 
 // What a range passes on, to the workspace.
@@ -379,21 +400,37 @@ __device__ __forceinline__ void pass_on(const SelCall& c, const SelPlan& p, int 
 
 // ---------------------------------------------------------------- forward
 
-// Where the first launch starts in a range: the start of the sequence that runs out of the
-// range, the range's first token if that lies before it; hi if none runs out.
-__device__ __forceinline__ int run_start(const Packed& s, int lo, int hi) {
-  if (hi >= s.tokens) return hi;
+// What a range passes on, and where the first launch takes it up: from the start of the
+// sequence that runs out of the range, its number seq, or from the range's first token if
+// that sequence began before it (seq -1).  By a whole wave.
+struct RangeEnd {
+  int at, seq;
+  uint32_t kind;
+};
+__device__ __forceinline__ RangeEnd range_end(const Packed& s, int lo, int hi) {
+  RangeEnd r{hi, -1, kSelNone};
+  if (hi >= s.tokens) return r;
   const int i = first_place(s, hi);  // the first offset >= hi
-  if (i <= s.nseq && place_of(s, i) == hi) return hi;
-  return i > 0 ? min(max(place_of(s, i - 1), lo), hi) : lo;
+  if (i <= s.nseq && place_of(s, i) == hi) return r;
+  const int o = i > 0 ? min(place_of(s, i - 1), hi - 1) : 0;
+  const bool starts = o >= lo && i > 0;
+  r.at = starts ? o : lo;
+  r.seq = starts ? i - 1 : -1;
+  r.kind = starts || lo == 0 ? kSelClosed : kSelOpen;
+  return r;
 }
-// ... and where the gradient's stops: the end of the sequence that runs into it.
-__device__ __forceinline__ int run_stop(const Packed& s, int lo, int hi) {
-  if (lo == 0) return lo;
+// The gradient's: up to the end of the sequence that runs into the range, if it ends in it.
+__device__ __forceinline__ RangeEnd range_start(const Packed& s, int lo, int hi) {
+  RangeEnd r{lo, -1, kSelNone};
+  if (lo == 0 || lo >= hi) return r;
   const int i = first_place(s, lo);
-  if (i > s.nseq) return hi;
-  const int o = place_of(s, i);
-  return o == lo ? lo : max(min(o, hi), lo);
+  const int o = i <= s.nseq ? place_of(s, i) : hi;
+  if (o == lo) return r;
+  const bool ends = o <= hi && i > 0 && i <= s.nseq;
+  r.at = max(lo, min(o, hi));
+  r.seq = ends ? i - 1 : -1;
+  r.kind = ends ? kSelClosed : kSelOpen;
+  return r;
 }
 
 template <class T, int LN>
@@ -406,23 +443,10 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS) void k_selective_ends(SelArg
   const int range = blockIdx.x / first.p.all_blocks, block = blockIdx.x % first.p.all_blocks;
   const SelPlace<LN> w(first.c, first.p, block);
   const int lo = range * first.p.range, hi = min(lo + first.p.range, first.c.seqs.tokens);
-  if (t < kWave) {
-    const int at = run_start(first.c.seqs, lo, hi);
-    if (t == 0) s.from = at;
-  }
-  __syncthreads();
-  const int from = s.from;
-  // A sequence that starts in the range, or one that runs through all of it.
-  int seq = -1;  // ... whose state before its first token counts, if it starts here
-  bool starts = from > lo || lo == 0;
-  if (!starts) {
-    const int i = first_place(first.c.seqs, lo);
-    starts = i <= first.c.seqs.nseq && place_of(first.c.seqs, i) == lo;
-  }
-  if (starts && from < hi)  // the last offset <= from
-    seq = max(0, min(first_place(first.c.seqs, from + 1) - 1, first.c.seqs.nseq - 1));
-  if (t == 0 && block == 0) first.p.info[range] = from == hi ? kSelNone : starts ? kSelClosed : kSelOpen;
-  if (from == hi) return;
+  const RangeEnd end = range_end(first.c.seqs, lo, hi);
+  const int from = end.at, seq = end.seq;
+  if (t == 0 && block == 0) first.p.info[range] = end.kind;
+  if (end.kind == kSelNone) return;
 
   const RowSpot xs = RowSpot::of((const T*)nullptr, first.c.ld_x, w.k0, w.q0);
   const RowSpot ds = RowSpot::of((const T*)nullptr, first.c.ld_delta, w.k0, w.q0);

@@ -97,14 +97,10 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS) void k_selective_grad_ends(S
   const int range = blockIdx.x / first.p.all_blocks, block = blockIdx.x % first.p.all_blocks;
   const SelPlace<LN> w(first.c, first.p, block);
   const int lo = range * first.p.range, hi = min(lo + first.p.range, first.c.seqs.tokens);
-  const int to = lo < hi ? run_stop(first.c.seqs, lo, hi) : lo;
-  int seq = -1;  // the sequence that ends at `to`, if one does
-  if (to > lo) {
-    const int i = first_place(first.c.seqs, to);
-    if (i > 0 && i <= first.c.seqs.nseq && place_of(first.c.seqs, i) == to) seq = i - 1;
-  }
-  if (t == 0 && block == 0) first.p.info[range] = to == lo ? kSelNone : seq >= 0 ? kSelClosed : kSelOpen;
-  if (to == lo) return;
+  const RangeEnd end = range_start(first.c.seqs, lo, hi);
+  const int to = end.at, seq = end.seq;
+  if (t == 0 && block == 0) first.p.info[range] = end.kind;
+  if (end.kind == kSelNone) return;
 
   int tile = (to - 1 - lo) / kSelTile;
   GradTile<T, LN> in;
@@ -446,13 +442,12 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 2) void k_selective_grad(Sel
 }
 
 // The sums over the ranges (dA, dskip, the bias's) and over the workgroups of a head's
-// channels (dB, dC).  64 sums to a workgroup, a quarter of the ranges to each thread.
+// channels (dB, dC).
 template <class T>
 __global__ __launch_bounds__(kBlock) void k_selective_sums(SelCall c, SelPlan p, int NP, int param_blocks) {
-  __shared__ float part[kBlock];
   const int t = threadIdx.x;
   if ((int)blockIdx.x < param_blocks) {
-    const int64_t o = (int64_t)blockIdx.x * kWave + t % kWave, n_a = (int64_t)c.D * c.N;
+    const int64_t o = (int64_t)blockIdx.x * kSumOutputs + t % kSumOutputs, n_a = (int64_t)c.D * c.N;
     const float* from = nullptr;
     int64_t ld = 0;
     float* to = nullptr;
@@ -467,14 +462,8 @@ __global__ __launch_bounds__(kBlock) void k_selective_sums(SelCall c, SelPlan p,
       if (i < c.D) to = c.dskip ? c.dskip + i : nullptr;
       else to = c.dbias ? c.dbias + i - c.D : nullptr;
     }
-    float v = 0.f;
-    if (from) {
-#pragma unroll 8
-      for (int r = t / kWave; r < p.ranges; r += kWavesPerBlock) v += from[r * ld];
-    }
-    part[t] = v;
-    __syncthreads();
-    if (t < kWave && to) *to = (part[t] + part[t + 64]) + (part[t + 128] + part[t + 192]);
+    const float v = sum_parts(from, ld, p.ranges, to != nullptr);
+    if (t < kSumOutputs && to) *to = v;
     return;
   }
   const int64_t width = (int64_t)c.groups * 2 * c.N, all = width * c.seqs.tokens;

@@ -12,7 +12,7 @@ hipError_t grad_of_lanes(const SelCall& c, const SelPlan& p, const Launch& L) {
   if (p.ranges > 1) e = pg_launch(k_selective_grad_ends<T, LN>, grid, block, 0, L, SelArgs{c, p});
   if (e == hipSuccess) e = pg_launch(k_selective_grad<T, LN>, grid, block, 0, L, SelArgs{c, p});
   if (e != hipSuccess) return e;
-  const int params = (int)(((int64_t)c.D * (c.N + 2) + kWave - 1) / kWave);
+  const int params = (int)(((int64_t)c.D * (c.N + 2) + kSumOutputs - 1) / kSumOutputs);
   const int64_t rest = p.blocks == 1 ? 0 : (int64_t)c.groups * 2 * c.N * c.seqs.tokens;
   const int sums = (int)std::min<int64_t>((rest + kBlock - 1) / kBlock, 16 * kCus);
   return pg_launch(k_selective_sums<T>, dim3(params + sums), dim3(kBlock), 0, L, c, p, 4 * LN, params);
