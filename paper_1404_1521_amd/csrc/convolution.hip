@@ -14,15 +14,15 @@ namespace {
 // and channel, takes four.
 constexpr int channels(size_t size, bool grad) { return size == 2 && !grad ? 8 : 4; }
 
-// As few lanes as hold all channels; chunks of whole steps that give a SIMD four waves.
-void cut(ConvCall& c, int V) {
+// As few lanes as hold all channels; chunks of whole steps.
+void cut(ConvCall& c, int V, int workgroups) {
   int log2 = 3;
   while (log2 < 6 && (V << log2) < c.D) ++log2;
   c.lanes_log2 = log2;
   c.blocks = ceil_div(c.D, V << log2);
   const int rows = kBlock >> log2;  // chunks of a workgroup
   const int64_t steps = std::max<int64_t>(1, ((int64_t)c.seqs.tokens + kConvStep - 1) / kConvStep);
-  const int64_t want = std::max(1, kConvWorkgroups / c.blocks) * (int64_t)rows;
+  const int64_t want = std::max(1, workgroups / c.blocks) * (int64_t)rows;
   const int64_t each = (steps + want - 1) / want;
   c.chunk = (int)(each * kConvStep);
   c.groups = (int)(((steps + each - 1) / each + rows - 1) / rows);
@@ -49,7 +49,7 @@ hipError_t launch_convolution(ConvCall c, int K, int dtype, const Launch& L) {
     using T = decltype(v);
     return by_taps(K, [&](auto k) {
       constexpr int V = channels(sizeof(T), false);
-      cut(c, V);
+      cut(c, V, kConvWorkgroups);
       return pg_launch(k_convolution<T, decltype(k)::value, V>, dim3((uint32_t)(c.groups * c.blocks)),
                        dim3(kBlock), 0, L, c);
     });
@@ -69,7 +69,7 @@ hipError_t launch_convolution_step(ConvCall c, int K, int dtype, const Launch& L
 }
 
 hipError_t launch_convolution_grad(ConvCall c, int K, int dtype, const Launch& L) {
-  cut(c, channels(4, true));
+  cut(c, channels(4, true), kCus * conv_grad_waves(dtype == POLYGLOT_F32 ? 4 : 2));
   hipError_t e = by_format(dtype, [&](auto v) {
     using T = decltype(v);
     return by_taps(K, [&](auto k) {

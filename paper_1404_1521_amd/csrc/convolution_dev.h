@@ -90,17 +90,26 @@ struct Strip {
   }
 };
 
-// A thread's chunk and channels.
+// A thread's chunk and channels.  The last lane of a row takes whole strips, too, where the
+// row has one: it starts `shift` channels early, and its neighbour computes and writes the
+// same values there.
 template <int V>
 struct ConvPlace {
-  int cl, tl, ch, nv;
+  int cl, tl, ch, nv, shift;
   __device__ __forceinline__ ConvPlace(const ConvCall& c, int block) {
     const int CT = 1 << c.lanes_log2;
     cl = threadIdx.x & (CT - 1);
     tl = threadIdx.x >> c.lanes_log2;
     ch = (block * CT + cl) * V;
     nv = max(0, min(V, c.D - ch));
-    if (nv == 0) ch = 0;
+    shift = 0;
+    if (nv == 0) {
+      ch = 0;
+    } else if (nv < V && c.D >= V) {
+      shift = V - nv;
+      ch -= shift;
+      nv = V;
+    }
   }
 };
 
@@ -182,7 +191,7 @@ __device__ __forceinline__ void conv_shift(float (&win)[K][V]) {
 template <class T, int K, int V>
 __global__ __launch_bounds__(kBlock) void k_convolution(ConvCall c) {
   constexpr int R = kConvStep;
-  __shared__ int list[kBlock];
+  __shared__ int list[kBlock + 1];
   const int group = blockIdx.x / c.blocks, block = blockIdx.x % c.blocks;
   const ConvPlace<V> w(c, block);
   check_places(c.seqs, group, c.groups, kBlock, c.last != nullptr && K > 1, list,
@@ -215,23 +224,25 @@ __global__ __launch_bounds__(kBlock) void k_convolution(ConvCall c) {
     Strip<T, V>::store(to, u, w.nv);
   };
   for (int at = t0; at < t1; at += R) {
-    if (walk.end > at + R && at + R <= t1) {  // the usual step, in the middle of a sequence
-      Strip<T, V> now[R];
+    Strip<T, V> now[R];
 #pragma unroll
-      for (int i = 0; i < R; ++i) now[i] = xv[i];
-      if (at + R < t1) fetch(at + R);
+    for (int i = 0; i < R; ++i) now[i] = xv[i];
+    if (at + R < t1) fetch(at + R);
+    T* to = y + (int64_t)at * c.ld_y;
+    if (walk.end > at + R && at + R <= t1) {  // the usual step, in the middle of a sequence
       each<R>([&](auto step) {
         constexpr int i = decltype(step)::value;
-        token(now[i], y + (at + (int64_t)i) * c.ld_y);
+        token(now[i], to + i * c.ld_y);
         conv_shift<K>(win);
       });
       continue;
     }
-    for (int k = at; k < min(at + R, t1); ++k) {
+    each<R>([&](auto step) {
+      constexpr int i = decltype(step)::value;
+      const int k = at + i;
+      if (k >= t1) return;
       if (walk.next(c.seqs, k)) conv_window<T, K>(c, w, k, walk.seq, 0, win);
-      Strip<T, V> in;
-      in.load(x + (int64_t)k * c.ld_x, w.nv);
-      token(in, y + (int64_t)k * c.ld_y);
+      token(now[i], to + i * c.ld_y);
       if (c.last && k + 1 == walk.end) {
 #pragma unroll
         for (int j = 1; j < K; ++j)
@@ -239,8 +250,7 @@ __global__ __launch_bounds__(kBlock) void k_convolution(ConvCall c) {
                              w.nv);
       }
       conv_shift<K>(win);
-    }
-    if (at + R < t1) fetch(at + R);
+    });
   }
 }
 
@@ -251,7 +261,7 @@ __global__ __launch_bounds__(kBlock) void k_convolution_step(ConvCall c) {
   const int64_t all = (int64_t)c.seqs.nseq * strips;
   for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < all; i += (int64_t)gridDim.x * kBlock) {
     const int row = (int)(i / strips);
-    ConvPlace<V> w(c, 0);
+    ConvPlace<V> w(c, 0);  // (last may be state: no channel twice)
     w.ch = (int)(i % strips) * V;
     w.nv = min(V, c.D - w.ch);
     float wt[K][V], bias[V], win[K][V], u[V];
@@ -277,9 +287,9 @@ __global__ __launch_bounds__(kBlock) void k_convolution_step(ConvCall c) {
 }
 
 template <class T, int K, int V>
-__global__ __launch_bounds__(kBlock) void k_convolution_grad(ConvCall c) {
-  constexpr int R = kConvStep;
-  __shared__ int list[kBlock];
+__global__ __launch_bounds__(kBlock, conv_grad_waves(sizeof(T))) void k_convolution_grad(ConvCall c) {
+  constexpr int R = sizeof(T) == 4 ? kConvStep : kConvStep / 2;
+  __shared__ int list[kBlock + 1];
   __shared__ __align__(16) float red[kBlock * V];
   const int t = threadIdx.x;
   const int group = blockIdx.x / c.blocks, block = blockIdx.x % c.blocks;
@@ -342,8 +352,7 @@ __global__ __launch_bounds__(kBlock) void k_convolution_grad(ConvCall c) {
 #pragma unroll
         for (int j = 0; j < V; ++j) acc[b][j] = __fmaf_rn(wt[K - 1 - b][j], g[j], acc[b][j]);
     };
-    const auto move_on = [&] {
-      conv_shift<K>(win);
+    const auto shift_sums = [&] {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
 #pragma unroll
@@ -351,13 +360,14 @@ __global__ __launch_bounds__(kBlock) void k_convolution_grad(ConvCall c) {
         acc[0][j] = 0.f;
       }
     };
-    for (int at = t0; at < end; at += R) {
+    bool over = false;  // the chunk's last sequence has ended
+    for (int at = t0; at < end && !over; at += R) {
+      Strip<T, V> xn[R], gn[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) xn[i] = xv[i], gn[i] = gv[i];
+      if (at + R < end) fetch(at + R);
       // the usual step: tokens of the chunk, whose sequence goes on behind them
       if (walk.end > at + R && at + R <= t1) {
-        Strip<T, V> xn[R], gn[R];
-#pragma unroll
-        for (int i = 0; i < R; ++i) xn[i] = xv[i], gn[i] = gv[i];
-        if (at + R < end) fetch(at + R);
         each<R>([&](auto step) {
           constexpr int i = decltype(step)::value;
           take(xn[i], gn[i], true);
@@ -366,56 +376,52 @@ __global__ __launch_bounds__(kBlock) void k_convolution_grad(ConvCall c) {
           else if (s < begin && begin >= t0 && c.dstate)
             Strip<T, V>::store(static_cast<T*>(c.dstate) + ((int64_t)walk.seq * (K - 1) + k - begin) * c.D + w.ch,
                                acc[K - 1], w.nv);
-          move_on();
+          shift_sums();
+          conv_shift<K>(win);
         });
         continue;
       }
-      for (int k = at; k < min(at + R, end); ++k) {
+      each<R>([&](auto step) {
+        constexpr int i = decltype(step)::value;
+        const int k = at + i;
+        if (k >= end || over) return;
         if (walk.next(c.seqs, k)) {
-          if (k >= t1) {  // the chunk's last sequence has ended
-            at = end;
-            break;
+          if (k >= t1) {
+            over = true;
+            return;
           }
           begin = k;
           conv_window<T, K>(c, w, k, walk.seq, 0, win);
         }
-        Strip<T, V> xi, gi;
-        xi.load(x + (int64_t)k * c.ld_x, w.nv);
-        gi.load(dy + (int64_t)k * c.ld_dy, w.nv);
-        take(xi, gi, k < t1);
+        take(xn[i], gn[i], k < t1);
         // What is complete leaves: the input b tokens back, or that row of the state.
-        const auto emit = [&](int b, const float (&v)[V]) {
+        const auto emit = [&](int b) {
           const int s = k - b;
           if (s >= begin) {
-            if (s >= t0 && s < t1) Strip<T, V>::store(dx + (int64_t)s * c.ld_dx, v, w.nv);
+            if (s >= t0 && s < t1) Strip<T, V>::store(dx + (int64_t)s * c.ld_dx, acc[K - 1], w.nv);
           } else if (c.dstate && begin >= t0 && begin < t1) {
             Strip<T, V>::store(
-                static_cast<T*>(c.dstate) + ((int64_t)walk.seq * (K - 1) + K - 1 + s - begin) * c.D + w.ch, v, w.nv);
+                static_cast<T*>(c.dstate) + ((int64_t)walk.seq * (K - 1) + K - 1 + s - begin) * c.D + w.ch,
+                acc[K - 1], w.nv);
           }
         };
-        if (k + 1 == walk.end) {  // all of them, with dlast's rows
-          for (int b = K - 1; b >= 0; --b) {
-            if (b < K - 1 && c.dlast) {
+        emit(K - 1);
+        shift_sums();
+        if (k + 1 == walk.end) {  // the others as well, with dlast's rows
+#pragma unroll 1
+          for (int b = K - 2; b >= 0; --b) {
+            if (c.dlast) {
               float d[V];
               conv_state<T>(c, c.dlast, K, walk.seq, K - 2 - b, w, d);
 #pragma unroll
               for (int j = 0; j < V; ++j) acc[K - 1][j] += d[j];
             }
-            emit(b, acc[K - 1]);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-#pragma unroll
-              for (int i = K - 1; i > 0; --i) acc[i][j] = acc[i - 1][j];
-              acc[0][j] = 0.f;
-            }
+            emit(b);
+            shift_sums();
           }
-          conv_shift<K>(win);
-        } else {
-          emit(K - 1, acc[K - 1]);
-          move_on();
         }
-      }
-      if (at + R < end) fetch(at + R);
+        conv_shift<K>(win);
+      });
     }
   }
 
@@ -430,10 +436,11 @@ __global__ __launch_bounds__(kBlock) void k_convolution_grad(ConvCall c) {
     }
     __syncthreads();
     for (int i = t; i < V * CT; i += kBlock) {
-      const int ch = block * V * CT + i;
+      const int ch = block * V * CT + i, first = ch - i % V;  // of the strip
       if (ch >= c.D) continue;
+      const int at = i + (c.D >= V ? max(0, first + V - c.D) : 0);
       float v = 0.f;
-      for (int j = 0; j < TL; ++j) v += red[j * V * CT + i];
+      for (int j = 0; j < TL; ++j) v += red[j * V * CT + at];
       c.part[((int64_t)group * (K + 1) + k) * c.D + ch] = v;
     }
   }

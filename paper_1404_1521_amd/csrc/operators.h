@@ -141,6 +141,8 @@ struct ConvCall {
 constexpr int kConvMaxK = 4;
 constexpr int kConvStep = 8;           // tokens that a row of threads reads ahead
 constexpr int kConvWorkgroups = 1024;  // where the tokens give as many
+// Waves to a SIMD of the gradient, whose workgroups are to run all at once.
+constexpr int conv_grad_waves(size_t size) { return size == 4 ? 2 : 3; }
 
 struct BeamCall {
   const void* scores;

@@ -112,17 +112,17 @@ __device__ __forceinline__ void mark_tile(const Packed& s, int lo, int hi, DownC
 
 // A workgroup's share of the sequences, the `part`-th of `parts`: raises the flag where
 // the offsets do not ascend from 0 to the tokens, and calls copy(i) with every thread for
-// each empty sequence i.
+// each empty sequence i.  list: a place for each thread and one more.
 template <class F>
 __device__ __forceinline__ void check_places(const Packed& s, int part, int parts, int threads,
                                              bool copies, int* list, F copy) {
   const int t = threadIdx.x;
   for (int64_t base = (int64_t)part * threads; base < s.nseq; base += (int64_t)parts * threads) {
+    if (copies && t == 0) list[threads] = 0;
+    if (copies) __syncthreads();
     const int i = (int)base + t;
-    bool empty = false;
     if (i < s.nseq) {
       const int o = place_of(s, i), e = place_of(s, i + 1);
-      empty = o == e;
       bool bad = e < o || (i == 0 && o != 0) || (i == s.nseq - 1 && e != s.tokens);
       if (s.offsets && s.offset_bytes == 8) {
         const int64_t* p = static_cast<const int64_t*>(s.offsets) + i;
@@ -132,13 +132,12 @@ __device__ __forceinline__ void check_places(const Packed& s, int part, int part
         bad |= p[0] < 0 || p[1] < 0 || p[0] > s.tokens || p[1] > s.tokens;
       }
       if (bad) atomicOr(s.flag, kFlagBadOffset);
+      if (copies && o == e) list[atomicAdd(&list[threads], 1)] = i;
     }
     if (!copies) continue;
-    if (!__syncthreads_or(empty)) continue;
-    list[t] = empty ? i : -1;
     __syncthreads();
-    for (int j = 0; j < threads; ++j)
-      if (list[j] >= 0) copy(__builtin_amdgcn_readfirstlane(list[j]));
+    const int n = __builtin_amdgcn_readfirstlane(list[threads]);
+    for (int j = 0; j < n; ++j) copy(__builtin_amdgcn_readfirstlane(list[j]));
     __syncthreads();
   }
 }

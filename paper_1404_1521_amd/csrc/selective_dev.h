@@ -511,7 +511,7 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 4) void k_selective(SelArgs)
   using S = SelShape<LN>;
   __shared__ SelLds<LN> s;
   __shared__ __align__(16) float sy[kSelTile * S::CB];
-  __shared__ int list[S::THREADS];
+  __shared__ int list[S::THREADS + 1];
   const SelArgsPtr args = sel_args();
   const SelArgs& first = again(args);
   const int t = threadIdx.x;

@@ -145,7 +145,7 @@ struct alignas(16) SelGradLds {
   SelLds<LN> in;
   float dv[kSelTile * S::CB], dstep[kSelTile * S::CB];
   float part[S::W][kSelTile][2][S::NP];
-  int list[S::THREADS];
+  int list[S::THREADS + 1];
 };
 
 template <class T, int LN>
