@@ -288,7 +288,7 @@ __global__ __launch_bounds__(kBlock) void k_convolution_step(ConvCall c) {
 
 template <class T, int K, int V>
 __global__ __launch_bounds__(kBlock, conv_grad_waves(sizeof(T))) void k_convolution_grad(ConvCall c) {
-  constexpr int R = sizeof(T) == 4 ? kConvStep : kConvStep / 2;
+  constexpr int R = kConvStep / 2;
   __shared__ int list[kBlock + 1];
   __shared__ __align__(16) float red[kBlock * V];
   const int t = threadIdx.x;
