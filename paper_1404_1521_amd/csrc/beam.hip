@@ -7,18 +7,28 @@
 
 namespace pg {
 
+namespace {
+
+constexpr int kJoinEach = 8;  // keys of a thread in a batch of the join
+
+template <class T>
+hipError_t parts_of(const BeamCall& c, int E, const Launch& L) {
+  auto k = E == 64 ? k_beam_parts<T, 64> : E == 32 ? k_beam_parts<T, 32> : E == 16 ? k_beam_parts<T, 16>
+         : E == 8  ? k_beam_parts<T, 8>  : k_beam_parts<T, 4>;
+  return pg_launch(k, dim3((uint32_t)(c.groups * c.beams * c.parts)), dim3(kBlock), 0, L, c);
+}
+
+}  // namespace
+
 hipError_t launch_beam(BeamCall c, int dtype, const Launch& L) {
-  // As many parts as give every CU two workgroups, of at least 1,024 words.
+  // Long parts are fewer picks to find and to join; short ones spread a few rows over the chip.
+  int E = 64;
   const int64_t rows = (int64_t)c.groups * c.beams;
-  const int64_t want = std::max<int64_t>(1, (2 * kCus + rows - 1) / rows);
-  const int64_t units = ((int64_t)c.V + kBeamMinPart - 1) / kBeamMinPart, each = (units + want - 1) / want;
-  c.part_words = (int)(each * kBeamMinPart);
-  c.parts = (int)((units + each - 1) / each);
-  const hipError_t e = by_format(dtype, [&](auto v) {
-    return pg_launch(k_beam_parts<decltype(v)>, dim3((uint32_t)(rows * c.parts)), dim3(kBlock), 0, L, c);
-  });
+  while (E > 4 && rows * ceil_div(c.V, E * kBlock) < 2 * kCus) E /= 2;
+  c.parts = ceil_div(c.V, E * kBlock);
+  const hipError_t e = by_format(dtype, [&](auto v) { return parts_of<decltype(v)>(c, E, L); });
   if (e != hipSuccess) return e;
-  return pg_launch(k_beam_join, dim3(c.groups), dim3(kBlock), 0, L, c);
+  return pg_launch(k_beam_join<kJoinEach>, dim3(c.groups), dim3(kBlock), 0, L, c);
 }
 
 hipError_t launch_reorder(const ReorderCall& c, const Launch& L) {

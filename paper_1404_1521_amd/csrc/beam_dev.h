@@ -4,11 +4,11 @@
 // complement of its place: larger keys are larger sums, and of equal ones the lower place.
 // No two candidates have the same key, so that the picks do not depend on who finds them.
 //
-// A wave keeps the k largest keys that it has met, the i-th largest in lane i, and looks a
-// batch of its words over: sums, the lanes' largest, and only where one of those is above the
-// wave's k-th is a word taken in, by its rank among the lanes.  Of its first batch the k-th
-// largest of the 64 lanes' largest keys is a bound already.  The four waves' keys are ranked by
-// counting how many are larger; a second launch does the same with the parts of a group.
+// A workgroup takes a part of a row into registers, E words to a thread.  The k-th largest of
+// the 256 threads' largest keys is a bound: the k picks are not below it, and only k threads
+// hold keys that are not, k E at most.  Those go to a list, a few more than k as a rule, whose
+// k largest, found by counting how many are larger, go out.  A second launch does the same
+// over a group's parts, a batch at a time.
 #pragma once
 #include "logits_dev.h"
 #include "operators.h"
@@ -31,130 +31,123 @@ __device__ __forceinline__ uint64_t lane_key(uint64_t v, int lane) {
   const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane);
   return (uint64_t)hi << 32 | lo;
 }
-// The k-th largest of a wave's keys `best` (0 where there are fewer).
-__device__ __forceinline__ uint64_t wave_bound(uint64_t best, int k) {
+template <int LIST>
+struct BeamLds {
+  uint64_t best[kWavesPerBlock][kBeamPicks];  // of each wave the k largest of its lanes' largest
+  uint64_t list[LIST];
+  uint64_t bound;
+  int n;
+};
+
+// The k-th largest of the threads' keys `best` (0 where there are fewer).  First in each wave
+// by its lanes one after the other, then among the waves' k largest.  Ends on a barrier; the
+// list is empty then.
+template <int LIST>
+__device__ __forceinline__ uint64_t group_bound(uint64_t best, int k, BeamLds<LIST>& l) {
+  const int lane = lane_id(), wave = threadIdx.x / kWave;
   int above = 0;
 #pragma unroll 16
   for (int i = 0; i < kWave; ++i) above += lane_key(best, i) > best;
-  const uint64_t at = __ballot(above == k - 1 && best);  // one lane: keys differ
-  return at ? lane_key(best, __builtin_ctzll(at)) : 0;
-}
-__device__ __forceinline__ uint32_t lane_before(uint32_t v) {  // the lane before's (DPP wave_shr:1)
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x138, 0xf, 0xf, false);
-}
-
-// A wave's k largest keys.
-struct WaveBest {
-  uint64_t held = 0;   // of lane i the i-th largest
-  uint64_t least = 1;  // a key has to be no smaller to be taken in
-  int k;
-  __device__ __forceinline__ explicit WaveBest(int k) : k(k) {}
-  // What the lanes bring: none of them has a key above `best`.
-  __device__ __forceinline__ void begin(uint64_t best) {
-    const uint64_t b = wave_bound(best, k);
-    if (b > least) least = b;
-  }
-  // Takes the lanes' keys in where `want`.
-  __device__ __forceinline__ void take(uint64_t key, bool want) {
-    uint64_t lanes = __ballot(want && key >= least);
-    while (lanes) {
-      const int l = __builtin_ctzll(lanes);
-      lanes &= lanes - 1;
-      const uint64_t own = lane_key(key, l);
-      const int rank = __popcll(__ballot(held > own));
-      if (rank >= k) continue;
-      const uint64_t before = (uint64_t)lane_before((uint32_t)(held >> 32)) << 32 | lane_before((uint32_t)held);
-      const int lane = lane_id();
-      held = lane < rank ? held : lane == rank ? own : before;
-      const uint64_t last = lane_key(held, k - 1);
-      if (last > least) least = last;
-    }
-  }
-};
-
-// The workgroup's k largest of its waves' to out[k], in their order (0: none).
-__device__ __forceinline__ void join_waves(const WaveBest& w, int k, uint64_t* list, uint64_t* out) {
-  const int lane = lane_id(), wave = threadIdx.x / kWave;
-  if (lane < k) list[wave * k + lane] = w.held;
+  if (lane < k) l.best[wave][lane] = 0;
+  if (threadIdx.x == 0) l.n = 0, l.bound = 0;
+  wave_lds_sync();
+  if (best && above < k) l.best[wave][above] = best;
   __syncthreads();
-  const int n = kWavesPerBlock * k;
-  if ((int)threadIdx.x >= n) return;
-  const uint64_t own = list[threadIdx.x];
-  int rank = 0;
-  for (int j = 0; j < n; j += 4) {
+  if (best && above < k) {
+    int rank = above;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) rank += list[j + e] > own || (list[j + e] == own && j + e < (int)threadIdx.x);
+    for (int w = 1; w < kWavesPerBlock; ++w) {
+      const uint64_t* other = l.best[(wave + w) % kWavesPerBlock];
+#pragma unroll 4
+      for (int i = 0; i < k; ++i) rank += other[i] > best;
+    }
+    if (rank == k - 1) l.bound = best;  // one thread: keys differ
   }
-  if (rank < k) out[rank] = own;  // (no keys, 0, are ranked by their places)
+  __syncthreads();
+  return l.bound;
 }
 
-constexpr int kBeamBatch = 16;  // words of a thread at a time, in quads 4 * 256 words apart
+// The k largest of the list, to out[k] in their order (0: none).
+template <int LIST>
+__device__ __forceinline__ void rank_list(const BeamLds<LIST>& l, int k, uint64_t* out) {
+  const int n = l.n;
+  for (int i = threadIdx.x; i < n; i += kBlock) {
+    const uint64_t own = l.list[i];
+    int rank = 0, j = 0;
+    for (; j + 8 <= n && rank < k; j += 8) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) rank += l.list[j + e] > own;
+    }
+    for (; j < n; ++j) rank += l.list[j] > own;
+    if (rank < k) out[rank] = own;
+  }
+  for (int i = n + threadIdx.x; i < k; i += kBlock) out[i] = 0;
+}
 
-template <class T>
+// E words to a thread, in quads 4 * 256 words apart.
+template <class T, int E>
 __global__ __launch_bounds__(kBlock) void k_beam_parts(BeamCall c) {
-  constexpr int E = kBeamBatch;
-  __shared__ uint64_t list[kWavesPerBlock * kBeamPicks];
+  __shared__ BeamLds<kBeamPicks * E> l;
   const int t = threadIdx.x;
   const int64_t r = blockIdx.x / c.parts;
   const int part = (int)(blockIdx.x - r * c.parts);
   uint64_t* out = c.keys + (int64_t)blockIdx.x * c.picks;
-  const int begin = (int)min((int64_t)part * c.part_words, (int64_t)c.V);
-  const int end = (int)min((int64_t)begin + c.part_words, (int64_t)c.V);
   const float total = c.total[r];
   if (c.finished && c.finished[r]) {  // its one candidate: nothing more is said
-    const bool here = c.end >= begin && c.end < end;
+    const bool here = c.end / (E * kBlock) == part;
     for (int i = t; i < c.picks; i += kBlock)
       out[i] = i == 0 && here ? beam_key(total, (uint32_t)c.end) : 0;
     return;
   }
+  const int v0 = part * (E * kBlock) + 4 * t;
+  const bool whole = (part + 1) * (E * kBlock) <= c.V;
   const T* in = static_cast<const T*>(c.scores) + r * c.ld;
-  Quad<T> next[E / 4];
-  const auto fetch = [&](int v0) {
-    const bool whole = v0 + E * kBlock <= c.V;
+  Quad<T> x[E / 4];
 #pragma unroll
-    for (int g = 0; g < E / 4; ++g) next[g] = row_quad<T>(in, v0 + 4 * t + g * 4 * kBlock, c.V, whole);
-  };
-  if (begin < end) fetch(begin);
+  for (int g = 0; g < E / 4; ++g) x[g] = row_quad<T>(in, v0 + g * 4 * kBlock, c.V, whole);
   const float base = c.lse ? __fsub_rn(total, c.lse[r]) : total;
-  WaveBest best(c.picks);
-  for (int v0 = begin; v0 < end; v0 += E * kBlock) {
-    float v[E], top = -__builtin_inff();
-    const bool whole = v0 + E * kBlock <= end;
+  const auto place = [&](int i) { return (i / 4) * 4 * kBlock + (i & 3); };
+  const auto sum = [&](int i) {
+    const float v = __fadd_rn(x[i / 4].get(i & 3), base);
+    return whole || v0 + place(i) < c.V ? v : -__builtin_inff();
+  };
+  // the largest sum, and the first place that has it
+  float top = -__builtin_inff();
+#pragma unroll
+  for (int i = 0; i < E; ++i) top = fmaxf(top, sum(i));  // (not a NaN)
+  int first = 0;
+#pragma unroll
+  for (int i = E - 1; i >= 0; --i)
+    if (sum(i) == top) first = place(i);
+  const uint64_t best = beam_key(top, (uint32_t)(v0 + first));
+  const uint64_t bound = group_bound(best, c.picks, l);
+  if (best >= bound && best) {
+    const float low = bound ? beam_value(bound) : -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      v[i] = __fadd_rn(next[i / 4].get(i & 3), base);
-      if (!whole && v0 + 4 * t + (i / 4) * 4 * kBlock + (i & 3) >= end) v[i] = -__builtin_inff();
-      top = fmaxf(top, v[i]);  // (not a NaN)
+      const float v = sum(i);
+      if (!(v >= low)) continue;
+      const uint64_t key = beam_key(v, (uint32_t)(v0 + place(i)));
+      if (key && key >= bound) l.list[atomicAdd(&l.n, 1)] = key;
     }
-    if (v0 + E * kBlock < end) fetch(v0 + E * kBlock);
-    const auto place = [&](int i) { return (uint32_t)(v0 + 4 * t + (i / 4) * 4 * kBlock + (i & 3)); };
-    if (v0 == begin) {
-      int first = 0;
-#pragma unroll
-      for (int i = E - 1; i >= 0; --i)
-        if (v[i] == top) first = i;
-      best.begin(beam_key(top, (uint32_t)(v0 + 4 * t + (first / 4) * 4 * kBlock + (first & 3))));
-    }
-    const float low = best.least > 1 ? beam_value(best.least) : -__builtin_inff();
-    if (!__ballot(top >= low)) continue;
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (__ballot(v[i] >= low)) best.take(beam_key(v[i], place(i)), v[i] >= low);
   }
-  join_waves(best, c.picks, list, out);
+  __syncthreads();
+  rank_list(l, c.picks, out);
 }
 
-// A workgroup for each group: its rows' parts.
+// A workgroup for each group: its rows' parts, 256 E keys at a time beside the picks so far.
+template <int E>
 __global__ __launch_bounds__(kBlock) void k_beam_join(BeamCall c) {
-  constexpr int E = 8;
-  __shared__ uint64_t list[kWavesPerBlock * kBeamPicks], picks[kBeamPicks];
+  __shared__ BeamLds<kBeamPicks * (E + 1)> l;
+  __shared__ uint64_t picks[kBeamPicks];
   const int t = threadIdx.x;
   const int64_t row0 = (int64_t)blockIdx.x * c.beams;
   const int64_t each = (int64_t)c.parts * c.picks, all = each * c.beams;
   const uint64_t* in = c.keys + row0 * each;
-  WaveBest best(c.picks);
+  if (t < kBeamPicks) picks[t] = 0;
+  __syncthreads();
   for (int64_t first = 0; first < all; first += E * kBlock) {
-    uint64_t key[E], top = 0;
+    uint64_t key[E + 1], best = 0;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       const int64_t at = first + i * kBlock + t;
@@ -167,14 +160,21 @@ __global__ __launch_bounds__(kBlock) void k_beam_join(BeamCall c) {
         const uint32_t b = all < (1ll << 32) ? (uint32_t)at / (uint32_t)each : (uint32_t)(at / each);
         key[i] = (key[i] & 0xffffffff00000000ull) | ~(~(uint32_t)key[i] + b * (uint32_t)c.V);
       }
-      top = key[i] > top ? key[i] : top;
+      best = key[i] > best ? key[i] : best;
     }
-    if (first == 0) best.begin(top);
+    if (!__syncthreads_or(best > picks[c.picks - 1])) continue;
+    key[E] = t < c.picks ? picks[t] : 0;
+    best = key[E] > best ? key[E] : best;
+    const uint64_t bound = group_bound(best, c.picks, l);
+    if (best >= bound && best) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) best.take(key[i], true);
+      for (int i = 0; i <= E; ++i)
+        if (key[i] && key[i] >= bound) l.list[atomicAdd(&l.n, 1)] = key[i];
+    }
+    __syncthreads();
+    rank_list(l, c.picks, picks);
+    __syncthreads();
   }
-  join_waves(best, c.picks, list, picks);
-  __syncthreads();
   if (t >= c.picks) return;
   const int64_t o = (int64_t)blockIdx.x * c.picks + t;
   const uint64_t key = picks[t];

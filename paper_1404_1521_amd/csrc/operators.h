@@ -153,7 +153,7 @@ struct BeamCall {
   uint64_t* keys;  // [rows][parts][picks]
   int64_t ld;
   int groups, beams, V, picks, end;
-  int parts, part_words;  // of a row
+  int parts;  // of a row
 };
 constexpr int kBeamPicks = 64;   // most
 constexpr int kBeamMinPart = 1024;  // words of the shortest part
