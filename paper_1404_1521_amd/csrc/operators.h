@@ -97,6 +97,7 @@ constexpr int kSelectiveTile = 16;  // POLYGLOT_SELECTIVE_MARK
 // What a range passes on: nothing (a sequence ends or starts at its end), the state of a
 // sequence that starts in it, or its own carry too.
 constexpr uint32_t kSelNone = 0, kSelClosed = 1, kSelOpen = 2;
+constexpr int kSelGroup = 16;  // ranges
 
 // A kernel's lanes to a channel (four states each), its waves and its channels.
 __host__ __device__ constexpr int sel_lanes(int N) { return N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
@@ -111,6 +112,10 @@ struct SelPlan {
   float* states;           // [ranges][D][places] what a range passes on
   float* sums;             // [ranges][D] the sum of its steps
   uint32_t* info;          // [ranges]
+  int groups;              // of kSelGroup ranges, or 0: states, sums and info of each of them
+  float* group_states;     //   lie behind those of the ranges
+  float* group_sums;
+  uint32_t* group_info;
   float* part_a;           // [ranges][D][places] dA
   float* part_s;           // [ranges][2][D] dskip and the bias's gradient
   float* part_bc;          // [blocks][tokens][groups][2][N] dB and dC

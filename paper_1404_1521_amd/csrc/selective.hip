@@ -11,7 +11,8 @@ hipError_t forward(const SelCall& c, const SelPlan& p, const Launch& L) {
   const dim3 block(SelShape<LN>::THREADS);
   const dim3 grid((uint32_t)p.ranges * p.all_blocks);
   if (p.ranges > 1) {
-    const hipError_t e = pg_launch(k_selective_ends<T, LN>, grid, block, 0, L, SelArgs{c, p});
+    hipError_t e = pg_launch(k_selective_ends<T, LN>, grid, block, 0, L, SelArgs{c, p});
+    if (e == hipSuccess) e = selective_groups<LN>(c, p, 1, L);
     if (e != hipSuccess) return e;
   }
   return pg_launch(k_selective<T, LN>, grid, block, 0, L, SelArgs{c, p});
@@ -37,10 +38,10 @@ SelRoom selective_room(int64_t tokens, int D, int N) {
   // the channels of a workgroup, which are taken at their most.
   SelRoom r;
   const int LN = sel_lanes(N), NP = 4 * LN;
-  const int64_t rc = range_channels(D, 1);
-  r.states = (size_t)rc * NP;
-  r.sums = (size_t)rc;
-  r.info = (size_t)std::max<int64_t>(kSelWorkgroups, 1);
+  const int64_t rc = range_channels(D, 1), grouped = rc + rc / kSelGroup + D;
+  r.states = (size_t)grouped * NP;
+  r.sums = (size_t)grouped;
+  r.info = 2 * (size_t)kSelWorkgroups;
   r.part_s = 2 * (size_t)rc;
   // blocks of a head's channels, where there are two or more: at most twice D / CB
   r.part_bc = (size_t)tokens * 2 * N * (2 * (size_t)D / sel_channels(LN) + 2);
@@ -48,7 +49,7 @@ SelRoom selective_room(int64_t tokens, int D, int N) {
 }
 
 hipError_t launch_selective(const SelCall& c, int dtype, SelSpace space, const Launch& L) {
-  const SelPlan p = selective_plan(c.seqs.tokens, c.D, c.N, c.groups, space);
+  const SelPlan p = selective_plan(c.seqs.tokens, c.seqs.nseq, c.D, c.N, c.groups, space);
   return by_format(dtype, [&](auto v) {
     using E = decltype(v);
     return by_lanes(c.N, [&](auto ln) { return forward<E, decltype(ln)::value>(c, p, L); });
@@ -59,7 +60,7 @@ template <class T>  // in a file for each format
 hipError_t selective_grad(const SelCall& c, const SelPlan& p, const Launch& L);
 
 hipError_t launch_selective_grad(const SelCall& c, int dtype, SelSpace space, const Launch& L) {
-  const SelPlan p = selective_plan(c.seqs.tokens, c.D, c.N, c.groups, space);
+  const SelPlan p = selective_plan(c.seqs.tokens, c.seqs.nseq, c.D, c.N, c.groups, space);
   return by_format(dtype, [&](auto v) { return selective_grad<decltype(v)>(c, p, L); });
 }
 

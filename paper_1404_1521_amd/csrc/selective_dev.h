@@ -322,57 +322,127 @@ __device__ __forceinline__ int quad_place(int e) {
   return kSelTile * S::QUADS >= S::THREADS || i < kSelTile * S::QUADS ? i * 4 : -1;
 }
 
-// The carry into a range from those before it (dir -1: the gradient's, from those after it):
-// the nearest one that does not pass its own carry on, then each one's whole decay and
-// what it adds, four of them at a time.
+// Takes `many` ranges (or groups of them) in, the last of them `at`, each by its whole decay and
+// what it adds, four of them asked for at a time.  fresh: nothing comes into the first.
 template <int LN>
-__device__ __forceinline__ void carry_into(const SelCall& c, const SelPlan& p, int range, int dir,
-                                           const SelPlace<LN>& w, const float (&A)[2][4],
-                                           float (&h)[2][4]) {
+__device__ __forceinline__ void take_in(const float* sums, const float* states, int at, int many, int dir, bool fresh,
+                                        const SelCall& c, const SelPlace<LN>& w, const float (&A)[2][4],
+                                        float (&h)[2][4]) {
   using S = SelShape<LN>;
-  int many = 0;  // ranges to take in
-  for (;;) {
-    const int j = range - dir * (many + 1 + lane_id());
-    const bool there = j >= 0 && j < p.ranges;
-    const uint64_t end = __ballot(!there || p.info[there ? j : 0] != kSelOpen);
-    if (end) {
-      many += __builtin_ctzll(end);
-      const int last = range - dir * (many + 1);
-      if (last >= 0 && last < p.ranges) ++many;
-      break;
-    }
-    many += kWave;
-  }
-#pragma unroll
-  for (int r = 0; r < S::RC; ++r)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) h[r][k] = 0.f;
   constexpr int BATCH = 4;
   const int own = w.has(0) ? w.lane_c : 0, two = w.has(1) ? 1 : 0;
-  for (int m = many; m > 0; m -= BATCH) {
+  for (int m = many - 1; m >= 0; m -= BATCH) {
     float d[BATCH][2];
     f4 s[BATCH][2];
 #pragma unroll
     for (int b = 0; b < BATCH; ++b) {
-      const int j = range - dir * max(m - b, 1);
+      const int j = at - dir * max(m - b, 0);
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        const int64_t at = (int64_t)j * c.D + w.c0 + own + r * two;
-        d[b][r] = p.sums[at];
-        s[b][r] = ld4(p.states + at * S::NP + 4 * w.nl);
+        const int64_t row = (int64_t)j * c.D + w.c0 + own + r * two;
+        d[b][r] = sums[row];
+        s[b][r] = ld4(states + row * S::NP + 4 * w.nl);
       }
     }
 #pragma unroll
     for (int b = 0; b < BATCH; ++b) {
-      if (m - b < 1) continue;
-      const bool furthest = m - b == many;  // nothing comes into it
+      if (m - b < 0) continue;
+      const bool alone = fresh && m - b == many - 1;
 #pragma unroll
       for (int r = 0; r < 2; ++r)
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          h[r][k] = furthest ? s[b][r][k] : __fmaf_rn(exp2_fast(d[b][r] * A[r][k]), h[r][k], s[b][r][k]);
+          h[r][k] = alone ? s[b][r][k] : __fmaf_rn(exp2_fast(d[b][r] * A[r][k]), h[r][k], s[b][r][k]);
     }
   }
+}
+// How many from `at` on, against dir, up to and with the first that does not pass its own
+// carry on, at most `most`; found: there is one.  By a whole wave.
+__device__ __forceinline__ int open_run(const uint32_t* info, int at, int dir, int most, bool& found) {
+  for (int many = 0; many < most; many += kWave) {
+    const int i = many + lane_id();
+    const uint64_t end = __ballot(i < most && info[at - dir * min(i, most - 1)] != kSelOpen);
+    if (end) {
+      found = true;
+      return many + __builtin_ctzll(end) + 1;
+    }
+  }
+  found = false;
+  return most;
+}
+// The carry into a range from those before it (dir -1: the gradient's, from those after it):
+// those of its group, and of the groups before that, since the last that starts afresh.
+template <int LN>
+__device__ __forceinline__ void carry_into(const SelCall& c, const SelPlan& p, int range, int dir,
+                                           const SelPlace<LN>& w, const float (&A)[2][4],
+                                           float (&h)[2][4]) {
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) h[r][k] = 0.f;
+  const int all = dir > 0 ? range : p.ranges - 1 - range;  // before it
+  bool found;
+  if (!p.groups) {
+    const int many = open_run(p.info, range - dir, dir, all, found);
+    take_in<LN>(p.sums, p.states, range - dir, many, dir, true, c, w, A, h);
+    return;
+  }
+  const int group = range / kSelGroup, place = range % kSelGroup;
+  const int near = min(all, dir > 0 ? place : kSelGroup - 1 - place);
+  const int many = open_run(p.info, range - dir, dir, near, found);
+  if (!found) {
+    bool any;
+    const int far = open_run(p.group_info, group - dir, dir, dir > 0 ? group : p.groups - 1 - group, any);
+    take_in<LN>(p.group_sums, p.group_states, group - dir, far, dir, true, c, w, A, h);
+  }
+  take_in<LN>(p.sums, p.states, range - dir, many, dir, found, c, w, A, h);
+}
+
+// What groups of ranges pass on together: a thread for four states of a channel and a group.
+template <int LN>
+__global__ __launch_bounds__(kBlock) void k_selective_groups(SelCall c, SelPlan p, int dir) {
+  constexpr int NP = SelShape<LN>::NP;
+  const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x, each = (int64_t)c.D * LN;
+  const int g = (int)(i / each);
+  if (g >= p.groups) return;
+  const int ch = (int)(i % each / LN), n0 = (int)(i % LN) * 4;
+  float A[4], h[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) A[k] = n0 + k < c.N ? c.A[(int64_t)ch * c.N + n0 + k] * kLog2e : 0.f;
+  const int from = g * kSelGroup, many = min(kSelGroup, p.ranges - from);
+  float d[kSelGroup];
+  f4 s[kSelGroup];
+  uint32_t kind[kSelGroup];
+#pragma unroll
+  for (int m = 0; m < kSelGroup; ++m) {
+    const int j = from + (dir > 0 ? min(m, many - 1) : max(many - 1 - m, 0));
+    const int64_t row = (int64_t)j * c.D + ch;
+    kind[m] = p.info[j];
+    d[m] = p.sums[row];
+    s[m] = ld4(p.states + row * NP + n0);
+  }
+  uint32_t all = kSelOpen;
+#pragma unroll
+  for (int m = 0; m < kSelGroup; ++m) {
+    if (m >= many) continue;
+    if (kind[m] != kSelOpen) all = kSelClosed, sum = 0.f;
+    if (kind[m] != kSelNone) sum += d[m];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      h[k] = kind[m] == kSelNone ? 0.f
+             : kind[m] == kSelOpen ? __fmaf_rn(exp2_fast(d[m] * A[k]), h[k], s[m][k]) : s[m][k];
+  }
+  const int64_t row = (int64_t)g * c.D + ch;
+  st4(p.group_states + row * NP + n0, f4{h[0], h[1], h[2], h[3]});
+  if (n0 == 0) p.group_sums[row] = sum;
+  if (n0 == 0 && ch == 0) p.group_info[g] = all;
+}
+template <int LN>
+hipError_t selective_groups(const SelCall& c, const SelPlan& p, int dir, const Launch& L) {
+  if (!p.groups || p.ranges <= 1) return hipSuccess;
+  const int64_t threads = (int64_t)p.groups * c.D * LN;
+  return pg_launch(k_selective_groups<LN>, dim3((uint32_t)((threads + kBlock - 1) / kBlock)), dim3(kBlock), 0, L, c, p,
+                   dir);
 }
 
 // A workgroup's tile in LDS.
@@ -550,7 +620,20 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 4) void k_selective(SelArgs)
   load_four(first.c.skip, w.q0, w.qn, skip);
   const bool skips = first.c.skip != nullptr;
   UpCursor cursor{};
-  if (t < kWave) cursor.read(first.c.seqs, first_place(first.c.seqs, lo));
+  {
+    const SelArgs& a = again(args);
+    const int next = first_place(a.c.seqs, lo);
+    if (t < kWave) cursor.read(a.c.seqs, next);
+    // unless a sequence starts here
+    if (lo > 0 && !(next <= a.c.seqs.nseq && place_of(a.c.seqs, next) == lo)) {
+      carry_into<LN>(a.c, a.p, range, 1, w, A, h);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h[r][j] = 0.f;
+    }
+  }
 
   for (int t0 = lo; t0 < hi; t0 += kSelTile) {
     const int count = min(kSelTile, hi - t0);
@@ -576,16 +659,6 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 4) void k_selective(SelArgs)
     const SelArgs& a = again(args);
     if (gated) zv.load(a.c.z, a.c.ld_z, zs, t0, count, whole, w);
     if (t0 + kSelTile < hi) fetch(t0 + kSelTile);
-    if (t0 == lo) {
-      if (!(starts & 1) && lo > 0) {
-        carry_into<LN>(a.c, a.p, range, 1, w, A, h);
-      } else {
-#pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) h[r][j] = 0.f;
-      }
-    }
     if (a.c.marks) {
 #pragma unroll
       for (int r = 0; r < 2; ++r) {

@@ -177,10 +177,16 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 2) void k_selective_grad(Sel
 #pragma unroll
     for (int j = 0; j < 4; ++j) dA[r][j] = mu[r][j] = 0.f;
   float dskip[4] = {0.f, 0.f, 0.f, 0.f}, dbias[4] = {0.f, 0.f, 0.f, 0.f};
-  const bool last_range = hi >= first.c.seqs.tokens;
   const int tiles = lo < hi ? ceil_div(hi - lo, kSelTile) : 0;
   DownCursor cursor{};
-  if (t < kWave) cursor.read(first.c.seqs, first_place(first.c.seqs, hi + 1));
+  if (tiles > 0) {
+    const SelArgs& a = again(args);
+    const int next = first_place(a.c.seqs, hi);
+    if (t < kWave) cursor.read(a.c.seqs, first_place(a.c.seqs, hi + 1));
+    // unless a sequence ends here
+    if (hi < a.c.seqs.tokens && !(next <= a.c.seqs.nseq && place_of(a.c.seqs, next) == hi))
+      carry_into<LN>(a.c, a.p, range, -1, w, A, mu);
+  }
 
   for (int tile = tiles - 1; tile >= 0; --tile) {
     const int t0 = lo + tile * kSelTile, count = min(kSelTile, hi - t0);
@@ -199,8 +205,6 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 2) void k_selective_grad(Sel
     float first_h[2][4], h[2][4];
     {
       const SelArgs& a = again(args);
-      if (tile == tiles - 1 && !(stops >> (count - 1) & 1) && !last_range)
-        carry_into<LN>(a.c, a.p, range, -1, w, A, mu);
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         f4 m = kZero4;

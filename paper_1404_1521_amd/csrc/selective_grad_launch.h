@@ -10,6 +10,7 @@ hipError_t grad_of_lanes(const SelCall& c, const SelPlan& p, const Launch& L) {
   const dim3 grid((uint32_t)p.ranges * p.all_blocks), block(SelShape<LN>::THREADS);
   hipError_t e = hipSuccess;
   if (p.ranges > 1) e = pg_launch(k_selective_grad_ends<T, LN>, grid, block, 0, L, SelArgs{c, p});
+  if (e == hipSuccess) e = selective_groups<LN>(c, p, -1, L);
   if (e == hipSuccess) e = pg_launch(k_selective_grad<T, LN>, grid, block, 0, L, SelArgs{c, p});
   if (e != hipSuccess) return e;
   const int params = (int)(((int64_t)c.D * (c.N + 2) + kSumOutputs - 1) / kSumOutputs);

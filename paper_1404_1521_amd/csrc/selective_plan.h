@@ -18,9 +18,10 @@ hipError_t by_lanes(int N, F f) {
 }
 
 constexpr int kSelWorkgroups = 4 * kCus;  // that the ranges are to give
+constexpr int kSelFewRanges = 4 * kSelGroup;  // of a sequence
 
 // How a call is cut, in the workspace.
-inline SelPlan selective_plan(int64_t tokens, int D, int N, int groups, const SelSpace& space) {
+inline SelPlan selective_plan(int64_t tokens, int nseq, int D, int N, int groups, const SelSpace& space) {
   SelPlan p{};
   const int CB = sel_channels(sel_lanes(N));
   p.blocks = ceil_div(D / groups, CB);
@@ -31,6 +32,14 @@ inline SelPlan selective_plan(int64_t tokens, int D, int N, int groups, const Se
   p.range = (int)(each * kSelectiveTile);
   p.ranges = (int)((tiles + each - 1) / each);
   p.NM = (N + 3) / 4 * 4;
+  // A range takes those before it in its sequence in one after the other, 0.2 us each; where
+  // they are many, groups of them are put together first, a launch of 5 us: one sequence of
+  // 16,384 x 64 forward 295 -> 75 us, but 700 sequences of 16,384 x 256 46 -> 56.
+  p.groups = p.ranges > kSelFewRanges * (int64_t)nseq ? (p.ranges + kSelGroup - 1) / kSelGroup : 0;
+  const int64_t rows = (int64_t)p.ranges * D, NP = 4 * sel_lanes(N);
+  p.group_states = space.states + rows * NP;
+  p.group_sums = space.sums + rows;
+  p.group_info = space.info + p.ranges;
   p.states = space.states;
   p.sums = space.sums;
   p.info = space.info;
