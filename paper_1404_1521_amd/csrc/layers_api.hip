@@ -36,7 +36,7 @@ bool all_aligned(std::initializer_list<const void*> all, size_t to) {
 // What the packed calls share.
 template <class A>
 int check_packed(polyglot_ctx* ctx, const A& a, const std::string& what) {
-  if (a.tokens < 0 || a.tokens > kMaxTokens || a.nseq < 1)
+  if (a.tokens < 0 || a.tokens > kMaxTokens || a.nseq < 1 || a.nseq > kMaxTokens)
     return fail(ctx, POLYGLOT_EBATCH, what + ": bad token or sequence count");
   if (a.D < 1 || a.D > kMaxChannels || !format_ok(a.dtype))
     return fail(ctx, POLYGLOT_EINVAL, what + ": bad width or storage format");

@@ -686,7 +686,7 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 4) void k_selective(SelArgs)
       if (w.nl == 0) *reinterpret_cast<float2*>(sy + k * S::CB + w.lane_c) = float2{out[0], out[1]};
     };
     if ((starts | stops) == 0) {  // (tokens past the range have no step and add nothing)
-#pragma unroll 2
+#pragma unroll 4
       for (int k = 0; k < kSelTile; ++k) token(k);
     } else {
       for (int k = 0; k < count; ++k) {

@@ -387,12 +387,11 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 2) void k_selective_grad(Sel
       for (int j = 0; j < 4; ++j) out[j] = st[j] * e[j];
       if (skips) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          out[j] = __fmaf_rn(skip[j], gv[j], out[j]);
-          dskip[j] = __fmaf_rn(gv[j], xv.q[el].get(j), dskip[j]);
-        }
+        for (int j = 0; j < 4; ++j) out[j] = __fmaf_rn(skip[j], gv[j], out[j]);
       }
       put(c.dx, c.ld_dx, out);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) dskip[j] = __fmaf_rn(gv[j], xv.q[el].get(j), dskip[j]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) out[j] = __fmaf_rn(xv.q[el].get(j), e[j], kLn2 * ds[j]);
       if (soft) {
