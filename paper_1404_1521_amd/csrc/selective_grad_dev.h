@@ -177,6 +177,7 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 2) void k_selective_grad(Sel
 #pragma unroll
     for (int j = 0; j < 4; ++j) dA[r][j] = mu[r][j] = 0.f;
   float dskip[4] = {0.f, 0.f, 0.f, 0.f}, dbias[4] = {0.f, 0.f, 0.f, 0.f};
+  const bool gated = first.c.z != nullptr;
   const int tiles = lo < hi ? ceil_div(hi - lo, kSelTile) : 0;
   DownCursor cursor{};
   if (tiles > 0) {
@@ -299,14 +300,13 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 2) void k_selective_grad(Sel
           float e[2], ds[2], v[2];
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            e[r] = ds[r] = v[r] = 0.f;
+            e[r] = ds[r] = 0.f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const float lam = __fmaf_rn(vv[r], C[j], mu[r][j]);
               both[j] = __fmaf_rn(lam, uu[r], both[j]);
               both[4 + j] = __fmaf_rn(vv[r], hs[i][r][j], both[4 + j]);
               e[r] = __fmaf_rn(lam, B[j], e[r]);
-              v[r] = __fmaf_rn(C[j], hs[i][r][j], v[r]);
               mu[r][j] = lam * exp2_fast(dd[r] * A[r][j]);
               const float q = mu[r][j] * hp[r][j];
               ds[r] = __fmaf_rn(q, A[r][j], ds[r]);
@@ -315,12 +315,21 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 2) void k_selective_grad(Sel
             }
             e[r] = sum_states<LN>(e[r]);
             ds[r] = sum_states<LN>(ds[r]);
-            v[r] = sum_states<LN>(v[r]);
+          }
+          if (gated) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              v[r] = 0.f;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) v[r] = __fmaf_rn(C[j], hs[i][r][j], v[r]);
+              v[r] = sum_states<LN>(v[r]);
+            }
+            if (w.nl == 0)
+              *reinterpret_cast<float2*>(g.dv + k * S::CB + w.lane_c) = float2{v[0], v[1]};
           }
           if (w.nl == 0) {
             *reinterpret_cast<float2*>(s.dx + k * S::CB + w.lane_c) = float2{e[0], e[1]};
             *reinterpret_cast<float2*>(g.dstep + k * S::CB + w.lane_c) = float2{ds[0], ds[1]};
-            *reinterpret_cast<float2*>(g.dv + k * S::CB + w.lane_c) = float2{v[0], v[1]};
           }
           float pair[2];
           sum_channels<LN>(both, pair);
@@ -348,7 +357,7 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 2) void k_selective_grad(Sel
 
     const SelArgs& a = again(args);
     const SelCall& c = a.c;
-    const bool whole = whole_tile<S>(w, count), gated = c.z != nullptr, skips = c.skip != nullptr;
+    const bool whole = whole_tile<S>(w, count), skips = c.skip != nullptr;
     const bool soft = c.softplus;
     const T* none = nullptr;
     QuadTile<T, S> raw, gy, xv, zv;
