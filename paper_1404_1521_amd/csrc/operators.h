@@ -78,6 +78,18 @@ struct Packed {
   int offset_bytes, tokens, nseq;
 };
 
+// Pieces dealt out to parts in their order, to the first `more` of them each + 1, to the others `each`.
+struct Shares {
+  int each, more;
+  Shares() = default;
+  Shares(int64_t pieces, int64_t parts) : each((int)(pieces / parts)), more((int)(pieces % parts)) {}
+  // The first piece of a part, a piece being `size` tokens; `tokens` where there is none.
+  __host__ __device__ int first(int64_t part, int size, int tokens) const {
+    const int64_t at = (part * each + (part < more ? part : more)) * size;
+    return (int)(at < tokens ? at : tokens);
+  }
+};
+
 // The selective scan and its gradient (the gradient's in the second half).
 struct SelCall {
   const void *x, *delta, *B, *C, *z;
@@ -106,7 +118,8 @@ __host__ __device__ constexpr int sel_channels(int lanes) { return sel_waves(lan
 
 // How a selective scan is cut: a workgroup for each range of tokens and block of channels.
 struct SelPlan {
-  int range, ranges;       // tokens of a range
+  Shares share;            // tiles of a range
+  int ranges;
   int blocks, all_blocks;  // of a head's channels, of all
   int NM;                  // places of a mark's row
   float* states;           // [ranges][D][places] what a range passes on

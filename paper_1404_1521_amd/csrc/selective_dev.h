@@ -512,7 +512,8 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS) void k_selective_ends(SelArg
   const int t = threadIdx.x;
   const int range = blockIdx.x / first.p.all_blocks, block = blockIdx.x % first.p.all_blocks;
   const SelPlace<LN> w(first.c, first.p, block);
-  const int lo = range * first.p.range, hi = min(lo + first.p.range, first.c.seqs.tokens);
+  const int lo = first.p.share.first(range, kSelTile, first.c.seqs.tokens);
+  const int hi = first.p.share.first(range + 1, kSelTile, first.c.seqs.tokens);
   const RangeEnd end = range_end(first.c.seqs, lo, hi);
   const int from = end.at, seq = end.seq;
   if (t == 0 && block == 0) first.p.info[range] = end.kind;
@@ -587,7 +588,8 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 4) void k_selective(SelArgs)
   const int t = threadIdx.x;
   const int range = blockIdx.x / first.p.all_blocks, block = blockIdx.x % first.p.all_blocks;
   const SelPlace<LN> w(first.c, first.p, block);
-  const int lo = range * first.p.range, hi = min(lo + first.p.range, first.c.seqs.tokens);
+  const int lo = first.p.share.first(range, kSelTile, first.c.seqs.tokens);
+  const int hi = first.p.share.first(range + 1, kSelTile, first.c.seqs.tokens);
 
   check_places(first.c.seqs, range, first.p.ranges, S::THREADS, first.c.last != nullptr, list, [&](int i) {
     const SelCall& c = again(args).c;

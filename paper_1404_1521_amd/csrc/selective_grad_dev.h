@@ -96,7 +96,8 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS) void k_selective_grad_ends(S
   const int t = threadIdx.x;
   const int range = blockIdx.x / first.p.all_blocks, block = blockIdx.x % first.p.all_blocks;
   const SelPlace<LN> w(first.c, first.p, block);
-  const int lo = range * first.p.range, hi = min(lo + first.p.range, first.c.seqs.tokens);
+  const int lo = first.p.share.first(range, kSelTile, first.c.seqs.tokens);
+  const int hi = first.p.share.first(range + 1, kSelTile, first.c.seqs.tokens);
   const RangeEnd end = range_start(first.c.seqs, lo, hi);
   const int to = end.at, seq = end.seq;
   if (t == 0 && block == 0) first.p.info[range] = end.kind;
@@ -159,7 +160,8 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 2) void k_selective_grad(Sel
   const int t = threadIdx.x, lane = t & (kWave - 1), wave = t / kWave;
   const int range = blockIdx.x / first.p.all_blocks, block = blockIdx.x % first.p.all_blocks;
   const SelPlace<LN> w(first.c, first.p, block);
-  const int lo = range * first.p.range, hi = min(lo + first.p.range, first.c.seqs.tokens);
+  const int lo = first.p.share.first(range, kSelTile, first.c.seqs.tokens);
+  const int hi = first.p.share.first(range + 1, kSelTile, first.c.seqs.tokens);
 
   check_places(first.c.seqs, range, first.p.ranges, S::THREADS, first.c.dh0 != nullptr, g.list, [&](int i) {
     const SelCall& c = again(args).c;

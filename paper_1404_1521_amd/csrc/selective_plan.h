@@ -18,7 +18,7 @@ hipError_t by_lanes(int N, F f) {
 }
 
 constexpr int kSelWorkgroups = 4 * kCus;  // that the ranges are to give
-constexpr int kSelFewRanges = 4 * kSelGroup;  // of a sequence
+constexpr int kSelFewRanges = 2 * kSelGroup;  // of a sequence
 
 // How a call is cut, in the workspace.
 inline SelPlan selective_plan(int64_t tokens, int nseq, int D, int N, int groups, const SelSpace& space) {
@@ -27,14 +27,13 @@ inline SelPlan selective_plan(int64_t tokens, int nseq, int D, int N, int groups
   p.blocks = ceil_div(D / groups, CB);
   p.all_blocks = p.blocks * groups;
   const int64_t tiles = std::max<int64_t>(1, (tokens + kSelectiveTile - 1) / kSelectiveTile);
-  const int64_t want = std::min<int64_t>(tiles, std::max(1, kSelWorkgroups / p.all_blocks));
-  const int64_t each = (tiles + want - 1) / want;
-  p.range = (int)(each * kSelectiveTile);
-  p.ranges = (int)((tiles + each - 1) / each);
+  p.ranges = (int)std::min<int64_t>(tiles, std::max(1, kSelWorkgroups / p.all_blocks));
+  p.share = Shares(tiles, p.ranges);
   p.NM = (N + 3) / 4 * 4;
   // A range takes those before it in its sequence in one after the other, 0.2 us each; where
   // they are many, groups of them are put together first, a launch of 5 us: one sequence of
-  // 16,384 x 64 forward 295 -> 75 us, but 700 sequences of 16,384 x 256 46 -> 56.
+  // 16,384 x 64 forward 295 -> 75 us and four of 4,096 x 256 (64 ranges each) 49 -> 39, but one
+  // of 16,384 x 2,048 (64 ranges) 289 -> 294 and 700 of 16,384 x 256 46 -> 56.
   p.groups = p.ranges > kSelFewRanges * (int64_t)nseq ? (p.ranges + kSelGroup - 1) / kSelGroup : 0;
   const int64_t rows = (int64_t)p.ranges * D, NP = 4 * sel_lanes(N);
   p.group_states = space.states + rows * NP;
