@@ -534,9 +534,10 @@ int polyglot_convolution_grad(polyglot_ctx* ctx, const polyglot_convolution_grad
  * Rows lie less than 2^25 elements apart.
  *
  * With one token per sequence (tokens == nseq, no offsets) and no marks this is a model's
- * step for single tokens, which needs no workspace and whose last may be h0.  Otherwise no output may be an input, and the call uses the workspace of
- * polyglot_reserve_selective.  Offsets that do not ascend from 0 to `tokens` raise
- * POLYGLOT_EOFFSETS; the outputs are then unspecified, and no access leaves the tensors. */
+ * step for single tokens, which needs no workspace and whose last may be h0.  Otherwise no
+ * output may be an input, and the call uses the workspace of polyglot_reserve_selective.
+ * Offsets that do not ascend from 0 to `tokens` raise POLYGLOT_EOFFSETS; the outputs are then
+ * unspecified, and no access leaves the tensors. */
 #define POLYGLOT_SELECTIVE_MARK 16
 typedef struct {
   const void* x;           /* [tokens][D] */
@@ -609,8 +610,8 @@ int polyglot_selective_grad(polyglot_ctx* ctx, const polyglot_selective_grad_arg
 
 /* Sizes the workspace of the selective scan, its gradient and the convolution's gradient for
  * calls of up to max_tokens tokens, max_D channels and max_states states; otherwise as
- * polyglot_reserve_recurrence.  Up to 16 states take about 2 bytes for each token and channel
- * and 128 for each token, up to 32 four times and up to 64 sixteen times as much, and 40 MB. */
+ * polyglot_reserve_recurrence.  Beside 26 to 155 MB, up to 16 states take about 2 bytes for each
+ * token and channel and 256 for each token, up to 32 four and up to 64 sixteen times as much. */
 int polyglot_reserve_selective(polyglot_ctx* ctx, int64_t max_tokens, int32_t max_D,
                                int32_t max_states);
 

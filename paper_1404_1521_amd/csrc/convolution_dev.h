@@ -9,6 +9,11 @@
 // where that ends, it keeps; no two waves wait for each other.  The gradient walks forward as
 // well: a token's g = dy act'(u) goes into K sums, for itself and the K - 1 inputs before it;
 // the oldest of them is complete and leaves.
+//
+// What bounds it is memory: 65,536 x 2,048 bfloat16 in 16 sequences, K 4, take 122 us forward
+// (537 MB, 4.4 TB/s; a copy of 1 GiB reaches 5.2) and 198 in the gradient (805 MB, 4.1).  Tiles
+// in LDS with barriers for the sequences' marks took 156; eight channels to a lane read 16
+// bytes at a time.
 #pragma once
 #include <type_traits>
 
@@ -254,7 +259,8 @@ __global__ __launch_bounds__(kBlock) void k_convolution(ConvCall c) {
   }
 }
 
-// One token for each sequence; a thread reads all that it needs before it writes.
+// One token for each sequence; a thread reads all that it needs before it writes.  64 x 512
+// takes 3.4 us, a launch and one round trip of loads.
 template <class T, int K, int V>
 __global__ __launch_bounds__(kBlock) void k_convolution_step(ConvCall c) {
   const int strips = ceil_div(c.D, V);
@@ -286,6 +292,9 @@ __global__ __launch_bounds__(kBlock) void k_convolution_step(ConvCall c) {
   }
 }
 
+// Four tokens ahead, not eight: x and dy of each, with the sums of K taps, are 130 to 175
+// registers.  16,411 x 255 float32 in 700 sequences, K 3: 19 us and 4 for the sums, where the
+// bytes are 10; two steps of four tokens to a row, then the join of the workgroup's sums.
 template <class T, int K, int V>
 __global__ __launch_bounds__(kBlock, conv_grad_waves(sizeof(T))) void k_convolution_grad(ConvCall c) {
   constexpr int R = kConvStep / 2;

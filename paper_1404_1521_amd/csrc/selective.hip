@@ -28,7 +28,7 @@ hipError_t step(const SelCall& c, const Launch& L) {
 // Channels times ranges of any call of up to D channels: one range, or as many as give
 // the workgroups of up to CB channels.
 int64_t range_channels(int D, int N) {
-  return std::max<int64_t>(D, (int64_t)kSelWorkgroups * sel_channels(sel_lanes(N)));
+  return std::max<int64_t>(D, (int64_t)kSelMostWorkgroups * sel_channels(sel_lanes(N)));
 }
 
 }  // namespace
@@ -41,7 +41,7 @@ SelRoom selective_room(int64_t tokens, int D, int N) {
   const int64_t rc = range_channels(D, 1), grouped = rc + rc / kSelGroup + D;
   r.states = (size_t)grouped * NP;
   r.sums = (size_t)grouped;
-  r.info = 2 * (size_t)kSelWorkgroups;
+  r.info = 2 * (size_t)kSelMostWorkgroups;
   r.part_s = 2 * (size_t)rc;
   // blocks of a head's channels, where there are two or more: at most twice D / CB
   r.part_bc = (size_t)tokens * 2 * N * (2 * (size_t)D / sel_channels(LN) + 2);

@@ -17,8 +17,15 @@ hipError_t by_lanes(int N, F f) {
   }
 }
 
-constexpr int kSelWorkgroups = 4 * kCus;  // that the ranges are to give
-constexpr int kSelFewRanges = 2 * kSelGroup;  // of a sequence
+// Workgroups that the ranges are to give: as many as run at once (half as many: 32,768 x 2,048
+// bfloat16 683 us for 553 and back 1,472 for 1,380, 16,384 x 256 of 8 states 70 for 46), and
+// up to twice as many where a range keeps kSelLongRange tiles: the chip is busy more evenly,
+// 32,768 x 2,048 553 -> 535 and back 1,380 -> 1,350, 16,384 x 1,024 of 64 states 470 -> 441,
+// but with four tiles to a range 16,384 x 1,024 of 4 states 123 -> 131 and 4,097 x 2,048
+// 98 -> 103.  Four times as many: 547 and 1,371.
+constexpr int kSelWorkgroups = 4 * kCus, kSelMostWorkgroups = 2 * kSelWorkgroups;
+constexpr int kSelLongRange = 8;
+constexpr int kSelFewRanges = 4 * kSelGroup;  // of a sequence
 
 // How a call is cut, in the workspace.
 inline SelPlan selective_plan(int64_t tokens, int nseq, int D, int N, int groups, const SelSpace& space) {
@@ -27,14 +34,17 @@ inline SelPlan selective_plan(int64_t tokens, int nseq, int D, int N, int groups
   p.blocks = ceil_div(D / groups, CB);
   p.all_blocks = p.blocks * groups;
   const int64_t tiles = std::max<int64_t>(1, (tokens + kSelectiveTile - 1) / kSelectiveTile);
-  p.ranges = (int)std::min<int64_t>(tiles, std::max(1, kSelWorkgroups / p.all_blocks));
+  const int few = std::max(1, kSelWorkgroups / p.all_blocks), most = std::max(1, kSelMostWorkgroups / p.all_blocks);
+  p.ranges = (int)std::clamp<int64_t>(tiles / kSelLongRange, std::min<int64_t>(tiles, few), most);
   p.share = Shares(tiles, p.ranges);
   p.NM = (N + 3) / 4 * 4;
   // A range takes those before it in its sequence in one after the other, 0.2 us each; where
-  // they are many, groups of them are put together first, a launch of 5 us: one sequence of
-  // 16,384 x 64 forward 295 -> 75 us and four of 4,096 x 256 (64 ranges each) 49 -> 39, but one
-  // of 16,384 x 2,048 (64 ranges) 289 -> 294 and 700 of 16,384 x 256 46 -> 56.
-  p.groups = p.ranges > kSelFewRanges * (int64_t)nseq ? (p.ranges + kSelGroup - 1) / kSelGroup : 0;
+  // a sequence has many (the longest of several taken to be twice the mean), groups of them
+  // are put together first, a launch of 5 to 10 us: one sequence of 16,384 x 64 forward 295 ->
+  // 75 us and four of 4,096 x 256 (256 ranges) 49 -> 39, but 700 of 16,384 x 256 46 -> 56 and
+  // one of 16,384 x 2,048 (64 ranges) 289 -> 294.
+  const int64_t longest = nseq > 1 ? 2 * (int64_t)p.ranges / nseq : p.ranges;
+  p.groups = longest > kSelFewRanges ? (p.ranges + kSelGroup - 1) / kSelGroup : 0;
   const int64_t rows = (int64_t)p.ranges * D, NP = 4 * sel_lanes(N);
   p.group_states = space.states + rows * NP;
   p.group_sums = space.sums + rows;
