@@ -297,6 +297,18 @@ def test_selective_over_many_ranges(ctx, tokens, D, N, nseq):
         assert torch.equal(a[k], b[k]), k
 
 
+@pytest.mark.parametrize("tokens,D,N,groups,nseq", [(5003, 64, 4, 64, 3), (4100, 100, 9, 50, 30), (3001, 120, 40, 120, 1)])
+def test_selective_of_long_ranges(ctx, tokens, D, N, groups, nseq):
+    """Many heads: few ranges of many tiles, not all of one length, more of them than run at once."""
+    gen = torch.Generator().manual_seed(tokens)
+    s = scan_inputs(gen, tokens, D, N, groups, nseq, "f32")
+    s["A"] = -torch.exp(normal(gen, D, N) - 1)
+    off = cuts(np.random.default_rng(tokens), tokens, nseq, empties=False)
+    o = torch.from_numpy(off).cuda()
+    want, err = scan_reference(s, off, True, tokens)
+    check_scan(scan_call(ctx, s, o, True), want, err, "f32", "long ranges")
+
+
 def test_selective_of_no_tokens(ctx):
     gen = torch.Generator().manual_seed(5)
     h0, D, N = normal(gen, 3, 20, 16).cuda(), 20, 16
