@@ -871,16 +871,16 @@ class Context:
             if t.is_contiguous():
                 width = ld_t = t.nbytes // have
             else:
-                width, ld_t = t[0].nbytes, t.stride(0) * t.element_size()
+                width = t[0].nbytes
+                ld_t = t.stride(0) * t.element_size() if have > 1 else width
                 if not t[0].is_contiguous():
                     raise ValueError("rows must be contiguous")
             ld_o = width
             if not o.is_contiguous():
                 if rows and not o[0].is_contiguous():
                     raise ValueError("rows must be contiguous")
-                ld_o = o.stride(0) * o.element_size()
-            items.append(RowCopy.pack(t.data_ptr(), o.data_ptr(), width, max(ld_t, width),
-                                      max(ld_o, width), have, 0))
+                ld_o = o.stride(0) * o.element_size() if rows > 1 else width
+            items.append(RowCopy.pack(t.data_ptr(), o.data_ptr(), width, ld_t, ld_o, have, 0))
         rc = self._lib.polyglot_reorder(self._h, b"".join(items), len(items), pid, rows)
         if rc != OK:
             self._check(rc, "reorder")

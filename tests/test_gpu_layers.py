@@ -446,6 +446,20 @@ def test_reorder(ctx, rows, in_rows):
     assert torch.equal(o._base, guard)
 
 
+def test_reorder_of_rows_over_each_other(pg, ctx):
+    """Rows closer than their length (a broadcast one, a window) are refused, read or written."""
+    ids = torch.tensor([3, 0], dtype=torch.int32).cuda()
+    one = torch.arange(8.0).cuda().view(1, 8)
+    window = torch.arange(16.0).cuda().as_strided((4, 8), (2, 1))
+    for t in (one.expand(4, 8), window):
+        with pytest.raises(pg.PolyglotError):
+            ctx.reorder([t], ids)
+        with pytest.raises(pg.PolyglotError):
+            ctx.reorder([torch.ones(4, 8, device="cuda")], ids, [t[:2]])
+    assert torch.equal(one.cpu(), torch.arange(8.0).view(1, 8))
+    assert torch.equal(ctx.reorder([one.expand(2, 8)[:1]], ids[1:])[0], one)
+
+
 def test_reorder_of_rows_that_are_not_there(pg, ctx):
     t = torch.arange(12.0, device="cuda").view(4, 3)
     out = torch.full((3, 3), -1.0, device="cuda")
