@@ -10,8 +10,8 @@
 // well: a token's g = dy act'(u) goes into K sums, for itself and the K - 1 inputs before it;
 // the oldest of them is complete and leaves.
 //
-// What bounds it is memory: 65,536 x 2,048 bfloat16 in 16 sequences, K 4, take 122 us forward
-// (537 MB, 4.4 TB/s; a copy of 1 GiB reaches 5.2) and 198 in the gradient (805 MB, 4.1).  Tiles
+// What bounds it is memory: 65,536 x 2,048 bfloat16 in 16 sequences, K 4, take 120 us forward
+// (537 MB, 4.5 TB/s; a copy of 1 GiB reaches 5.2) and 198 in the gradient (805 MB, 4.1).  Tiles
 // in LDS with barriers for the sequences' marks took 156; eight channels to a lane read 16
 // bytes at a time.
 #pragma once

@@ -16,8 +16,8 @@
 //
 // What bounds it are vector instructions: an operation takes a wave 4 cycles, the exponential
 // 8, a state and token 20 in the first launch and 24 in the second.  At 32,768 x 2,048
-// bfloat16 with 16 states and a gate that is 137 and 164 us of the 220 and 345 measured; the
-// bytes are 104.  The rest is what a token and channel take by themselves: softplus, the
+// bfloat16 with 16 states and a gate that is 137 and 164 us of the 208 and 325 measured; the
+// bytes are 103.  The rest is what a token and channel take by themselves: softplus, the
 // gate's sigmoid, conversions, LDS, the sum over lanes.  Every state has a decay of its own, so
 // that nothing here is a matrix product.
 #pragma once
@@ -513,7 +513,7 @@ __device__ __forceinline__ RangeEnd range_start(const Packed& s, int lo, int hi)
 // The next tile is on its way while one is worked on.  A range costs here what it costs
 // again below, without C, z and y: splitting time is what fills the chip (8 sequences of 2,048
 // channels alone are 128 workgroups), and correcting outputs behind a single pass would take
-// the same exponential and products of every state.  4,097 x 2,048, one sequence: 36 us.
+// the same exponential and products of every state.  4,097 x 2,048, one sequence: 34 us.
 template <class T, int LN>
 __global__ __launch_bounds__(SelShape<LN>::THREADS) void k_selective_ends(SelArgs) {
   using S = SelShape<LN>;
@@ -588,9 +588,9 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS) void k_selective_ends(SelArg
   pass_on(last.c, last.p, range, w, h, sum);
 }
 
-// Four waves to a SIMD (128 registers).  Five left the tile's loads no room and spilled: 584 us
-// for 555 of both launches at 32,768 x 2,048.  Tiles where no sequence starts or stops take a
-// loop without a branch, four tokens unrolled (561 us with two).
+// Four waves to a SIMD (128 registers).  Five left the tile's loads no room and spilled: both
+// launches 5% longer at 32,768 x 2,048.  Tiles where no sequence starts or stops take a loop
+// without a branch, four tokens unrolled (1% longer with two).  4,097 x 2,048: 63 us.
 template <class T, int LN>
 __global__ __launch_bounds__(SelShape<LN>::THREADS, 4) void k_selective(SelArgs) {
   using S = SelShape<LN>;

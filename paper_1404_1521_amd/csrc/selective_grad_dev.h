@@ -14,8 +14,8 @@
 // What bounds it are vector instructions, as in the forward pass: a state and token take 48
 // cycles on the way back, 20 for the states again and 10 for those of a first half that are
 // needed to reach the second, and about 15 for the sums over lanes.  At 32,768 x 2,048
-// bfloat16 with 16 states and a gate: 268 us for what comes back, 1,095 for the tiles, whose
-// vector pipes are busy 83% of the time, and 19 for the sums; its bytes are 234.  Halves of
+// bfloat16 with 16 states and a gate: 252 us for what comes back, 1,082 for the tiles, whose
+// vector pipes are busy 83% of the time, and 21 for the sums; its bytes are 234.  Halves of
 // eight tokens, because the states of eight are 64 registers and those of 16, 128, beside what
 // the way back needs.
 #pragma once
@@ -158,8 +158,8 @@ struct alignas(16) SelGradLds {
 };
 
 // Two waves to a SIMD: 250 registers hold the half tile's states, decays computed twice.  Loads
-// of the next tile kept through a tile do not fit beside them (1,461 us for 1,382 of all three
-// launches, with registers spilled).
+// of the next tile kept through a tile do not fit beside them (all three launches 6% longer,
+// with registers spilled).
 template <class T, int LN>
 __global__ __launch_bounds__(SelShape<LN>::THREADS, 2) void k_selective_grad(SelArgs) {
   using S = SelShape<LN>;
