@@ -43,8 +43,7 @@ __device__ __forceinline__ float exp_neg(float x) {
 // log(1 + e^v) = max(v, 0) + log(1 + e), e = e^-|v|, and log(1 + e) = 2 atanh(e / (2 + e));
 // the argument is at most 1/3, and the Maclaurin series' first term left out, s^17 / 17, is
 // below 2^-29 of s.
-__device__ __forceinline__ float softplus(float v) {
-  const float e = exp_neg(v);
+__device__ __forceinline__ float softplus(float v, float e) {
   const float s = e * __builtin_amdgcn_rcpf(2.f + e), q = s * s;
   float p = 2.f / 15.f;
   p = __fmaf_rn(p, q, 2.f / 13.f);
@@ -56,11 +55,12 @@ __device__ __forceinline__ float softplus(float v) {
   const float l = __fmaf_rn(s * q, p, s + s);
   return __fmaf_rn(v + __builtin_fabsf(v), 0.5f, l);  // (NaN stays)
 }
-__device__ __forceinline__ float sigmoid(float v) {
-  const float e = exp_neg(v);
+__device__ __forceinline__ float softplus(float v) { return softplus(v, exp_neg(v)); }
+__device__ __forceinline__ float sigmoid(float v, float e) {  // with that e
   const float r = __builtin_amdgcn_rcpf(1.f + e);
   return v >= 0.f ? r : e * r;
 }
+__device__ __forceinline__ float sigmoid(float v) { return sigmoid(v, exp_neg(v)); }
 
 // A value of another lane of the row of 16 (DPP).
 template <int CTRL>
@@ -297,12 +297,18 @@ struct StateTile {
   }
 };
 
+// The place of a thread's quad in a tile's [tokens][channels]; -1 for a thread without one.
+template <class S>
+__device__ __forceinline__ int quad_place(int e) {
+  const int i = threadIdx.x + e * S::THREADS;
+  return kSelTile * S::QUADS >= S::THREADS || i < kSelTile * S::QUADS ? i * 4 : -1;
+}
 // A thread's steps of a tile: what comes in, its bias, softplus; none where no token or
-// channel is.
-template <class T, int LN>
+// channel is.  slope: receives the softplus' slopes.
+template <class T, int LN, bool SLOPE = false>
 __device__ __forceinline__ void tile_steps(const QuadTile<T, SelShape<LN>>& raw, const float (&bias)[4],
                                            bool soft, const SelPlace<LN>& w, int count, bool whole,
-                                           float (&d)[SelShape<LN>::EACH][4]) {
+                                           float (&d)[SelShape<LN>::EACH][4], float* slope = nullptr) {
   using S = SelShape<LN>;
 #pragma unroll
   for (int e = 0; e < S::EACH; ++e)
@@ -310,9 +316,16 @@ __device__ __forceinline__ void tile_steps(const QuadTile<T, SelShape<LN>>& raw,
     for (int j = 0; j < 4; ++j) d[e][j] = raw.q[e].get(j) + bias[j];
   if (soft) {
 #pragma unroll
-    for (int e = 0; e < S::EACH; ++e)
+    for (int e = 0; e < S::EACH; ++e) {
+      f4 of;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) d[e][j] = softplus(d[e][j]);
+      for (int j = 0; j < 4; ++j) {
+        const float x = exp_neg(d[e][j]);
+        if (SLOPE) of[j] = sigmoid(d[e][j], x);
+        d[e][j] = softplus(d[e][j], x);
+      }
+      if (SLOPE && quad_place<S>(e) >= 0) st4(slope + quad_place<S>(e), of);
+    }
   }
   if (!whole) {
 #pragma unroll
@@ -321,12 +334,6 @@ __device__ __forceinline__ void tile_steps(const QuadTile<T, SelShape<LN>>& raw,
       for (int j = 0; j < 4; ++j)
         if (w.k0 + e * S::STEP >= count || j >= w.qn) d[e][j] = 0.f;
   }
-}
-// The place of a thread's quad in a tile's [tokens][channels]; -1 for a thread without one.
-template <class S>
-__device__ __forceinline__ int quad_place(int e) {
-  const int i = threadIdx.x + e * S::THREADS;
-  return kSelTile * S::QUADS >= S::THREADS || i < kSelTile * S::QUADS ? i * 4 : -1;
 }
 
 // Takes `many` ranges (or groups of them) in, the last of them `at`, each by its whole decay and

@@ -14,7 +14,7 @@
 // What bounds it are vector instructions, as in the forward pass: a state and token take 48
 // cycles on the way back, 20 for the states again and 10 for those of a first half that are
 // needed to reach the second, and about 15 for the sums over lanes.  At 32,768 x 2,048
-// bfloat16 with 16 states and a gate: 252 us for what comes back, 1,082 for the tiles, whose
+// bfloat16 with 16 states and a gate: 253 us for what comes back, 1,043 for the tiles, whose
 // vector pipes are busy 83% of the time, and 21 for the sums; its bytes are 234.  Halves of
 // eight tokens, because the states of eight are 64 registers and those of 16, 128, beside what
 // the way back needs.
@@ -64,13 +64,14 @@ struct GradTile {
     states.load(X ? c.B : nullptr, c.ld_B, c.C, c.ld_C, t0, count, w.head, c.N);
   }
   // The tile's steps, D x and v' to LDS.  Tokens past the tile's and channels past the
-  // workgroup's: zeros, which change nothing.
-  template <bool X>
+  // workgroup's: zeros, which change nothing.  KEEP: the softplus' slopes and the gate's
+  // sigmoid, too.
+  template <bool X, bool KEEP = false>
   __device__ __forceinline__ void put(const SelCall& c, const SelPlace<LN>& w, int count, float* step,
-                                      float* dx, float* dv) const {
+                                      float* dx, float* dv, float* slope = nullptr, float* gate = nullptr) const {
     float bias[4], d[S::EACH][4];
     load_four(c.bias, w.q0, w.qn, bias);
-    tile_steps<T, LN>(raw, bias, c.softplus, w, count, whole_tile<S>(w, count), d);
+    tile_steps<T, LN, KEEP>(raw, bias, c.softplus, w, count, whole_tile<S>(w, count), d, slope);
     const bool gated = c.z != nullptr;
 #pragma unroll
     for (int e = 0; e < S::EACH; ++e) {
@@ -83,8 +84,13 @@ struct GradTile {
         v[j] = gy.q[e].get(j);
       }
       if (gated) {
+        f4 sg;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] *= zv.q[e].get(j) * sigmoid(zv.q[e].get(j));
+        for (int j = 0; j < 4; ++j) {
+          sg[j] = sigmoid(zv.q[e].get(j));
+          v[j] *= zv.q[e].get(j) * sg[j];
+        }
+        if (KEEP) st4(gate + at, sg);
       }
       st4(step + at, f4{d[e][0], d[e][1], d[e][2], d[e][3]});
       if (X) st4(dx + at, u);
@@ -154,6 +160,12 @@ struct alignas(16) SelGradLds {
   SelLds<LN> in;
   float dv[kSelTile * S::CB], dstep[kSelTile * S::CB];
   float part[S::W][kSelTile][2][S::NP];
+  // The softplus' slopes and the gate's sigmoid, kept by the thread that reads them: 20
+  // operations less for a token and channel, 32,768 x 2,048 of 16 states 1,350 -> 1,312 us,
+  // 16,384 x 1,024 of 32 states 663 -> 652; but of 64, where a token and channel weigh little,
+  // 1,315 -> 1,354, and with up to 8 states a CU has no room for all of its workgroups.
+  static constexpr bool KEEP = LN == 4 || LN == 8;
+  float slope[KEEP ? kSelTile * S::CB : 1], gate[KEEP ? kSelTile * S::CB : 1];
   int list[S::THREADS + 1];
 };
 
@@ -208,7 +220,7 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 2) void k_selective_grad(Sel
       const SelCall& c = again(args).c;
       GradTile<T, LN> in;
       in.template load<true>(c, w, t0, count);
-      in.template put<true>(c, w, count, s.step, s.dx, g.dv);
+      in.template put<true, SelGradLds<LN>::KEEP>(c, w, count, s.step, s.dx, g.dv, g.slope, g.gate);
       in.states.put(s.B, s.C);
       if (t < kWave) mark_tile(c.seqs, t0, t0 + count, cursor, s.marks);
     }
@@ -372,12 +384,13 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 2) void k_selective_grad(Sel
     const SelCall& c = a.c;
     const bool whole = whole_tile<S>(w, count), skips = c.skip != nullptr;
     const bool soft = c.softplus;
+    constexpr bool KEEP = SelGradLds<LN>::KEEP;
     const T* none = nullptr;
     QuadTile<T, S> raw, gy, xv, zv;
     gy.load(c.dy, c.ld_dy, RowSpot::of(none, c.ld_dy, w.k0, w.q0), t0, count, whole, w);
     xv.load(c.x, c.ld_x, RowSpot::of(none, c.ld_x, w.k0, w.q0), t0, count, whole, w);
     if (gated) zv.load(c.z, c.ld_z, RowSpot::of(none, c.ld_z, w.k0, w.q0), t0, count, whole, w);
-    if (soft) raw.load(c.delta, c.ld_delta, RowSpot::of(none, c.ld_delta, w.k0, w.q0), t0, count, whole, w);
+    if (soft && !KEEP) raw.load(c.delta, c.ld_delta, RowSpot::of(none, c.ld_delta, w.k0, w.q0), t0, count, whole, w);
     float bias[4], skip[4];
     load_four(c.bias, w.q0, w.qn, bias);
     load_four(c.skip, w.q0, w.qn, skip);
@@ -396,9 +409,11 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 2) void k_selective_grad(Sel
       for (int j = 0; j < 4; ++j) gv[j] = gy.q[el].get(j);
       if (gated) {
         const f4 sv = ld4(g.dv + at);
+        f4 kept;
+        if (KEEP) kept = ld4(g.gate + at);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float zj = zv.q[el].get(j), sg = sigmoid(zj);
+          const float zj = zv.q[el].get(j), sg = KEEP ? kept[j] : sigmoid(zj);
           const float v = __fmaf_rn(skip[j], skips ? xv.q[el].get(j) : 0.f, sv[j]);
           out[j] = gv[j] * v * (sg * __fmaf_rn(zj, 1.f - sg, 1.f));
           gv[j] *= zj * sg;
@@ -417,8 +432,10 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 2) void k_selective_grad(Sel
 #pragma unroll
       for (int j = 0; j < 4; ++j) out[j] = __fmaf_rn(xv.q[el].get(j), e[j], kLn2 * ds[j]);
       if (soft) {
+        f4 kept;
+        if (KEEP) kept = ld4(g.slope + at);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) out[j] *= sigmoid(raw.q[el].get(j) + bias[j]);
+        for (int j = 0; j < 4; ++j) out[j] *= KEEP ? kept[j] : sigmoid(raw.q[el].get(j) + bias[j]);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) dbias[j] += out[j];
