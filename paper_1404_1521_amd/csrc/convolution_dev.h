@@ -294,7 +294,7 @@ __global__ __launch_bounds__(kBlock) void k_convolution_step(ConvCall c) {
 
 // Four tokens ahead, not eight: x and dy of each, with the sums of K taps, are 130 to 175
 // registers.  16,411 x 255 float32 in 700 sequences, K 3: 19 us and 4 for the sums, where the
-// bytes are 10; two steps of four tokens to a row, then the join of the workgroup's sums.
+// bytes are 10; four steps of four tokens to a row, then the join of the workgroup's sums.
 template <class T, int K, int V>
 __global__ __launch_bounds__(kBlock, conv_grad_waves(sizeof(T))) void k_convolution_grad(ConvCall c) {
   constexpr int R = kConvStep / 2;
