@@ -529,8 +529,10 @@ int polyglot_convolution_grad(polyglot_ctx* ctx, const polyglot_convolution_grad
  * NULL); last[s], if not NULL, receives the state after the sequence (h0[s] or zeros for
  * an empty one).  States are carried in 32 bits.  marks, if not NULL, receives what
  * polyglot_selective_grad needs: the states before every token that
- * POLYGLOT_SELECTIVE_MARK divides.  What is infinite may come out as NaN further on in its
- * sequence and channel.  States in whole fours, and 8, 16, 32 or 64 of them, are the fast ones.
+ * POLYGLOT_SELECTIVE_MARK divides.  With softplus a delta of -infinity is a step of 0: the
+ * token leaves the state as it is.  What else is infinite may come out as NaN further on in
+ * its sequence and channel.  States in whole fours, and 8, 16, 32 or 64 of them, are the fast
+ * ones.
  * Rows lie less than 2^25 elements apart.
  *
  * With one token per sequence (tokens == nseq, no offsets) and no marks this is a model's

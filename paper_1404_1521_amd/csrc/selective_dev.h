@@ -42,7 +42,7 @@ __device__ __forceinline__ float exp_neg(float x) {
 
 // log(1 + e^v) = max(v, 0) + log(1 + e), e = e^-|v|, and log(1 + e) = 2 atanh(e / (2 + e));
 // the argument is at most 1/3, and the Maclaurin series' first term left out, s^17 / 17, is
-// below 2^-29 of s.
+// below 2^-29 of s.  (max(v, 0) by a comparison: -infinity gives zero, NaN stays.)
 __device__ __forceinline__ float softplus(float v, float e) {
   const float s = e * __builtin_amdgcn_rcpf(2.f + e), q = s * s;
   float p = 2.f / 15.f;
@@ -53,7 +53,7 @@ __device__ __forceinline__ float softplus(float v, float e) {
   p = __fmaf_rn(p, q, 2.f / 5.f);
   p = __fmaf_rn(p, q, 2.f / 3.f);
   const float l = __fmaf_rn(s * q, p, s + s);
-  return __fmaf_rn(v + __builtin_fabsf(v), 0.5f, l);  // (NaN stays)
+  return l + (v < 0.f ? 0.f : v);
 }
 __device__ __forceinline__ float softplus(float v) { return softplus(v, exp_neg(v)); }
 __device__ __forceinline__ float sigmoid(float v, float e) {  // with that e

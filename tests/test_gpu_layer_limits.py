@@ -1,0 +1,97 @@
+"""The selective layer and beam search at their limits: steps of no length and of any length,
+sums that are exact, sizes that take every form of the kernels, calls without the reserved
+workspace.  The operators' ordinary tests are in test_gpu_layers.py."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import layer_refs as ref  # noqa: E402
+from test_gpu_layers import (DT, F32_OUT, check_scan, cuda, cuts, near, normal, scan_call,  # noqa: E402
+                             scan_inputs, scan_reference, wide)
+
+
+@pytest.fixture(scope="module")
+def pg():
+    import paper_1404_1521_amd as pg
+    return pg
+
+
+@pytest.fixture(scope="module")
+def ctx(pg):
+    c = pg.Context(1000, 16, 5, 8, max_batch=1)
+    c.reserve_selective(70_000, 1100, 64)
+    c.reserve_beam(512, 100_003, 64)
+    yield c
+    assert c.status() == pg.OK
+    c.close()
+
+
+# ------------------------------------------------------------------ steps
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_selective_steps_of_no_length(ctx, dtype):
+    """A delta of -infinity, whose softplus is 0, leaves the state as it was: what the other
+    tokens give is what they give without it, bit for bit, and every gradient is finite."""
+    gen = torch.Generator().manual_seed(21)
+    n, D, N = 14, 9, 8
+    out = [0, 3, 4, 9, 13]  # the tokens left out: the first and the last among them
+    keep = [t for t in range(n) if t not in out]
+    s = scan_inputs(gen, n, D, N, 1, 1, dtype)
+    s["delta"][out] = -math.inf
+    o = torch.tensor([0, n], dtype=torch.int32).cuda()
+    got = scan_call(ctx, s, o, True)
+    for k, v in got.items():
+        assert torch.isfinite(v).all(), k
+    rows = ("x", "delta", "B", "C", "z", "dy")
+    less = {k: v[keep].contiguous() if k in rows else v for k, v in s.items()}
+    want = scan_call(ctx, less, torch.tensor([0, len(keep)], dtype=torch.int32).cuda(), True)
+    at = torch.tensor(keep).cuda()
+    assert torch.equal(got["y"][at], want["y"]) and torch.equal(got["last"], want["last"])
+    assert not got["delta"][out].any() and not got["B"][out].any()
+    # against the formulas, where a softplus of -200 is e^-200: nothing in 32 bits, and below
+    # the least normal number nothing is promised
+    far = {k: None if v is None else v.clone() for k, v in s.items()}
+    far["delta"][out] = -200.0
+    values, err = scan_reference(far, [0, n], True, 0)
+    for k in err:
+        err[k] = err[k] + 1e-36
+    check_scan(got, values, err, dtype, "no length")
+    # token by token
+    c = {k: cuda(v) for k, v in s.items()}
+    state = c["h0"]
+    for t in range(n):
+        row = lambda k: c[k][t:t + 1]
+        y, new = ctx.selective_step(row("x"), row("delta"), c["A"], row("B"), row("C"), state, skip=c["skip"],
+                                    z=row("z"), delta_bias=c["bias"])
+        if t in out:
+            assert torch.equal(new, state), t
+        near(y, values["y"][t:t + 1], ref.rounded(err["y"][t:t + 1], values["y"][t:t + 1], dtype), t)
+        state = new
+    near(state, values["last"], ref.rounded(err["last"], values["last"], "f32"), "last")
+
+
+def test_selective_steps_of_any_length(ctx):
+    """A delta above half of the largest number is its own softplus: the state decays to
+    nothing, and with x = 0 nothing comes in."""
+    gen = torch.Generator().manual_seed(22)
+    n, D, N = 6, 5, 16
+    s = scan_inputs(gen, n, D, N, 1, 1, "f32", bias=False)
+    s["delta"][2], s["x"][2] = 3e38, 0.0
+    o = torch.tensor([0, n], dtype=torch.int32).cuda()
+    got = scan_call(ctx, s, o, True)
+    for k, v in got.items():
+        if k != "x":  # (its gradient is the step times what comes back)
+            assert torch.isfinite(v).all(), k
+    tail = {k: v[3:].contiguous() if k in ("x", "delta", "B", "C", "z", "dy") else v for k, v in s.items()}
+    tail["h0"] = torch.zeros_like(s["h0"])
+    want = scan_call(ctx, tail, torch.tensor([0, n - 3], dtype=torch.int32).cuda(), True)
+    assert torch.equal(got["y"][3:], want["y"]) and torch.equal(got["last"], want["last"])
+    c = {k: cuda(v) for k, v in s.items()}
+    _, new = ctx.selective_step(c["x"][2:3], c["delta"][2:3], c["A"], c["B"][2:3], c["C"][2:3], c["h0"])
+    assert not new.any()
