@@ -71,6 +71,10 @@ struct LogitsCall {
   int64_t stride;        // parts that a row has room for
 };
 
+// Of sequences of T tokens each, one behind the other: the first that starts at lo or later.
+// (No sum of the two: a sequence may have 2^30 tokens, and lo lie past them.)
+__host__ __device__ inline int first_equal(int lo, int T) { return T ? lo / T + (lo % T != 0) : 0; }
+
 // Packed sequences of a call.
 struct Packed {
   const void* offsets;  // [nseq + 1] of offset_bytes each, or null: tokens / nseq tokens each

@@ -18,10 +18,7 @@ __device__ __forceinline__ int place_of(const Packed& s, int i) {
 // The first of the offsets that is >= lo (nseq + 1 if none is), found by a whole wave:
 // 64 probes split the range into 65 parts.
 __device__ __forceinline__ int first_place(const Packed& s, int lo) {
-  if (!s.offsets) {
-    const int T = s.tokens / s.nseq;
-    return T ? ceil_div(lo, T) : 0;
-  }
+  if (!s.offsets) return first_equal(lo, s.tokens / s.nseq);
   int l = 0, n = s.nseq + 1;  // the answer is in [l, l + n]
   while (n > 0) {
     const int step = ceil_div(n, kWave + 1);

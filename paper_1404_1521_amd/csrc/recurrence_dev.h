@@ -152,10 +152,7 @@ __device__ __forceinline__ int seq_offset(const RecCall& c, int i) {
 // The first of the nseq + 1 offsets that is >= lo (nseq + 1 if none is), found by
 // the whole wave: 64 probes split the range into 65 parts.
 __device__ __forceinline__ int first_offset(const RecCall& c, int lo) {
-  if (!c.offsets) {
-    const int T = c.tokens / c.nseq;
-    return T ? ceil_div(lo, T) : 0;
-  }
+  if (!c.offsets) return first_equal(lo, c.tokens / c.nseq);
   int l = 0, n = c.nseq + 1;  // the answer is in [l, l + n]
   while (n > 0) {
     const int step = ceil_div(n, kWave + 1);

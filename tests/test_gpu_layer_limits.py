@@ -95,3 +95,30 @@ def test_selective_steps_of_any_length(ctx):
     c = {k: cuda(v) for k, v in s.items()}
     _, new = ctx.selective_step(c["x"][2:3], c["delta"][2:3], c["A"], c["B"][2:3], c["C"][2:3], c["h0"])
     assert not new.any()
+
+
+# ------------------------------------------------------------------ sizes
+
+
+def test_selective_of_the_most_tokens(pg):
+    """One sequence of 2^30 tokens whose steps are 0: the state at its end is the one before it,
+    and so is the gradient, going back."""
+    n = 1 << 30
+    ctx = pg.Context(1000, 16, 5, 8, max_batch=1)
+    ctx.reserve_selective(n, 1, 1)
+    none = torch.zeros(n, 1, dtype=torch.bfloat16, device="cuda")  # every input is the same zeros
+    A = -torch.ones(1, 1, device="cuda")
+    h0 = torch.full((1, 1, 1), 3.0, device="cuda")
+    ins = (none, none, A, none, none)
+    y, last, marks = ctx.selective_scan(*ins, state=h0, softplus=False, marks=True)
+    zero = not y.any().item()  # (a failure is to print no tensor of this size)
+    assert zero and torch.equal(last, h0)
+    del y
+    g = ctx.selective_backward(*ins, none, marks, state=h0, dlast=h0 + 2, softplus=False)
+    # ddelta is A times what comes back, 5, times the state before, 3
+    right = [(g.delta == -15).all().item(), not g.x.any().item(), not g.C.any().item(), not g.A.any().item()]
+    assert all(right) and torch.equal(g.state, h0 + 2), right
+    assert ctx.status() == pg.OK
+    ctx.close()
+    del g, marks, none, ins
+    torch.cuda.empty_cache()
