@@ -611,9 +611,11 @@ typedef struct {
 int polyglot_selective_grad(polyglot_ctx* ctx, const polyglot_selective_grad_args* args);
 
 /* Sizes the workspace of the selective scan, its gradient and the convolution's gradient for
- * calls of up to max_tokens tokens, max_D channels and max_states states; otherwise as
- * polyglot_reserve_recurrence.  Beside 26 to 155 MB, up to 16 states take about 2 bytes for each
- * token and channel and 256 for each token, up to 32 four and up to 64 sixteen times as much. */
+ * calls of up to max_D channels and max_states states, of the scan's gradient also of up to
+ * max_tokens tokens: the other calls take any number, and a program that does not train
+ * reserves 0.  Otherwise as polyglot_reserve_recurrence.  Beside 26 to 155 MB, up to 16 states
+ * take about 2 bytes for each of these tokens and each channel and 256 for each token, up to
+ * 32 four and up to 64 sixteen times as much. */
 int polyglot_reserve_selective(polyglot_ctx* ctx, int64_t max_tokens, int32_t max_D,
                                int32_t max_states);
 

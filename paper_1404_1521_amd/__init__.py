@@ -619,8 +619,9 @@ class Context:
         return out, token, lse
 
     def reserve_selective(self, max_tokens: int, max_width: int, max_states: int) -> None:
-        """Workspace for selective scans and their gradients of up to max_tokens tokens,
-        max_width channels and max_states states, and for the convolution's gradient."""
+        """Workspace for selective scans, their gradients and the convolution's of up to max_width
+        channels and max_states states; for the scan's gradient of up to max_tokens tokens (0
+        where nothing is trained)."""
         self._check(self._lib.polyglot_reserve_selective(self._h, max_tokens, max_width,
                                                          max_states), "reserve_selective")
 

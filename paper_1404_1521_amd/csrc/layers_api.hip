@@ -80,11 +80,14 @@ int check_selective(polyglot_ctx* ctx, const A& a, const std::string& what) {
   return POLYGLOT_OK;
 }
 
+// Only the gradient's room goes by the tokens (dB and dC of the workgroups).
 template <class A>
-int check_selective_room(polyglot_ctx* ctx, const A& a, const std::string& what) {
+int check_selective_room(polyglot_ctx* ctx, const A& a, bool grad, const std::string& what) {
   const OpWorkspace& op = ctx->op;
-  if (!op.sel || a.tokens > op.sel_tokens || a.D > op.sel_D || a.states > op.sel_states)
-    return fail(ctx, POLYGLOT_EBATCH, what + ": above the reserved tokens, channels or states");
+  if (!op.sel || a.D > op.sel_D || a.states > op.sel_states)
+    return fail(ctx, POLYGLOT_EBATCH, what + ": above the reserved channels or states");
+  if (grad && a.tokens > op.sel_tokens)
+    return fail(ctx, POLYGLOT_EBATCH, what + ": above the reserved tokens");
   return POLYGLOT_OK;
 }
 
@@ -216,7 +219,7 @@ int polyglot_selective(polyglot_ctx* ctx, const polyglot_selective_args* args) {
       Timed tm(ctx, kOpKernels + POLYGLOT_OPK_SELECTIVE);
       e = launch_selective_step(c, a.dtype, tm.L);
     } else {
-      rc = check_selective_room(ctx, a, "selective");
+      rc = check_selective_room(ctx, a, false, "selective");
       if (rc) return rc;
       Timed tm(ctx, kOpKernels + POLYGLOT_OPK_SELECTIVE);
       e = launch_selective(c, a.dtype, ctx->op.sel_space, tm.L);
@@ -246,7 +249,7 @@ int polyglot_selective_grad(polyglot_ctx* ctx, const polyglot_selective_grad_arg
     if (!apart({a.dx, a.ddelta, a.dB, a.dC, a.z ? a.dz : nullptr, a.dA, a.dskip, a.ddelta_bias, a.dh0},
                {a.x, a.delta, a.B, a.C, a.z, a.dy, a.A, a.skip, a.delta_bias, a.h0, a.dlast, a.marks}))
       return fail(ctx, POLYGLOT_EINVAL, "selective_grad: an output overlaps another tensor");
-    rc = check_selective_room(ctx, a, "selective_grad");
+    rc = check_selective_room(ctx, a, true, "selective_grad");
     if (rc) return rc;
     SelCall c = selective_call(ctx, a);
     c.dy = a.dy;

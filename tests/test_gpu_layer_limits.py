@@ -122,3 +122,30 @@ def test_selective_of_the_most_tokens(pg):
     ctx.close()
     del g, marks, none, ins
     torch.cuda.empty_cache()
+
+
+# ------------------------------------------------------------------ workspace
+
+
+@pytest.mark.parametrize("D,N,groups", [(40, 16, 1), (64, 24, 2), (33, 4, 1), (20, 64, 1)])
+def test_reservations_without_tokens(pg, ctx, D, N, groups):
+    """Scans take what channels and states need, however many tokens; their gradient does not."""
+    gen = torch.Generator().manual_seed(D)
+    n, nseq = 3000, 4
+    small = pg.Context(1000, 16, 5, 8, max_batch=1)
+    small.reserve_selective(0, D, N)
+    c = {k: cuda(v) for k, v in scan_inputs(gen, n, D, N, groups, nseq, "bf16").items()}
+    o = torch.from_numpy(cuts(np.random.default_rng(D), n, nseq)).cuda()
+    ins = (c["x"], c["delta"], c["A"], c["B"], c["C"])
+    form = dict(state=c["h0"], skip=c["skip"], z=c["z"], delta_bias=c["bias"])
+    want = ctx.selective_scan(*ins, o, marks=True, **form)
+    for a, b in zip(small.selective_scan(*ins, o, marks=True, **form), want):
+        assert torch.equal(a, b)
+    with pytest.raises(pg.PolyglotError) as e:
+        small.selective_backward(*ins, c["dy"], want[2], o, dlast=c["dlast"], **form)
+    assert e.value.rc == pg.EBATCH
+    w = normal(gen, D, 4).cuda()
+    a, b = (k.convolution_backward(c["x"], w, None, c["dy"], o) for k in (small, ctx))
+    assert torch.equal(a.x, b.x) and torch.equal(a.weight, b.weight)
+    assert small.status() == pg.OK
+    small.close()
