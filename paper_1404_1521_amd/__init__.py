@@ -641,6 +641,8 @@ class Context:
         poff, off_bytes = _offsets(offsets)
         if last is None:
             last = x.new_empty((nseq, K - 1, D))
+        elif last is False:
+            last = None
         px, ld_x = _row_tensor(x, dtype, "x", tokens, D)
         py, ld_y = _row_tensor(_flat(out), dtype, "out", tokens, D)
         rows = (nseq, K - 1, D)
@@ -659,7 +661,7 @@ class Context:
         weight[:, k] x_{t - taps + 1 + k} (silu: times its sigmoid), over the sequences of x
         as in recurrence.  weight[D][taps] and bias[D] are float32; state and last
         [nseq][taps - 1][D], in x's type, are the inputs before and at the end of each
-        sequence.  Returns (y, last)."""
+        sequence; last=False leaves the latter out.  Returns (y, last)."""
         if out is None:
             out = _like(x)
         return self._convolution("convolution", _flat(x), weight, bias, offsets,
@@ -734,6 +736,8 @@ class Context:
         shape = (nseq, D, N)
         if last is None:
             last = x.new_empty(shape, dtype=torch.float32)
+        elif last is False:
+            last = None
         room = (-(-tokens // SELECTIVE_MARK), D, -(-N // 4) * 4)
         if marks is True:
             marks = x.new_empty(room, dtype=torch.float32)
@@ -758,7 +762,8 @@ class Context:
         (or delta + delta_bias), over the sequences of x as in recurrence.  A[D][states],
         skip[D], delta_bias[D] and the states[nseq][D][states] are float32; B and C have
         states columns, or as many for each of several heads of consecutive channels.
-        marks=True keeps what selective_backward needs.  Returns (y, last, marks)."""
+        marks=True keeps what selective_backward needs, last=False leaves the sequences' last
+        states out.  Returns (y, last, marks)."""
         if out is None:
             out = _like(x)
         return self._selective("selective_scan", _flat(x), _flat(delta), A, _flat(B), _flat(C),
