@@ -114,6 +114,7 @@ constexpr int kSelectiveTile = 16;  // POLYGLOT_SELECTIVE_MARK
 // sequence that starts in it, or its own carry too.
 constexpr uint32_t kSelNone = 0, kSelClosed = 1, kSelOpen = 2;
 constexpr int kSelGroup = 16;  // ranges
+constexpr int kSelNear = 32;   // ranges that are taken in one by one where there are groups
 
 // A kernel's lanes to a channel (four states each), its waves and its channels.
 __host__ __device__ constexpr int sel_lanes(int N) { return N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }

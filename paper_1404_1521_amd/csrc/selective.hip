@@ -49,7 +49,7 @@ SelRoom selective_room(int64_t tokens, int D, int N) {
 }
 
 hipError_t launch_selective(const SelCall& c, int dtype, SelSpace space, const Launch& L) {
-  const SelPlan p = selective_plan(c.seqs.tokens, c.seqs.nseq, c.D, c.N, c.groups, space);
+  const SelPlan p = selective_plan(c.seqs, c.D, c.N, c.groups, space);
   return by_format(dtype, [&](auto v) {
     using E = decltype(v);
     return by_lanes(c.N, [&](auto ln) { return forward<E, decltype(ln)::value>(c, p, L); });
@@ -60,7 +60,7 @@ template <class T>  // in a file for each format
 hipError_t selective_grad(const SelCall& c, const SelPlan& p, const Launch& L);
 
 hipError_t launch_selective_grad(const SelCall& c, int dtype, SelSpace space, const Launch& L) {
-  const SelPlan p = selective_plan(c.seqs.tokens, c.seqs.nseq, c.D, c.N, c.groups, space);
+  const SelPlan p = selective_plan(c.seqs, c.D, c.N, c.groups, space);
   return by_format(dtype, [&](auto v) { return selective_grad<decltype(v)>(c, p, L); });
 }
 

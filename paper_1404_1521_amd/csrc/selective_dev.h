@@ -384,8 +384,15 @@ __device__ __forceinline__ int open_run(const uint32_t* info, int at, int dir, i
   found = false;
   return most;
 }
+// How many from `at` on, along dir, are open one after the other; of `there`, kSelNear at most.
+__device__ __forceinline__ int open_ranges(const uint32_t* info, int at, int dir, int there) {
+  const int i = lane_id(), most = min(there, kSelNear);
+  const uint64_t end = __ballot(i >= most || info[at + dir * min(i, most - 1)] != kSelOpen);
+  return __builtin_ctzll(end);  // (kSelNear is less than a wave)
+}
 // The carry into a range from those before it (dir -1: the gradient's, from those after it):
-// those of its group, and of the groups before that, since the last that starts afresh.
+// since the last that starts afresh, each by itself where they are few, otherwise those of its
+// group and the groups before that.
 template <int LN>
 __device__ __forceinline__ void carry_into(const SelCall& c, const SelPlan& p, int range, int dir,
                                            const SelPlace<LN>& w, const float (&A)[2][4],
@@ -396,30 +403,34 @@ __device__ __forceinline__ void carry_into(const SelCall& c, const SelPlan& p, i
     for (int k = 0; k < 4; ++k) h[r][k] = 0.f;
   const int all = dir > 0 ? range : p.ranges - 1 - range;  // before it
   bool found;
-  if (!p.groups) {
-    const int many = open_run(p.info, range - dir, dir, all, found);
+  const int many = open_run(p.info, range - dir, dir, p.groups ? min(all, kSelNear) : all, found);
+  if (found || many == all) {
     take_in<LN>(p.sums, p.states, range - dir, many, dir, true, c, w, A, h);
     return;
   }
   const int group = range / kSelGroup, place = range % kSelGroup;
-  const int near = min(all, dir > 0 ? place : kSelGroup - 1 - place);
-  const int many = open_run(p.info, range - dir, dir, near, found);
-  if (!found) {
-    bool any;
-    const int far = open_run(p.group_info, group - dir, dir, dir > 0 ? group : p.groups - 1 - group, any);
-    take_in<LN>(p.group_sums, p.group_states, group - dir, far, dir, true, c, w, A, h);
-  }
-  take_in<LN>(p.sums, p.states, range - dir, many, dir, found, c, w, A, h);
+  const int near = min(all, dir > 0 ? place : kSelGroup - 1 - place);  // (all of them open)
+  bool any;
+  const int far = open_run(p.group_info, group - dir, dir, dir > 0 ? group : p.groups - 1 - group, any);
+  take_in<LN>(p.group_sums, p.group_states, group - dir, far, dir, true, c, w, A, h);
+  take_in<LN>(p.sums, p.states, range - dir, near, dir, false, c, w, A, h);
 }
 
-// What groups of ranges pass on together: a thread for four states of a channel and a group.
+// What groups of ranges pass on together: a thread for four states of a channel, a row of
+// workgroups for a group.
 template <int LN>
 __global__ __launch_bounds__(kBlock) void k_selective_groups(SelCall c, SelPlan p, int dir) {
   constexpr int NP = SelShape<LN>::NP;
-  const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x, each = (int64_t)c.D * LN;
-  const int g = (int)(i / each);
-  if (g >= p.groups) return;
-  const int ch = (int)(i % each / LN), n0 = (int)(i % LN) * 4;
+  const int blocks = (int)(((int64_t)c.D * LN + kBlock - 1) / kBlock), g = blockIdx.x / blocks;
+  // Nothing reads it but behind kSelNear open ranges: those that the group ends on and those
+  // that go on behind it.
+  const int end = dir > 0 ? min((g + 1) * kSelGroup, p.ranges) - 1 : g * kSelGroup;
+  if (open_ranges(p.info, end, -dir, dir > 0 ? end + 1 : p.ranges - end) +
+          open_ranges(p.info, end + dir, dir, dir > 0 ? p.ranges - 1 - end : end) < kSelNear)
+    return;
+  const int64_t i = (int64_t)(blockIdx.x - g * blocks) * kBlock + threadIdx.x;
+  if (i >= (int64_t)c.D * LN) return;
+  const int ch = (int)(i / LN), n0 = (int)(i % LN) * 4;
   float A[4], h[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
 #pragma unroll
   for (int k = 0; k < 4; ++k) A[k] = n0 + k < c.N ? c.A[(int64_t)ch * c.N + n0 + k] * kLog2e : 0.f;
@@ -454,9 +465,8 @@ __global__ __launch_bounds__(kBlock) void k_selective_groups(SelCall c, SelPlan 
 template <int LN>
 hipError_t selective_groups(const SelCall& c, const SelPlan& p, int dir, const Launch& L) {
   if (!p.groups || p.ranges <= 1) return hipSuccess;
-  const int64_t threads = (int64_t)p.groups * c.D * LN;
-  return pg_launch(k_selective_groups<LN>, dim3((uint32_t)((threads + kBlock - 1) / kBlock)), dim3(kBlock), 0, L, c, p,
-                   dir);
+  const int64_t blocks = ((int64_t)c.D * LN + kBlock - 1) / kBlock;
+  return pg_launch(k_selective_groups<LN>, dim3((uint32_t)(p.groups * blocks)), dim3(kBlock), 0, L, c, p, dir);
 }
 
 // A workgroup's tile in LDS.

@@ -28,8 +28,9 @@ constexpr int kSelLongRange = 8;
 constexpr int kSelFewRanges = 4 * kSelGroup;  // of a sequence
 
 // How a call is cut, in the workspace.
-inline SelPlan selective_plan(int64_t tokens, int nseq, int D, int N, int groups, const SelSpace& space) {
+inline SelPlan selective_plan(const Packed& seqs, int D, int N, int groups, const SelSpace& space) {
   SelPlan p{};
+  const int64_t tokens = seqs.tokens;
   const int CB = sel_channels(sel_lanes(N));
   p.blocks = ceil_div(D / groups, CB);
   p.all_blocks = p.blocks * groups;
@@ -39,11 +40,15 @@ inline SelPlan selective_plan(int64_t tokens, int nseq, int D, int N, int groups
   p.share = Shares(tiles, p.ranges);
   p.NM = (N + 3) / 4 * 4;
   // A range takes those before it in its sequence in one after the other, 0.2 us each; where
-  // a sequence has many (the longest of several taken to be twice the mean), groups of them
-  // are put together first, a launch of 5 to 10 us: one sequence of 16,384 x 64 forward 295 ->
-  // 75 us and four of 4,096 x 256 (256 ranges) 49 -> 39, but 700 of 16,384 x 256 46 -> 56 and
-  // one of 16,384 x 2,048 (64 ranges) 289 -> 294.
-  const int64_t longest = nseq > 1 ? 2 * (int64_t)p.ranges / nseq : p.ranges;
+  // they may be many, groups of them are put together first, in a launch of 8 to 10 us, of 2
+  // where no run of ranges is long enough to need it.  Offsets lie on the device: any of several
+  // sequences may have nearly all ranges.  One long sequence beside 32 short ones, 16,384 x 64
+  // (1,024 ranges), 270 -> 60 us forward and 305 -> 89 back, 16,384 x 256 165 -> 65 and 216 ->
+  // 120; but 700 in 16,384 x 256 42 -> 44 and 80 -> 82.  At up to 128 ranges groups would cost
+  // several even sequences what they save uneven ones: 2,048 x 64 25 -> 32, 44 -> 30; 32,768 x
+  // 2,048 498 -> 505, 555 -> 527.  One sequence of 16,384 x 64 is 295 us without them, one of
+  // 16,384 x 2,048 (64 ranges) 289, and 294 with them.
+  const int64_t longest = seqs.nseq == 1 ? p.ranges : seqs.offsets ? p.ranges / 2 : p.ranges / seqs.nseq + 2;
   p.groups = longest > kSelFewRanges ? (p.ranges + kSelGroup - 1) / kSelGroup : 0;
   const int64_t rows = (int64_t)p.ranges * D, NP = 4 * sel_lanes(N);
   p.group_states = space.states + rows * NP;
