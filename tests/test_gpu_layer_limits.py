@@ -222,7 +222,7 @@ def uneven(kind, tokens):
 @pytest.mark.parametrize("tokens,D,N,groups,kind", [
     (9000, 40, 32, 1, "first"), (9000, 40, 16, 1, "last"), (9000, 24, 4, 1, "middle"), (9001, 16, 40, 2, "two"),
     (12_000, 36, 24, 1, "one"), (20_005, 5, 4, 1, "one"), (20_005, 5, 16, 1, "middle"), (33_000, 3, 2, 1, "first"),
-    (5000, 300, 8, 2, "two"), (3001, 1030, 4, 1, "last")])
+    (5000, 300, 8, 2, "two"), (3001, 1030, 4, 1, "last"), (2000, 24, 16, 1, "middle"), (1990, 40, 24, 1, "last")])
 def test_selective_of_uneven_sequences(ctx, tokens, D, N, groups, kind):
     """A sequence through hundreds of ranges (and groups of them), alone and beside short ones.
     Values, and the same bits in two runs."""
