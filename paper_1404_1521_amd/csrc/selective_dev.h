@@ -384,11 +384,15 @@ __device__ __forceinline__ int open_run(const uint32_t* info, int at, int dir, i
   found = false;
   return most;
 }
-// How many from `at` on, along dir, are open one after the other; of `there`, kSelNear at most.
-__device__ __forceinline__ int open_ranges(const uint32_t* info, int at, int dir, int there) {
-  const int i = lane_id(), most = min(there, kSelNear);
-  const uint64_t end = __ballot(i >= most || info[at + dir * min(i, most - 1)] != kSelOpen);
-  return __builtin_ctzll(end);  // (kSelNear is less than a wave)
+// Whether kSelNear ranges or more are open one after the other across the place behind `end`:
+// those up to and with it, and those that follow.  By a whole wave, half of it for each.
+__device__ __forceinline__ bool open_across(const uint32_t* info, int end, int dir, int ranges) {
+  static_assert(kSelNear == kWave / 2, "a lane for each");
+  const int l = lane_id(), i = l < kSelNear ? end - dir * l : end + dir * (l - kSelNear + 1);
+  const uint64_t closed = __ballot(i < 0 || i >= ranges || info[i] != kSelOpen);
+  const int before = __builtin_ctzll(closed | 1ull << kSelNear);
+  const int behind = __builtin_ctzll(closed >> kSelNear | 1ull << kSelNear);
+  return before + behind >= kSelNear;
 }
 // The carry into a range from those before it (dir -1: the gradient's, from those after it):
 // since the last that starts afresh, each by itself where they are few, otherwise those of its
@@ -422,12 +426,8 @@ template <int LN>
 __global__ __launch_bounds__(kBlock) void k_selective_groups(SelCall c, SelPlan p, int dir) {
   constexpr int NP = SelShape<LN>::NP;
   const int blocks = (int)(((int64_t)c.D * LN + kBlock - 1) / kBlock), g = blockIdx.x / blocks;
-  // Nothing reads it but behind kSelNear open ranges: those that the group ends on and those
-  // that go on behind it.
-  const int end = dir > 0 ? min((g + 1) * kSelGroup, p.ranges) - 1 : g * kSelGroup;
-  if (open_ranges(p.info, end, -dir, dir > 0 ? end + 1 : p.ranges - end) +
-          open_ranges(p.info, end + dir, dir, dir > 0 ? p.ranges - 1 - end : end) < kSelNear)
-    return;
+  // Nothing reads it but behind kSelNear open ranges.
+  if (!open_across(p.info, dir > 0 ? min((g + 1) * kSelGroup, p.ranges) - 1 : g * kSelGroup, dir, p.ranges)) return;
   const int64_t i = (int64_t)(blockIdx.x - g * blocks) * kBlock + threadIdx.x;
   if (i >= (int64_t)c.D * LN) return;
   const int ch = (int)(i / LN), n0 = (int)(i % LN) * 4;
