@@ -16,7 +16,7 @@
 //
 // What bounds it are vector instructions: an operation takes a wave 4 cycles, the exponential
 // 8, a state and token 20 in the first launch and 24 in the second.  At 32,768 x 2,048
-// bfloat16 with 16 states and a gate that is 137 and 164 us of the 208 and 325 measured; the
+// bfloat16 with 16 states and a gate that is 137 and 164 us of the 212 and 320 measured; the
 // bytes are 103.  The rest is what a token and channel take by themselves: softplus, the
 // gate's sigmoid, conversions, LDS, the sum over lanes.  Every state has a decay of its own, so
 // that nothing here is a matrix product.
@@ -759,7 +759,7 @@ __global__ __launch_bounds__(SelShape<LN>::THREADS, 4) void k_selective(SelArgs)
 
 // One token for each sequence: LN lanes of four states each for a channel of a row, a channel
 // to each group of lanes, so that a workgroup's states are one contiguous piece.  Its bytes are
-// the states, in and out: 64 x 2,048 with 16 states 7.5 us for 18 MB, 3.4 at a copy's rate;
+// the states, in and out: 64 x 2,048 with 16 states 7.7 us for 18 MB, 3.4 at a copy's rate;
 // the rest is one round trip of loads and the launch.
 template <class T, int LN>
 __global__ __launch_bounds__(kBlock) void k_selective_step(SelCall c, int blocks) {

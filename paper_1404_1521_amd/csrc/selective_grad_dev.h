@@ -14,10 +14,10 @@
 // What bounds it are vector instructions, as in the forward pass: a state and token take 48
 // cycles on the way back, 20 for the states again and 10 for those of a first half that are
 // needed to reach the second, and about 15 for the sums over lanes.  At 32,768 x 2,048
-// bfloat16 with 16 states and a gate: 253 us for what comes back, 1,043 for the tiles, whose
-// vector pipes are busy 83% of the time, and 21 for the sums; its bytes are 234.  Halves of
-// eight tokens, because the states of eight are 64 registers and those of 16, 128, beside what
-// the way back needs.
+// bfloat16 with 16 states and a gate: 252 us for what comes back, 1,037 for the tiles (462 M
+// vector instructions, 0.84 of the cycles by the counters), and 22 for the sums; its bytes are
+// 234.  Halves of eight tokens, because the states of eight are 64 registers and those of 16,
+// 128, beside what the way back needs.
 #pragma once
 #include "selective_dev.h"
 
