@@ -240,6 +240,63 @@ def test_selective_of_uneven_sequences(ctx, tokens, D, N, groups, kind):
         assert torch.equal(a[k], b[k]), k
 
 
+def test_replays_with_other_offsets(pg):
+    """A captured scan and its gradient, replayed with sequences of other lengths: even ones, a
+    long one first, in the middle and last, one alone beside empty ones."""
+    stream = torch.cuda.Stream()
+    gen = torch.Generator().manual_seed(41)
+    n, D, N, nseq = 9000, 24, 16, 33
+    c = {k: cuda(v) for k, v in scan_inputs(gen, n, D, N, 1, nseq, "f32").items()}
+    c["bias"] -= 3
+    even = np.linspace(0, n, nseq + 1).astype(np.int64)
+    alone = np.concatenate([[0] * 5, [n] * (nseq - 4)])
+    o = torch.from_numpy(even).cuda()
+    with torch.cuda.stream(stream):
+        ctx = pg.Context(1000, 16, 5, 8, max_batch=1, stream=stream)
+        ctx.reserve_selective(n, D, N)
+
+        def work():
+            form = dict(state=c["h0"], skip=c["skip"], z=c["z"], delta_bias=c["bias"])
+            ins = (c["x"], c["delta"], c["A"], c["B"], c["C"])
+            y, last, marks = ctx.selective_scan(*ins, o, marks=True, **form)
+            return [y, last, *ctx.selective_backward(*ins, c["dy"], marks, o, dlast=c["dlast"], **form)]
+
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            held = work()
+        seen = []
+        for off in (uneven("first", n), even, uneven("middle", n), alone, uneven("last", n), even):
+            o.copy_(torch.from_numpy(off))
+            graph.replay()
+            torch.cuda.synchronize()
+            first = [t.clone() for t in held]
+            for a, e in zip(first, work()):
+                assert torch.equal(a, e)
+            torch.cuda.synchronize()
+            seen.append(first[0])
+        assert torch.equal(seen[1], seen[5]) and not torch.equal(seen[0], seen[1])
+        assert ctx.status() == pg.OK
+        ctx.close()
+
+
+@pytest.mark.parametrize("bad", [[0, 5000, 3000, 9000], [0, 9000, 2_000_000_000, 9000], [8999, 0, 0, 0], [0, 0, 0, 0],
+                                 [9000, 9000, 9000, 9000]])
+def test_offsets_that_do_not_ascend_over_many_ranges(pg, ctx, bad):
+    """The flag, and a right answer to the next call."""
+    gen = torch.Generator().manual_seed(42)
+    n, D, N = 9000, 24, 8
+    s = scan_inputs(gen, n, D, N, 1, 3, "f32")
+    good = torch.tensor([0, 10, 8990, n], dtype=torch.int32, device="cuda")
+    want = scan_call(ctx, s, good, True)
+    assert ctx.status() == pg.OK
+    scan_call(ctx, s, torch.tensor(bad, dtype=torch.int32, device="cuda"), True)
+    assert ctx.status() == pg.EOFFSETS and ctx.status() == pg.OK
+    got = scan_call(ctx, s, good, True)
+    for k in want:
+        assert torch.equal(got[k], want[k]), k
+
+
 @pytest.mark.parametrize("dtype", list(DT))
 @pytest.mark.parametrize("tokens,D,N,groups,nseq", [(9000, 40, 4, 1, 600), (9001, 36, 16, 2, 500), (6000, 20, 24, 1, 400),
                                                     (5000, 24, 64, 1, 300), (5003, 64, 4, 64, 3), (3001, 120, 32, 120, 1),
